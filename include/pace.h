@@ -412,6 +412,107 @@ pace_status_t pace_topk_gather(const float* scores, int N, int K, const void* hi
 pace_status_t pace_gather_rows(const void* src, int src_rows, size_t row_bytes,
                                const int32_t* idx, int n_idx, void* dst, hipStream_t stream);
 
+/* ---------------------------------------------------------------- decode over a pruned context */
+
+/*
+ * A paged cache of rotated keys and values (caller-owned device memory).  Token t of a sequence
+ * lies in page block_table[t / page], slot t % page, of every head.
+ *   k, v      bf16 (bits = 16) or OCP e4m3 codes (bits = 8), [num_pages, heads, page, dim],
+ *             16-byte aligned.
+ *   k_scale, v_scale  bits = 8: fp32 [num_pages, heads], a positive finite factor for each page and head
+ *             (value = code * scale); bits = 16: not read, may be NULL.
+ *   page      tokens per page: 16, 32, 64, 128 or 256.  dim in {80, 128}.
+ * Nothing needs to be initialised: slots at or past a sequence's length, and scales of pages that
+ * hold none of its tokens, are never used.  The pool may exceed 4 GiB.
+ */
+typedef struct pace_kv_cache {
+  void *k, *v;
+  float *k_scale, *v_scale;
+  int num_pages, heads, page, dim;
+  int bits;                       /* 16 or 8 */
+} pace_kv_cache;
+
+/*
+ * Rotates new queries and keys by their positions and appends keys and values to a paged cache:
+ * what an LLM layer does between its projections and its attention, here also with the selection's
+ * row gather (Section 3.3: the kept tokens keep their positions) on the way.
+ *   q, k, v   bf16 rows of n_src tokens: row i of q starts at q + i * q_stride and holds Hq heads of
+ *             dim values one after the other (k, v: cache->heads heads).  Strides in elements, multiples
+ *             of 8, at least the row's values; pointers 16-byte aligned (slices of one fused projection
+ *             are fine).  q may be NULL (then q_out is not used).
+ *   rows      int32 [n_new] (device): source row of new token r; NULL: row r (n_new <= n_src then).
+ *   cu_new    int32 [B+1] (device): sequence b's new tokens are [cu_new[b], cu_new[b+1]), at most
+ *             max_new of them; cu_new[B] <= n_new.
+ *   ctx_len   int32 [B] (device): tokens sequence b holds already; its new tokens take the places
+ *             ctx_len[b], ctx_len[b] + 1, ...
+ *   block_table int32 [B, max_pages] (device).  No page that is written may belong to two sequences.
+ *   positions int32 [axes, n_src] (device), axes 1 or 3; inv_freq fp32 [dim / 2] (device).  Frequency f
+ *             turns the pair (x_f, x_{f + dim/2}) by positions[a][row] * inv_freq[f], where a = 0 for one
+ *             axis; for three (time, height, width) sections (HOST, 3 counts, sum dim / 2) says how many
+ *             consecutive frequencies belong to each.  positions NULL: no rotation (inv_freq NULL too).
+ *             Angles are formed and reduced in 64 bits, products in fp32, one rounding on the store.
+ *   q_out     bf16 [n_new, Hq, dim]: the rotated queries in the new tokens' order.  Rows at or past
+ *             cu_new[B] are left as they were.
+ * 8-bit pages: the scale is a power of two, 2^e with the least e >= -120 that keeps the page's largest
+ * new magnitude (finite values, head by head) within 448 * 2^e; a page that already holds tokens of the
+ * sequence keeps its scale unless the new tokens need a larger one, and then its codes are moved to it (exact
+ * between powers of two, except where a code becomes subnormal).  Values that are not finite are
+ * stored as NaN.
+ * A source row outside [0, n_src), a place past the table and a page outside [0, num_pages) are not
+ * written.  Asynchronous on `stream`; no workspace.
+ */
+pace_status_t pace_cache_append(const uint16_t* q, long long q_stride, const uint16_t* k, long long k_stride,
+                                const uint16_t* v, long long v_stride, int n_src, int Hq, const int32_t* rows,
+                                const int32_t* cu_new, int B, int n_new, int max_new, const int32_t* ctx_len,
+                                const int32_t* block_table, int max_pages, const int32_t* positions, int axes,
+                                const int* sections, const float* inv_freq, const pace_kv_cache* cache,
+                                uint16_t* q_out, hipStream_t stream);
+
+/*
+ * Workspace bytes for pace_cache_attention with these arguments (partial results where few rows share
+ * a long context; 0 where none are needed).
+ */
+size_t pace_cache_attention_workspace_size(int n_q, int Hq, int heads, int dim, int B, int max_q, int max_len,
+                                           int window, int sinks);
+
+/*
+ * Attention of a few or many new tokens over a paged cache that already holds them (decode, drafted
+ * tokens, the next chunk of a prompt), grouped-query as in the prefill.
+ *   q         bf16 [n_q, Hq, dim], rotated; Hq a multiple of cache->heads; query head h reads KV head
+ *             h / (Hq / heads).
+ *   cu_q      int32 [B+1] (device): sequence b's queries are rows [cu_q[b], cu_q[b+1]), at most max_q.
+ *   seq_len   int32 [B] (device): tokens of sequence b in the cache, its queries' own tokens included, at
+ *             most max_len.  Its last query has place seq_len[b] - 1, the one before seq_len[b] - 2, ...
+ *   block_table int32 [B, max_pages] (device).
+ *   window, sinks  a query at place p sees the keys j <= p with j > p - window or j < sinks; window 0
+ *             is all keys j <= p.
+ *   o         bf16 [n_q, Hq, dim]; lse fp32 [Hq, n_q], natural log, or NULL.  A query that sees no key (or
+ *             whose scores are all -inf) gets o = 0 and lse = -inf.  Rows at or past cu_q[B] are left as they were.
+ * Keys that a query does not see have no effect on it, whatever their K and V hold.  A page outside
+ * [0, num_pages) counts as unseen.  Results do not depend on the order in which workgroups run.
+ * The workspace must be 16-byte aligned; calls that may run at the same time need one each.
+ */
+pace_status_t pace_cache_attention(const uint16_t* q, int n_q, int Hq, const pace_kv_cache* cache,
+                                   const int32_t* cu_q, int B, int max_q, const int32_t* seq_len, int max_len,
+                                   const int32_t* block_table, int max_pages, int window, int sinks, float scale,
+                                   uint16_t* o, float* lse, void* workspace, size_t workspace_bytes,
+                                   hipStream_t stream);
+
+/*
+ * C = x W^T for a few rows x and weights of 4 bits: pace_gemm_bf16's product and epilogues with
+ *   W[n, k] = (q[n, k] - zero[n, k / group]) * scale[n, k / group],
+ *   w         uint8 [N, K / 2]: q[n, k] is the low half of byte k / 2 for even k, the high half for odd k.
+ *   scale     bf16 [N, K / group]; zero uint8 [N, K / group] with values 0..15, or NULL (8 everywhere).
+ *   group     32, 64 or 128; K a positive multiple of group.
+ *   x         bf16 [M, K] row-major; x and w 16-byte aligned.  Any M >= 1; the weights are read once for every
+ *             64 rows.
+ *   bias, residual, epilogue, C  as in pace_gemm_bf16.
+ * Products accumulate in fp32.  x must be finite.  Each operand under 2 GiB.
+ */
+pace_status_t pace_gemm_w4(const uint16_t* x, const uint8_t* w, const uint16_t* scale, const uint8_t* zero,
+                           const float* bias, const uint16_t* residual, uint16_t* C, int M, int N, int K, int group,
+                           int epilogue, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -16,8 +16,10 @@ Modules:
              fusion, top-K ranking and the gather of the kept tokens.
   preview    Section 3.2's shallow feature preview: one vision-encoder block (patch
              embedding, window attention, SwiGLU MLP) with seeded weights.
+  cache      A decode step over the pruned context: position rotation, paged cache in 16 and 8
+             bits, attention over it, 4-bit weights.
 
 Every function is pinned by the CPU tests (tests/test_oracle_*.py) against
 closed forms, invariants, brute force on tiny inputs or library routines.
 """
-from . import apc, attention, ddae, preview  # noqa: F401
+from . import apc, attention, cache, ddae, preview  # noqa: F401

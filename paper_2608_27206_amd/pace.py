@@ -24,6 +24,7 @@ _lib = None
 
 c_int, c_size, c_double, c_float, c_void = (ctypes.c_int, ctypes.c_size_t, ctypes.c_double,
                                             ctypes.c_float, ctypes.c_void_p)
+c_ll = ctypes.c_longlong
 c_int_p = ctypes.POINTER(ctypes.c_int)
 
 # name -> (restype, argtypes)
@@ -73,6 +74,14 @@ _PROTOS = {
     "pace_topk_gather": (c_int, [c_void, c_int, c_int, c_void, c_size, c_void, c_void, c_void, c_size,
                                  c_void]),
     "pace_gather_rows": (c_int, [c_void, c_int, c_size, c_void, c_int, c_void, c_void]),
+    "pace_cache_append": (c_int, [c_void, c_ll, c_void, c_ll, c_void, c_ll, c_int, c_int, c_void, c_void, c_int, c_int,
+                                  c_int, c_void, c_void, c_int, c_void, c_int, c_int_p, c_void, c_void, c_void,
+                                  c_void]),
+    "pace_cache_attention_workspace_size": (c_size, [c_int] * 9),
+    "pace_cache_attention": (c_int, [c_void, c_int, c_int, c_void, c_void, c_int, c_int, c_void, c_int, c_void, c_int,
+                                     c_int, c_int, c_float, c_void, c_void, c_void, c_size, c_void]),
+    "pace_gemm_w4": (c_int, [c_void, c_void, c_void, c_void, c_void, c_void, c_void, c_int, c_int, c_int, c_int, c_int,
+                             c_void]),
 }
 
 EXPORTED = tuple(_PROTOS.keys())
@@ -115,6 +124,24 @@ def _ptr(t: Optional[torch.Tensor]):
 
 def _stream():
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+class _Nothing:
+    def __enter__(self):
+        pass
+
+    def __exit__(self, *exc):
+        pass
+
+
+_NOTHING = _Nothing()
+
+
+def _on(device: torch.device):
+    """Makes `device` current for a call whose tensors live on another one."""
+    if device.type != "cuda":
+        raise PaceError("tensor must live on the GPU")
+    return _NOTHING if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
 
 def _ws(nbytes: int, device) -> torch.Tensor:
@@ -499,4 +526,176 @@ def gather_rows(src: torch.Tensor, idx: torch.Tensor, out: Optional[torch.Tensor
     row_bytes = src[0].numel() * src.element_size() if src.shape[0] > 0 else 0
     _check(lib().pace_gather_rows(_ptr(src), src.shape[0], row_bytes, _ptr(idx), n, _ptr(out),
                                   _stream()), "pace_gather_rows")
+    return out
+
+
+# ---------------------------------------------------------------- decode over a pruned context
+class _KvCacheStruct(ctypes.Structure):
+    """Mirror of pace_kv_cache (include/pace.h)."""
+    _fields_ = [("k", c_void), ("v", c_void), ("k_scale", c_void), ("v_scale", c_void), ("num_pages", c_int),
+                ("heads", c_int), ("page", c_int), ("dim", c_int), ("bits", c_int)]
+
+
+class KvCache:
+    """A paged cache over the caller's tensors: k, v [num_pages, heads, page, dim], bfloat16 or
+    float8_e4m3fn; with the latter k_scale, v_scale fp32 [num_pages, heads]."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
+            raise PaceError("k and v must be [num_pages, heads, page, dim] of one shape and type")
+        if k.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            raise PaceError(f"cache type {k.dtype} is not bfloat16 or float8_e4m3fn")
+        bits = 16 if k.dtype == torch.bfloat16 else 8
+        n, heads, page, dim = k.shape
+        for s in (k_scale, v_scale):
+            if bits == 8 and (s is None or s.dtype != torch.float32 or s.shape != (n, heads)):
+                raise PaceError("8-bit pages need float32 scales [num_pages, heads]")
+        if bits == 16:
+            k_scale = v_scale = None
+        _one_device(k, v, k_scale, v_scale)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.struct = _KvCacheStruct(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), n, heads, page, dim, bits)
+        self.ref = ctypes.byref(self.struct)
+
+    @classmethod
+    def empty(cls, num_pages: int, heads: int, page: int, dim: int, dtype=torch.bfloat16, device="cuda"):
+        """A cache over newly allocated, uninitialised pages."""
+        k, v = (torch.empty((num_pages, heads, page, dim), dtype=dtype, device=device) for _ in range(2))
+        if dtype == torch.bfloat16:
+            return cls(k, v)
+        return cls(k, v, *(torch.empty((num_pages, heads), dtype=torch.float32, device=device) for _ in range(2)))
+
+
+def _one_device(first, *others):
+    dev = first.device
+    for t in others:
+        if t is not None and t.device != dev:
+            raise PaceError(f"tensors on {dev} and {t.device}: all must be on one device")
+
+
+def _typed(t: Optional[torch.Tensor], dtype, name: str, *shape):
+    """The device pointer of a contiguous tensor of this type and shape (None: any size)."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise PaceError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise PaceError(f"{name} must have shape {list(shape)}, not {list(t.shape)}")
+    return _ptr(t)
+
+
+def _strided_rows(t: torch.Tensor, name: str, heads: Optional[int], dim: int):
+    """Pointer and row stride of bf16 rows [n, heads, dim] whose heads lie one after the other."""
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
+        raise PaceError(f"{name} must be bfloat16 [tokens, {'heads' if heads is None else heads}, {dim}], not {t.dtype} "
+                        f"{list(t.shape)}")
+    if not t.is_cuda:
+        raise PaceError("tensor must live on the GPU")
+    n, h, d = t.shape
+    if t.stride(2) != 1 or (h > 1 and t.stride(1) != d):
+        raise PaceError(f"{name}: the heads of a row must lie one after the other")
+    return ctypes.c_void_p(t.data_ptr()), t.stride(0) if n > 1 else h * d
+
+
+def cache_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cache: KvCache, cu_new: torch.Tensor,
+                 ctx_len: torch.Tensor, block_table: torch.Tensor, max_new: int,
+                 positions: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None,
+                 sections: Optional[Sequence[int]] = None, rows: Optional[torch.Tensor] = None,
+                 q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Rotates q and k by positions (int32 [n_src] or [axes, n_src]; None: no rotation) and appends k and v to the
+    cache.  q, k, v: bf16 [n_src, heads, dim], rows of any stride (slices of a fused projection); rows int32 [n_new]:
+    the source rows to take (a selection's kept indices).  Returns the rotated queries [n_new, Hq, dim], or None
+    without q."""
+    dim, heads = cache.struct.dim, cache.struct.heads
+    n_src = k.shape[0]
+    kp, ks = _strided_rows(k, "k", heads, dim)
+    vp, vs = _strided_rows(v, "v", heads, dim)
+    if v.shape[0] != n_src or (q is not None and q.shape[0] != n_src):
+        raise PaceError("q, k and v must have one number of rows")
+    B, max_pages = block_table.shape if block_table.dim() == 2 else (0, 0)
+    n_new = n_src if rows is None else rows.numel()
+    qp, qs, hq = None, 0, 0
+    if q is not None:
+        qp, qs = _strided_rows(q, "q", None, dim)
+        hq = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty((n_new, hq, dim), dtype=torch.bfloat16, device=q.device)
+    axes = 1
+    if positions is not None:
+        axes = 1 if positions.dim() == 1 else positions.shape[0]
+        if positions.dtype != torch.int32 or positions.numel() != axes * n_src:
+            raise PaceError(f"positions must be int32 [n_src] or [axes, n_src], not {positions.dtype} "
+                            f"{list(positions.shape)}")
+        if axes == 3 and (sections is None or len(sections) != 3):
+            raise PaceError("three position axes need three sections")
+    _one_device(cache.k, q, k, v, cu_new, ctx_len, block_table, positions, inv_freq, rows, q_out)
+    with _on(cache.k.device):
+        _check(lib().pace_cache_append(
+            qp, qs, kp, ks, vp, vs, n_src, hq, _typed(rows, torch.int32, "rows", None),
+            _typed(cu_new, torch.int32, "cu_new", B + 1), B, n_new, int(max_new),
+            _typed(ctx_len, torch.int32, "ctx_len", B), _typed(block_table, torch.int32, "block_table", None, None),
+            max_pages, _ptr(positions), axes, (ctypes.c_int * 3)(*sections) if axes == 3 else None,
+            _typed(inv_freq, torch.float32, "inv_freq", dim // 2), cache.ref,
+            _typed(q_out if q is not None else None, torch.bfloat16, "q_out", n_new, hq, dim), _stream()),
+            "pace_cache_append")
+    return q_out if q is not None else None
+
+
+def cache_attention(q: torch.Tensor, cache: KvCache, cu_q: torch.Tensor, seq_len: torch.Tensor,
+                    block_table: torch.Tensor, max_q: int, max_len: int, scale: Optional[float] = None,
+                    window: int = 0, sinks: int = 0, want_lse: bool = True, o: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Attention of q bf16 [n_q, Hq, dim] over a paged cache that holds its tokens already.  cu_q int32 [B + 1],
+    seq_len int32 [B], block_table int32 [B, max_pages] on the GPU.  Returns (o, lse [Hq, n_q] or None)."""
+    n_q, hq, dim = q.shape
+    c = cache.struct
+    if dim != c.dim:
+        raise PaceError(f"q has head dim {dim}, the cache {c.dim}")
+    B, max_pages = block_table.shape if block_table.dim() == 2 else (0, 0)
+    if o is None:
+        o = torch.empty_like(q)
+    if not want_lse:
+        lse = None
+    elif lse is None:
+        lse = torch.empty((hq, n_q), dtype=torch.float32, device=q.device)
+    _one_device(cache.k, q, cu_q, seq_len, block_table, o, lse, workspace)
+    if workspace is None:
+        need = lib().pace_cache_attention_workspace_size(n_q, hq, c.heads, dim, B, int(max_q), int(max_len),
+                                                         int(window), int(sinks))
+        if need:
+            workspace = _ws(need, q.device)
+    with _on(q.device):
+        _check(lib().pace_cache_attention(
+            _typed(q, torch.bfloat16, "q", None, None, None), n_q, hq, cache.ref,
+            _typed(cu_q, torch.int32, "cu_q", B + 1), B, int(max_q), _typed(seq_len, torch.int32, "seq_len", B),
+            int(max_len), _typed(block_table, torch.int32, "block_table", None, None), max_pages, int(window), int(sinks),
+            1.0 / math.sqrt(dim) if scale is None else float(scale), _typed(o, torch.bfloat16, "o", n_q, hq, dim),
+            _typed(lse, torch.float32, "lse", hq, n_q), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+            _stream()), "pace_cache_attention")
+    return o, lse
+
+
+def gemm_w4(x: torch.Tensor, w: torch.Tensor, scale: torch.Tensor, zero: Optional[torch.Tensor] = None,
+            bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, epilogue: int = 0,
+            out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """C = x W^T with 4-bit weights: x bf16 [M, K]; w uint8 [N, K / 2] (low half first); scale bf16 [N, K / group];
+    zero uint8 like scale, or None (8); bias, residual and epilogue as in gemm_bf16."""
+    if x.dim() != 2 or scale.dim() != 2 or scale.shape[1] < 1:
+        raise PaceError("x and scale must be 2-D")
+    M, K = x.shape
+    N, groups = scale.shape
+    if K % groups:
+        raise PaceError(f"K={K} is not a multiple of the {groups} groups")
+    cols = N // 2 if epilogue == 2 else N
+    if out is None:
+        out = torch.empty((M, cols), dtype=torch.bfloat16, device=x.device)
+    _one_device(x, w, scale, zero, bias, residual, out)
+    with _on(x.device):
+        _check(lib().pace_gemm_w4(
+            _typed(x, torch.bfloat16, "x", M, K), _typed(w, torch.uint8, "w", N, K // 2),
+            _typed(scale, torch.bfloat16, "scale", N, groups), _typed(zero, torch.uint8, "zero", N, groups),
+            _typed(bias, torch.float32, "bias", N), _typed(residual, torch.bfloat16, "residual", M, cols),
+            _typed(out, torch.bfloat16, "out", M, cols), M, N, K, K // groups, int(epilogue), _stream()),
+            "pace_gemm_w4")
     return out
