@@ -297,89 +297,512 @@ pace_status_t launch_append(const AppendParams& p, int bits, long long row_block
 }
 
 // ---------------------------------------------------------------- attention
+// Rows of one KV head: row x of sequence b is its query x / group, query head hk * group + x % group.
+// Scores are kept in the log2 domain.  The keys that the rows of a workgroup may see are visited in
+// tiles of 32, aligned to 32: first those of the sinks, then those of the window.
 struct AttendParams {
   const uint16_t* q;
   const int32_t *cu, *len;
   uint16_t* o;
   float* lse;
+  float *part, *ml;          // partial results [splits, n_q * Hq, D] and their (maximum, sum)
   Pool pool;
   int n_q, Hq, group, B, max_q, max_len, window, sinks;
+  int row_blocks, splits;
   float scale_log2;
 };
 
-// One workgroup per (query, head), a key per thread and step.
-template <int D, int BITS>
-__global__ __launch_bounds__(256) void attend(const AttendParams p) {
-  __shared__ float qs[D], ps[256], red[4], os[256];
-  __shared__ long long at[256];
-  int id = blockIdx.x;
-  const int h = id % p.Hq;
-  id /= p.Hq;
-  const int b = id / p.max_q, i = id % p.max_q;
-  const int row = p.cu[b] + i, nq = p.cu[b + 1] - p.cu[b];
-  if (i >= nq || row < 0 || row >= p.n_q) return;
-  int len = p.len[b];
-  len = len > p.max_len ? p.max_len : len;
-  const int place = len - nq + i, t = threadIdx.x;
-  const int hk = h / p.group;
-  if (t < D) {
-    const uint32_t u = p.q[(static_cast<long long>(row) * p.Hq + h) * D + t];
-    qs[t] = __uint_as_float(u << 16) * p.scale_log2;
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kTile = 32;          // keys per step of a wave
+constexpr int kSplitTiles = 8;     // least tiles per split of a sequence
+
+__device__ __forceinline__ f32x4 mfma16(uint4 a, uint4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Two e4m3 codes (the low or high pair of a dword) as two bf16 values: exact.
+template <bool HI>
+__device__ __forceinline__ uint32_t e4m3_bf16(uint32_t u) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.0f, HI));
+}
+__device__ __forceinline__ uint4 e4m3_bf16x8(uint32_t a, uint32_t b) {
+  return make_uint4(e4m3_bf16<false>(a), e4m3_bf16<true>(a), e4m3_bf16<false>(b), e4m3_bf16<true>(b));
+}
+
+// What a sequence's queries are and the tiles that queries i_lo..i_hi of it see.
+struct Span {
+  int row0, nq, len;         // first row of q, queries, cached tokens
+  int p_lo, p_hi;            // places of the first and last query
+  int head_tiles, tail0, tiles;   // tiles [0, head_tiles) and [tail0, ...), tiles in all
+  __device__ __forceinline__ int base(int x) const { return kTile * (x < head_tiles ? x : tail0 + x - head_tiles); }
+};
+__device__ __forceinline__ Span queries_of(const AttendParams& p, int b) {
+  Span s;
+  s.row0 = p.cu[b];
+  s.nq = p.cu[b + 1] - s.row0;
+  s.nq = s.nq > p.max_q ? p.max_q : s.nq;
+  if (s.row0 < 0 || s.nq < 0) s.nq = 0;
+  if (s.nq > p.n_q - s.row0) s.nq = p.n_q - s.row0;
+  s.len = p.len[b];
+  s.len = s.len > p.max_len ? p.max_len : s.len;
+  return s;
+}
+__device__ __forceinline__ void tiles_of(const AttendParams& p, int i_lo, int i_hi, Span* s) {
+  s->p_lo = s->len - s->nq + i_lo;
+  s->p_hi = s->len - s->nq + i_hi;
+  const int end = s->p_hi < 0 ? 0 : s->p_hi / kTile + 1;
+  const int first = p.window == 0 ? 0 : s->p_lo - p.window + 1;      // p_lo < 2^31 and window >= 0: no overflow
+  s->tail0 = first <= 0 ? 0 : first / kTile;
+  const int sinks = p.sinks < s->p_hi + 1 ? p.sinks : s->p_hi + 1;
+  s->head_tiles = sinks <= 0 ? 0 : (sinks + kTile - 1) / kTile;
+  if (s->tail0 <= s->head_tiles) { s->tail0 = 0; s->head_tiles = 0; }
+  s->tiles = end - s->tail0 + s->head_tiles;
+}
+// How many parts a sequence's tiles are split into.
+__device__ __forceinline__ int splits_of(const AttendParams& p, int tiles) {
+  const int most = (tiles + kSplitTiles - 1) / kSplitTiles;
+  return most < 1 ? 1 : most < p.splits ? most : p.splits;
+}
+
+// A sequence's page of a 16-key half tile, or -1.
+__device__ __forceinline__ int page_of(const AttendParams& p, const int32_t* table, int key) {
+  const int j = key >> p.pool.shift;
+  const int pg = j < p.pool.max_pages ? table[j] : -1;
+  return pg >= 0 && pg < p.pool.num_pages ? pg : -1;
+}
+
+// Few rows over many keys: memory-bound.  A workgroup = W waves over one (sequence, KV head, block of 16 R
+// rows, part of the keys); the waves take its tiles in turn, each with its own running maximum and sum, and
+// join at the end.  Nothing passes through LDS before that:
+//  S^T = K Q^T by 16x16x32 products.  Row m of the A operand may be any key; with key 8 (m / 4) + 4 t + m % 4 in
+//    row m of product t, lane (r, g) ends with the scores of query row r and keys 8 g .. 8 g + 7, which is
+//    where the B operand of the next product wants P^T.  The contracted d is permuted as the loads like it.
+//  O^T = V^T P^T: a lane loads 8 values of each of its 8 keys (8 r .. 8 r + 7 of a row) and turns the 8 x 8
+//    block in registers (one v_perm for two values), so that row m of product c is d = 8 m + c, and a lane
+//    ends with 8 consecutive d of each of four blocks.
+// A row's maximum is only raised when a score passes it by 2^8 (a wave-wide vote), so most tiles need no
+// exchange between lanes; probabilities of up to 256 round like others.
+template <int D, int BITS, int R, int W>
+__global__ __launch_bounds__(64 * W) void attend_few(const AttendParams p) {
+  constexpr int KS = (D + 31) / 32;                   // products along d
+  constexpr int KW = BITS == 16 ? 4 : 2;              // dwords of 8 values
+  __shared__ float join[W / 2][8 * 4 * R + 2 * R][64];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  int id = remap_block_id(blockIdx.x, gridDim.x);
+  const int split = id % p.splits;
+  id /= p.splits;
+  const int rb = id % p.row_blocks;
+  id /= p.row_blocks;
+  const int hk = id % p.pool.heads, b = id / p.pool.heads;
+  Span sp = queries_of(p, b);
+  const int rows = sp.nq * p.group, x0 = rb * 16 * R;
+  if (x0 >= rows) return;
+  const int x1 = x0 + 16 * R < rows ? x0 + 16 * R - 1 : rows - 1;
+  tiles_of(p, x0 / p.group, x1 / p.group, &sp);
+  const int splits = splits_of(p, sp.tiles);
+  if (split >= splits) return;
+  const int t0 = static_cast<int>(static_cast<long long>(sp.tiles) * split / splits);
+  const int t1 = static_cast<int>(static_cast<long long>(sp.tiles) * (split + 1) / splits);
+
+  uint4 qf[R][KS];
+  int place[R];
+#pragma unroll
+  for (int t = 0; t < R; ++t) {
+    const int x = x0 + 16 * t + r, xi = x <= x1 ? x : x1;
+    place[t] = sp.len - sp.nq + xi / p.group;
+    const uint16_t* from = p.q + (static_cast<long long>(sp.row0 + xi / p.group) * p.Hq + hk * p.group + xi % p.group) * D;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int d = BITS == 8 && D == 128 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
+      qf[t][s] = d < D ? *reinterpret_cast<const uint4*>(from + d) : make_uint4(0, 0, 0, 0);
+    }
   }
-  constexpr int GR = 256 / D;
-  float m = -INFINITY, l = 0.f, acc = 0.f;
-  const int dd = t % D, gg = t / D;
-  for (int j0 = 0; j0 <= place; j0 += 256) {
-    __syncthreads();
-    const int j = j0 + t;
-    float s = -INFINITY;
-    long long off = -1;
-    if (j <= place && (p.window == 0 || j > place - p.window || j < p.sinks)) {
-      const int pi = j >> p.pool.shift;
-      const int pg = pi < p.pool.max_pages ? p.pool.table[static_cast<long long>(b) * p.pool.max_pages + pi] : -1;
-      if (pg >= 0 && pg < p.pool.num_pages) {
-        const long long ph = static_cast<long long>(pg) * p.pool.heads + hk;
-        off = (ph * p.pool.page + (j & (p.pool.page - 1))) * D;
-        float a = 0.f;
-        for (int d = 0; d < D; ++d) {
-          float kv;
-          if constexpr (BITS == 16) kv = __uint_as_float(static_cast<uint32_t>(static_cast<uint16_t*>(p.pool.k)[off + d]) << 16);
-          else kv = __builtin_amdgcn_cvt_f32_fp8(static_cast<uint8_t*>(p.pool.k)[off + d], 0);
-          a += kv * qs[d];
+
+  const int32_t* table = p.pool.table + static_cast<long long>(b) * p.pool.max_pages;
+  const long long head_bytes = static_cast<long long>(p.pool.page) * D * (BITS / 8);
+  const int slot_mask = p.pool.page - 1;
+  // lane constants: the K rows (product 0; product 1 is 4 rows on) and V rows of a tile that a lane loads
+  const int krow = 8 * (r >> 2) + (r & 3), khalf = r >> 3, vhalf = g >> 1;
+  const int kd = BITS == 8 && D == 128 ? 16 * g : 8 * g;
+  const int koff = ((krow & 15) * D + kd) * (BITS / 8);
+  const int voff = ((8 * g & 15) * D + (8 * r < D ? 8 * r : 0)) * (BITS / 8);
+
+  uint32_t kr[2][KS][KW], vr[8][KW];
+  float ks = 1.f, vs = 1.f, ks_n = 1.f, vs_n = 1.f;
+  int pa, pb;                                          // pages of the loaded tile's halves
+
+  const auto half_base = [&](const void* pool, int key, int pg) {
+    return static_cast<const char*>(pool) + (static_cast<long long>(pg < 0 ? 0 : pg) * p.pool.heads + hk) * head_bytes +
+           static_cast<long long>(key & slot_mask) * D * (BITS / 8);
+  };
+  const auto load_k = [&](int base, int a, int c) {
+    const char* from = (khalf ? half_base(p.pool.k, base + 16, c) : half_base(p.pool.k, base, a)) + koff;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const char* f = from + 4 * t * D * (BITS / 8);
+      if constexpr (BITS == 8 && D == 128) {
+#pragma unroll
+        for (int u = 0; u < KS / 2; ++u) {
+          const uint4 x = *reinterpret_cast<const uint4*>(f + 64 * u);
+          kr[t][2 * u][0] = x.x; kr[t][2 * u][1] = x.y; kr[t][2 * u + 1][0] = x.z; kr[t][2 * u + 1][1] = x.w;
         }
-        if constexpr (BITS == 8) a *= p.pool.k_scale[ph];
-        s = a;
+      } else {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          // D = 80: the last product has 16 values, its upper lanes load the lower ones' again
+          const int at = (32 * s - (32 * s + 32 > D && g >= 2 ? 16 : 0)) * (BITS / 8);
+          if constexpr (BITS == 8) {
+            const uint2 x = *reinterpret_cast<const uint2*>(f + at);
+            kr[t][s][0] = x.x; kr[t][s][1] = x.y;
+          } else {
+            const uint4 x = *reinterpret_cast<const uint4*>(f + at);
+            kr[t][s][0] = x.x; kr[t][s][1] = x.y; kr[t][s][2] = x.z; kr[t][s][3] = x.w;
+          }
+        }
       }
     }
-    at[t] = off;
-    const float mt = fmaxf(m, block_reduce<1>(s, red));
-    const float mz = mt == -INFINITY ? 0.f : mt;
-    const float e = off >= 0 ? exp2f(s - mz) : 0.f;
-    const float f = exp2f(m - mz);
-    m = mt;
-    l = l * f + block_reduce<0>(e, red);
-    float w = e;
-    if constexpr (BITS == 8) { if (off >= 0) w *= p.pool.v_scale[off / (static_cast<long long>(p.pool.page) * D)]; }
-    ps[t] = w;
-    __syncthreads();
-    acc *= f;
-    if (gg < GR)
-      for (int k = gg; k < 256; k += GR)
-        if (at[k] >= 0) {
-          float vv;
-          if constexpr (BITS == 16) vv = __uint_as_float(static_cast<uint32_t>(static_cast<uint16_t*>(p.pool.v)[at[k] + dd]) << 16);
-          else vv = __builtin_amdgcn_cvt_f32_fp8(static_cast<uint8_t*>(p.pool.v)[at[k] + dd], 0);
-          acc += ps[k] * vv;
+    if constexpr (BITS == 8) {
+      const int pg = vhalf ? c : a;
+      ks_n = p.pool.k_scale[static_cast<long long>(pg < 0 ? 0 : pg) * p.pool.heads + hk];
+    }
+  };
+  const auto load_v = [&](int base, int a, int c) {
+    const char* from = (vhalf ? half_base(p.pool.v, base + 16, c) : half_base(p.pool.v, base, a)) + voff;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const char* f = from + j * D * (BITS / 8);
+      if constexpr (BITS == 8) {
+        const uint2 x = *reinterpret_cast<const uint2*>(f);
+        vr[j][0] = x.x; vr[j][1] = x.y;
+      } else {
+        const uint4 x = *reinterpret_cast<const uint4*>(f);
+        vr[j][0] = x.x; vr[j][1] = x.y; vr[j][2] = x.z; vr[j][3] = x.w;
+      }
+    }
+    if constexpr (BITS == 8) {
+      const int pg = vhalf ? c : a;
+      vs_n = p.pool.v_scale[static_cast<long long>(pg < 0 ? 0 : pg) * p.pool.heads + hk];
+    }
+  };
+  // the A operand of O^T's product c from the loaded V rows (those of key `only`, or all: -1)
+  const auto v_operand = [&](int c, int only) {
+    uint32_t a[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (BITS == 8) {
+        const uint32_t y = __builtin_amdgcn_perm(vr[2 * k + 1][c >> 2], vr[2 * k][c >> 2], (c & 2) ? 0x07030602u : 0x05010400u);
+        a[k] = (c & 1) ? e4m3_bf16<true>(y) : e4m3_bf16<false>(y);
+      } else {
+        a[k] = __builtin_amdgcn_perm(vr[2 * k + 1][c >> 1], vr[2 * k][c >> 1], (c & 1) ? 0x07060302u : 0x05040100u);
+      }
+      if (only >= 0) a[k] = 8 * g + 2 * k == only ? a[k] & 0xffffu : 8 * g + 2 * k + 1 == only ? a[k] & 0xffff0000u : 0u;
+    }
+    return make_uint4(a[0], a[1], a[2], a[3]);
+  };
+
+  f32x4 acc[R][8];
+  float m[R], l[R];
+#pragma unroll
+  for (int t = 0; t < R; ++t) {
+    m[t] = -INFINITY;
+    l[t] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  int x = t0 + w;
+  int pa_n = -1, pb_n = -1;
+  if (x < t1) {
+    const int base = sp.base(x);
+    pa = page_of(p, table, base);
+    pb = page_of(p, table, base + 16);
+    load_k(base, pa, pb);
+    load_v(base, pa, pb);
+    if (x + W < t1) {
+      const int nb = sp.base(x + W);
+      pa_n = page_of(p, table, nb);
+      pb_n = page_of(p, table, nb + 16);
+    }
+  }
+  for (; x < t1; x += W) {
+    const int base = sp.base(x);
+    const bool more = x + W < t1;
+    const int nbase = more ? sp.base(x + W) : 0;
+    const bool ok_a = pa >= 0, ok_b = pb >= 0;
+    if constexpr (BITS == 8) { ks = ks_n; vs = vs_n; }
+    // every key of the tile is seen by every row
+    const bool full = ok_a && ok_b && base + kTile - 1 <= sp.p_lo &&
+                      (p.window == 0 || base > sp.p_hi - p.window || base + kTile <= p.sinks);
+    f32x4 st[R][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int t = 0; t < R; ++t) st[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        uint4 a;
+        if constexpr (BITS == 8) a = e4m3_bf16x8(kr[u][s][0], kr[u][s][1]);
+        else a = make_uint4(kr[u][s][0], kr[u][s][1], kr[u][s][2], kr[u][s][3]);
+        if (32 * s + 32 > D && g >= 2) a = make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < R; ++t) st[t][u] = mfma16(a, qf[t][s], st[t][u]);
+      }
+    }
+    pa = pa_n;
+    pb = pb_n;
+    if (more) {
+      load_k(nbase, pa, pb);
+      if (x + 2 * W < t1) {
+        const int nb = sp.base(x + 2 * W);
+        pa_n = page_of(p, table, nb);
+        pb_n = page_of(p, table, nb + 16);
+      }
+    }
+    const float f = BITS == 8 ? p.scale_log2 * ks : p.scale_log2;
+    uint4 pf[R];
+    uint32_t seen[R];                                  // bit j: row sees key base + 8 g + j
+    bool odd = false;                                  // some key is seen by some rows only and its V is not finite
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+      float s[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] = st[t][j >> 2][j & 3] * f;
+      seen[t] = 0xffu;
+      if (!full) {
+        seen[t] = 0;
+        const bool ok = vhalf ? ok_b : ok_a;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int key = base + 8 * g + j;
+          const bool sees = ok && key <= place[t] && (p.window == 0 || key > place[t] - p.window || key < p.sinks);
+          seen[t] |= sees ? 1u << j : 0u;
+          s[j] = sees ? s[j] : -INFINITY;
         }
+      }
+      float top = s[0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) top = fmaxf(top, s[j]);
+      if (__any(top > m[t] + 8.f)) {
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float mn = fmaxf(m[t], top);
+        const float k = mn == m[t] ? 1.f : exp2_fast(m[t] - mn);
+        m[t] = mn;
+        l[t] *= k;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) acc[t][c] *= k;
+      }
+      const float mz = m[t] == -INFINITY ? 0.f : m[t];
+      float e[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        e[j] = exp2_fast(s[j] - mz);
+        l[t] += e[j];
+        if constexpr (BITS == 8) e[j] *= vs;
+      }
+      if (!full && BITS == 8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = (seen[t] >> j & 1u) ? e[j] : 0.f;     // a scale nobody set may be NaN
+      }
+      // probabilities are rounded to bf16 for the product (relative 2^-8); their sum is not
+      pf[t] = pack8(e);
+    }
+    if (!full) {
+      // V rows that no row sees become 0 (0 * NaN is NaN)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int key = base + 8 * g + j;
+        const bool sees = (vhalf ? ok_b : ok_a) && key <= sp.p_hi && (p.window == 0 || key > sp.p_lo - p.window || key < p.sinks);
+#pragma unroll
+        for (int d = 0; d < KW; ++d) vr[j][d] = sees ? vr[j][d] : 0u;
+      }
+      if (sp.p_lo != sp.p_hi) {
+        // where the rows differ, V values that are not finite must reach only the rows that see them
+        bool bad = false;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int d = 0; d < KW; ++d) {
+            const uint32_t u = vr[j][d];
+            if constexpr (BITS == 16) {
+              bad |= (u & 0x7f80u) == 0x7f80u || (u & 0x7f800000u) == 0x7f800000u;
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) bad |= (u >> 8 * e & 0x7fu) == 0x7fu;
+            }
+          }
+        odd = __any(bad);
+      }
+    }
+    if (!odd) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const uint4 a = v_operand(c, -1);
+#pragma unroll
+        for (int t = 0; t < R; ++t) acc[t][c] = mfma16(a, pf[t], acc[t][c]);
+      }
+    } else {
+      // key by key, each added to the rows that see it alone
+#pragma unroll 1
+      for (int key = 0; key < kTile; ++key) {
+        bool mine[R];
+#pragma unroll
+        for (int t = 0; t < R; ++t)
+          mine[t] = __shfl(seen[t], (key >> 3) * 16 + r, 64) >> (key & 7) & 1u;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          const uint4 a = v_operand(c, key);
+#pragma unroll
+          for (int t = 0; t < R; ++t) {
+            const f32x4 y = mfma16(a, pf[t], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[t][c][i] += mine[t] ? y[i] : 0.f;
+          }
+        }
+      }
+    }
+    if (more) load_v(nbase, pa, pb);
   }
-  os[t] = acc;
-  __syncthreads();
-  if (t < D) {
-    float r = 0.f;
-    for (int g = 0; g < GR; ++g) r += os[g * D + t];
-    p.o[(static_cast<long long>(row) * p.Hq + h) * D + t] = static_cast<uint16_t>(pack_bf16x2(l > 0.f || l != l ? r / l : 0.f, 0.f));
-    if (t == 0 && p.lse) p.lse[static_cast<long long>(h) * p.n_q + row] = l > 0.f || l != l ? (m + log2f(l)) * kLn2 : -INFINITY;
+
+  // the waves join in halves: maximum, sum and O of the upper half go through LDS
+#pragma unroll
+  for (int h = W / 2; h >= 1; h >>= 1) {
+    if (w >= h && w < 2 * h) {
+#pragma unroll
+      for (int t = 0; t < R; ++t) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) join[w - h][(t * 8 + c) * 4 + i][lane] = acc[t][c][i];
+        join[w - h][32 * R + 2 * t][lane] = m[t];
+        join[w - h][32 * R + 2 * t + 1][lane] = l[t];
+      }
+    }
+    __syncthreads();
+    if (w < h) {
+#pragma unroll
+      for (int t = 0; t < R; ++t) {
+        const float m2 = join[w][32 * R + 2 * t][lane], l2 = join[w][32 * R + 2 * t + 1][lane];
+        const float mn = fmaxf(m[t], m2);
+        const float k1 = mn == m[t] ? 1.f : exp2_fast(m[t] - mn), k2 = mn == m2 ? 1.f : exp2_fast(m2 - mn);
+        m[t] = mn;
+        l[t] = l[t] * k1 + l2 * k2;
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[t][c][i] = acc[t][c][i] * k1 + join[w][(t * 8 + c) * 4 + i][lane] * k2;
+      }
+    }
+    __syncthreads();
   }
+  if (w != 0) return;
+#pragma unroll
+  for (int t = 0; t < R; ++t) {
+    float sum = l[t] + __shfl_xor(l[t], 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    const int x = x0 + 16 * t + r;
+    if (x > x1) continue;
+    const int n = sp.row0 + x / p.group, h = hk * p.group + x % p.group;
+    const long long row = static_cast<long long>(n) * p.Hq + h;
+    if (splits > 1) {
+      const long long at = static_cast<long long>(split) * p.n_q * p.Hq + row;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int d = 8 * (4 * g + i);
+        if (d >= D) continue;
+        float4* to = reinterpret_cast<float4*>(p.part + at * D + d);
+        to[0] = make_float4(acc[t][0][i], acc[t][1][i], acc[t][2][i], acc[t][3][i]);
+        to[1] = make_float4(acc[t][4][i], acc[t][5][i], acc[t][6][i], acc[t][7][i]);
+      }
+      if (g == 0) *reinterpret_cast<float2*>(p.ml + 2 * at) = make_float2(m[t], sum);
+      continue;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int d = 8 * (4 * g + i);
+      if (d >= D) continue;
+      float y[8];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) y[c] = acc[t][c][i] * inv;
+      *reinterpret_cast<uint4*>(p.o + row * D + d) = pack8(y);
+    }
+    if (g == 0 && p.lse) p.lse[static_cast<long long>(h) * p.n_q + n] = sum == 0.f ? -INFINITY : (m[t] + log2f(sum)) * kLn2;
+  }
+}
+
+// Joins the parts of the rows whose keys were split: one wave per row.
+template <int D>
+__global__ __launch_bounds__(256) void attend_join(const AttendParams p, int rows_per_block) {
+  const int lane = threadIdx.x & 63;
+  const long long id = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int h = static_cast<int>(id % p.Hq);
+  const int i = static_cast<int>(id / p.Hq % p.max_q), b = static_cast<int>(id / p.Hq / p.max_q);
+  if (b >= p.B) return;
+  Span sp = queries_of(p, b);
+  if (i >= sp.nq) return;
+  // the tiles of the row block that this row was in
+  const int rows = sp.nq * p.group, x = i * p.group + h % p.group, x0 = x / rows_per_block * rows_per_block;
+  const int x1 = x0 + rows_per_block < rows ? x0 + rows_per_block - 1 : rows - 1;
+  tiles_of(p, x0 / p.group, x1 / p.group, &sp);
+  const int splits = splits_of(p, sp.tiles);
+  if (splits == 1) return;
+  const int n = sp.row0 + i;
+  const long long row = static_cast<long long>(n) * p.Hq + h, all = static_cast<long long>(p.n_q) * p.Hq;
+  float top = -INFINITY;
+  for (int s = 0; s < splits; ++s) top = fmaxf(top, p.ml[2 * (s * all + row)]);
+  float sum = 0.f, y0 = 0.f, y1 = 0.f;
+  for (int s = 0; s < splits; ++s) {
+    const long long at = s * all + row;
+    const float m = p.ml[2 * at], k = m == top ? 1.f : exp2_fast(m - top);
+    sum += p.ml[2 * at + 1] * k;
+    if (2 * lane < D) {
+      const float2 v = *reinterpret_cast<const float2*>(p.part + at * D + 2 * lane);
+      y0 += v.x * k;
+      y1 += v.y * k;
+    }
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  if (2 * lane < D) *reinterpret_cast<uint32_t*>(p.o + row * D + 2 * lane) = pack_bf16x2(y0 * inv, y1 * inv);
+  if (lane == 0 && p.lse) p.lse[static_cast<long long>(h) * p.n_q + n] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+}
+
+// How a call is laid out: rows of a KV head per workgroup, and parts that a sequence's keys are split into.
+struct AttendPlan {
+  int rows, row_blocks, splits;
+  long long blocks;
+};
+constexpr int kWaves = 8;
+AttendPlan plan_attention(int Hq, int heads, int B, int max_q, int max_len, int window, int sinks) {
+  AttendPlan a;
+  const long long rows = static_cast<long long>(max_q) * (Hq / heads);
+  a.rows = rows > 16 ? 32 : 16;
+  a.row_blocks = static_cast<int>((rows + a.rows - 1) / a.rows);
+  const long long base = static_cast<long long>(B) * heads * a.row_blocks;
+  long long keys = max_len;
+  if (window > 0 && static_cast<long long>(window) + sinks + max_q < keys) keys = static_cast<long long>(window) + sinks + max_q;
+  const long long most = ((keys + kTile - 1) / kTile + kSplitTiles - 1) / kSplitTiles;
+  // enough workgroups for two on every CU
+  long long s = (512 + base - 1) / base;
+  s = s > most ? most : s;
+  a.splits = s < 1 ? 1 : static_cast<int>(s);
+  a.blocks = base * a.splits;
+  return a;
+}
+
+template <int D, int BITS>
+pace_status_t launch_attend(const AttendParams& p, const AttendPlan& a, hipStream_t stream) {
+  const dim3 g(static_cast<unsigned>(a.blocks)), th(64 * kWaves);
+  if (a.rows == 16) hipLaunchKernelGGL((attend_few<D, BITS, 1, kWaves>), g, th, 0, stream, p);
+  else hipLaunchKernelGGL((attend_few<D, BITS, 2, kWaves>), g, th, 0, stream, p);
+  if (a.splits > 1) {
+    const long long rows = static_cast<long long>(p.B) * p.max_q * p.Hq;
+    hipLaunchKernelGGL(attend_join<D>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, stream, p, a.rows);
+  }
+  return check_launch("pace_cache_attention");
 }
 
 // ---------------------------------------------------------------- host checks
@@ -524,7 +947,11 @@ pace_status_t pace_cache_append(const uint16_t* q, long long q_stride, const uin
 
 size_t pace_cache_attention_workspace_size(int n_q, int Hq, int heads, int dim, int B, int max_q, int max_len,
                                            int window, int sinks) {
-  return 0;
+  if (n_q < 1 || heads < 1 || Hq < heads || Hq % heads != 0 || dim < 1 || B < 1 || max_q < 1 || max_len < 0 ||
+      window < 0 || sinks < 0)
+    return 0;
+  const AttendPlan a = plan_attention(Hq, heads, B, max_q, max_len, window, sinks);
+  return a.splits == 1 ? 0 : static_cast<size_t>(a.splits) * n_q * Hq * (dim + 2) * sizeof(float);
 }
 
 pace_status_t pace_cache_attention(const uint16_t* q, int n_q, int Hq, const pace_kv_cache* cache,
@@ -547,9 +974,21 @@ pace_status_t pace_cache_attention(const uint16_t* q, int n_q, int Hq, const pac
   if (max_q == 0) return PACE_OK;
   p.q = q; p.cu = cu_q; p.len = seq_len; p.o = o; p.lse = lse;
   p.n_q = n_q; p.Hq = Hq; p.group = Hq / cache->heads; p.B = B; p.max_q = max_q; p.max_len = max_len;
-  p.window = window; p.sinks = sinks; p.scale_log2 = scale * kLog2e;
-  const long long blocks = static_cast<long long>(B) * max_q * Hq;
-  PACE_REQUIRE(blocks < (1ll << 31), "pace_cache_attention: too many queries and heads");
+  p.window = window >= max_len ? 0 : window;          // such a window hides nothing
+  p.sinks = sinks; p.scale_log2 = scale * kLog2e;
+  const AttendPlan a = plan_attention(Hq, cache->heads, B, max_q, max_len, window, sinks);
+  PACE_REQUIRE(a.blocks < (1ll << 31) && static_cast<long long>(B) * max_q * Hq < (1ll << 31),
+               "pace_cache_attention: too many queries and heads");
+  p.row_blocks = a.row_blocks;
+  p.splits = a.splits;
+  const size_t need = pace_cache_attention_workspace_size(n_q, Hq, cache->heads, cache->dim, B, max_q, max_len, window, sinks);
+  if (need) {
+    if (workspace == nullptr || workspace_bytes < need)
+      return set_error(PACE_ERR_WORKSPACE, "pace_cache_attention: workspace %zu < %zu bytes", workspace_bytes, need);
+    PACE_REQUIRE(aligned16(workspace), "pace_cache_attention: workspace must be 16-byte aligned");
+    p.part = static_cast<float*>(workspace);
+    p.ml = p.part + static_cast<size_t>(a.splits) * n_q * Hq * cache->dim;
+  }
   if (debug_checks()) {
     try {
       if ((st = debug_attention(p, stream)) != PACE_OK) return st;
@@ -557,12 +996,9 @@ pace_status_t pace_cache_attention(const uint16_t* q, int n_q, int Hq, const pac
       return set_error(PACE_ERR_INVALID_ARG, "pace_cache_attention: no host memory for the debug checks");
     }
   }
-  const dim3 g(static_cast<unsigned>(blocks)), th(256);
-  if (cache->dim == 128 && cache->bits == 16) hipLaunchKernelGGL((attend<128, 16>), g, th, 0, stream, p);
-  else if (cache->dim == 128) hipLaunchKernelGGL((attend<128, 8>), g, th, 0, stream, p);
-  else if (cache->bits == 16) hipLaunchKernelGGL((attend<80, 16>), g, th, 0, stream, p);
-  else hipLaunchKernelGGL((attend<80, 8>), g, th, 0, stream, p);
-  return check_launch("pace_cache_attention");
+  if (cache->dim == 128)
+    return cache->bits == 16 ? launch_attend<128, 16>(p, a, stream) : launch_attend<128, 8>(p, a, stream);
+  return cache->bits == 16 ? launch_attend<80, 16>(p, a, stream) : launch_attend<80, 8>(p, a, stream);
 }
 
 }  // extern "C"
