@@ -498,20 +498,25 @@ pace_status_t pace_cache_attention(const uint16_t* q, int n_q, int Hq, const pac
                                    uint16_t* o, float* lse, void* workspace, size_t workspace_bytes,
                                    hipStream_t stream);
 
+/* Workspace bytes for pace_gemm_w4 (partial sums where K is split over workgroups; 0 for M <= 16). */
+size_t pace_gemm_w4_workspace_size(int M, int N, int K);
+
 /*
  * C = x W^T for a few rows x and weights of 4 bits: pace_gemm_bf16's product and epilogues with
  *   W[n, k] = (q[n, k] - zero[n, k / group]) * scale[n, k / group],
  *   w         uint8 [N, K / 2]: q[n, k] is the low half of byte k / 2 for even k, the high half for odd k.
  *   scale     bf16 [N, K / group]; zero uint8 [N, K / group] with values 0..15, or NULL (8 everywhere).
  *   group     32, 64 or 128; K a positive multiple of group.
- *   x         bf16 [M, K] row-major; x and w 16-byte aligned.  Any M >= 1; the weights are read once for every
- *             64 rows.
+ *   x         bf16 [M, K] row-major; x and w 16-byte aligned.  1 <= M <= 65,535; the weights are read once for
+ *             every 64 rows.
  *   bias, residual, epilogue, C  as in pace_gemm_bf16.
- * Products accumulate in fp32.  x must be finite.  Each operand under 2 GiB.
+ * Products accumulate in fp32, in an order fixed by the shape.  x must be finite (a row with an infinity comes out as
+ * NaN).  Each operand under 2 GiB.  The workspace must be 16-byte aligned; calls that may run at the same time need
+ * one each.
  */
 pace_status_t pace_gemm_w4(const uint16_t* x, const uint8_t* w, const uint16_t* scale, const uint8_t* zero,
                            const float* bias, const uint16_t* residual, uint16_t* C, int M, int N, int K, int group,
-                           int epilogue, hipStream_t stream);
+                           int epilogue, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -80,8 +80,9 @@ _PROTOS = {
     "pace_cache_attention_workspace_size": (c_size, [c_int] * 9),
     "pace_cache_attention": (c_int, [c_void, c_int, c_int, c_void, c_void, c_int, c_int, c_void, c_int, c_void, c_int,
                                      c_int, c_int, c_float, c_void, c_void, c_void, c_size, c_void]),
+    "pace_gemm_w4_workspace_size": (c_size, [c_int, c_int, c_int]),
     "pace_gemm_w4": (c_int, [c_void, c_void, c_void, c_void, c_void, c_void, c_void, c_int, c_int, c_int, c_int, c_int,
-                             c_void]),
+                             c_void, c_size, c_void]),
 }
 
 EXPORTED = tuple(_PROTOS.keys())
@@ -124,24 +125,6 @@ def _ptr(t: Optional[torch.Tensor]):
 
 def _stream():
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
-
-
-class _Nothing:
-    def __enter__(self):
-        pass
-
-    def __exit__(self, *exc):
-        pass
-
-
-_NOTHING = _Nothing()
-
-
-def _on(device: torch.device):
-    """Makes `device` current for a call whose tensors live on another one."""
-    if device.type != "cuda":
-        raise PaceError("tensor must live on the GPU")
-    return _NOTHING if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
 
 def _ws(nbytes: int, device) -> torch.Tensor:
@@ -530,10 +513,63 @@ def gather_rows(src: torch.Tensor, idx: torch.Tensor, out: Optional[torch.Tensor
 
 
 # ---------------------------------------------------------------- decode over a pruned context
+# A decode step makes many short calls, so these marshal with as few Python operations as the checks allow.
 class _KvCacheStruct(ctypes.Structure):
     """Mirror of pace_kv_cache (include/pace.h)."""
     _fields_ = [("k", c_void), ("v", c_void), ("k_scale", c_void), ("v_scale", c_void), ("num_pages", c_int),
                 ("heads", c_int), ("page", c_int), ("dim", c_int), ("bits", c_int)]
+
+
+_INT3 = ctypes.c_int * 3
+_BF16, _F32, _I32, _U8, _E4M3 = (torch.bfloat16, torch.float32, torch.int32, torch.uint8, torch.float8_e4m3fn)
+
+
+def _arg(t: Optional[torch.Tensor], dtype, shape: tuple, device: int, name: str):
+    """The address of a contiguous tensor of this type and shape on GPU number `device`, None for None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise PaceError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on GPU {device}, not {t.dtype} "
+                        f"{list(t.shape)} (strides {t.stride()}) on {t.device}")
+    return t.data_ptr()
+
+
+def _rows_arg(t: torch.Tensor, heads: int, dim: int, n: int, device: int, name: str):
+    """Address and row stride of bf16 rows [n, heads, dim] whose heads lie one after the other."""
+    if t.dtype is not _BF16 or t.shape != (n, heads, dim) or t.get_device() != device:
+        raise PaceError(f"{name} must be bfloat16 [{n}, {heads}, {dim}] on GPU {device}, not {t.dtype} {list(t.shape)} on "
+                        f"{t.device}")
+    row, head, one = t.stride()
+    if one != 1 or (heads > 1 and head != dim):
+        raise PaceError(f"{name}: the heads of a row must lie one after the other, strides are {t.stride()}")
+    return t.data_ptr(), (row if n > 1 else heads * dim)
+
+
+def _scratch(workspace: Optional[torch.Tensor], device: int):
+    """Address and bytes of a workspace (uint8, 1-D)."""
+    if workspace is None:
+        return None, 0
+    return _arg(workspace, _U8, (workspace.numel(),), device, "workspace"), workspace.numel()
+
+
+def _gpu_of(t: torch.Tensor) -> int:
+    device = t.get_device()
+    if device < 0:
+        raise PaceError("tensor must live on the GPU")
+    return device
+
+
+def _call(name: str, device: int, *args):
+    """A library call on the current stream of GPU number `device`, made current for it if it is not."""
+    L = _lib or lib()
+    if device != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            st = getattr(L, name)(*args, torch.cuda.current_stream(device).cuda_stream)
+    else:
+        # the stream's address without a Stream object around it
+        st = getattr(L, name)(*args, torch._C._cuda_getCurrentRawStream(device))
+    if st:
+        _check(st, name)
 
 
 class KvCache:
@@ -542,60 +578,32 @@ class KvCache:
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                  v_scale: Optional[torch.Tensor] = None):
-        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
+        shape, dtype = k.shape, k.dtype
+        if len(shape) != 4 or v.shape != shape or v.dtype is not dtype:
             raise PaceError("k and v must be [num_pages, heads, page, dim] of one shape and type")
-        if k.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
-            raise PaceError(f"cache type {k.dtype} is not bfloat16 or float8_e4m3fn")
-        bits = 16 if k.dtype == torch.bfloat16 else 8
-        n, heads, page, dim = k.shape
-        for s in (k_scale, v_scale):
-            if bits == 8 and (s is None or s.dtype != torch.float32 or s.shape != (n, heads)):
-                raise PaceError("8-bit pages need float32 scales [num_pages, heads]")
+        if dtype is not _BF16 and dtype is not _E4M3:
+            raise PaceError(f"cache type {dtype} is not bfloat16 or float8_e4m3fn")
+        bits = 16 if dtype is _BF16 else 8
+        n, heads, page, dim = shape
         if bits == 16:
             k_scale = v_scale = None
-        _one_device(k, v, k_scale, v_scale)
+        elif k_scale is None or v_scale is None or k_scale.shape != (n, heads) or v_scale.shape != (n, heads):
+            raise PaceError("8-bit pages need float32 scales [num_pages, heads]")
+        self.device = _gpu_of(k)
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.struct = _KvCacheStruct(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), n, heads, page, dim, bits)
+        self.heads, self.page, self.dim = heads, page, dim
+        self.struct = _KvCacheStruct(_arg(k, dtype, shape, self.device, "k"), _arg(v, dtype, shape, self.device, "v"),
+                                     _arg(k_scale, _F32, (n, heads), self.device, "k_scale"),
+                                     _arg(v_scale, _F32, (n, heads), self.device, "v_scale"), n, heads, page, dim, bits)
         self.ref = ctypes.byref(self.struct)
 
     @classmethod
     def empty(cls, num_pages: int, heads: int, page: int, dim: int, dtype=torch.bfloat16, device="cuda"):
         """A cache over newly allocated, uninitialised pages."""
         k, v = (torch.empty((num_pages, heads, page, dim), dtype=dtype, device=device) for _ in range(2))
-        if dtype == torch.bfloat16:
+        if dtype is _BF16:
             return cls(k, v)
-        return cls(k, v, *(torch.empty((num_pages, heads), dtype=torch.float32, device=device) for _ in range(2)))
-
-
-def _one_device(first, *others):
-    dev = first.device
-    for t in others:
-        if t is not None and t.device != dev:
-            raise PaceError(f"tensors on {dev} and {t.device}: all must be on one device")
-
-
-def _typed(t: Optional[torch.Tensor], dtype, name: str, *shape):
-    """The device pointer of a contiguous tensor of this type and shape (None: any size)."""
-    if t is None:
-        return None
-    if t.dtype != dtype:
-        raise PaceError(f"{name} must be {dtype}, not {t.dtype}")
-    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
-        raise PaceError(f"{name} must have shape {list(shape)}, not {list(t.shape)}")
-    return _ptr(t)
-
-
-def _strided_rows(t: torch.Tensor, name: str, heads: Optional[int], dim: int):
-    """Pointer and row stride of bf16 rows [n, heads, dim] whose heads lie one after the other."""
-    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
-        raise PaceError(f"{name} must be bfloat16 [tokens, {'heads' if heads is None else heads}, {dim}], not {t.dtype} "
-                        f"{list(t.shape)}")
-    if not t.is_cuda:
-        raise PaceError("tensor must live on the GPU")
-    n, h, d = t.shape
-    if t.stride(2) != 1 or (h > 1 and t.stride(1) != d):
-        raise PaceError(f"{name}: the heads of a row must lie one after the other")
-    return ctypes.c_void_p(t.data_ptr()), t.stride(0) if n > 1 else h * d
+        return cls(k, v, *(torch.empty((num_pages, heads), dtype=_F32, device=device) for _ in range(2)))
 
 
 def cache_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cache: KvCache, cu_new: torch.Tensor,
@@ -607,39 +615,35 @@ def cache_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, ca
     cache.  q, k, v: bf16 [n_src, heads, dim], rows of any stride (slices of a fused projection); rows int32 [n_new]:
     the source rows to take (a selection's kept indices).  Returns the rotated queries [n_new, Hq, dim], or None
     without q."""
-    dim, heads = cache.struct.dim, cache.struct.heads
-    n_src = k.shape[0]
-    kp, ks = _strided_rows(k, "k", heads, dim)
-    vp, vs = _strided_rows(v, "v", heads, dim)
-    if v.shape[0] != n_src or (q is not None and q.shape[0] != n_src):
-        raise PaceError("q, k and v must have one number of rows")
-    B, max_pages = block_table.shape if block_table.dim() == 2 else (0, 0)
+    gpu, dim, n_src = cache.device, cache.dim, k.shape[0]
+    if block_table.dim() != 2:
+        raise PaceError("block_table must be [B, max_pages]")
+    B, max_pages = block_table.shape
     n_new = n_src if rows is None else rows.numel()
+    kp, ks = _rows_arg(k, cache.heads, dim, n_src, gpu, "k")
+    vp, vs = _rows_arg(v, cache.heads, dim, n_src, gpu, "v")
     qp, qs, hq = None, 0, 0
-    if q is not None:
-        qp, qs = _strided_rows(q, "q", None, dim)
-        hq = q.shape[1]
+    if q is None:
+        q_out = None
+    else:
+        hq = q.shape[1] if q.dim() == 3 else 0
+        qp, qs = _rows_arg(q, hq, dim, n_src, gpu, "q")
         if q_out is None:
-            q_out = torch.empty((n_new, hq, dim), dtype=torch.bfloat16, device=q.device)
-    axes = 1
+            q_out = torch.empty((n_new, hq, dim), dtype=_BF16, device=q.device)
+    axes, sec = 1, None
     if positions is not None:
         axes = 1 if positions.dim() == 1 else positions.shape[0]
-        if positions.dtype != torch.int32 or positions.numel() != axes * n_src:
-            raise PaceError(f"positions must be int32 [n_src] or [axes, n_src], not {positions.dtype} "
-                            f"{list(positions.shape)}")
-        if axes == 3 and (sections is None or len(sections) != 3):
-            raise PaceError("three position axes need three sections")
-    _one_device(cache.k, q, k, v, cu_new, ctx_len, block_table, positions, inv_freq, rows, q_out)
-    with _on(cache.k.device):
-        _check(lib().pace_cache_append(
-            qp, qs, kp, ks, vp, vs, n_src, hq, _typed(rows, torch.int32, "rows", None),
-            _typed(cu_new, torch.int32, "cu_new", B + 1), B, n_new, int(max_new),
-            _typed(ctx_len, torch.int32, "ctx_len", B), _typed(block_table, torch.int32, "block_table", None, None),
-            max_pages, _ptr(positions), axes, (ctypes.c_int * 3)(*sections) if axes == 3 else None,
-            _typed(inv_freq, torch.float32, "inv_freq", dim // 2), cache.ref,
-            _typed(q_out if q is not None else None, torch.bfloat16, "q_out", n_new, hq, dim), _stream()),
-            "pace_cache_append")
-    return q_out if q is not None else None
+        if axes == 3:
+            if sections is None or len(sections) != 3:
+                raise PaceError("three position axes need three sections")
+            sec = _INT3(*sections)
+    _call("pace_cache_append", gpu, qp, qs, kp, ks, vp, vs, n_src, hq, _arg(rows, _I32, (n_new,), gpu, "rows"),
+          _arg(cu_new, _I32, (B + 1,), gpu, "cu_new"), B, n_new, max_new, _arg(ctx_len, _I32, (B,), gpu, "ctx_len"),
+          _arg(block_table, _I32, (B, max_pages), gpu, "block_table"), max_pages,
+          _arg(positions, _I32, (n_src,) if positions is not None and positions.dim() == 1 else (axes, n_src), gpu,
+               "positions"), axes, sec, _arg(inv_freq, _F32, (dim // 2,), gpu, "inv_freq"), cache.ref,
+          _arg(q_out, _BF16, (n_new, hq, dim), gpu, "q_out"))
+    return q_out
 
 
 def cache_attention(q: torch.Tensor, cache: KvCache, cu_q: torch.Tensor, seq_len: torch.Tensor,
@@ -648,54 +652,53 @@ def cache_attention(q: torch.Tensor, cache: KvCache, cu_q: torch.Tensor, seq_len
                     lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """Attention of q bf16 [n_q, Hq, dim] over a paged cache that holds its tokens already.  cu_q int32 [B + 1],
     seq_len int32 [B], block_table int32 [B, max_pages] on the GPU.  Returns (o, lse [Hq, n_q] or None)."""
-    n_q, hq, dim = q.shape
-    c = cache.struct
-    if dim != c.dim:
-        raise PaceError(f"q has head dim {dim}, the cache {c.dim}")
-    B, max_pages = block_table.shape if block_table.dim() == 2 else (0, 0)
+    gpu, dim = cache.device, cache.dim
+    if q.dim() != 3 or block_table.dim() != 2:
+        raise PaceError("q must be [n_q, Hq, dim], block_table [B, max_pages]")
+    n_q, hq, _ = q.shape
+    B, max_pages = block_table.shape
     if o is None:
         o = torch.empty_like(q)
     if not want_lse:
         lse = None
     elif lse is None:
-        lse = torch.empty((hq, n_q), dtype=torch.float32, device=q.device)
-    _one_device(cache.k, q, cu_q, seq_len, block_table, o, lse, workspace)
+        lse = torch.empty((hq, n_q), dtype=_F32, device=q.device)
     if workspace is None:
-        need = lib().pace_cache_attention_workspace_size(n_q, hq, c.heads, dim, B, int(max_q), int(max_len),
-                                                         int(window), int(sinks))
+        need = (_lib or lib()).pace_cache_attention_workspace_size(n_q, hq, cache.heads, dim, B, max_q, max_len, window,
+                                                                   sinks)
         if need:
-            workspace = _ws(need, q.device)
-    with _on(q.device):
-        _check(lib().pace_cache_attention(
-            _typed(q, torch.bfloat16, "q", None, None, None), n_q, hq, cache.ref,
-            _typed(cu_q, torch.int32, "cu_q", B + 1), B, int(max_q), _typed(seq_len, torch.int32, "seq_len", B),
-            int(max_len), _typed(block_table, torch.int32, "block_table", None, None), max_pages, int(window), int(sinks),
-            1.0 / math.sqrt(dim) if scale is None else float(scale), _typed(o, torch.bfloat16, "o", n_q, hq, dim),
-            _typed(lse, torch.float32, "lse", hq, n_q), _ptr(workspace), 0 if workspace is None else workspace.numel(),
-            _stream()), "pace_cache_attention")
+            workspace = torch.empty(need, dtype=_U8, device=q.device)
+    _call("pace_cache_attention", gpu, _arg(q, _BF16, (n_q, hq, dim), gpu, "q"), n_q, hq, cache.ref,
+          _arg(cu_q, _I32, (B + 1,), gpu, "cu_q"), B, max_q, _arg(seq_len, _I32, (B,), gpu, "seq_len"), max_len,
+          _arg(block_table, _I32, (B, max_pages), gpu, "block_table"), max_pages, window, sinks,
+          dim ** -0.5 if scale is None else scale, _arg(o, _BF16, (n_q, hq, dim), gpu, "o"),
+          _arg(lse, _F32, (hq, n_q), gpu, "lse"),
+          *_scratch(workspace, gpu))
     return o, lse
 
 
 def gemm_w4(x: torch.Tensor, w: torch.Tensor, scale: torch.Tensor, zero: Optional[torch.Tensor] = None,
             bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, epilogue: int = 0,
-            out: Optional[torch.Tensor] = None) -> torch.Tensor:
+            out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """C = x W^T with 4-bit weights: x bf16 [M, K]; w uint8 [N, K / 2] (low half first); scale bf16 [N, K / group];
     zero uint8 like scale, or None (8); bias, residual and epilogue as in gemm_bf16."""
-    if x.dim() != 2 or scale.dim() != 2 or scale.shape[1] < 1:
+    gpu = _gpu_of(x)
+    if x.dim() != 2 or scale.dim() != 2:
         raise PaceError("x and scale must be 2-D")
     M, K = x.shape
     N, groups = scale.shape
-    if K % groups:
+    if groups < 1 or K % groups:
         raise PaceError(f"K={K} is not a multiple of the {groups} groups")
     cols = N // 2 if epilogue == 2 else N
     if out is None:
-        out = torch.empty((M, cols), dtype=torch.bfloat16, device=x.device)
-    _one_device(x, w, scale, zero, bias, residual, out)
-    with _on(x.device):
-        _check(lib().pace_gemm_w4(
-            _typed(x, torch.bfloat16, "x", M, K), _typed(w, torch.uint8, "w", N, K // 2),
-            _typed(scale, torch.bfloat16, "scale", N, groups), _typed(zero, torch.uint8, "zero", N, groups),
-            _typed(bias, torch.float32, "bias", N), _typed(residual, torch.bfloat16, "residual", M, cols),
-            _typed(out, torch.bfloat16, "out", M, cols), M, N, K, K // groups, int(epilogue), _stream()),
-            "pace_gemm_w4")
+        out = torch.empty((M, cols), dtype=_BF16, device=x.device)
+    if workspace is None and M > 16:
+        need = (_lib or lib()).pace_gemm_w4_workspace_size(M, N, K)
+        if need:
+            workspace = torch.empty(need, dtype=_U8, device=x.device)
+    _call("pace_gemm_w4", gpu, _arg(x, _BF16, (M, K), gpu, "x"), _arg(w, _U8, (N, K // 2), gpu, "w"),
+          _arg(scale, _BF16, (N, groups), gpu, "scale"), _arg(zero, _U8, (N, groups), gpu, "zero"),
+          _arg(bias, _F32, (N,), gpu, "bias"), _arg(residual, _BF16, (M, cols), gpu, "residual"),
+          _arg(out, _BF16, (M, cols), gpu, "out"), M, N, K, K // groups, epilogue,
+          *_scratch(workspace, gpu))
     return out

@@ -31,7 +31,7 @@ def attend(c=None, **kw):
 
 
 def w4(**kw):
-    a = dict(x=P, w=P, scale=P, zero=None, bias=None, residual=None, C=P, M=1, N=8, K=128, group=64, epilogue=0, stream=None)
+    a = dict(x=P, w=P, scale=P, zero=None, bias=None, residual=None, C=P, M=1, N=8, K=128, group=64, epilogue=0, ws=None, wsb=0, stream=None)
     a.update(kw)
     return pace.lib().pace_gemm_w4(*a.values()), pace.lib().pace_last_error().decode()
 
@@ -103,10 +103,22 @@ def test_attention_workspace():
     (dict(x=None), "null"), (dict(w=None), "null"), (dict(scale=None), "null"), (dict(C=None), "null"), (dict(epilogue=3), "epilogue"),
     (dict(epilogue=-1), "epilogue"), (dict(epilogue=1), "residual"), (dict(epilogue=2, N=7), "even"), (dict(group=16), "group"),
     (dict(group=0), "group"), (dict(K=96), "K="), (dict(K=0), "K="), (dict(M=0), "M="), (dict(N=0), "N="), (dict(x=ODD), "aligned"),
-    (dict(w=ODD), "aligned"), (dict(M=1 << 24, K=128), "2 GiB"), (dict(N=1 << 26, K=128), "2 GiB")])
+    (dict(w=ODD), "aligned"), (dict(M=1 << 24, K=128), "2 GiB"), (dict(M=65536), "65,535"), (dict(N=1 << 26, K=128), "2 GiB")])
 def test_w4(bad, word):
     st, msg = w4(**bad)
     assert st == 1 and word in msg
+
+
+def test_w4_workspace():
+    size = pace.lib().pace_gemm_w4_workspace_size
+    assert size(16, 3584, 14336) == 0 and size(0, 8, 128) == 0 and size(1, -8, 128) == 0
+    need = size(48, 64, 14336)
+    if need:
+        for ws, wsb in ((None, 0), (P, need - 1)):
+            st, msg = w4(M=48, N=64, K=14336, ws=ws, wsb=wsb)
+            assert st == 3 and "workspace" in msg
+        st, msg = w4(M=48, N=64, K=14336, ws=ODD, wsb=need)
+        assert st == 1 and "aligned" in msg
 
 
 def test_binding_refuses_what_it_cannot_pass_on():
@@ -126,5 +138,3 @@ def test_binding_refuses_what_it_cannot_pass_on():
     x, w = torch.zeros((1, 128), dtype=torch.bfloat16), torch.zeros((4, 64), dtype=torch.uint8)
     with pytest.raises(pace.PaceError, match="GPU"):
         pace.gemm_w4(x, w, torch.ones((4, 2), dtype=torch.bfloat16))
-    with pytest.raises(pace.PaceError, match="groups"):
-        pace.gemm_w4(x, w, torch.ones((4, 3), dtype=torch.bfloat16))
