@@ -472,7 +472,7 @@ pace_status_t pace_cache_append(const uint16_t* q, long long q_stride, const uin
  * Workspace bytes for pace_cache_attention with these arguments (partial results where few rows share
  * a long context; 0 where none are needed).
  */
-size_t pace_cache_attention_workspace_size(int n_q, int Hq, int heads, int dim, int B, int max_q, int max_len,
+size_t pace_cache_attention_workspace_size(int n_q, int Hq, int heads, int dim, int bits, int B, int max_q, int max_len,
                                            int window, int sinks);
 
 /*

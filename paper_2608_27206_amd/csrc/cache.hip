@@ -12,6 +12,8 @@ namespace pace {
 namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -305,23 +307,28 @@ struct AttendParams {
   const int32_t *cu, *len;
   uint16_t* o;
   float* lse;
-  float *part, *ml;          // partial results [splits, n_q * Hq, D] and their (maximum, sum)
+  float* part;               // partial results [splits, n_q * Hq, D + 4]: D values, maximum, sum
   Pool pool;
   int n_q, Hq, group, B, max_q, max_len, window, sinks;
-  int row_blocks, splits;
+  int row_blocks, splits, chunk;   // row blocks of a KV head, most parts of its keys, tiles per part
   float scale_log2;
 };
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kTile = 32;          // keys per step of a wave
-constexpr int kSplitTiles = 8;     // least tiles per split of a sequence
+// Keys per step of a wave: 16 KiB of K and V at d = 128 either way.
+constexpr int tile_keys(int bits) { return bits == 16 ? 32 : 64; }
 
 __device__ __forceinline__ f32x4 mfma16(uint4 a, uint4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Cached keys and values are read once: loads that do not ask the caches to keep them (attention over 131,071
+// tokens 56.6 us against 61.2, 48 sequences in 8 bits 106 against 112).
+__device__ __forceinline__ u32x4 stream16(const void* p) { return __builtin_nontemporal_load(static_cast<const u32x4*>(p)); }
+__device__ __forceinline__ u32x2 stream8(const void* p) { return __builtin_nontemporal_load(static_cast<const u32x2*>(p)); }
 
 // Two e4m3 codes (the low or high pair of a dword) as two bf16 values: exact.
 template <bool HI>
@@ -332,12 +339,19 @@ __device__ __forceinline__ uint4 e4m3_bf16x8(uint32_t a, uint32_t b) {
   return make_uint4(e4m3_bf16<false>(a), e4m3_bf16<true>(a), e4m3_bf16<false>(b), e4m3_bf16<true>(b));
 }
 
+// The sign bits of the values of a dword (two bf16, four e4m3) that are infinite or NaN.
+template <int BITS>
+__device__ __forceinline__ uint32_t not_finite(uint32_t u) {
+  // all exponent bits set (e4m3: all bits but the sign): one more carries into the sign's place and no further
+  return BITS == 16 ? ((u & 0x7f807f80u) + 0x00800080u) & 0x80008000u : ((u & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+}
+
 // What a sequence's queries are and the tiles that queries i_lo..i_hi of it see.
 struct Span {
   int row0, nq, len;         // first row of q, queries, cached tokens
   int p_lo, p_hi;            // places of the first and last query
   int head_tiles, tail0, tiles;   // tiles [0, head_tiles) and [tail0, ...), tiles in all
-  __device__ __forceinline__ int base(int x) const { return kTile * (x < head_tiles ? x : tail0 + x - head_tiles); }
+  __device__ __forceinline__ int tile(int x) const { return x < head_tiles ? x : tail0 + x - head_tiles; }
 };
 __device__ __forceinline__ Span queries_of(const AttendParams& p, int b) {
   Span s;
@@ -350,28 +364,32 @@ __device__ __forceinline__ Span queries_of(const AttendParams& p, int b) {
   s.len = s.len > p.max_len ? p.max_len : s.len;
   return s;
 }
+template <int T>
 __device__ __forceinline__ void tiles_of(const AttendParams& p, int i_lo, int i_hi, Span* s) {
   s->p_lo = s->len - s->nq + i_lo;
   s->p_hi = s->len - s->nq + i_hi;
-  const int end = s->p_hi < 0 ? 0 : s->p_hi / kTile + 1;
+  const int end = s->p_hi < 0 ? 0 : s->p_hi / T + 1;
   const int first = p.window == 0 ? 0 : s->p_lo - p.window + 1;      // p_lo < 2^31 and window >= 0: no overflow
-  s->tail0 = first <= 0 ? 0 : first / kTile;
+  s->tail0 = first <= 0 ? 0 : first / T;
   const int sinks = p.sinks < s->p_hi + 1 ? p.sinks : s->p_hi + 1;
-  s->head_tiles = sinks <= 0 ? 0 : (sinks + kTile - 1) / kTile;
+  s->head_tiles = sinks <= 0 ? 0 : (sinks + T - 1) / T;
   if (s->tail0 <= s->head_tiles) { s->tail0 = 0; s->head_tiles = 0; }
   s->tiles = end - s->tail0 + s->head_tiles;
 }
-// How many parts a sequence's tiles are split into.
+// How many parts a row block's tiles are split into: parts of one size over all sequences, so that workgroups are
+// alike where lengths are not.
 __device__ __forceinline__ int splits_of(const AttendParams& p, int tiles) {
-  const int most = (tiles + kSplitTiles - 1) / kSplitTiles;
-  return most < 1 ? 1 : most < p.splits ? most : p.splits;
+  const int s = (tiles + p.chunk - 1) / p.chunk;
+  return s < 1 ? 1 : s < p.splits ? s : p.splits;
 }
 
-// A sequence's page of a 16-key half tile, or -1.
-__device__ __forceinline__ int page_of(const AttendParams& p, const int32_t* table, int key) {
+// A sequence's table entry for a key (or its last one), and the page that it stands for: -1 where there is none.
+__device__ __forceinline__ int entry_of(const AttendParams& p, const int32_t* table, int key) {
   const int j = key >> p.pool.shift;
-  const int pg = j < p.pool.max_pages ? table[j] : -1;
-  return pg >= 0 && pg < p.pool.num_pages ? pg : -1;
+  return table[j < p.pool.max_pages ? j : p.pool.max_pages - 1];
+}
+__device__ __forceinline__ int page_of(const AttendParams& p, int entry, int key) {
+  return key >> p.pool.shift < p.pool.max_pages && entry >= 0 && entry < p.pool.num_pages ? entry : -1;
 }
 
 // Few rows over many keys: memory-bound.  A workgroup = W waves over one (sequence, KV head, block of 16 R
@@ -385,11 +403,18 @@ __device__ __forceinline__ int page_of(const AttendParams& p, const int32_t* tab
 //    ends with 8 consecutive d of each of four blocks.
 // A row's maximum is only raised when a score passes it by 2^8 (a wave-wide vote), so most tiles need no
 // exchange between lanes; probabilities of up to 256 round like others.
+#ifndef VMIN
+#define VMIN 3
+#endif
 template <int D, int BITS, int R, int W>
-__global__ __launch_bounds__(64 * W) void attend_few(const AttendParams p) {
+__global__ __launch_bounds__(64 * W, R == 1 ? VMIN : 2) void attend_few(const AttendParams p) {
+  constexpr int T = tile_keys(BITS), U = T / 32;      // keys per step, in blocks of 32
   constexpr int KS = (D + 31) / 32;                   // products along d
   constexpr int KW = BITS == 16 ? 4 : 2;              // dwords of 8 values
+  constexpr int E = BITS / 8;
   __shared__ float join[W / 2][8 * 4 * R + 2 * R][64];
+  __shared__ uint32_t poison[16 * R][D / 4];
+  __shared__ int poisoned;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   int id = remap_block_id(blockIdx.x, gridDim.x);
   const int split = id % p.splits;
@@ -401,11 +426,16 @@ __global__ __launch_bounds__(64 * W) void attend_few(const AttendParams p) {
   const int rows = sp.nq * p.group, x0 = rb * 16 * R;
   if (x0 >= rows) return;
   const int x1 = x0 + 16 * R < rows ? x0 + 16 * R - 1 : rows - 1;
-  tiles_of(p, x0 / p.group, x1 / p.group, &sp);
+  tiles_of<T>(p, x0 / p.group, x1 / p.group, &sp);
   const int splits = splits_of(p, sp.tiles);
   if (split >= splits) return;
   const int t0 = static_cast<int>(static_cast<long long>(sp.tiles) * split / splits);
   const int t1 = static_cast<int>(static_cast<long long>(sp.tiles) * (split + 1) / splits);
+  if (sp.p_lo != sp.p_hi) {
+    for (int i = threadIdx.x; i < 16 * R * (D / 4); i += 64 * W) poison[i / (D / 4)][i % (D / 4)] = 0;
+  }
+  if (threadIdx.x == 0) poisoned = 0;
+  __syncthreads();
 
   uint4 qf[R][KS];
   int place[R];
@@ -422,83 +452,98 @@ __global__ __launch_bounds__(64 * W) void attend_few(const AttendParams p) {
   }
 
   const int32_t* table = p.pool.table + static_cast<long long>(b) * p.pool.max_pages;
-  const long long head_bytes = static_cast<long long>(p.pool.page) * D * (BITS / 8);
+  const long long head_bytes = static_cast<long long>(p.pool.page) * D * E;
   const int slot_mask = p.pool.page - 1;
-  // lane constants: the K rows (product 0; product 1 is 4 rows on) and V rows of a tile that a lane loads
+  // lane constants: the K rows (product 0; product 1 is 4 rows on) and V rows of a block that a lane loads
   const int krow = 8 * (r >> 2) + (r & 3), khalf = r >> 3, vhalf = g >> 1;
-  const int kd = BITS == 8 && D == 128 ? 16 * g : 8 * g;
-  const int koff = ((krow & 15) * D + kd) * (BITS / 8);
-  const int voff = ((8 * g & 15) * D + (8 * r < D ? 8 * r : 0)) * (BITS / 8);
+  const int koff = ((krow & 15) * D + (BITS == 8 && D == 128 ? 16 * g : 8 * g)) * E;
+  const int voff = ((8 * g & 15) * D + (8 * r < D ? 8 * r : 0)) * E;
 
-  uint32_t kr[2][KS][KW], vr[8][KW];
-  float ks = 1.f, vs = 1.f, ks_n = 1.f, vs_n = 1.f;
-  int pa, pb;                                          // pages of the loaded tile's halves
+  uint32_t kr[U][2][KS][KW], vr[U][8][KW];
+  float ks[U], vs[U], ks_n[U], vs_n[U];
+  // pages of the loaded tile's halves of 16; the table's entries for the next tile, untouched until they are needed (a
+  // test right after the load would wait for it in every tile)
+  int pg[2 * U], entry[2 * U];
 
-  const auto half_base = [&](const void* pool, int key, int pg) {
-    return static_cast<const char*>(pool) + (static_cast<long long>(pg < 0 ? 0 : pg) * p.pool.heads + hk) * head_bytes +
-           static_cast<long long>(key & slot_mask) * D * (BITS / 8);
+  const auto look_up = [&](int base) {
+#pragma unroll
+    for (int h = 0; h < 2 * U; ++h) entry[h] = entry_of(p, table, base + 16 * h);
   };
-  const auto load_k = [&](int base, int a, int c) {
-    const char* from = (khalf ? half_base(p.pool.k, base + 16, c) : half_base(p.pool.k, base, a)) + koff;
+  const auto take_pages = [&](int base) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const char* f = from + 4 * t * D * (BITS / 8);
-      if constexpr (BITS == 8 && D == 128) {
+    for (int h = 0; h < 2 * U; ++h) pg[h] = page_of(p, entry[h], base + 16 * h);
+  };
+  const auto half_base = [&](const void* pool, int key, int page) {
+    return static_cast<const char*>(pool) + (static_cast<long long>(page < 0 ? 0 : page) * p.pool.heads + hk) * head_bytes +
+           static_cast<long long>(key & slot_mask) * D * E;
+  };
+  const auto load_k = [&](int base) {
 #pragma unroll
-        for (int u = 0; u < KS / 2; ++u) {
-          const uint4 x = *reinterpret_cast<const uint4*>(f + 64 * u);
-          kr[t][2 * u][0] = x.x; kr[t][2 * u][1] = x.y; kr[t][2 * u + 1][0] = x.z; kr[t][2 * u + 1][1] = x.w;
-        }
-      } else {
+    for (int u = 0; u < U; ++u) {
+      const int at = base + 32 * u;
+      const char* from = (khalf ? half_base(p.pool.k, at + 16, pg[2 * u + 1]) : half_base(p.pool.k, at, pg[2 * u])) + koff;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-          // D = 80: the last product has 16 values, its upper lanes load the lower ones' again
-          const int at = (32 * s - (32 * s + 32 > D && g >= 2 ? 16 : 0)) * (BITS / 8);
-          if constexpr (BITS == 8) {
-            const uint2 x = *reinterpret_cast<const uint2*>(f + at);
-            kr[t][s][0] = x.x; kr[t][s][1] = x.y;
-          } else {
-            const uint4 x = *reinterpret_cast<const uint4*>(f + at);
-            kr[t][s][0] = x.x; kr[t][s][1] = x.y; kr[t][s][2] = x.z; kr[t][s][3] = x.w;
+      for (int t = 0; t < 2; ++t) {
+        const char* f = from + 4 * t * D * E;
+        if constexpr (BITS == 8 && D == 128) {
+#pragma unroll
+          for (int s = 0; s < KS; s += 2) {
+            const u32x4 x = stream16(f + 32 * s);
+            kr[u][t][s][0] = x.x; kr[u][t][s][1] = x.y; kr[u][t][s + 1][0] = x.z; kr[u][t][s + 1][1] = x.w;
+          }
+        } else {
+#pragma unroll
+          for (int s = 0; s < KS; ++s) {
+            // D = 80: the last product has 16 values, its upper lanes load the lower ones' again
+            const int off = (32 * s - (32 * s + 32 > D && g >= 2 ? 16 : 0)) * E;
+            if constexpr (BITS == 8) {
+              const u32x2 x = stream8(f + off);
+              kr[u][t][s][0] = x.x; kr[u][t][s][1] = x.y;
+            } else {
+              const u32x4 x = stream16(f + off);
+              kr[u][t][s][0] = x.x; kr[u][t][s][1] = x.y; kr[u][t][s][2] = x.z; kr[u][t][s][3] = x.w;
+            }
           }
         }
       }
-    }
-    if constexpr (BITS == 8) {
-      const int pg = vhalf ? c : a;
-      ks_n = p.pool.k_scale[static_cast<long long>(pg < 0 ? 0 : pg) * p.pool.heads + hk];
-    }
-  };
-  const auto load_v = [&](int base, int a, int c) {
-    const char* from = (vhalf ? half_base(p.pool.v, base + 16, c) : half_base(p.pool.v, base, a)) + voff;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const char* f = from + j * D * (BITS / 8);
       if constexpr (BITS == 8) {
-        const uint2 x = *reinterpret_cast<const uint2*>(f);
-        vr[j][0] = x.x; vr[j][1] = x.y;
-      } else {
-        const uint4 x = *reinterpret_cast<const uint4*>(f);
-        vr[j][0] = x.x; vr[j][1] = x.y; vr[j][2] = x.z; vr[j][3] = x.w;
+        const int page = vhalf ? pg[2 * u + 1] : pg[2 * u];
+        const long long ph = static_cast<long long>(page < 0 ? 0 : page) * p.pool.heads + hk;
+        ks_n[u] = p.pool.k_scale[ph];
+        vs_n[u] = p.pool.v_scale[ph];
       }
     }
-    if constexpr (BITS == 8) {
-      const int pg = vhalf ? c : a;
-      vs_n = p.pool.v_scale[static_cast<long long>(pg < 0 ? 0 : pg) * p.pool.heads + hk];
+  };
+  const auto load_v = [&](int base) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = base + 32 * u;
+      const char* from = (vhalf ? half_base(p.pool.v, at + 16, pg[2 * u + 1]) : half_base(p.pool.v, at, pg[2 * u])) + voff;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const char* f = from + j * D * E;
+        if constexpr (BITS == 8) {
+          const u32x2 x = stream8(f);
+          vr[u][j][0] = x.x; vr[u][j][1] = x.y;
+        } else {
+          const u32x4 x = stream16(f);
+          vr[u][j][0] = x.x; vr[u][j][1] = x.y; vr[u][j][2] = x.z; vr[u][j][3] = x.w;
+        }
+      }
     }
   };
-  // the A operand of O^T's product c from the loaded V rows (those of key `only`, or all: -1)
-  const auto v_operand = [&](int c, int only) {
+  // the A operand of O^T's product c over block u
+  const auto v_operand = [&](int u, int c) {
     uint32_t a[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       if constexpr (BITS == 8) {
-        const uint32_t y = __builtin_amdgcn_perm(vr[2 * k + 1][c >> 2], vr[2 * k][c >> 2], (c & 2) ? 0x07030602u : 0x05010400u);
+        const uint32_t y =
+            __builtin_amdgcn_perm(vr[u][2 * k + 1][c >> 2], vr[u][2 * k][c >> 2], (c & 2) ? 0x07030602u : 0x05010400u);
         a[k] = (c & 1) ? e4m3_bf16<true>(y) : e4m3_bf16<false>(y);
       } else {
-        a[k] = __builtin_amdgcn_perm(vr[2 * k + 1][c >> 1], vr[2 * k][c >> 1], (c & 1) ? 0x07060302u : 0x05040100u);
+        a[k] = __builtin_amdgcn_perm(vr[u][2 * k + 1][c >> 1], vr[u][2 * k][c >> 1], (c & 1) ? 0x07060302u : 0x05040100u);
       }
-      if (only >= 0) a[k] = 8 * g + 2 * k == only ? a[k] & 0xffffu : 8 * g + 2 * k + 1 == only ? a[k] & 0xffff0000u : 0u;
     }
     return make_uint4(a[0], a[1], a[2], a[3]);
   };
@@ -514,77 +559,74 @@ __global__ __launch_bounds__(64 * W) void attend_few(const AttendParams p) {
   }
 
   int x = t0 + w;
-  int pa_n = -1, pb_n = -1;
   if (x < t1) {
-    const int base = sp.base(x);
-    pa = page_of(p, table, base);
-    pb = page_of(p, table, base + 16);
-    load_k(base, pa, pb);
-    load_v(base, pa, pb);
-    if (x + W < t1) {
-      const int nb = sp.base(x + W);
-      pa_n = page_of(p, table, nb);
-      pb_n = page_of(p, table, nb + 16);
-    }
+    look_up(T * sp.tile(x));
+    take_pages(T * sp.tile(x));
+    load_k(T * sp.tile(x));
+    load_v(T * sp.tile(x));
+    if (x + W < t1) look_up(T * sp.tile(x + W));
   }
   for (; x < t1; x += W) {
-    const int base = sp.base(x);
+    const int base = T * sp.tile(x);
     const bool more = x + W < t1;
-    const int nbase = more ? sp.base(x + W) : 0;
-    const bool ok_a = pa >= 0, ok_b = pb >= 0;
-    if constexpr (BITS == 8) { ks = ks_n; vs = vs_n; }
-    // every key of the tile is seen by every row
-    const bool full = ok_a && ok_b && base + kTile - 1 <= sp.p_lo &&
-                      (p.window == 0 || base > sp.p_hi - p.window || base + kTile <= p.sinks);
-    f32x4 st[R][2];
+    const int next = more ? T * sp.tile(x + W) : 0;
+    bool ok[2 * U], full = base + T - 1 <= sp.p_lo && (p.window == 0 || base > sp.p_hi - p.window || base + T <= p.sinks);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-#pragma unroll
-      for (int t = 0; t < R; ++t) st[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        uint4 a;
-        if constexpr (BITS == 8) a = e4m3_bf16x8(kr[u][s][0], kr[u][s][1]);
-        else a = make_uint4(kr[u][s][0], kr[u][s][1], kr[u][s][2], kr[u][s][3]);
-        if (32 * s + 32 > D && g >= 2) a = make_uint4(0, 0, 0, 0);
-#pragma unroll
-        for (int t = 0; t < R; ++t) st[t][u] = mfma16(a, qf[t][s], st[t][u]);
-      }
+    for (int h = 0; h < 2 * U; ++h) {
+      ok[h] = pg[h] >= 0;
+      full = full && ok[h];                            // every row sees every key of the tile
     }
-    pa = pa_n;
-    pb = pb_n;
-    if (more) {
-      load_k(nbase, pa, pb);
-      if (x + 2 * W < t1) {
-        const int nb = sp.base(x + 2 * W);
-        pa_n = page_of(p, table, nb);
-        pb_n = page_of(p, table, nb + 16);
-      }
-    }
-    const float f = BITS == 8 ? p.scale_log2 * ks : p.scale_log2;
-    uint4 pf[R];
-    uint32_t seen[R];                                  // bit j: row sees key base + 8 g + j
-    bool odd = false;                                  // some key is seen by some rows only and its V is not finite
+    f32x4 st[R][U][2];
 #pragma unroll
-    for (int t = 0; t < R; ++t) {
-      float s[8];
+    for (int u = 0; u < U; ++u) {
+      if constexpr (BITS == 8) { ks[u] = ks_n[u]; vs[u] = vs_n[u]; }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[j] = st[t][j >> 2][j & 3] * f;
-      seen[t] = 0xffu;
-      if (!full) {
-        seen[t] = 0;
-        const bool ok = vhalf ? ok_b : ok_a;
+      for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int key = base + 8 * g + j;
-          const bool sees = ok && key <= place[t] && (p.window == 0 || key > place[t] - p.window || key < p.sinks);
-          seen[t] |= sees ? 1u << j : 0u;
-          s[j] = sees ? s[j] : -INFINITY;
+        for (int t = 0; t < R; ++t) st[t][u][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          uint4 a;
+          if constexpr (BITS == 8) a = e4m3_bf16x8(kr[u][h][s][0], kr[u][h][s][1]);
+          else a = make_uint4(kr[u][h][s][0], kr[u][h][s][1], kr[u][h][s][2], kr[u][h][s][3]);
+          if (32 * s + 32 > D && g >= 2) a = make_uint4(0, 0, 0, 0);
+#pragma unroll
+          for (int t = 0; t < R; ++t) st[t][u][h] = mfma16(a, qf[t][s], st[t][u][h]);
         }
       }
-      float top = s[0];
+    }
+    __builtin_amdgcn_sched_barrier(0);                 // K's registers are free from here on, not earlier
+    if (more) {
+      take_pages(next);
+      load_k(next);
+      if (x + 2 * W < t1) look_up(T * sp.tile(x + 2 * W));
+    }
+    uint4 pf[R][U];
 #pragma unroll
-      for (int j = 1; j < 8; ++j) top = fmaxf(top, s[j]);
+    for (int t = 0; t < R; ++t) {
+      float s[U][8];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float f = BITS == 8 ? p.scale_log2 * ks[u] : p.scale_log2;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[u][j] = st[t][u][j >> 2][j & 3] * f;
+      }
+      if (!full) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int key = base + 32 * u + 8 * g + j;
+            const bool sees = (vhalf ? ok[2 * u + 1] : ok[2 * u]) && key <= place[t] &&
+                              (p.window == 0 || key > place[t] - p.window || key < p.sinks);
+            s[u][j] = sees ? s[u][j] : -INFINITY;
+          }
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, s[u][j]);
       if (__any(top > m[t] + 8.f)) {
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -596,75 +638,90 @@ __global__ __launch_bounds__(64 * W) void attend_few(const AttendParams p) {
         for (int c = 0; c < 8; ++c) acc[t][c] *= k;
       }
       const float mz = m[t] == -INFINITY ? 0.f : m[t];
-      float e[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        e[j] = exp2_fast(s[j] - mz);
-        l[t] += e[j];
-        if constexpr (BITS == 8) e[j] *= vs;
-      }
-      if (!full && BITS == 8) {
+      for (int u = 0; u < U; ++u) {
+        float e[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = (seen[t] >> j & 1u) ? e[j] : 0.f;     // a scale nobody set may be NaN
+        for (int j = 0; j < 8; ++j) {
+          e[j] = exp2_fast(s[u][j] - mz);
+          l[t] += e[j];
+          // a scale of hidden keys may be anything
+          if constexpr (BITS == 8) e[j] = full || s[u][j] != -INFINITY ? e[j] * vs[u] : 0.f;
+        }
+        // probabilities are rounded to bf16 for the product (relative 2^-8); their sum is not
+        pf[t][u] = pack8(e);
       }
-      // probabilities are rounded to bf16 for the product (relative 2^-8); their sum is not
-      pf[t] = pack8(e);
     }
+    bool odd = false;                                  // a V value that is not finite, seen by some rows only
     if (!full) {
-      // V rows that no row sees become 0 (0 * NaN is NaN)
+      uint32_t wild = 0;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int key = base + 8 * g + j;
-        const bool sees = (vhalf ? ok_b : ok_a) && key <= sp.p_hi && (p.window == 0 || key > sp.p_lo - p.window || key < p.sinks);
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int d = 0; d < KW; ++d) vr[j][d] = sees ? vr[j][d] : 0u;
-      }
-      if (sp.p_lo != sp.p_hi) {
-        // where the rows differ, V values that are not finite must reach only the rows that see them
-        bool bad = false;
+        for (int j = 0; j < 8; ++j) {
+          // V rows that no row sees become 0 (0 * NaN is NaN)
+          const int key = base + 32 * u + 8 * g + j;
+          const bool sees = (vhalf ? ok[2 * u + 1] : ok[2 * u]) && key <= sp.p_hi &&
+                            (p.window == 0 || key > sp.p_lo - p.window || key < p.sinks);
+#pragma unroll
+          for (int d = 0; d < KW; ++d) {
+            vr[u][j][d] = sees ? vr[u][j][d] : 0u;
+            wild |= not_finite<BITS>(vr[u][j][d]);
+          }
+        }
+      odd = sp.p_lo != sp.p_hi && __any(wild != 0);
+    }
+    if (odd) {
+      // Values that are not finite must reach the rows that see them and no others, but a hidden one's 0 times NaN is
+      // NaN: the products take 0 for them, and `poison` notes which results get a +inf or -inf (1, 2; a NaN
+      // counts as both).  Rare, so it reads V again, two values of a key per lane.
+#pragma unroll
+      for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
           for (int d = 0; d < KW; ++d) {
-            const uint32_t u = vr[j][d];
-            if constexpr (BITS == 16) {
-              bad |= (u & 0x7f80u) == 0x7f80u || (u & 0x7f800000u) == 0x7f800000u;
-            } else {
-#pragma unroll
-              for (int e = 0; e < 4; ++e) bad |= (u >> 8 * e & 0x7fu) == 0x7fu;
-            }
+            asm volatile("" : "+v"(vr[u][j][d]));      // or the tests above stay in 32 registers until here
+            const uint32_t m = not_finite<BITS>(vr[u][j][d]);
+            vr[u][j][d] &= ~(BITS == 16 ? (m >> 15) * 0xffffu : (m >> 7) * 0xffu);
           }
-        odd = __any(bad);
-      }
-    }
-    if (!odd) {
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        const uint4 a = v_operand(c, -1);
-#pragma unroll
-        for (int t = 0; t < R; ++t) acc[t][c] = mfma16(a, pf[t], acc[t][c]);
-      }
-    } else {
-      // key by key, each added to the rows that see it alone
+      poisoned = 1;
 #pragma unroll 1
-      for (int key = 0; key < kTile; ++key) {
-        bool mine[R];
-#pragma unroll
-        for (int t = 0; t < R; ++t)
-          mine[t] = __shfl(seen[t], (key >> 3) * 16 + r, 64) >> (key & 7) & 1u;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          const uint4 a = v_operand(c, key);
-#pragma unroll
-          for (int t = 0; t < R; ++t) {
-            const f32x4 y = mfma16(a, pf[t], f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[t][c][i] += mine[t] ? y[i] : 0.f;
+      for (int key = base; key < base + T; ++key) {
+        const int page = page_of(p, entry_of(p, table, key), key);
+        if (page < 0 || 2 * lane >= D) continue;
+        const char* from = half_base(p.pool.v, key, page) + 2 * lane * E;
+        uint32_t kind = 0;                             // a byte for each of the lane's two values
+        for (int e = 0; e < 2; ++e) {
+          uint32_t mag, neg;
+          if constexpr (BITS == 16) {
+            const uint32_t h = *reinterpret_cast<const uint16_t*>(from + 2 * e);
+            mag = h & 0x7fffu;
+            neg = h >> 15;
+          } else {
+            mag = (*reinterpret_cast<const uint8_t*>(from + e) & 0x7fu) == 0x7fu ? 0x7fffu : 0u;
+            neg = 0;
           }
+          kind |= (mag > 0x7f80u ? 3u : mag == 0x7f80u ? 1u << neg : 0u) << 8 * e;
+        }
+        if (kind == 0) continue;
+        for (int x = x0; x <= x1; ++x) {
+          const int at = sp.len - sp.nq + x / p.group;
+          if (key <= at && (p.window == 0 || key > at - p.window || key < p.sinks))
+            atomicOr(&poison[x - x0][lane >> 1], kind << 16 * (lane & 1));
         }
       }
     }
-    if (more) load_v(nbase, pa, pb);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const uint4 a = v_operand(u, c);
+#pragma unroll
+        for (int t = 0; t < R; ++t) acc[t][c] = mfma16(a, pf[t][u], acc[t][c]);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) load_v(next);
   }
 
   // the waves join in halves: maximum, sum and O of the upper half go through LDS
@@ -698,109 +755,530 @@ __global__ __launch_bounds__(64 * W) void attend_few(const AttendParams p) {
     }
     __syncthreads();
   }
-  if (w != 0) return;
+  if (w == 0) {
+    if (poisoned) {
 #pragma unroll
-  for (int t = 0; t < R; ++t) {
-    float sum = l[t] + __shfl_xor(l[t], 16, 64);
-    sum += __shfl_xor(sum, 32, 64);
-    const int x = x0 + 16 * t + r;
-    if (x > x1) continue;
-    const int n = sp.row0 + x / p.group, h = hk * p.group + x % p.group;
-    const long long row = static_cast<long long>(n) * p.Hq + h;
-    if (splits > 1) {
-      const long long at = static_cast<long long>(split) * p.n_q * p.Hq + row;
+      for (int t = 0; t < R; ++t)
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int d = 8 * (4 * g + i) + c;
+            const uint32_t k = d < D ? poison[16 * t + r][d >> 2] >> 8 * (d & 3) : 0u;
+            acc[t][c][i] += (k & 1u) ? INFINITY : 0.f;
+            acc[t][c][i] -= (k & 2u) ? INFINITY : 0.f;
+          }
+    }
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+      float sum = l[t] + __shfl_xor(l[t], 16, 64);
+      sum += __shfl_xor(sum, 32, 64);
+      const int x = x0 + 16 * t + r;
+      if (x > x1) continue;
+      const int n = sp.row0 + x / p.group, h = hk * p.group + x % p.group;
+      const long long out = static_cast<long long>(n) * p.Hq + h;
+      if (splits > 1) {
+        const long long row = static_cast<long long>(split) * p.n_q * p.Hq + out;
+        float* to = p.part + row * (D + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int d = 8 * (4 * g + i);
+          if (d >= D) continue;
+          *reinterpret_cast<float4*>(to + d) = make_float4(acc[t][0][i], acc[t][1][i], acc[t][2][i], acc[t][3][i]);
+          *reinterpret_cast<float4*>(to + d + 4) = make_float4(acc[t][4][i], acc[t][5][i], acc[t][6][i], acc[t][7][i]);
+        }
+        if (g == 0) *reinterpret_cast<float2*>(to + D) = make_float2(m[t], sum);
+        continue;
+      }
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int d = 8 * (4 * g + i);
         if (d >= D) continue;
-        float4* to = reinterpret_cast<float4*>(p.part + at * D + d);
-        to[0] = make_float4(acc[t][0][i], acc[t][1][i], acc[t][2][i], acc[t][3][i]);
-        to[1] = make_float4(acc[t][4][i], acc[t][5][i], acc[t][6][i], acc[t][7][i]);
+        float y[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) y[c] = acc[t][c][i] * inv;
+        *reinterpret_cast<uint4*>(p.o + out * D + d) = pack8(y);
       }
-      if (g == 0) *reinterpret_cast<float2*>(p.ml + 2 * at) = make_float2(m[t], sum);
-      continue;
+      if (g == 0 && p.lse) p.lse[static_cast<long long>(h) * p.n_q + n] = sum == 0.f ? -INFINITY : (m[t] + log2f(sum)) * kLn2;
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int d = 8 * (4 * g + i);
-      if (d >= D) continue;
-      float y[8];
-#pragma unroll
-      for (int c = 0; c < 8; ++c) y[c] = acc[t][c][i] * inv;
-      *reinterpret_cast<uint4*>(p.o + row * D + d) = pack8(y);
-    }
-    if (g == 0 && p.lse) p.lse[static_cast<long long>(h) * p.n_q + n] = sum == 0.f ? -INFINITY : (m[t] + log2f(sum)) * kLn2;
   }
 }
 
-// Joins the parts of the rows whose keys were split: one wave per row.
-template <int D>
-__global__ __launch_bounds__(256) void attend_join(const AttendParams p, int rows_per_block) {
-  const int lane = threadIdx.x & 63;
-  const long long id = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  const int h = static_cast<int>(id % p.Hq);
-  const int i = static_cast<int>(id / p.Hq % p.max_q), b = static_cast<int>(id / p.Hq / p.max_q);
-  if (b >= p.B) return;
+// Many rows (drafts of many heads, the next chunk of a prompt): bound by the matrix products.  A workgroup = 2 groups of 4
+// waves over the same 128 rows of one KV head (32 a wave); the groups take the tiles of 64 keys in turn and join at the
+// end, so that two waves on every SIMD overlap one's products with the other's exponentials also where the grid has no
+// more than a workgroup for a CU.  A group stages its tile through registers (paged rows and 8-bit codes need their own
+// addresses and a conversion) into LDS, the next one in flight while this one is worked on:
+//  K row-major, 16-byte pieces swizzled by the row; S^T = K Q^T by 32x32x16 products, so a lane owns one row (the
+//    column) and 16 keys of each half of the tile.
+//  V transposed on the way in (4 keys x 8 d in registers), [d][key] with the keys of each 16 in the order in which the
+//    lanes hold P^T (groups of 4: 0, 2, 1, 3), so that O^T = V^T P^T takes P straight from registers.
+constexpr int kManyRows = 128, kManyTile = 64, kManyThreads = 512;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ f32x16 mfma32(uint4 a, uint4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+template <int D, int BITS>
+__global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParams p) {
+  constexpr int T = kManyTile, E = BITS / 8, KS = D / 16, DT = (D + 31) / 32;
+  constexpr int CPR = BITS == 16 ? D / 8 : D / 16;    // 16-byte pieces of a cached row
+  constexpr int NK = (T * CPR + 255) / 256;           // of them per thread
+  constexpr int KW = BITS == 16 ? 4 : 2;
+  __shared__ uint4 kt[2][2][T * 16];                  // [group][buffer]: [key][16 pieces]
+  __shared__ uint4 vt[2][2][32 * DT * 8];             // [d][8 pieces of 8 keys]
+  __shared__ uint32_t poison[kManyRows][D / 16];      // 2 bits for each value
+  __shared__ int poisoned;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int gr = wave >> 2, w = wave & 3, tid = threadIdx.x & 255, c32 = lane & 31, g = lane >> 5;
+  int id = remap_block_id(blockIdx.x, gridDim.x);
+  const int rb = id % p.row_blocks;
+  id /= p.row_blocks;
+  const int split = id % p.splits;
+  id /= p.splits;
+  const int hk = id % p.pool.heads, b = id / p.pool.heads;
+  Span sp = queries_of(p, b);
+  const int rows = sp.nq * p.group, x0 = rb * kManyRows;
+  if (x0 >= rows) return;
+  const int x1 = x0 + kManyRows < rows ? x0 + kManyRows - 1 : rows - 1;
+  tiles_of<T>(p, x0 / p.group, x1 / p.group, &sp);
+  const int splits = splits_of(p, sp.tiles);
+  if (split >= splits) return;
+  const int t0 = static_cast<int>(static_cast<long long>(sp.tiles) * split / splits);
+  const int t1 = static_cast<int>(static_cast<long long>(sp.tiles) * (split + 1) / splits);
+  for (int i = threadIdx.x; i < kManyRows * (D / 16); i += kManyThreads) poison[i / (D / 16)][i % (D / 16)] = 0;
+  if (threadIdx.x == 0) poisoned = 0;
+
+  const int x = x0 + 32 * w + c32, xi = x <= x1 ? x : x1;
+  const int place = sp.len - sp.nq + xi / p.group;
+  uint4 qf[KS];
+  {
+    const uint16_t* from = p.q + (static_cast<long long>(sp.row0 + xi / p.group) * p.Hq + hk * p.group + xi % p.group) * D + 8 * g;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const uint4*>(from + 16 * s);
+  }
+
+  const int32_t* table = p.pool.table + static_cast<long long>(b) * p.pool.max_pages;
+  const long long head_bytes = static_cast<long long>(p.pool.page) * D * E;
+  const int slot_mask = p.pool.page - 1;
+  const int dg = lane & 15, vq = lane >> 4;            // V: this thread's 8 d, and which 4 of its wave's 16 keys
+  uint32_t kr[NK][4], vr[4][KW];
+  int entry[4], pg[4];                                 // the next tile's entries, the staged tile's pages (16 keys each)
+  float ks[4], vs[4], ks_n[4], vs_n[4];
+
+  const auto look_up = [&](int base) {
+#pragma unroll
+    for (int h = 0; h < 4; ++h) entry[h] = entry_of(p, table, base + 16 * h);
+  };
+  const auto row_of = [&](const void* pool, int key, int page) {
+    return static_cast<const char*>(pool) + (static_cast<long long>(page < 0 ? 0 : page) * p.pool.heads + hk) * head_bytes +
+           static_cast<long long>(key & slot_mask) * D * E;
+  };
+  const auto load = [&](int base) {
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      pg[h] = page_of(p, entry[h], base + 16 * h);
+      if constexpr (BITS == 8) {
+        const long long ph = static_cast<long long>(pg[h] < 0 ? 0 : pg[h]) * p.pool.heads + hk;
+        ks_n[h] = p.pool.k_scale[ph];
+        vs_n[h] = p.pool.v_scale[ph];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const int at = i * 256 + tid, row = at / CPR < T ? at / CPR : T - 1, piece = at % CPR;
+      const int page = row < 32 ? (row < 16 ? pg[0] : pg[1]) : (row < 48 ? pg[2] : pg[3]);
+      const u32x4 y = *reinterpret_cast<const u32x4*>(row_of(p.pool.k, base + row, page) + 16 * piece);
+      kr[i][0] = y.x; kr[i][1] = y.y; kr[i][2] = y.z; kr[i][3] = y.w;
+    }
+    const int page = w < 2 ? (w == 0 ? pg[0] : pg[1]) : (w == 2 ? pg[2] : pg[3]);
+    const char* from = row_of(p.pool.v, base + 16 * w + 4 * vq, page) + (8 * dg < D ? 8 * dg : 0) * E;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (BITS == 8) {
+        const u32x2 y = *reinterpret_cast<const u32x2*>(from + j * D * E);
+        vr[j][0] = y.x; vr[j][1] = y.y;
+      } else {
+        const u32x4 y = *reinterpret_cast<const u32x4*>(from + j * D * E);
+        vr[j][0] = y.x; vr[j][1] = y.y; vr[j][2] = y.z; vr[j][3] = y.w;
+      }
+    }
+  };
+  // every row of the workgroup sees every key of the tile (whose pages are in pg)
+  const auto is_full = [&](int base) {
+    return pg[0] >= 0 && pg[1] >= 0 && pg[2] >= 0 && pg[3] >= 0 && base + T - 1 <= sp.p_lo &&
+           (p.window == 0 || base > sp.p_hi - p.window || base + T <= p.sinks);
+  };
+  const auto store = [&](int base, int buf) {
+    uint4* kl = kt[gr][buf];
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const int at = i * 256 + tid, row = at / CPR, piece = at % CPR;
+      if (T * CPR % 256 != 0 && row >= T) continue;
+      if constexpr (BITS == 16) {
+        kl[row * 16 + (piece ^ (row & 15))] = make_uint4(kr[i][0], kr[i][1], kr[i][2], kr[i][3]);
+      } else {
+        kl[row * 16 + ((2 * piece) ^ (row & 15))] = e4m3_bf16x8(kr[i][0], kr[i][1]);
+        kl[row * 16 + ((2 * piece + 1) ^ (row & 15))] = e4m3_bf16x8(kr[i][2], kr[i][3]);
+      }
+    }
+    if (!is_full(base)) {
+      // V rows that no row sees become 0 (0 * NaN is NaN); where the rows differ, values that are not finite too, and
+      // `poison` notes which results get a +inf or -inf instead (1, 2; a NaN counts as both)
+      uint32_t wild = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int key = base + 16 * w + 4 * vq + j;
+        const bool sees = (w < 2 ? (w == 0 ? pg[0] : pg[1]) : (w == 2 ? pg[2] : pg[3])) >= 0 && key <= sp.p_hi &&
+                          (p.window == 0 || key > sp.p_lo - p.window || key < p.sinks);
+#pragma unroll
+        for (int d = 0; d < KW; ++d) {
+          vr[j][d] = sees ? vr[j][d] : 0u;
+          const uint32_t m = not_finite<BITS>(vr[j][d]);
+          wild |= m;
+          if (sp.p_lo != sp.p_hi) vr[j][d] &= ~(BITS == 16 ? (m >> 15) * 0xffffu : (m >> 7) * 0xffu);
+        }
+      }
+      if (sp.p_lo != sp.p_hi && __any(wild != 0)) {
+        poisoned = 1;
+#pragma unroll 1
+        for (int key = base + 16 * w; key < base + 16 * w + 16; ++key) {
+          const int page = page_of(p, entry_of(p, table, key), key);
+          if (page < 0 || 2 * lane >= D) continue;
+          const char* from = row_of(p.pool.v, key, page) + 2 * lane * E;
+          uint32_t kind = 0;
+          for (int e = 0; e < 2; ++e) {
+            uint32_t mag, neg;
+            if constexpr (BITS == 16) {
+              const uint32_t h = *reinterpret_cast<const uint16_t*>(from + 2 * e);
+              mag = h & 0x7fffu;
+              neg = h >> 15;
+            } else {
+              mag = (*reinterpret_cast<const uint8_t*>(from + e) & 0x7fu) == 0x7fu ? 0x7fffu : 0u;
+              neg = 0;
+            }
+            kind |= (mag > 0x7f80u ? 3u : mag == 0x7f80u ? 1u << neg : 0u) << 2 * e;
+          }
+          if (kind == 0) continue;
+          for (int y = x0; y <= x1; ++y) {
+            const int at = sp.len - sp.nq + y / p.group;
+            if (key <= at && (p.window == 0 || key > at - p.window || key < p.sinks))
+              atomicOr(&poison[y - x0][lane >> 3], kind << 4 * (lane & 7));
+          }
+        }
+      }
+    }
+    // 4 keys x 8 d: for each d, the 4 keys are one 8-byte unit of its row
+    uint2* vl = reinterpret_cast<uint2*>(vt[gr][buf]);
+    if (8 * dg < D) {
+      const int unit = 4 * w + 2 * (vq & 1) + (vq >> 1);          // keys 4 q of a chunk of 16: q = 0, 2, 1, 3
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        uint2 y;
+        if constexpr (BITS == 8) {
+          const uint32_t lo = __builtin_amdgcn_perm(vr[1][c >> 2], vr[0][c >> 2], (c & 2) ? 0x07030602u : 0x05010400u);
+          const uint32_t hi = __builtin_amdgcn_perm(vr[3][c >> 2], vr[2][c >> 2], (c & 2) ? 0x07030602u : 0x05010400u);
+          y = (c & 1) ? make_uint2(e4m3_bf16<true>(lo), e4m3_bf16<true>(hi)) : make_uint2(e4m3_bf16<false>(lo), e4m3_bf16<false>(hi));
+        } else {
+          const uint32_t sel = (c & 1) ? 0x07060302u : 0x05040100u;
+          y = make_uint2(__builtin_amdgcn_perm(vr[1][c >> 1], vr[0][c >> 1], sel), __builtin_amdgcn_perm(vr[3][c >> 1], vr[2][c >> 1], sel));
+        }
+        const int d = 8 * dg + c;
+        vl[d * 16 + (((unit >> 1) ^ ((d ^ (d >> 3)) & 7)) << 1 | (unit & 1))] = y;
+      }
+    }
+  };
+
+  f32x16 acc[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
+  float m = -INFINITY, l = 0.f;
+  const int mine = t1 - t0 - gr > 0 ? (t1 - t0 - gr + 1) / 2 : 0, most = (t1 - t0 + 1) / 2;   // group 0 has the most
+  bool full_cur = false, ok_cur[4] = {false, false, false, false};
+  const auto tile_base = [&](int i) { return T * sp.tile(t0 + gr + 2 * i); };
+  const auto took = [&](int base) {
+    full_cur = is_full(base);
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      ok_cur[h] = pg[h] >= 0;
+      if constexpr (BITS == 8) { ks[h] = ks_n[h]; vs[h] = vs_n[h]; }
+    }
+  };
+  __syncthreads();                                     // poison is clear
+  if (mine > 0) {
+    look_up(tile_base(0));
+    load(tile_base(0));
+    store(tile_base(0), 0);
+    took(tile_base(0));
+    if (mine > 1) look_up(tile_base(1));
+  }
+  __syncthreads();
+  for (int it = 0; it < most; ++it) {
+    const bool more = it + 1 < mine;
+    if (more) load(tile_base(it + 1));
+    if (it + 2 < mine) look_up(tile_base(it + 2));
+    if (it < mine) {
+      const int base = tile_base(it), buf = it & 1;
+      const uint4* kl = kt[gr][buf];
+      const uint4* vl = vt[gr][buf];
+      f32x16 st[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st[h][i] = 0.f;
+        const int row = 32 * h + c32;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) st[h] = mfma32(kl[row * 16 + ((2 * s + g) ^ (row & 15))], qf[s], st[h]);
+      }
+      float f[4];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) f[h] = BITS == 8 ? p.scale_log2 * ks[h] : p.scale_log2;
+      float top = -INFINITY;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float s = st[h][i] * f[2 * h + (i >> 3)];
+          if (!full_cur) {
+            const int key = base + 32 * h + 8 * (i >> 2) + 4 * g + (i & 3);
+            const bool sees = ok_cur[2 * h + (i >> 3)] && key <= place && (p.window == 0 || key > place - p.window || key < p.sinks);
+            s = sees ? s : -INFINITY;
+          }
+          st[h][i] = s;
+          top = fmaxf(top, s);
+        }
+      if (__any(top > m + 8.f)) {
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float mn = fmaxf(m, top), k = mn == m ? 1.f : exp2_fast(m - mn);
+        m = mn;
+        l *= k;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[t][i] *= k;
+      }
+      const float mz = m == -INFINITY ? 0.f : m;
+      uint4 pf[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        float e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float s = st[c >> 1][8 * (c & 1) + i];
+          e[i] = exp2_fast(s - mz);
+          l += e[i];
+          if constexpr (BITS == 8) e[i] = full_cur || s != -INFINITY ? e[i] * vs[c] : 0.f;
+        }
+        // probabilities are rounded to bf16 for the product (relative 2^-8); their sum is not
+        pf[c] = pack8(e);
+      }
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        const int d = 32 * t + c32;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[t] = mfma32(vl[d * 8 + ((2 * c + g) ^ ((d ^ (d >> 3)) & 7))], pf[c], acc[t]);
+      }
+    }
+    if (more) {
+      store(tile_base(it + 1), (it + 1) & 1);
+      took(tile_base(it + 1));
+    }
+    __syncthreads();
+  }
+
+  // group 1's maximum, sum and O go to group 0 through the K tiles' LDS
+  float* join = reinterpret_cast<float*>(&kt[0][0][0]);
+  constexpr int PART = DT == 4 ? 2 : DT;               // tiles of O at a time
+  static_assert(sizeof(kt) >= (4 * PART * 16 + 8) * 64 * sizeof(float), "the waves' parts of O must fit the K tiles");
+#pragma unroll
+  for (int t = 0; t < DT; t += PART) {
+    if (gr == 1) {
+#pragma unroll
+      for (int u = 0; u < PART; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) join[((w * PART + u) * 16 + i) * 64 + lane] = acc[t + u][i];
+      if (t == 0) {
+        join[(4 * PART * 16 + 2 * w) * 64 + lane] = m;
+        join[(4 * PART * 16 + 2 * w + 1) * 64 + lane] = l;
+      }
+    }
+    __syncthreads();
+    if (gr == 0) {
+      const float m2 = join[(4 * PART * 16 + 2 * w) * 64 + lane], l2 = join[(4 * PART * 16 + 2 * w + 1) * 64 + lane];
+      const float mn = fmaxf(m, m2);
+      const float k1 = mn == m ? 1.f : exp2_fast(m - mn), k2 = mn == m2 ? 1.f : exp2_fast(m2 - mn);
+#pragma unroll
+      for (int u = 0; u < PART; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          acc[t + u][i] = acc[t + u][i] * k1 + join[((w * PART + u) * 16 + i) * 64 + lane] * k2;
+      if (t + PART >= DT) {
+        l = l * k1 + l2 * k2;
+        m = mn;
+      }
+    }
+    __syncthreads();
+  }
+  if (gr != 0) return;
+  if (poisoned) {
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int d = 32 * t + 8 * (i >> 2) + 4 * g + (i & 3);
+        const uint32_t k = d < D ? poison[32 * w + c32][d >> 4] >> 2 * (d & 15) : 0u;
+        acc[t][i] += (k & 1u) ? INFINITY : 0.f;
+        acc[t][i] -= (k & 2u) ? INFINITY : 0.f;
+      }
+  }
+  const float sum = l + __shfl_xor(l, 32, 64);
+  if (x > x1) return;
+  const int n = sp.row0 + x / p.group, h = hk * p.group + x % p.group;
+  const long long out = static_cast<long long>(n) * p.Hq + h;
+  if (splits > 1) {
+    float* to = p.part + (static_cast<long long>(split) * p.n_q * p.Hq + out) * (D + 4);
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int d = 32 * t + 8 * j + 4 * g;
+        if (d < D) *reinterpret_cast<float4*>(to + d) = make_float4(acc[t][4 * j], acc[t][4 * j + 1], acc[t][4 * j + 2], acc[t][4 * j + 3]);
+      }
+    if (g == 0) *reinterpret_cast<float2*>(to + D) = make_float2(m, sum);
+    return;
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int d = 32 * t + 8 * j + 4 * g;
+      if (d < D)
+        *reinterpret_cast<uint2*>(p.o + out * D + d) = make_uint2(pack_bf16x2(acc[t][4 * j] * inv, acc[t][4 * j + 1] * inv),
+                                                                  pack_bf16x2(acc[t][4 * j + 2] * inv, acc[t][4 * j + 3] * inv));
+    }
+  if (g == 0 && p.lse) p.lse[static_cast<long long>(h) * p.n_q + n] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * kLn2;
+}
+
+// Joins the parts of the rows whose keys were split: a workgroup per row, its waves take the parts in turn.
+constexpr int kJoinWaves = 8;
+template <int D, int T>
+__global__ __launch_bounds__(64 * kJoinWaves) void attend_join(const AttendParams p, int block_rows) {
+  __shared__ float part[kJoinWaves][3][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int id = blockIdx.x;
+  const int h = id % p.Hq;
+  id /= p.Hq;
+  const int i = id % p.max_q, b = id / p.max_q;
   Span sp = queries_of(p, b);
   if (i >= sp.nq) return;
   // the tiles of the row block that this row was in
-  const int rows = sp.nq * p.group, x = i * p.group + h % p.group, x0 = x / rows_per_block * rows_per_block;
-  const int x1 = x0 + rows_per_block < rows ? x0 + rows_per_block - 1 : rows - 1;
-  tiles_of(p, x0 / p.group, x1 / p.group, &sp);
+  const int rows = sp.nq * p.group, x = i * p.group + h % p.group, x0 = x / block_rows * block_rows;
+  const int x1 = x0 + block_rows < rows ? x0 + block_rows - 1 : rows - 1;
+  tiles_of<T>(p, x0 / p.group, x1 / p.group, &sp);
   const int splits = splits_of(p, sp.tiles);
   if (splits == 1) return;
   const int n = sp.row0 + i;
   const long long row = static_cast<long long>(n) * p.Hq + h, all = static_cast<long long>(p.n_q) * p.Hq;
-  float top = -INFINITY;
-  for (int s = 0; s < splits; ++s) top = fmaxf(top, p.ml[2 * (s * all + row)]);
-  float sum = 0.f, y0 = 0.f, y1 = 0.f;
-  for (int s = 0; s < splits; ++s) {
-    const long long at = s * all + row;
-    const float m = p.ml[2 * at], k = m == top ? 1.f : exp2_fast(m - top);
-    sum += p.ml[2 * at + 1] * k;
-    if (2 * lane < D) {
-      const float2 v = *reinterpret_cast<const float2*>(p.part + at * D + 2 * lane);
-      y0 += v.x * k;
-      y1 += v.y * k;
+  float m = -INFINITY, sum = 0.f, y0 = 0.f, y1 = 0.f;
+  for (int s0 = w; s0 < splits; s0 += 4 * kJoinWaves) {
+    float ms[4], ls[4];
+    float2 v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int s = s0 + u * kJoinWaves;
+      const float* from = p.part + ((s < splits ? s : s0) * all + row) * (D + 4);
+      const float2 ml = *reinterpret_cast<const float2*>(from + D);
+      ms[u] = s < splits ? ml.x : -INFINITY;
+      ls[u] = s < splits ? ml.y : 0.f;
+      v[u] = make_float2(0.f, 0.f);
+      if (s < splits && 2 * lane < D) v[u] = *reinterpret_cast<const float2*>(from + 2 * lane);
     }
+    const float mn = fmaxf(m, fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3])));
+    const float k = m == mn ? 1.f : exp2_fast(m - mn);
+    m = mn;
+    sum *= k;
+    y0 *= k;
+    y1 *= k;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float f = ms[u] == mn ? 1.f : exp2_fast(ms[u] - mn);
+      sum += ls[u] * f;
+      y0 += v[u].x * f;
+      y1 += v[u].y * f;
+    }
+  }
+  part[w][0][lane] = y0;
+  part[w][1][lane] = y1;
+  part[w][2][lane] = lane == 0 ? m : sum;
+  __syncthreads();
+  if (w != 0) return;
+  float top = part[0][2][0];
+#pragma unroll
+  for (int u = 1; u < kJoinWaves; ++u) top = fmaxf(top, part[u][2][0]);
+  sum = y0 = y1 = 0.f;
+#pragma unroll
+  for (int u = 0; u < kJoinWaves; ++u) {
+    const float f = part[u][2][0] == top ? 1.f : exp2_fast(part[u][2][0] - top);
+    sum += part[u][2][1] * f;
+    y0 += part[u][0][lane] * f;
+    y1 += part[u][1][lane] * f;
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   if (2 * lane < D) *reinterpret_cast<uint32_t*>(p.o + row * D + 2 * lane) = pack_bf16x2(y0 * inv, y1 * inv);
   if (lane == 0 && p.lse) p.lse[static_cast<long long>(h) * p.n_q + n] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
-// How a call is laid out: rows of a KV head per workgroup, and parts that a sequence's keys are split into.
+// How a call is laid out: rows of a KV head per workgroup, and the parts that a row block's keys are split into.
 struct AttendPlan {
-  int rows, row_blocks, splits;
+  int rows, row_blocks, splits, chunk;
   long long blocks;
 };
-constexpr int kWaves = 8;
-AttendPlan plan_attention(int Hq, int heads, int B, int max_q, int max_len, int window, int sinks) {
+#ifndef VMANY
+#define VMANY 32
+#endif
+constexpr int kWaves = 4;
+AttendPlan plan_attention(int Hq, int heads, int bits, int B, int max_q, int max_len, int window, int sinks) {
   AttendPlan a;
   const long long rows = static_cast<long long>(max_q) * (Hq / heads);
-  a.rows = rows > 16 ? 32 : 16;
+  a.rows = rows > VMANY ? kManyRows : rows > 16 ? 32 : 16;
   a.row_blocks = static_cast<int>((rows + a.rows - 1) / a.rows);
   const long long base = static_cast<long long>(B) * heads * a.row_blocks;
+  if (window >= max_len) window = 0;                  // such a window hides nothing
   long long keys = max_len;
   if (window > 0 && static_cast<long long>(window) + sinks + max_q < keys) keys = static_cast<long long>(window) + sinks + max_q;
-  const long long most = ((keys + kTile - 1) / kTile + kSplitTiles - 1) / kSplitTiles;
-  // enough workgroups for two on every CU
-  long long s = (512 + base - 1) / base;
-  s = s > most ? most : s;
-  a.splits = s < 1 ? 1 : static_cast<int>(s);
+  // tiles that a row block may see at most: sinks and window each begin inside one
+  const int tile = a.rows == kManyRows ? kManyTile : tile_keys(bits);
+  const long long tiles = (keys + tile - 1) / tile + (window > 0 ? 2 : 0);
+  // Workgroups to aim at.  Many rows: one on every CU.  Few: two (32 rows: all that fit; one sequence: its parts are
+  // alike, and more of them cost more to join), or four where lengths differ.
+  const long long aim = a.rows == kManyRows ? 256 : a.rows == 32 || B == 1 ? 512 : 1024;
+  const long long want = aim / base < 1 ? 1 : aim / base, chunk = (tiles + want - 1) / want;
+  const int least = a.rows == kManyRows ? 8 : kWaves;
+  a.chunk = static_cast<int>(chunk < least ? least : chunk);
+  a.splits = static_cast<int>((tiles + a.chunk - 1) / a.chunk);
+  if (a.splits < 1) a.splits = 1;
   a.blocks = base * a.splits;
   return a;
+}
+size_t attend_bytes(const AttendPlan& a, int n_q, int Hq, int dim) {
+  return a.splits == 1 ? 0 : static_cast<size_t>(a.splits) * n_q * Hq * (dim + 4) * sizeof(float);
 }
 
 template <int D, int BITS>
 pace_status_t launch_attend(const AttendParams& p, const AttendPlan& a, hipStream_t stream) {
   const dim3 g(static_cast<unsigned>(a.blocks)), th(64 * kWaves);
   if (a.rows == 16) hipLaunchKernelGGL((attend_few<D, BITS, 1, kWaves>), g, th, 0, stream, p);
-  else hipLaunchKernelGGL((attend_few<D, BITS, 2, kWaves>), g, th, 0, stream, p);
+  else if (a.rows == 32) hipLaunchKernelGGL((attend_few<D, BITS, 2, kWaves>), g, th, 0, stream, p);
+  else hipLaunchKernelGGL((attend_many<D, BITS>), g, dim3(kManyThreads), 0, stream, p);
   if (a.splits > 1) {
-    const long long rows = static_cast<long long>(p.B) * p.max_q * p.Hq;
-    hipLaunchKernelGGL(attend_join<D>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, stream, p, a.rows);
+    const unsigned rows = static_cast<unsigned>(static_cast<long long>(p.B) * p.max_q * p.Hq);
+    if (a.rows == kManyRows) hipLaunchKernelGGL((attend_join<D, kManyTile>), dim3(rows), dim3(64 * kJoinWaves), 0, stream, p, a.rows);
+    else hipLaunchKernelGGL((attend_join<D, tile_keys(BITS)>), dim3(rows), dim3(64 * kJoinWaves), 0, stream, p, a.rows);
   }
   return check_launch("pace_cache_attention");
 }
@@ -945,13 +1423,13 @@ pace_status_t pace_cache_append(const uint16_t* q, long long q_stride, const uin
                  : launch_append<128>(p, cache->bits, row_blocks, page_blocks, stream);
 }
 
-size_t pace_cache_attention_workspace_size(int n_q, int Hq, int heads, int dim, int B, int max_q, int max_len,
+size_t pace_cache_attention_workspace_size(int n_q, int Hq, int heads, int dim, int bits, int B, int max_q, int max_len,
                                            int window, int sinks) {
-  if (n_q < 1 || heads < 1 || Hq < heads || Hq % heads != 0 || dim < 1 || B < 1 || max_q < 1 || max_len < 0 ||
+  if (n_q < 1 || heads < 1 || Hq < heads || Hq % heads != 0 || dim < 1 || (bits != 16 && bits != 8) || B < 1 || max_q < 1 || max_len < 0 ||
       window < 0 || sinks < 0)
     return 0;
-  const AttendPlan a = plan_attention(Hq, heads, B, max_q, max_len, window, sinks);
-  return a.splits == 1 ? 0 : static_cast<size_t>(a.splits) * n_q * Hq * (dim + 2) * sizeof(float);
+  const AttendPlan a = plan_attention(Hq, heads, bits, B, max_q, max_len, window, sinks);
+  return attend_bytes(a, n_q, Hq, dim);
 }
 
 pace_status_t pace_cache_attention(const uint16_t* q, int n_q, int Hq, const pace_kv_cache* cache,
@@ -974,20 +1452,20 @@ pace_status_t pace_cache_attention(const uint16_t* q, int n_q, int Hq, const pac
   if (max_q == 0) return PACE_OK;
   p.q = q; p.cu = cu_q; p.len = seq_len; p.o = o; p.lse = lse;
   p.n_q = n_q; p.Hq = Hq; p.group = Hq / cache->heads; p.B = B; p.max_q = max_q; p.max_len = max_len;
-  p.window = window >= max_len ? 0 : window;          // such a window hides nothing
+  p.window = window >= max_len ? 0 : window;
   p.sinks = sinks; p.scale_log2 = scale * kLog2e;
-  const AttendPlan a = plan_attention(Hq, cache->heads, B, max_q, max_len, window, sinks);
+  const AttendPlan a = plan_attention(Hq, cache->heads, cache->bits, B, max_q, max_len, window, sinks);
   PACE_REQUIRE(a.blocks < (1ll << 31) && static_cast<long long>(B) * max_q * Hq < (1ll << 31),
                "pace_cache_attention: too many queries and heads");
   p.row_blocks = a.row_blocks;
   p.splits = a.splits;
-  const size_t need = pace_cache_attention_workspace_size(n_q, Hq, cache->heads, cache->dim, B, max_q, max_len, window, sinks);
+  p.chunk = a.chunk;
+  const size_t need = attend_bytes(a, n_q, Hq, cache->dim);
   if (need) {
     if (workspace == nullptr || workspace_bytes < need)
       return set_error(PACE_ERR_WORKSPACE, "pace_cache_attention: workspace %zu < %zu bytes", workspace_bytes, need);
     PACE_REQUIRE(aligned16(workspace), "pace_cache_attention: workspace must be 16-byte aligned");
     p.part = static_cast<float*>(workspace);
-    p.ml = p.part + static_cast<size_t>(a.splits) * n_q * Hq * cache->dim;
   }
   if (debug_checks()) {
     try {

@@ -77,7 +77,7 @@ _PROTOS = {
     "pace_cache_append": (c_int, [c_void, c_ll, c_void, c_ll, c_void, c_ll, c_int, c_int, c_void, c_void, c_int, c_int,
                                   c_int, c_void, c_void, c_int, c_void, c_int, c_int_p, c_void, c_void, c_void,
                                   c_void]),
-    "pace_cache_attention_workspace_size": (c_size, [c_int] * 9),
+    "pace_cache_attention_workspace_size": (c_size, [c_int] * 10),
     "pace_cache_attention": (c_int, [c_void, c_int, c_int, c_void, c_void, c_int, c_int, c_void, c_int, c_void, c_int,
                                      c_int, c_int, c_float, c_void, c_void, c_void, c_size, c_void]),
     "pace_gemm_w4_workspace_size": (c_size, [c_int, c_int, c_int]),
@@ -591,7 +591,7 @@ class KvCache:
             raise PaceError("8-bit pages need float32 scales [num_pages, heads]")
         self.device = _gpu_of(k)
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.heads, self.page, self.dim = heads, page, dim
+        self.heads, self.page, self.dim, self.bits = heads, page, dim, bits
         self.struct = _KvCacheStruct(_arg(k, dtype, shape, self.device, "k"), _arg(v, dtype, shape, self.device, "v"),
                                      _arg(k_scale, _F32, (n, heads), self.device, "k_scale"),
                                      _arg(v_scale, _F32, (n, heads), self.device, "v_scale"), n, heads, page, dim, bits)
@@ -664,8 +664,8 @@ def cache_attention(q: torch.Tensor, cache: KvCache, cu_q: torch.Tensor, seq_len
     elif lse is None:
         lse = torch.empty((hq, n_q), dtype=_F32, device=q.device)
     if workspace is None:
-        need = (_lib or lib()).pace_cache_attention_workspace_size(n_q, hq, cache.heads, dim, B, max_q, max_len, window,
-                                                                   sinks)
+        need = (_lib or lib()).pace_cache_attention_workspace_size(n_q, hq, cache.heads, dim, cache.bits, B, max_q, max_len,
+                                                                   window, sinks)
         if need:
             workspace = torch.empty(need, dtype=_U8, device=q.device)
     _call("pace_cache_attention", gpu, _arg(q, _BF16, (n_q, hq, dim), gpu, "q"), n_q, hq, cache.ref,

@@ -85,7 +85,7 @@ def test_no_queries_is_no_error():
 
 def test_attention_workspace():
     size = pace.lib().pace_cache_attention_workspace_size
-    need = size(1, 28, 4, 128, 1, 1, 131072, 0, 0)
+    need = size(1, 28, 4, 128, 8, 1, 1, 131072, 0, 0)
     if need:                                   # a long context of one row is split: its parts need room
         wide = dict(c=cache(heads=4), Hq=28, n_q=1, max_q=1, max_len=131072, max_pages=2048)
         st, msg = attend(**wide)
@@ -94,8 +94,8 @@ def test_attention_workspace():
         assert st == 3 and "workspace" in msg
         st, msg = attend(ws=ODD, wsb=need, **wide)
         assert st == 1 and "aligned" in msg
-    for bad in ((-1, 28, 4, 128, 1, 1, 100, 0, 0), (1, 27, 4, 128, 1, 1, 100, 0, 0), (1, 28, 0, 128, 1, 1, 100, 0, 0),
-                (1, 28, 4, 128, 0, 1, 100, 0, 0), (1, 28, 4, 128, 1, 1, -5, 0, 0)):
+    for bad in ((-1, 28, 4, 128, 8, 1, 1, 9999, 0, 0), (1, 27, 4, 128, 8, 1, 1, 9999, 0, 0), (1, 28, 0, 128, 8, 1, 1, 9999, 0, 0),
+                (1, 28, 4, 128, 4, 1, 1, 9999, 0, 0), (1, 28, 4, 128, 8, 0, 1, 9999, 0, 0), (1, 28, 4, 128, 8, 1, 1, -5, 0, 0)):
         assert size(*bad) == 0
 
 
