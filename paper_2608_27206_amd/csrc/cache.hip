@@ -324,6 +324,13 @@ __device__ __forceinline__ f32x4 mfma16(uint4 a, uint4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// Maximum of three in one instruction.  fmaxf would first canonicalise values fresh from a matrix product; a NaN loses
+// either way.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 
 // Cached keys and values are read once: loads that do not ask the caches to keep them (attention over 131,071
 // tokens 56.6 us against 61.2, 48 sequences in 8 bits 106 against 112).
@@ -622,11 +629,10 @@ __global__ __launch_bounds__(64 * W, R == 1 ? VMIN : 2) void attend_few(const At
             s[u][j] = sees ? s[u][j] : -INFINITY;
           }
       }
-      float top = s[0][0];
+      float top = -INFINITY;
 #pragma unroll
       for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) top = fmaxf(top, s[u][j]);
+        top = fmaxf(top, max3(max3(s[u][0], s[u][1], s[u][2]), max3(s[u][3], s[u][4], s[u][5]), fmaxf(s[u][6], s[u][7])));
       if (__any(top > m[t] + 8.f)) {
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -810,10 +816,14 @@ __global__ __launch_bounds__(64 * W, R == 1 ? VMIN : 2) void attend_few(const At
 // end, so that two waves on every SIMD overlap one's products with the other's exponentials also where the grid has no
 // more than a workgroup for a CU.  A group stages its tile through registers (paged rows and 8-bit codes need their own
 // addresses and a conversion) into LDS, the next one in flight while this one is worked on:
-//  K row-major, 16-byte pieces swizzled by the row; S^T = K Q^T by 32x32x16 products, so a lane owns one row (the
+//  K row-major, rows 16 bytes apart in their banks; S^T = K Q^T by 32x32x16 products, so a lane owns one row (the
 //    column) and 16 keys of each half of the tile.
 //  V transposed on the way in (4 keys x 8 d in registers), [d][key] with the keys of each 16 in the order in which the
-//    lanes hold P^T (groups of 4: 0, 2, 1, 3), so that O^T = V^T P^T takes P straight from registers.
+//    lanes hold P^T (groups of 4: 0, 2, 1, 3), so that O^T = V^T P^T takes P straight from registers; 16-byte pieces
+//    swizzled by d.
+// Operands are read from LDS four products ahead: one at a time, each product waited out its read (253 us against 211;
+// eight ahead do not fit the registers, 239).
+// NP: the pages of a tile, 1 (64 or more tokens a page) or 4 (one for each 16 keys).
 constexpr int kManyRows = 128, kManyTile = 64, kManyThreads = 512;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -821,13 +831,13 @@ __device__ __forceinline__ f32x16 mfma32(uint4 a, uint4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-template <int D, int BITS>
+template <int D, int BITS, int NP>
 __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParams p) {
-  constexpr int T = kManyTile, E = BITS / 8, KS = D / 16, DT = (D + 31) / 32;
+  constexpr int T = kManyTile, E = BITS / 8, KS = D / 16, DT = (D + 31) / 32, KEYS = T / NP;
   constexpr int CPR = BITS == 16 ? D / 8 : D / 16;    // 16-byte pieces of a cached row
   constexpr int NK = (T * CPR + 255) / 256;           // of them per thread
-  constexpr int KW = BITS == 16 ? 4 : 2;
-  __shared__ uint4 kt[2][2][T * 16];                  // [group][buffer]: [key][16 pieces]
+  constexpr int KW = BITS == 16 ? 4 : 2, KROW = 17;   // KROW: a K row's pieces in LDS
+  __shared__ uint4 kt[2][2][T * KROW];                // [group][buffer]: [key][pieces]
   __shared__ uint4 vt[2][2][32 * DT * 8];             // [d][8 pieces of 8 keys]
   __shared__ uint32_t poison[kManyRows][D / 16];      // 2 bits for each value
   __shared__ int poisoned;
@@ -853,11 +863,11 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
 
   const int x = x0 + 32 * w + c32, xi = x <= x1 ? x : x1;
   const int place = sp.len - sp.nq + xi / p.group;
-  uint4 qf[KS];
+  u32x4 qf[KS];
   {
     const uint16_t* from = p.q + (static_cast<long long>(sp.row0 + xi / p.group) * p.Hq + hk * p.group + xi % p.group) * D + 8 * g;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const uint4*>(from + 16 * s);
+    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const u32x4*>(from + 16 * s);
   }
 
   const int32_t* table = p.pool.table + static_cast<long long>(b) * p.pool.max_pages;
@@ -865,21 +875,36 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
   const int slot_mask = p.pool.page - 1;
   const int dg = lane & 15, vq = lane >> 4;            // V: this thread's 8 d, and which 4 of its wave's 16 keys
   uint32_t kr[NK][4], vr[4][KW];
-  int entry[4], pg[4];                                 // the next tile's entries, the staged tile's pages (16 keys each)
-  float ks[4], vs[4], ks_n[4], vs_n[4];
+  int entry[NP], pg[NP], pg_v = -1;                    // the next tile's entries, the staged tile's pages
+  float ks[NP], vs[NP], ks_n[NP], vs_n[NP];
 
   const auto look_up = [&](int base) {
 #pragma unroll
-    for (int h = 0; h < 4; ++h) entry[h] = entry_of(p, table, base + 16 * h);
+    for (int h = 0; h < NP; ++h) entry[h] = entry_of(p, table, base + KEYS * h);
   };
   const auto row_of = [&](const void* pool, int key, int page) {
     return static_cast<const char*>(pool) + (static_cast<long long>(page < 0 ? 0 : page) * p.pool.heads + hk) * head_bytes +
            static_cast<long long>(key & slot_mask) * D * E;
   };
-  const auto load = [&](int base) {
+  // lane constants: the part of a tile that a thread's K pieces lie in, and where there; its V rows
+  int koff[NK], kpart[NK];
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
-      pg[h] = page_of(p, entry[h], base + 16 * h);
+  for (int i = 0; i < NK; ++i) {
+    const int at = i * 256 + tid, row = at / CPR < T ? at / CPR : T - 1;
+    kpart[i] = row / KEYS;
+    koff[i] = (row % KEYS) * D * E + at % CPR * 16;
+  }
+  const int voff = ((16 * w % KEYS + 4 * vq) * D + (8 * dg < D ? 8 * dg : 0)) * E;
+  const auto load = [&](int base) {
+    const char *kb[NP], *vb = nullptr;                 // the same for all lanes
+#pragma unroll
+    for (int h = 0; h < NP; ++h) {
+      pg[h] = page_of(p, entry[h], base + KEYS * h);
+      kb[h] = row_of(p.pool.k, base + KEYS * h, pg[h]);
+      if (NP == 1 || w == h) {
+        vb = row_of(p.pool.v, base + KEYS * h, pg[h]);
+        pg_v = pg[h];
+      }
       if constexpr (BITS == 8) {
         const long long ph = static_cast<long long>(pg[h] < 0 ? 0 : pg[h]) * p.pool.heads + hk;
         ks_n[h] = p.pool.k_scale[ph];
@@ -888,28 +913,32 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
     }
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
-      const int at = i * 256 + tid, row = at / CPR < T ? at / CPR : T - 1, piece = at % CPR;
-      const int page = row < 32 ? (row < 16 ? pg[0] : pg[1]) : (row < 48 ? pg[2] : pg[3]);
-      const u32x4 y = *reinterpret_cast<const u32x4*>(row_of(p.pool.k, base + row, page) + 16 * piece);
+      const char* from = kb[0];
+      if constexpr (NP > 1) {
+        // with whole rows in 256 threads the part is the same for a wave
+        const int part = CPR == 16 ? i : CPR == 8 ? 2 * i + (w >> 1) : kpart[i];
+        from = part < 2 ? (part == 0 ? kb[0] : kb[1]) : (part == 2 ? kb[2] : kb[3]);
+      }
+      const u32x4 y = *reinterpret_cast<const u32x4*>(from + koff[i]);
       kr[i][0] = y.x; kr[i][1] = y.y; kr[i][2] = y.z; kr[i][3] = y.w;
     }
-    const int page = w < 2 ? (w == 0 ? pg[0] : pg[1]) : (w == 2 ? pg[2] : pg[3]);
-    const char* from = row_of(p.pool.v, base + 16 * w + 4 * vq, page) + (8 * dg < D ? 8 * dg : 0) * E;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if constexpr (BITS == 8) {
-        const u32x2 y = *reinterpret_cast<const u32x2*>(from + j * D * E);
+        const u32x2 y = *reinterpret_cast<const u32x2*>(vb + voff + j * D * E);
         vr[j][0] = y.x; vr[j][1] = y.y;
       } else {
-        const u32x4 y = *reinterpret_cast<const u32x4*>(from + j * D * E);
+        const u32x4 y = *reinterpret_cast<const u32x4*>(vb + voff + j * D * E);
         vr[j][0] = y.x; vr[j][1] = y.y; vr[j][2] = y.z; vr[j][3] = y.w;
       }
     }
   };
   // every row of the workgroup sees every key of the tile (whose pages are in pg)
   const auto is_full = [&](int base) {
-    return pg[0] >= 0 && pg[1] >= 0 && pg[2] >= 0 && pg[3] >= 0 && base + T - 1 <= sp.p_lo &&
-           (p.window == 0 || base > sp.p_hi - p.window || base + T <= p.sinks);
+    bool ok = base + T - 1 <= sp.p_lo && (p.window == 0 || base > sp.p_hi - p.window || base + T <= p.sinks);
+#pragma unroll
+    for (int h = 0; h < NP; ++h) ok = ok && pg[h] >= 0;
+    return ok;
   };
   const auto store = [&](int base, int buf) {
     uint4* kl = kt[gr][buf];
@@ -918,10 +947,10 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
       const int at = i * 256 + tid, row = at / CPR, piece = at % CPR;
       if (T * CPR % 256 != 0 && row >= T) continue;
       if constexpr (BITS == 16) {
-        kl[row * 16 + (piece ^ (row & 15))] = make_uint4(kr[i][0], kr[i][1], kr[i][2], kr[i][3]);
+        kl[row * KROW + piece] = make_uint4(kr[i][0], kr[i][1], kr[i][2], kr[i][3]);
       } else {
-        kl[row * 16 + ((2 * piece) ^ (row & 15))] = e4m3_bf16x8(kr[i][0], kr[i][1]);
-        kl[row * 16 + ((2 * piece + 1) ^ (row & 15))] = e4m3_bf16x8(kr[i][2], kr[i][3]);
+        kl[row * KROW + 2 * piece] = e4m3_bf16x8(kr[i][0], kr[i][1]);
+        kl[row * KROW + 2 * piece + 1] = e4m3_bf16x8(kr[i][2], kr[i][3]);
       }
     }
     if (!is_full(base)) {
@@ -931,8 +960,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int key = base + 16 * w + 4 * vq + j;
-        const bool sees = (w < 2 ? (w == 0 ? pg[0] : pg[1]) : (w == 2 ? pg[2] : pg[3])) >= 0 && key <= sp.p_hi &&
-                          (p.window == 0 || key > sp.p_lo - p.window || key < p.sinks);
+        const bool sees = pg_v >= 0 && key <= sp.p_hi && (p.window == 0 || key > sp.p_lo - p.window || key < p.sinks);
 #pragma unroll
         for (int d = 0; d < KW; ++d) {
           vr[j][d] = sees ? vr[j][d] : 0u;
@@ -998,12 +1026,14 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
     for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
   float m = -INFINITY, l = 0.f;
   const int mine = t1 - t0 - gr > 0 ? (t1 - t0 - gr + 1) / 2 : 0, most = (t1 - t0 + 1) / 2;   // group 0 has the most
-  bool full_cur = false, ok_cur[4] = {false, false, false, false};
+  bool full_cur = false, ok_cur[NP];
+#pragma unroll
+  for (int h = 0; h < NP; ++h) ok_cur[h] = false;
   const auto tile_base = [&](int i) { return T * sp.tile(t0 + gr + 2 * i); };
   const auto took = [&](int base) {
     full_cur = is_full(base);
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
+    for (int h = 0; h < NP; ++h) {
       ok_cur[h] = pg[h] >= 0;
       if constexpr (BITS == 8) { ks[h] = ks_n[h]; vs[h] = vs_n[h]; }
     }
@@ -1016,6 +1046,9 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
     took(tile_base(0));
     if (mine > 1) look_up(tile_base(1));
   }
+  // the queries have arrived: or the loop's first product waits, in every step, for whatever was loaded last
+#pragma unroll
+  for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[s]));
   __syncthreads();
   for (int it = 0; it < most; ++it) {
     const bool more = it + 1 < mine;
@@ -1023,34 +1056,53 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
     if (it + 2 < mine) look_up(tile_base(it + 2));
     if (it < mine) {
       const int base = tile_base(it), buf = it & 1;
-      const uint4* kl = kt[gr][buf];
-      const uint4* vl = vt[gr][buf];
+      const uint4* kl = kt[gr][buf] + c32 * KROW + g;
+      const uint4* vl[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) vl[c] = vt[gr][buf] + c32 * 8 + ((2 * c + g) ^ ((c32 ^ (c32 >> 3)) & 7));
+      // d = 32 t + c32: an odd t flips bit 2 of the swizzle, which is bit 1 of c
+      const auto v_at = [&](int k) { return vl[(k & 3) ^ ((k >> 2 & 1) << 1)][(k >> 2) * 256]; };
+      const auto k_at = [&](int k) { return kl[(k & 1) * 32 * KROW + 2 * (k >> 1)]; };   // halves in turn
       f32x16 st[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) st[h][i] = 0.f;
-        const int row = 32 * h + c32;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) st[h] = mfma32(kl[row * 16 + ((2 * s + g) ^ (row & 15))], qf[s], st[h]);
-      }
-      float f[4];
-#pragma unroll
-      for (int h = 0; h < 4; ++h) f[h] = BITS == 8 ? p.scale_log2 * ks[h] : p.scale_log2;
-      float top = -INFINITY;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float s = st[h][i] * f[2 * h + (i >> 3)];
-          if (!full_cur) {
+        for (int i = 0; i < 16; ++i) st[h][i] = 0.f;
+      uint4 a[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) a[k] = k_at(k);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int k = 0; k < 2 * KS; ++k) {
+        st[k & 1] = mfma32(a[k & 3], __builtin_bit_cast(uint4, qf[k >> 1]), st[k & 1]);
+        if (k + 4 < 2 * KS) a[k & 3] = k_at(k + 4);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) a[k] = v_at(k);
+      __builtin_amdgcn_sched_barrier(0);
+      float f[NP];
+#pragma unroll
+      for (int h = 0; h < NP; ++h) f[h] = BITS == 8 ? p.scale_log2 * ks[h] : p.scale_log2;
+      if (!full_cur) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
             const int key = base + 32 * h + 8 * (i >> 2) + 4 * g + (i & 3);
-            const bool sees = ok_cur[2 * h + (i >> 3)] && key <= place && (p.window == 0 || key > place - p.window || key < p.sinks);
-            s = sees ? s : -INFINITY;
+            const bool sees = ok_cur[(2 * h + (i >> 3)) % NP] && key <= place &&
+                              (p.window == 0 || key > place - p.window || key < p.sinks);
+            st[h][i] = sees ? st[h][i] : -INFINITY;
           }
-          st[h][i] = s;
-          top = fmaxf(top, s);
-        }
+      }
+      float top = -INFINITY;                           // scales are positive: the largest product times its scale
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int o = 8 * (c & 1);
+        const float y = max3(max3(st[c >> 1][o], st[c >> 1][o + 1], st[c >> 1][o + 2]),
+                             max3(st[c >> 1][o + 3], st[c >> 1][o + 4], st[c >> 1][o + 5]), fmaxf(st[c >> 1][o + 6], st[c >> 1][o + 7]));
+        top = fmaxf(top, (full_cur || ok_cur[c % NP]) ? y * f[c % NP] : -INFINITY);
+      }
       if (__any(top > m + 8.f)) {
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         const float mn = fmaxf(m, top), k = mn == m ? 1.f : exp2_fast(m - mn);
@@ -1063,24 +1115,29 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
       }
       const float mz = m == -INFINITY ? 0.f : m;
       uint4 pf[4];
+      float sum = 0.f;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         float e[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float s = st[c >> 1][8 * (c & 1) + i];
-          e[i] = exp2_fast(s - mz);
-          l += e[i];
-          if constexpr (BITS == 8) e[i] = full_cur || s != -INFINITY ? e[i] * vs[c] : 0.f;
+          e[i] = exp2_fast(fmaf(s, f[c % NP], -mz));
+          // the scales of pages that hold hidden keys alone may be anything
+          if constexpr (BITS == 8) e[i] = full_cur || s != -INFINITY ? e[i] : 0.f;
+          sum += e[i];
+          if constexpr (BITS == 8) e[i] = full_cur || s != -INFINITY ? e[i] * vs[c % NP] : 0.f;
         }
         // probabilities are rounded to bf16 for the product (relative 2^-8); their sum is not
         pf[c] = pack8(e);
       }
+      l += sum;
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int t = 0; t < DT; ++t) {
-        const int d = 32 * t + c32;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) acc[t] = mfma32(vl[d * 8 + ((2 * c + g) ^ ((d ^ (d >> 3)) & 7))], pf[c], acc[t]);
+      for (int k = 0; k < 4 * DT; ++k) {
+        acc[k >> 2] = mfma32(a[k & 3], pf[k & 3], acc[k >> 2]);
+        if (k + 4 < 4 * DT) a[k & 3] = v_at(k + 4);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     if (more) {
@@ -1274,7 +1331,8 @@ pace_status_t launch_attend(const AttendParams& p, const AttendPlan& a, hipStrea
   const dim3 g(static_cast<unsigned>(a.blocks)), th(64 * kWaves);
   if (a.rows == 16) hipLaunchKernelGGL((attend_few<D, BITS, 1, kWaves>), g, th, 0, stream, p);
   else if (a.rows == 32) hipLaunchKernelGGL((attend_few<D, BITS, 2, kWaves>), g, th, 0, stream, p);
-  else hipLaunchKernelGGL((attend_many<D, BITS>), g, dim3(kManyThreads), 0, stream, p);
+  else if (p.pool.page >= kManyTile) hipLaunchKernelGGL((attend_many<D, BITS, 1>), g, dim3(kManyThreads), 0, stream, p);
+  else hipLaunchKernelGGL((attend_many<D, BITS, 4>), g, dim3(kManyThreads), 0, stream, p);
   if (a.splits > 1) {
     const unsigned rows = static_cast<unsigned>(static_cast<long long>(p.B) * p.max_q * p.Hq);
     if (a.rows == kManyRows) hipLaunchKernelGGL((attend_join<D, kManyTile>), dim3(rows), dim3(64 * kJoinWaves), 0, stream, p, a.rows);
