@@ -811,10 +811,10 @@ __global__ __launch_bounds__(64 * W, R == 1 ? VMIN : 2) void attend_few(const At
   }
 }
 
-// Many rows (drafts of many heads, the next chunk of a prompt): bound by the matrix products.  A workgroup = 2 groups of 4
-// waves over the same 128 rows of one KV head (32 a wave); the groups take the tiles of 64 keys in turn and join at the
-// end, so that two waves on every SIMD overlap one's products with the other's exponentials also where the grid has no
-// more than a workgroup for a CU.  A group stages its tile through registers (paged rows and 8-bit codes need their own
+// Many rows (drafts of many heads, the next chunk of a prompt): bound by the matrix products.  A workgroup = 8 waves
+// of 32 rows of one KV head, as G groups: one over 256 rows, or two over the same 128 rows that take the tiles of 64 keys
+// in turn and join at the end (so that two waves on every SIMD overlap one's products with the other's exponentials also
+// where there are few rows).  A group stages its tile through registers (paged rows and 8-bit codes need their own
 // addresses and a conversion) into LDS, the next one in flight while this one is worked on:
 //  K row-major, rows 16 bytes apart in their banks; S^T = K Q^T by 32x32x16 products, so a lane owns one row (the
 //    column) and 16 keys of each half of the tile.
@@ -824,25 +824,28 @@ __global__ __launch_bounds__(64 * W, R == 1 ? VMIN : 2) void attend_few(const At
 // Operands are read from LDS four products ahead: one at a time, each product waited out its read (253 us against 211;
 // eight ahead do not fit the registers, 239).
 // NP: the pages of a tile, 1 (64 or more tokens a page) or 4 (one for each 16 keys).
-constexpr int kManyRows = 128, kManyTile = 64, kManyThreads = 512;
+constexpr int kManyTile = 64, kManyThreads = 512;
+constexpr int many_rows(int groups) { return 256 / groups; }
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ f32x16 mfma32(uint4 a, uint4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-template <int D, int BITS, int NP>
+template <int D, int BITS, int NP, int G>
 __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParams p) {
   constexpr int T = kManyTile, E = BITS / 8, KS = D / 16, DT = (D + 31) / 32, KEYS = T / NP;
   constexpr int CPR = BITS == 16 ? D / 8 : D / 16;    // 16-byte pieces of a cached row
-  constexpr int NK = (T * CPR + 255) / 256;           // of them per thread
-  constexpr int KW = BITS == 16 ? 4 : 2, KROW = 17;   // KROW: a K row's pieces in LDS
-  __shared__ uint4 kt[2][2][T * KROW];                // [group][buffer]: [key][pieces]
-  __shared__ uint4 vt[2][2][32 * DT * 8];             // [d][8 pieces of 8 keys]
-  __shared__ uint32_t poison[kManyRows][D / 16];      // 2 bits for each value
+  constexpr int NT = kManyThreads / G, WAVES = 8 / G, ROWS = 32 * WAVES;
+  constexpr int NK = (T * CPR + NT - 1) / NT;         // of them per thread
+  constexpr int KROW = 17;                            // a K row's pieces in LDS
+  constexpr int VD = 4 * G, VW = VD * E / 4, DG = 128 / VD;   // V: d per thread, their dwords, threads along d
+  __shared__ uint4 kt[G][2][T * KROW];                // [group][buffer]: [key][pieces]
+  __shared__ uint4 vt[G][2][32 * DT * 8];             // [d][8 pieces of 8 keys]
+  __shared__ uint32_t poison[ROWS][D / 16];      // 2 bits for each value
   __shared__ int poisoned;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int gr = wave >> 2, w = wave & 3, tid = threadIdx.x & 255, c32 = lane & 31, g = lane >> 5;
+  const int gr = wave / WAVES, w = wave % WAVES, tid = threadIdx.x % NT, c32 = lane & 31, g = lane >> 5;
   int id = remap_block_id(blockIdx.x, gridDim.x);
   const int rb = id % p.row_blocks;
   id /= p.row_blocks;
@@ -850,15 +853,15 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
   id /= p.splits;
   const int hk = id % p.pool.heads, b = id / p.pool.heads;
   Span sp = queries_of(p, b);
-  const int rows = sp.nq * p.group, x0 = rb * kManyRows;
+  const int rows = sp.nq * p.group, x0 = rb * ROWS;
   if (x0 >= rows) return;
-  const int x1 = x0 + kManyRows < rows ? x0 + kManyRows - 1 : rows - 1;
+  const int x1 = x0 + ROWS < rows ? x0 + ROWS - 1 : rows - 1;
   tiles_of<T>(p, x0 / p.group, x1 / p.group, &sp);
   const int splits = splits_of(p, sp.tiles);
   if (split >= splits) return;
   const int t0 = static_cast<int>(static_cast<long long>(sp.tiles) * split / splits);
   const int t1 = static_cast<int>(static_cast<long long>(sp.tiles) * (split + 1) / splits);
-  for (int i = threadIdx.x; i < kManyRows * (D / 16); i += kManyThreads) poison[i / (D / 16)][i % (D / 16)] = 0;
+  for (int i = threadIdx.x; i < ROWS * (D / 16); i += kManyThreads) poison[i / (D / 16)][i % (D / 16)] = 0;
   if (threadIdx.x == 0) poisoned = 0;
 
   const int x = x0 + 32 * w + c32, xi = x <= x1 ? x : x1;
@@ -873,8 +876,9 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
   const int32_t* table = p.pool.table + static_cast<long long>(b) * p.pool.max_pages;
   const long long head_bytes = static_cast<long long>(p.pool.page) * D * E;
   const int slot_mask = p.pool.page - 1;
-  const int dg = lane & 15, vq = lane >> 4;            // V: this thread's 8 d, and which 4 of its wave's 16 keys
-  uint32_t kr[NK][4], vr[4][KW];
+  const int dg = lane % DG, vkey = (64 / DG) * 4 * w + 4 * (lane / DG);   // V: this thread's VD d's and 4 keys
+  const int vpart = NP == 1 ? 0 : w * 4 / WAVES;       // the part of the tile that they lie in
+  uint32_t kr[NK][4], vr[4][VW];
   int entry[NP], pg[NP], pg_v = -1;                    // the next tile's entries, the staged tile's pages
   float ks[NP], vs[NP], ks_n[NP], vs_n[NP];
 
@@ -890,18 +894,18 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
   int koff[NK], kpart[NK];
 #pragma unroll
   for (int i = 0; i < NK; ++i) {
-    const int at = i * 256 + tid, row = at / CPR < T ? at / CPR : T - 1;
+    const int at = i * NT + tid, row = at / CPR < T ? at / CPR : T - 1;
     kpart[i] = row / KEYS;
     koff[i] = (row % KEYS) * D * E + at % CPR * 16;
   }
-  const int voff = ((16 * w % KEYS + 4 * vq) * D + (8 * dg < D ? 8 * dg : 0)) * E;
+  const int voff = (vkey % KEYS * D + (VD * dg < D ? VD * dg : 0)) * E;
   const auto load = [&](int base) {
     const char *kb[NP], *vb = nullptr;                 // the same for all lanes
 #pragma unroll
     for (int h = 0; h < NP; ++h) {
       pg[h] = page_of(p, entry[h], base + KEYS * h);
       kb[h] = row_of(p.pool.k, base + KEYS * h, pg[h]);
-      if (NP == 1 || w == h) {
+      if (h == vpart) {
         vb = row_of(p.pool.v, base + KEYS * h, pg[h]);
         pg_v = pg[h];
       }
@@ -915,8 +919,8 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
     for (int i = 0; i < NK; ++i) {
       const char* from = kb[0];
       if constexpr (NP > 1) {
-        // with whole rows in 256 threads the part is the same for a wave
-        const int part = CPR == 16 ? i : CPR == 8 ? 2 * i + (w >> 1) : kpart[i];
+        // where the pieces of 16 rows fill whole waves, the part is the same for a wave
+        const int part = 16 * CPR % 64 == 0 ? (i * NT + 64 * w) / (16 * CPR) : kpart[i];
         from = part < 2 ? (part == 0 ? kb[0] : kb[1]) : (part == 2 ? kb[2] : kb[3]);
       }
       const u32x4 y = *reinterpret_cast<const u32x4*>(from + koff[i]);
@@ -924,12 +928,15 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if constexpr (BITS == 8) {
-        const u32x2 y = *reinterpret_cast<const u32x2*>(vb + voff + j * D * E);
+      const char* from = vb + voff + j * D * E;
+      if constexpr (VW == 4) {
+        const u32x4 y = *reinterpret_cast<const u32x4*>(from);
+        vr[j][0] = y.x; vr[j][1] = y.y; vr[j][2] = y.z; vr[j][3] = y.w;
+      } else if constexpr (VW == 2) {
+        const u32x2 y = *reinterpret_cast<const u32x2*>(from);
         vr[j][0] = y.x; vr[j][1] = y.y;
       } else {
-        const u32x4 y = *reinterpret_cast<const u32x4*>(vb + voff + j * D * E);
-        vr[j][0] = y.x; vr[j][1] = y.y; vr[j][2] = y.z; vr[j][3] = y.w;
+        vr[j][0] = *reinterpret_cast<const uint32_t*>(from);
       }
     }
   };
@@ -944,8 +951,8 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
     uint4* kl = kt[gr][buf];
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
-      const int at = i * 256 + tid, row = at / CPR, piece = at % CPR;
-      if (T * CPR % 256 != 0 && row >= T) continue;
+      const int at = i * NT + tid, row = at / CPR, piece = at % CPR;
+      if (T * CPR % NT != 0 && row >= T) continue;
       if constexpr (BITS == 16) {
         kl[row * KROW + piece] = make_uint4(kr[i][0], kr[i][1], kr[i][2], kr[i][3]);
       } else {
@@ -959,10 +966,10 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
       uint32_t wild = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int key = base + 16 * w + 4 * vq + j;
+        const int key = base + vkey + j;
         const bool sees = pg_v >= 0 && key <= sp.p_hi && (p.window == 0 || key > sp.p_lo - p.window || key < p.sinks);
 #pragma unroll
-        for (int d = 0; d < KW; ++d) {
+        for (int d = 0; d < VW; ++d) {
           vr[j][d] = sees ? vr[j][d] : 0u;
           const uint32_t m = not_finite<BITS>(vr[j][d]);
           wild |= m;
@@ -972,7 +979,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
       if (sp.p_lo != sp.p_hi && __any(wild != 0)) {
         poisoned = 1;
 #pragma unroll 1
-        for (int key = base + 16 * w; key < base + 16 * w + 16; ++key) {
+        for (int key = base + (T / WAVES) * w; key < base + (T / WAVES) * (w + 1); ++key) {
           const int page = page_of(p, entry_of(p, table, key), key);
           if (page < 0 || 2 * lane >= D) continue;
           const char* from = row_of(p.pool.v, key, page) + 2 * lane * E;
@@ -998,12 +1005,12 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
         }
       }
     }
-    // 4 keys x 8 d: for each d, the 4 keys are one 8-byte unit of its row
+    // 4 keys x VD d: for each d, the 4 keys are one 8-byte unit of its row
     uint2* vl = reinterpret_cast<uint2*>(vt[gr][buf]);
-    if (8 * dg < D) {
-      const int unit = 4 * w + 2 * (vq & 1) + (vq >> 1);          // keys 4 q of a chunk of 16: q = 0, 2, 1, 3
+    if (VD * dg < D) {
+      const int q = vkey >> 2, unit = (q & ~3) + 2 * (q & 1) + (q >> 1 & 1);       // keys 4 q of a chunk of 16: 0, 2, 1, 3
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
+      for (int c = 0; c < VD; ++c) {
         uint2 y;
         if constexpr (BITS == 8) {
           const uint32_t lo = __builtin_amdgcn_perm(vr[1][c >> 2], vr[0][c >> 2], (c & 2) ? 0x07030602u : 0x05010400u);
@@ -1013,7 +1020,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
           const uint32_t sel = (c & 1) ? 0x07060302u : 0x05040100u;
           y = make_uint2(__builtin_amdgcn_perm(vr[1][c >> 1], vr[0][c >> 1], sel), __builtin_amdgcn_perm(vr[3][c >> 1], vr[2][c >> 1], sel));
         }
-        const int d = 8 * dg + c;
+        const int d = VD * dg + c;
         vl[d * 16 + (((unit >> 1) ^ ((d ^ (d >> 3)) & 7)) << 1 | (unit & 1))] = y;
       }
     }
@@ -1025,11 +1032,11 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
   float m = -INFINITY, l = 0.f;
-  const int mine = t1 - t0 - gr > 0 ? (t1 - t0 - gr + 1) / 2 : 0, most = (t1 - t0 + 1) / 2;   // group 0 has the most
+  const int mine = t1 - t0 - gr > 0 ? (t1 - t0 - gr + G - 1) / G : 0, most = (t1 - t0 + G - 1) / G;   // group 0 has the most
   bool full_cur = false, ok_cur[NP];
 #pragma unroll
   for (int h = 0; h < NP; ++h) ok_cur[h] = false;
-  const auto tile_base = [&](int i) { return T * sp.tile(t0 + gr + 2 * i); };
+  const auto tile_base = [&](int i) { return T * sp.tile(t0 + gr + G * i); };
   const auto took = [&](int base) {
     full_cur = is_full(base);
 #pragma unroll
@@ -1147,38 +1154,40 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
     __syncthreads();
   }
 
-  // group 1's maximum, sum and O go to group 0 through the K tiles' LDS
-  float* join = reinterpret_cast<float*>(&kt[0][0][0]);
-  constexpr int PART = DT == 4 ? 2 : DT;               // tiles of O at a time
-  static_assert(sizeof(kt) >= (4 * PART * 16 + 8) * 64 * sizeof(float), "the waves' parts of O must fit the K tiles");
+  if constexpr (G == 2) {
+    // group 1's maximum, sum and O go to group 0 through the K tiles' LDS
+    float* join = reinterpret_cast<float*>(&kt[0][0][0]);
+    constexpr int PART = DT == 4 ? 2 : DT;               // tiles of O at a time
+    static_assert(sizeof(kt) >= (4 * PART * 16 + 8) * 64 * sizeof(float), "the waves' parts of O must fit the K tiles");
 #pragma unroll
-  for (int t = 0; t < DT; t += PART) {
-    if (gr == 1) {
+    for (int t = 0; t < DT; t += PART) {
+      if (gr == 1) {
 #pragma unroll
-      for (int u = 0; u < PART; ++u)
+        for (int u = 0; u < PART; ++u)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) join[((w * PART + u) * 16 + i) * 64 + lane] = acc[t + u][i];
-      if (t == 0) {
-        join[(4 * PART * 16 + 2 * w) * 64 + lane] = m;
-        join[(4 * PART * 16 + 2 * w + 1) * 64 + lane] = l;
+          for (int i = 0; i < 16; ++i) join[((w * PART + u) * 16 + i) * 64 + lane] = acc[t + u][i];
+        if (t == 0) {
+          join[(4 * PART * 16 + 2 * w) * 64 + lane] = m;
+          join[(4 * PART * 16 + 2 * w + 1) * 64 + lane] = l;
+        }
       }
-    }
-    __syncthreads();
-    if (gr == 0) {
-      const float m2 = join[(4 * PART * 16 + 2 * w) * 64 + lane], l2 = join[(4 * PART * 16 + 2 * w + 1) * 64 + lane];
-      const float mn = fmaxf(m, m2);
-      const float k1 = mn == m ? 1.f : exp2_fast(m - mn), k2 = mn == m2 ? 1.f : exp2_fast(m2 - mn);
+      __syncthreads();
+      if (gr == 0) {
+        const float m2 = join[(4 * PART * 16 + 2 * w) * 64 + lane], l2 = join[(4 * PART * 16 + 2 * w + 1) * 64 + lane];
+        const float mn = fmaxf(m, m2);
+        const float k1 = mn == m ? 1.f : exp2_fast(m - mn), k2 = mn == m2 ? 1.f : exp2_fast(m2 - mn);
 #pragma unroll
-      for (int u = 0; u < PART; ++u)
+        for (int u = 0; u < PART; ++u)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          acc[t + u][i] = acc[t + u][i] * k1 + join[((w * PART + u) * 16 + i) * 64 + lane] * k2;
-      if (t + PART >= DT) {
-        l = l * k1 + l2 * k2;
-        m = mn;
+          for (int i = 0; i < 16; ++i)
+            acc[t + u][i] = acc[t + u][i] * k1 + join[((w * PART + u) * 16 + i) * 64 + lane] * k2;
+        if (t + PART >= DT) {
+          l = l * k1 + l2 * k2;
+          m = mn;
+        }
       }
+      __syncthreads();
     }
-    __syncthreads();
   }
   if (gr != 0) return;
   if (poisoned) {
@@ -1221,16 +1230,18 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
   if (g == 0 && p.lse) p.lse[static_cast<long long>(h) * p.n_q + n] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * kLn2;
 }
 
-// Joins the parts of the rows whose keys were split: a workgroup per row, its waves take the parts in turn.
+// Joins the parts of the rows whose keys were split.  W = 8: a workgroup per row, its waves take the parts in turn;
+// W = 1: a wave per row, for up to 8 parts.
 constexpr int kJoinWaves = 8;
-template <int D, int T>
+template <int D, int T, int W>
 __global__ __launch_bounds__(64 * kJoinWaves) void attend_join(const AttendParams p, int block_rows) {
-  __shared__ float part[kJoinWaves][3][64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int id = blockIdx.x;
+  __shared__ float part[W][3][64];
+  const int lane = threadIdx.x & 63, w = W == 1 ? 0 : threadIdx.x >> 6;
+  int id = W == 1 ? blockIdx.x * kJoinWaves + (threadIdx.x >> 6) : blockIdx.x;
   const int h = id % p.Hq;
   id /= p.Hq;
   const int i = id % p.max_q, b = id / p.max_q;
+  if (W == 1 && b >= p.B) return;
   Span sp = queries_of(p, b);
   if (i >= sp.nq) return;
   // the tiles of the row block that this row was in
@@ -1242,12 +1253,12 @@ __global__ __launch_bounds__(64 * kJoinWaves) void attend_join(const AttendParam
   const int n = sp.row0 + i;
   const long long row = static_cast<long long>(n) * p.Hq + h, all = static_cast<long long>(p.n_q) * p.Hq;
   float m = -INFINITY, sum = 0.f, y0 = 0.f, y1 = 0.f;
-  for (int s0 = w; s0 < splits; s0 += 4 * kJoinWaves) {
+  for (int s0 = w; s0 < splits; s0 += 4 * W) {
     float ms[4], ls[4];
     float2 v[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int s = s0 + u * kJoinWaves;
+      const int s = s0 + u * W;
       const float* from = p.part + ((s < splits ? s : s0) * all + row) * (D + 4);
       const float2 ml = *reinterpret_cast<const float2*>(from + D);
       ms[u] = s < splits ? ml.x : -INFINITY;
@@ -1269,21 +1280,24 @@ __global__ __launch_bounds__(64 * kJoinWaves) void attend_join(const AttendParam
       y1 += v[u].y * f;
     }
   }
-  part[w][0][lane] = y0;
-  part[w][1][lane] = y1;
-  part[w][2][lane] = lane == 0 ? m : sum;
-  __syncthreads();
-  if (w != 0) return;
-  float top = part[0][2][0];
+  float top = m;
+  if constexpr (W > 1) {
+    part[w][0][lane] = y0;
+    part[w][1][lane] = y1;
+    part[w][2][lane] = lane == 0 ? m : sum;
+    __syncthreads();
+    if (w != 0) return;
+    top = part[0][2][0];
 #pragma unroll
-  for (int u = 1; u < kJoinWaves; ++u) top = fmaxf(top, part[u][2][0]);
-  sum = y0 = y1 = 0.f;
+    for (int u = 1; u < W; ++u) top = fmaxf(top, part[u][2][0]);
+    sum = y0 = y1 = 0.f;
 #pragma unroll
-  for (int u = 0; u < kJoinWaves; ++u) {
-    const float f = part[u][2][0] == top ? 1.f : exp2_fast(part[u][2][0] - top);
-    sum += part[u][2][1] * f;
-    y0 += part[u][0][lane] * f;
-    y1 += part[u][1][lane] * f;
+    for (int u = 0; u < W; ++u) {
+      const float f = part[u][2][0] == top ? 1.f : exp2_fast(part[u][2][0] - top);
+      sum += part[u][2][1] * f;
+      y0 += part[u][0][lane] * f;
+      y1 += part[u][1][lane] * f;
+    }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   if (2 * lane < D) *reinterpret_cast<uint32_t*>(p.o + row * D + 2 * lane) = pack_bf16x2(y0 * inv, y1 * inv);
@@ -1295,6 +1309,9 @@ struct AttendPlan {
   int rows, row_blocks, splits, chunk;
   long long blocks;
 };
+#ifndef VMANY2
+#define VMANY2 128
+#endif
 #ifndef VMANY
 #define VMANY 32
 #endif
@@ -1302,20 +1319,20 @@ constexpr int kWaves = 4;
 AttendPlan plan_attention(int Hq, int heads, int bits, int B, int max_q, int max_len, int window, int sinks) {
   AttendPlan a;
   const long long rows = static_cast<long long>(max_q) * (Hq / heads);
-  a.rows = rows > VMANY ? kManyRows : rows > 16 ? 32 : 16;
+  a.rows = rows > VMANY2 ? many_rows(1) : rows > VMANY ? many_rows(2) : rows > 16 ? 32 : 16;
   a.row_blocks = static_cast<int>((rows + a.rows - 1) / a.rows);
   const long long base = static_cast<long long>(B) * heads * a.row_blocks;
   if (window >= max_len) window = 0;                  // such a window hides nothing
   long long keys = max_len;
   if (window > 0 && static_cast<long long>(window) + sinks + max_q < keys) keys = static_cast<long long>(window) + sinks + max_q;
   // tiles that a row block may see at most: sinks and window each begin inside one
-  const int tile = a.rows == kManyRows ? kManyTile : tile_keys(bits);
+  const int tile = a.rows > 32 ? kManyTile : tile_keys(bits);
   const long long tiles = (keys + tile - 1) / tile + (window > 0 ? 2 : 0);
   // Workgroups to aim at.  Many rows: one on every CU.  Few: two (32 rows: all that fit; one sequence: its parts are
   // alike, and more of them cost more to join), or four where lengths differ.
-  const long long aim = a.rows == kManyRows ? 256 : a.rows == 32 || B == 1 ? 512 : 1024;
+  const long long aim = a.rows > 32 ? 256 : a.rows == 32 || B == 1 ? 512 : 1024;
   const long long want = aim / base < 1 ? 1 : aim / base, chunk = (tiles + want - 1) / want;
-  const int least = a.rows == kManyRows ? 8 : kWaves;
+  const int least = a.rows > 32 ? 8 : kWaves;
   a.chunk = static_cast<int>(chunk < least ? least : chunk);
   a.splits = static_cast<int>((tiles + a.chunk - 1) / a.chunk);
   if (a.splits < 1) a.splits = 1;
@@ -1326,17 +1343,32 @@ size_t attend_bytes(const AttendPlan& a, int n_q, int Hq, int dim) {
   return a.splits == 1 ? 0 : static_cast<size_t>(a.splits) * n_q * Hq * (dim + 4) * sizeof(float);
 }
 
+template <int D, int BITS, int G>
+void launch_many(const AttendParams& p, dim3 grid, hipStream_t stream) {
+  if (p.pool.page >= kManyTile) hipLaunchKernelGGL((attend_many<D, BITS, 1, G>), grid, dim3(kManyThreads), 0, stream, p);
+  else hipLaunchKernelGGL((attend_many<D, BITS, 4, G>), grid, dim3(kManyThreads), 0, stream, p);
+}
+
+template <int D, int T>
+void launch_join(const AttendParams& p, const AttendPlan& a, hipStream_t stream) {
+  const long long rows = static_cast<long long>(p.B) * p.max_q * p.Hq;
+  const dim3 th(64 * kJoinWaves);
+  if (a.splits <= 8)
+    hipLaunchKernelGGL((attend_join<D, T, 1>), dim3(static_cast<unsigned>((rows + kJoinWaves - 1) / kJoinWaves)), th, 0, stream, p, a.rows);
+  else
+    hipLaunchKernelGGL((attend_join<D, T, kJoinWaves>), dim3(static_cast<unsigned>(rows)), th, 0, stream, p, a.rows);
+}
+
 template <int D, int BITS>
 pace_status_t launch_attend(const AttendParams& p, const AttendPlan& a, hipStream_t stream) {
   const dim3 g(static_cast<unsigned>(a.blocks)), th(64 * kWaves);
   if (a.rows == 16) hipLaunchKernelGGL((attend_few<D, BITS, 1, kWaves>), g, th, 0, stream, p);
   else if (a.rows == 32) hipLaunchKernelGGL((attend_few<D, BITS, 2, kWaves>), g, th, 0, stream, p);
-  else if (p.pool.page >= kManyTile) hipLaunchKernelGGL((attend_many<D, BITS, 1>), g, dim3(kManyThreads), 0, stream, p);
-  else hipLaunchKernelGGL((attend_many<D, BITS, 4>), g, dim3(kManyThreads), 0, stream, p);
+  else if (a.rows == many_rows(2)) launch_many<D, BITS, 2>(p, g, stream);
+  else launch_many<D, BITS, 1>(p, g, stream);
   if (a.splits > 1) {
-    const unsigned rows = static_cast<unsigned>(static_cast<long long>(p.B) * p.max_q * p.Hq);
-    if (a.rows == kManyRows) hipLaunchKernelGGL((attend_join<D, kManyTile>), dim3(rows), dim3(64 * kJoinWaves), 0, stream, p, a.rows);
-    else hipLaunchKernelGGL((attend_join<D, tile_keys(BITS)>), dim3(rows), dim3(64 * kJoinWaves), 0, stream, p, a.rows);
+    if (a.rows > 32) launch_join<D, kManyTile>(p, a, stream);
+    else launch_join<D, tile_keys(BITS)>(p, a, stream);
   }
   return check_launch("pace_cache_attention");
 }
