@@ -2,6 +2,8 @@
 // zero) for each group of k, and the epilogues of the bf16 product.
 #include <math.h>
 
+#include <type_traits>
+
 #include "pace_internal.h"
 
 namespace pace {
@@ -10,6 +12,7 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 struct W4Params {
   const uint16_t* x;
@@ -23,13 +26,65 @@ struct W4Params {
   int M, N, K, mode, splits, ntiles;
 };
 
-constexpr int kBlockK = 128;       // k per step of a wave: 16 bytes of weights per lane
-
 __device__ __forceinline__ float bf16_f32(uint16_t b) { return __uint_as_float(static_cast<uint32_t>(b) << 16); }
 __device__ __forceinline__ uint16_t f32_bf16(float f) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(f)); }
 __device__ __forceinline__ f32x4 mfma16(uint4 a, uint4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
+
+// What both kernels do: C = x W^T by 16x16x32 products with x as the A operand (rows m) and W as B (columns n), so that a
+// lane's column has one scale.
+//  A lane loads 16 bytes of its column's row: the 32 k's 32 g .. 32 g + 31 of a block of 128 (lane group g).  A 4 x 4
+//    transpose of dwords between the lane groups (v_permlane32_swap, v_permlane16_swap) makes that 8 k's of each 32, so
+//    that every product lies in one scale group of 32 or more.
+//  (w >> 4 i) & 0xf000f | 0x43004300 is the bf16 pair 128 + q of nibbles i and i + 4: exact, one instruction past the
+//    shift.  The products thus sum x (128 + q); (128 + zero) sum x comes off for each group in fp32.  The A operand
+//    takes x in the same order of k (0 4, 1 5, 2 6, 3 7 of every 8).
+__device__ __forceinline__ void transpose_groups(uint32_t (&d)[4]) {
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const u32x2 y = __builtin_amdgcn_permlane32_swap(d[q], d[q + 2], false, false);
+    d[q] = y.x;
+    d[q + 2] = y.y;
+  }
+#pragma unroll
+  for (int q = 0; q < 4; q += 2) {
+    const u32x2 y = __builtin_amdgcn_permlane16_swap(d[q], d[q + 1], false, false);
+    d[q] = y.x;
+    d[q + 1] = y.y;
+  }
+}
+__device__ __forceinline__ uint4 nibbles(uint32_t v) {
+  return make_uint4((v & 0xf000fu) | 0x43004300u, (v >> 4 & 0xf000fu) | 0x43004300u, (v >> 8 & 0xf000fu) | 0x43004300u,
+                    (v >> 12 & 0xf000fu) | 0x43004300u);
+}
+__device__ __forceinline__ uint4 nibble_order(uint4 u) {
+  return make_uint4(__builtin_amdgcn_perm(u.z, u.x, 0x05040100u), __builtin_amdgcn_perm(u.z, u.x, 0x07060302u),
+                    __builtin_amdgcn_perm(u.w, u.y, 0x05040100u), __builtin_amdgcn_perm(u.w, u.y, 0x07060302u));
+}
+// Raw scales and zeros of groups first .. first + N - 1 of the row that begins at group `row` of the arrays.  TAIL: past
+// the row's end, its last one's.  They are turned into numbers where they are used, so that the loads stay in flight.
+template <int N>
+struct Groups {
+  uint16_t s[N];
+  uint8_t z[N];
+  template <bool TAIL>
+  __device__ __forceinline__ void load(const W4Params& p, unsigned row, int first, int groups) {
+    if constexpr (!TAIL) {
+      __builtin_memcpy(s, p.scale + first + row, 2 * N);       // any alignment
+      if (p.zero) __builtin_memcpy(z, p.zero + first + row, N);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const unsigned at = row + (first + i < groups ? first + i : groups - 1);
+        s[i] = p.scale[at];
+        if (p.zero) z[i] = p.zero[at];
+      }
+    }
+  }
+  __device__ __forceinline__ float scale(int i) const { return bf16_f32(s[i]); }
+  __device__ __forceinline__ float zero(const W4Params& p, int i) const { return p.zero ? 128.f + static_cast<float>(z[i]) : 136.f; }
+};
 
 // One output value (or a SwiGLU pair's) from its finished sum.
 __device__ __forceinline__ void w4_store(const W4Params& p, int m, int n, float y, float y_pair) {
@@ -40,141 +95,98 @@ __device__ __forceinline__ void w4_store(const W4Params& p, int m, int n, float 
   p.C[at] = f32_bf16(y);
 }
 
-// C = x W^T by 16x16x32 products with x as the A operand (rows m) and W as B (columns n), so that a lane's
-// column has one scale.  Bound by the weights' bytes: a wave streams 16 bytes per lane (32 k of one row) and step, the
-// waves of a workgroup take the steps of K in turn and join through LDS.
-//  A 4 x 4 transpose of dwords between the lane groups (v_permlane32_swap, v_permlane16_swap) turns the 32
-//    consecutive k of a lane into 8 of each 32, so that every product lies in one scale group of 32 or more.
-//  (w >> 4 i) & 0xf000f | 0x43004300 is the bf16 pair 128 + q of nibbles i and i + 4: exact, one instruction past the
-//    shift.  The products thus sum x (128 + q); (128 + zero) sum x comes off for each group in fp32, sum x from one
-//    more product with ones.  The A operand takes x in the same order of k.
-template <int MT, int NT, int W, int GROUP>
-__global__ __launch_bounds__(64 * W) void gemm_w4(const W4Params p) {
-  constexpr int GB = kBlockK / GROUP, SPG = 4 / GB;             // groups per step, products per group
-  __shared__ float join[W > 1 ? W / 2 : 1][MT * NT * 4][64];
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-  const int id = remap_block_id(blockIdx.x, gridDim.x);
-  const int n0 = id % p.ntiles * 16 * NT, split = id / p.ntiles, m0 = blockIdx.y * 16 * MT;
-  const int steps = (p.K + kBlockK - 1) / kBlockK;
-  const int s0 = static_cast<int>(static_cast<long long>(steps) * split / p.splits);
-  const int s1 = static_cast<int>(static_cast<long long>(steps) * (split + 1) / p.splits);
-  const int groups = p.K / GROUP;
+// Up to 16 rows: bound by the weights' bytes.  A wave streams 256 k's of NT tiles of 16 columns a step (whole 128-byte
+// lines of each row); W waves share the columns, take consecutive parts of K and join through LDS.  sum x comes from one
+// more product with ones.
+constexpr int kW4Waves = 8;
+template <int NT, int W, int GROUP>
+__global__ __launch_bounds__(64 * kW4Waves) void gemm_w4_few(const W4Params p) {
+  constexpr int STEP = 256, GB = 128 / GROUP, SPG = 4 / GB;      // groups per 128 k's, products per group
+  __shared__ float join[kW4Waves / W][W > 1 ? W / 2 : 1][NT * 4][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  const int w = wave % W, set = wave / W;
+  const int n0 = (remap_block_id(blockIdx.x, gridDim.x) * (kW4Waves / W) + set) * 16 * NT;
+  const int steps = (p.K + STEP - 1) / STEP, s0 = steps * w / W, s1 = steps * (w + 1) / W, groups = p.K / GROUP;
 
-  const uint8_t* wrow[NT];
-  const uint16_t* srow[NT];
-  const uint8_t* zrow[NT];
+  // lane constants beside a base that only the step moves (every operand is under 2 GiB)
+  unsigned woff[NT], row[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const int n = n0 + 16 * t + r < p.N ? n0 + 16 * t + r : p.N - 1;
-    wrow[t] = p.w + static_cast<long long>(n) * (p.K / 2);
-    srow[t] = p.scale + static_cast<long long>(n) * groups;
-    zrow[t] = p.zero ? p.zero + static_cast<long long>(n) * groups : nullptr;
+    const unsigned n = n0 + 16 * t + r < p.N ? n0 + 16 * t + r : p.N - 1;
+    woff[t] = n * (p.K / 2) + 16 * g;
+    row[t] = n * groups;
   }
-  const uint16_t* xrow[MT];
-#pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int m = m0 + 16 * t + r < p.M ? m0 + 16 * t + r : p.M - 1;
-    xrow[t] = p.x + static_cast<long long>(m) * p.K;
-  }
+  const unsigned xoff = (r < p.M ? r : p.M - 1) * p.K + 8 * g;
 
-  uint4 wq[NT];
-  float sc[NT][GB], zc[NT][GB];
-  uint4 xf[MT][4];
-  const auto load_w = [&](int s) {
-    const int k = s * kBlockK + 32 * g;
+  uint4 wq[NT][2], xf[2][4];
+  Groups<2 * GB> gq[NT];
+  const auto load_step = [&](int s, auto tail) {
+    constexpr bool TAIL = decltype(tail)::value;
+    const uint8_t* wb = p.w + static_cast<size_t>(s) * (STEP / 2);
+    const uint16_t* xb = p.x + static_cast<size_t>(s) * STEP;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      wq[t] = *reinterpret_cast<const uint4*>(wrow[t] + (k < p.K ? k / 2 : 0));
+    for (int u = 0; u < 2; ++u) {
 #pragma unroll
-      for (int q = 0; q < GB; ++q) {
-        const int gi = s * GB + q < groups ? s * GB + q : groups - 1;
-        sc[t][q] = bf16_f32(srow[t][gi]);
-        zc[t][q] = 128.f + (p.zero ? static_cast<float>(zrow[t][gi]) : 8.f);
+      for (int t = 0; t < NT; ++t) {
+        // past the end: the row's first block again, for x's zeros there
+        const bool in = !TAIL || s * STEP + 128 * u + 32 * g < p.K;
+        const u32x4 y = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>((in ? wb + 64 * u : p.w) + woff[t]));
+        wq[t][u] = make_uint4(y.x, y.y, y.z, y.w);
       }
-    }
-  };
-  const auto load_x = [&](int s) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int k = s * kBlockK + 32 * q + 8 * g;
-#pragma unroll
-      for (int t = 0; t < MT; ++t)
-        xf[t][q] = k < p.K ? *reinterpret_cast<const uint4*>(xrow[t] + k) : make_uint4(0, 0, 0, 0);
-    }
-  };
-
-  f32x4 acc[MT][NT];
-#pragma unroll
-  for (int a = 0; a < MT; ++a)
-#pragma unroll
-    for (int t = 0; t < NT; ++t) acc[a][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const uint4 ones = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
-
-  int s = s0 + w;
-  if (s < s1) {
-    load_w(s);
-    load_x(s);
-  }
-  for (; s < s1; s += W) {
-    // x in the nibbles' order (0 4, 1 5, 2 6, 3 7), and its sums by group
-    uint4 xa[MT][4];
-    f32x4 xs[MT][GB];
-#pragma unroll
-    for (int a = 0; a < MT; ++a) {
-#pragma unroll
-      for (int q = 0; q < GB; ++q) xs[a][q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const uint4 u = xf[a][q];
-        xa[a][q] = make_uint4(__builtin_amdgcn_perm(u.z, u.x, 0x05040100u), __builtin_amdgcn_perm(u.z, u.x, 0x07060302u),
-                              __builtin_amdgcn_perm(u.w, u.y, 0x05040100u), __builtin_amdgcn_perm(u.w, u.y, 0x07060302u));
-        xs[a][q / SPG] = mfma16(xa[a][q], ones, xs[a][q / SPG]);
+        xf[u][q] = make_uint4(0, 0, 0, 0);
+        if (!TAIL || s * STEP + 128 * u + 32 * q + 8 * g < p.K)
+          xf[u][q] = *reinterpret_cast<const uint4*>(xb + 128 * u + 32 * q + xoff);
       }
     }
-    uint32_t d[NT][4];
-    float sg[NT][GB], zg[NT][GB];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      d[t][0] = wq[t].x; d[t][1] = wq[t].y; d[t][2] = wq[t].z; d[t][3] = wq[t].w;
+    for (int t = 0; t < NT; ++t) gq[t].template load<TAIL>(p, row[t], s * 2 * GB, groups);
+  };
+  const auto load = [&](int s) {
+    if ((s + 1) * STEP <= p.K) load_step(s, std::false_type());
+    else load_step(s, std::true_type());
+  };
+
+  f32x4 acc[NT];
 #pragma unroll
-      for (int q = 0; q < GB; ++q) { sg[t][q] = sc[t][q]; zg[t][q] = zc[t][q]; }
+  for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const uint4 ones = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+
+  if (s0 < s1) load(s0);
+  for (int s = s0; s < s1; ++s) {
+    uint32_t d[NT][2][4];
+    uint4 xa[2][4];
+    Groups<2 * GB> gc[NT];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) { d[t][u][0] = wq[t][u].x; d[t][u][1] = wq[t][u].y; d[t][u][2] = wq[t][u].z; d[t][u][3] = wq[t][u].w; }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) xa[u][q] = nibble_order(xf[u][q]);
     }
-    if (s + W < s1) {
-      load_w(s + W);
-      load_x(s + W);
-    }
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
+    for (int t = 0; t < NT; ++t) gc[t] = gq[t];
+    if (s + 1 < s1) load(s + 1);
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const u32x2 y = __builtin_amdgcn_permlane32_swap(d[t][q], d[t][q + 2], false, false);
-        d[t][q] = y.x;
-        d[t][q + 2] = y.y;
-      }
+    for (int u = 0; u < 2; ++u) {
+      f32x4 xs[GB];
 #pragma unroll
-      for (int q = 0; q < 4; q += 2) {
-        const u32x2 y = __builtin_amdgcn_permlane16_swap(d[t][q], d[t][q + 1], false, false);
-        d[t][q] = y.x;
-        d[t][q + 1] = y.y;
-      }
+      for (int q = 0; q < GB; ++q) xs[q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int q = 0; q < GB; ++q) {
-        f32x4 sum[MT];
+      for (int q = 0; q < 4; ++q) xs[q / SPG] = mfma16(xa[u][q], ones, xs[q / SPG]);
 #pragma unroll
-        for (int a = 0; a < MT; ++a) sum[a] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < NT; ++t) {
+        transpose_groups(d[t][u]);
 #pragma unroll
-        for (int e = q * SPG; e < (q + 1) * SPG; ++e) {
-          const uint32_t v = d[t][e];
-          const uint4 b = make_uint4((v & 0xf000fu) | 0x43004300u, (v >> 4 & 0xf000fu) | 0x43004300u,
-                                     (v >> 8 & 0xf000fu) | 0x43004300u, (v >> 12 & 0xf000fu) | 0x43004300u);
+        for (int q = 0; q < GB; ++q) {
+          f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int a = 0; a < MT; ++a) sum[a] = mfma16(xa[a][e], b, sum[a]);
+          for (int e = q * SPG; e < (q + 1) * SPG; ++e) sum = mfma16(xa[u][e], nibbles(d[t][u][e]), sum);
+          const float sg = gc[t].scale(GB * u + q), zg = gc[t].zero(p, GB * u + q);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[t][i] = fmaf(sg, fmaf(-zg, xs[q][i], sum[i]), acc[t][i]);
         }
-#pragma unroll
-        for (int a = 0; a < MT; ++a)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            acc[a][t][i] = fmaf(sg[t][q], fmaf(-zg[t][q], xs[a][q][i], sum[a][i]), acc[a][t][i]);
       }
     }
   }
@@ -183,24 +195,162 @@ __global__ __launch_bounds__(64 * W) void gemm_w4(const W4Params p) {
   for (int h = W / 2; h >= 1; h >>= 1) {
     if (w >= h && w < 2 * h) {
 #pragma unroll
-      for (int a = 0; a < MT; ++a)
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) join[w - h][(a * NT + t) * 4 + i][lane] = acc[a][t][i];
+        for (int i = 0; i < 4; ++i) join[set][w - h][t * 4 + i][lane] = acc[t][i];
     }
     __syncthreads();
     if (w < h) {
 #pragma unroll
-      for (int a = 0; a < MT; ++a)
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[a][t][i] += join[w][(a * NT + t) * 4 + i][lane];
+        for (int i = 0; i < 4; ++i) acc[t][i] += join[set][w][t * 4 + i][lane];
     }
     __syncthreads();
   }
   if (w != 0) return;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int n = n0 + 16 * t + r;
+    const float bias = p.bias && n < p.N ? p.bias[n] : 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int m = 4 * g + i;
+      const float y = acc[t][i] + bias;
+      const float pair = dpp_f32<kDppQuadXor1>(y);             // SwiGLU: the up value of an even lane's gate
+      if (m < p.M && n < p.N && (p.mode != 2 || (n & 1) == 0)) w4_store(p, m, n, y, pair);
+    }
+  }
+}
+
+// More rows (16 MT at a time): here x would be read far more often than the weights, so the 4 waves of a workgroup take 32
+// columns each and share x through LDS, 128 k's at a time (in the nibbles' order, with its sums over every 32 k's);
+// workgroups split K where the columns give too few, and w4_join adds their sums.
+template <int MT, int GROUP>
+__global__ __launch_bounds__(256) void gemm_w4_rows(const W4Params p) {
+  constexpr int NT = 2, STEP = 128, GB = STEP / GROUP, SPG = 4 / GB, ROWS = 16 * MT, LROW = 17;
+  __shared__ uint4 xt[2][ROWS * LROW];                 // [row][16 pieces of 8 k's]
+  __shared__ float xs[2][4][ROWS];                     // [32 k's][row]
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  const int id = remap_block_id(blockIdx.x, gridDim.x);
+  const int n0 = (id % p.ntiles * 4 + w) * 16 * NT, split = id / p.ntiles, m0 = blockIdx.y * ROWS;
+  const int steps = (p.K + STEP - 1) / STEP, groups = p.K / GROUP;
+  const int s0 = static_cast<int>(static_cast<long long>(steps) * split / p.splits);
+  const int s1 = static_cast<int>(static_cast<long long>(steps) * (split + 1) / p.splits);
+
+  unsigned woff[NT], row[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const unsigned n = n0 + 16 * t + r < p.N ? n0 + 16 * t + r : p.N - 1;
+    woff[t] = n * (p.K / 2) + 16 * g;
+    row[t] = n * groups;
+  }
+  // x: thread t stages piece t % 16 of rows t / 16 + 16 i
+  const int piece = threadIdx.x & 15, xr = threadIdx.x >> 4;
+  unsigned xoff[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int m = m0 + xr + 16 * i;
+    xoff[i] = static_cast<unsigned>(m < p.M ? m : p.M - 1) * p.K + 8 * piece;
+  }
+
+  uint4 wq[NT], xq[MT];
+  Groups<GB> gq[NT];
+  const auto load_step = [&](int s, auto tail) {
+    constexpr bool TAIL = decltype(tail)::value;
+    const uint8_t* wb = p.w + static_cast<size_t>(s) * (STEP / 2);
+    const uint16_t* xb = p.x + static_cast<size_t>(s) * STEP;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const bool in = !TAIL || s * STEP + 32 * g < p.K;
+      const u32x4 y = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>((in ? wb : p.w) + woff[t]));
+      wq[t] = make_uint4(y.x, y.y, y.z, y.w);
+      gq[t].template load<TAIL>(p, row[t], s * GB, groups);
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      xq[i] = make_uint4(0, 0, 0, 0);
+      if (!TAIL || s * STEP + 8 * piece < p.K) xq[i] = *reinterpret_cast<const uint4*>(xb + xoff[i]);
+    }
+  };
+  const auto load = [&](int s) {
+    if ((s + 1) * STEP <= p.K) load_step(s, std::false_type());
+    else load_step(s, std::true_type());
+  };
+  const auto stage = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const uint4 u = xq[i];
+      float sum = 0.f;
+      const uint32_t v[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += __uint_as_float(v[e] << 16) + __uint_as_float(v[e] & 0xffff0000u);
+      sum += dpp_f32<kDppQuadXor1>(sum);
+      sum += dpp_f32<kDppQuadXor2>(sum);
+      xt[buf][(xr + 16 * i) * LROW + piece] = nibble_order(u);
+      if ((piece & 3) == 0) xs[buf][piece >> 2][xr + 16 * i] = sum;
+    }
+  };
+
+  f32x4 acc[MT][NT];
+#pragma unroll
+  for (int a = 0; a < MT; ++a)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[a][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  load(s0);                                            // splits never exceed the steps
+  for (int s = s0; s < s1; ++s) {
+    const int buf = (s - s0) & 1;
+    stage(buf);
+    uint32_t d[NT][4];
+    Groups<GB> gc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      d[t][0] = wq[t].x; d[t][1] = wq[t].y; d[t][2] = wq[t].z; d[t][3] = wq[t].w;
+      gc[t] = gq[t];
+    }
+    if (s + 1 < s1) load(s + 1);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) transpose_groups(d[t]);
+    __syncthreads();                                   // the buffer is written again two steps on, past the next barrier
+#pragma unroll
+    for (int q = 0; q < GB; ++q) {
+      f32x4 sum[MT][NT];
+#pragma unroll
+      for (int a = 0; a < MT; ++a)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sum[a][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = q * SPG; e < (q + 1) * SPG; ++e) {
+        uint4 b[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) b[t] = nibbles(d[t][e]);
+#pragma unroll
+        for (int a = 0; a < MT; ++a) {
+          const uint4 x = xt[buf][(16 * a + r) * LROW + 4 * e + g];
+#pragma unroll
+          for (int t = 0; t < NT; ++t) sum[a][t] = mfma16(x, b[t], sum[a][t]);
+        }
+      }
+#pragma unroll
+      for (int a = 0; a < MT; ++a) {
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int e = q * SPG; e < (q + 1) * SPG; ++e) {
+          const float4 y = *reinterpret_cast<const float4*>(&xs[buf][e][16 * a + 4 * g]);
+          x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const float sg = gc[t].scale(q), zg = gc[t].zero(p, q);
+          acc[a][t][0] = fmaf(sg, fmaf(-zg, x.x, sum[a][t][0]), acc[a][t][0]);
+          acc[a][t][1] = fmaf(sg, fmaf(-zg, x.y, sum[a][t][1]), acc[a][t][1]);
+          acc[a][t][2] = fmaf(sg, fmaf(-zg, x.z, sum[a][t][2]), acc[a][t][2]);
+          acc[a][t][3] = fmaf(sg, fmaf(-zg, x.w, sum[a][t][3]), acc[a][t][3]);
+        }
+      }
+    }
+  }
 #pragma unroll
   for (int a = 0; a < MT; ++a)
 #pragma unroll
@@ -211,7 +361,7 @@ __global__ __launch_bounds__(64 * W) void gemm_w4(const W4Params p) {
       for (int i = 0; i < 4; ++i) {
         const int m = m0 + 16 * a + 4 * g + i;
         const float y = acc[a][t][i] + bias;
-        const float pair = dpp_f32<kDppQuadXor1>(y);         // SwiGLU: the up value of an even lane's gate
+        const float pair = dpp_f32<kDppQuadXor1>(y);           // SwiGLU: the up value of an even lane's gate
         if (m >= p.M || n >= p.N) continue;
         if (p.splits > 1) p.part[(static_cast<long long>(split) * p.M + m) * p.N + n] = y;
         else if (p.mode != 2 || (n & 1) == 0) w4_store(p, m, n, y, pair);
@@ -234,29 +384,58 @@ __global__ __launch_bounds__(256) void w4_join(const W4Params p) {
 }
 
 struct W4Plan {
-  int mt, nt, ntiles, splits;
+  int mt, nt, waves, ntiles, splits;   // ntiles: workgroups along the columns
 };
-constexpr int kW4Waves = 8;
+#ifndef VW4
+#define VW4 512
+#endif
+#ifndef VNT4
+#define VNT4 100000
+#endif
+#ifndef VWV
+#define VWV 4096
+#endif
 W4Plan plan_w4(int M, int N, int K) {
   W4Plan a;
-  a.mt = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-  a.nt = a.mt;
-  a.ntiles = (N + 16 * a.nt - 1) / (16 * a.nt);
   a.splits = 1;
-  if (a.mt > 1) {
-    const int most = ((K + kBlockK - 1) / kBlockK + 2 * kW4Waves - 1) / (2 * kW4Waves);
-    const int s = 512 / a.ntiles;
-    a.splits = s < 1 ? 1 : s < most ? s : most;
+  if (M <= 16) {
+    a.mt = 1;
+    const int tiles = (N + 15) / 16;
+    a.nt = tiles >= VNT4 ? 2 : 1;
+    a.waves = 8;
+    while (a.waves > 1 && tiles / a.nt * a.waves > VWV) a.waves /= 2;
+    a.ntiles = ((tiles + a.nt - 1) / a.nt * a.waves + kW4Waves - 1) / kW4Waves;
+    return a;
   }
+  a.mt = M <= 32 ? 2 : M <= 48 ? 3 : 4;
+  a.nt = 2;
+  a.ntiles = (N + 127) / 128;
+  const int steps = (K + 127) / 128, rows = (M + 63) / 64;
+  const int s = VW4 / (a.ntiles * rows), most = (steps + 3) / 4;       // at least four steps each
+  a.splits = s < 1 ? 1 : s < most ? s : most;
   return a;
 }
 
-template <int MT, int NT>
-void launch_w4(const W4Params& p, int group, hipStream_t stream) {
-  const dim3 g(p.ntiles * p.splits, (p.M + 16 * MT - 1) / (16 * MT)), th(64 * kW4Waves);
-  if (group == 32) hipLaunchKernelGGL((gemm_w4<MT, NT, kW4Waves, 32>), g, th, 0, stream, p);
-  else if (group == 64) hipLaunchKernelGGL((gemm_w4<MT, NT, kW4Waves, 64>), g, th, 0, stream, p);
-  else hipLaunchKernelGGL((gemm_w4<MT, NT, kW4Waves, 128>), g, th, 0, stream, p);
+template <int NT, int W>
+void launch_few(const W4Params& p, int group, hipStream_t stream) {
+  const dim3 g(p.ntiles), th(64 * kW4Waves);
+  if (group == 32) hipLaunchKernelGGL((gemm_w4_few<NT, W, 32>), g, th, 0, stream, p);
+  else if (group == 64) hipLaunchKernelGGL((gemm_w4_few<NT, W, 64>), g, th, 0, stream, p);
+  else hipLaunchKernelGGL((gemm_w4_few<NT, W, 128>), g, th, 0, stream, p);
+}
+template <int NT>
+void launch_few(const W4Params& p, int waves, int group, hipStream_t stream) {
+  if (waves == 8) launch_few<NT, 8>(p, group, stream);
+  else if (waves == 4) launch_few<NT, 4>(p, group, stream);
+  else if (waves == 2) launch_few<NT, 2>(p, group, stream);
+  else launch_few<NT, 1>(p, group, stream);
+}
+template <int MT>
+void launch_rows(const W4Params& p, int group, hipStream_t stream) {
+  const dim3 g(p.ntiles * p.splits, (p.M + 16 * MT - 1) / (16 * MT)), th(256);
+  if (group == 32) hipLaunchKernelGGL((gemm_w4_rows<MT, 32>), g, th, 0, stream, p);
+  else if (group == 64) hipLaunchKernelGGL((gemm_w4_rows<MT, 64>), g, th, 0, stream, p);
+  else hipLaunchKernelGGL((gemm_w4_rows<MT, 128>), g, th, 0, stream, p);
 }
 
 }  // namespace
@@ -295,9 +474,11 @@ pace_status_t pace_gemm_w4(const uint16_t* x, const uint8_t* w, const uint16_t* 
     PACE_REQUIRE(aligned16(workspace), "pace_gemm_w4: workspace must be 16-byte aligned");
   }
   const W4Params p{x, w, scale, zero, bias, residual, C, static_cast<float*>(workspace), M, N, K, epilogue, a.splits, a.ntiles};
-  if (a.mt == 1) launch_w4<1, 1>(p, group, stream);
-  else if (a.mt == 2) launch_w4<2, 2>(p, group, stream);
-  else launch_w4<4, 4>(p, group, stream);
+  if (a.mt == 1 && a.nt == 1) launch_few<1>(p, a.waves, group, stream);
+  else if (a.mt == 1) launch_few<2>(p, a.waves, group, stream);
+  else if (a.mt == 2) launch_rows<2>(p, group, stream);
+  else if (a.mt == 3) launch_rows<3>(p, group, stream);
+  else launch_rows<4>(p, group, stream);
   if (a.splits > 1)
     hipLaunchKernelGGL(w4_join, dim3(((epilogue == 2 ? N / 2 : N) + 255) / 256, M), dim3(256), 0, stream, p);
   return check_launch("pace_gemm_w4");
