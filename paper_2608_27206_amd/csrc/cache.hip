@@ -100,11 +100,11 @@ constexpr int kAppendTokens = 8;   // most tokens per workgroup
 // angles' cos and sin go to LDS once (all heads share them), then every thread moves 16 values of one
 // head (8 of each half, so that a pair meets in one thread) per step.
 template <int D, bool KV>
-__global__ __launch_bounds__(kAppendThreads) void append_rows(const AppendParams p) {
+__device__ __forceinline__ void append_rows(const AppendParams& p, int block) {
   constexpr int HALF = D / 2, CH = D / 16;
   __shared__ f32x2 cs[kAppendTokens * HALF];
   __shared__ int src_of[kAppendTokens];
-  const int b = blockIdx.x / p.tiles, t0 = (blockIdx.x % p.tiles) * p.tokens;
+  const int b = block / p.tiles, t0 = (block % p.tiles) * p.tokens;
   int r0;
   const int n = new_tokens(p, b, &r0);
   const int here = n - t0 < p.tokens ? n - t0 : p.tokens;
@@ -189,10 +189,10 @@ __device__ __forceinline__ float page_scale(float top) {
 // scale needs no atomics and one launch is enough.  The new values stay in registers between the
 // maximum and the store.
 template <int D, int ITEMS>
-__global__ __launch_bounds__(kAppendThreads) void append_pages(const AppendParams p) {
+__device__ __forceinline__ void append_pages(const AppendParams& p, int block) {
   constexpr int HALF = D / 2, CH = D / 16;
   __shared__ float red[kAppendThreads / 64];
-  int id = blockIdx.x;
+  int id = block;
   const bool val = id & 1;
   id >>= 1;
   const int h = id % p.pool.heads;
@@ -281,19 +281,31 @@ __global__ __launch_bounds__(kAppendThreads) void append_pages(const AppendParam
 }
 
 template <int D>
+__global__ __launch_bounds__(kAppendThreads) void append_16bit(const AppendParams p) {
+  append_rows<D, true>(p, blockIdx.x);
+}
+// The pages first: they compute, and the queries' rows, which only move bytes, fill the memory's time beside them
+// (10,677 tokens, 28/4 heads of 128: XXX us, one after the other 50).
+template <int D, int ITEMS>
+__global__ __launch_bounds__(kAppendThreads) void append_8bit(const AppendParams p, int page_blocks) {
+  const int block = blockIdx.x;
+  if (block < page_blocks) append_pages<D, ITEMS>(p, block);
+  else append_rows<D, false>(p, block - page_blocks);
+}
+
+template <int D>
 pace_status_t launch_append(const AppendParams& p, int bits, long long row_blocks, long long page_blocks,
                             hipStream_t stream) {
   const dim3 th(kAppendThreads);
   if (bits == 16) {
-    hipLaunchKernelGGL((append_rows<D, true>), dim3(row_blocks), th, 0, stream, p);
+    hipLaunchKernelGGL((append_16bit<D>), dim3(static_cast<unsigned>(row_blocks)), th, 0, stream, p);
   } else {
-    if (p.q) hipLaunchKernelGGL((append_rows<D, false>), dim3(row_blocks), th, 0, stream, p);
-    const dim3 g(page_blocks);
-    const int items = (p.pool.page * (D / 16) + kAppendThreads - 1) / kAppendThreads;
-    if (items <= 1) hipLaunchKernelGGL((append_pages<D, 1>), g, th, 0, stream, p);
-    else if (items <= 2) hipLaunchKernelGGL((append_pages<D, 2>), g, th, 0, stream, p);
-    else if (items <= 4) hipLaunchKernelGGL((append_pages<D, 4>), g, th, 0, stream, p);
-    else hipLaunchKernelGGL((append_pages<D, 8>), g, th, 0, stream, p);
+    const dim3 g(static_cast<unsigned>(page_blocks + (p.q ? row_blocks : 0)));
+    const int items = (p.pool.page * (D / 16) + kAppendThreads - 1) / kAppendThreads, n = static_cast<int>(page_blocks);
+    if (items <= 1) hipLaunchKernelGGL((append_8bit<D, 1>), g, th, 0, stream, p, n);
+    else if (items <= 2) hipLaunchKernelGGL((append_8bit<D, 2>), g, th, 0, stream, p, n);
+    else if (items <= 4) hipLaunchKernelGGL((append_8bit<D, 4>), g, th, 0, stream, p, n);
+    else hipLaunchKernelGGL((append_8bit<D, 8>), g, th, 0, stream, p, n);
   }
   return check_launch("pace_cache_append");
 }
@@ -1499,7 +1511,7 @@ pace_status_t pace_cache_append(const uint16_t* q, long long q_stride, const uin
   p.pages = (max_new - 1 + cache->page - 1) / cache->page + 1;
   const long long row_blocks = static_cast<long long>(B) * p.tiles;
   const long long page_blocks = 2ll * B * p.pages * hkv;
-  PACE_REQUIRE(row_blocks < (1ll << 31) && page_blocks < (1ll << 31) &&
+  PACE_REQUIRE(row_blocks + page_blocks < (1ll << 31) &&
                    static_cast<long long>(kAppendTokens) * (static_cast<long long>(Hq) + 2 * hkv) * d < (1ll << 31),
                "pace_cache_append: too many sequences, tokens or heads");
   if (debug_checks()) {

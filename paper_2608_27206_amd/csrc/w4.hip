@@ -95,18 +95,41 @@ __device__ __forceinline__ void w4_store(const W4Params& p, int m, int n, float 
   p.C[at] = f32_bf16(y);
 }
 
-// Up to 16 rows: bound by the weights' bytes.  A wave streams 256 k's of NT tiles of 16 columns a step (whole 128-byte
-// lines of each row); W waves share the columns, take consecutive parts of K and join through LDS.  sum x comes from one
-// more product with ones.
+// Stages 8 k's of a row of x for the kernels below: in the nibbles' order to *to, and the sum over each group of G k's,
+// which 16 consecutive lanes hold 128 of, by the lanes whose piece begins one.
+template <int G>
+__device__ __forceinline__ void stage_x(uint4 u, int piece, uint4* to, float* sums) {
+  const uint32_t v[4] = {u.x, u.y, u.z, u.w};
+  float s = 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) s += __uint_as_float(v[e] << 16) + __uint_as_float(v[e] & 0xffff0000u);
+  s += dpp_f32<kDppQuadXor1>(s);
+  s += dpp_f32<kDppQuadXor2>(s);
+  if (G >= 64) s += dpp_f32<kDppRowHalfMirror>(s);
+  if (G >= 128) s += dpp_f32<kDppRowMirror>(s);
+  *to = nibble_order(u);
+  if (piece % (G / 8) == 0) *sums = s;
+}
+
+// Up to MR = 8 or 16 rows: bound by the weights' bytes.  Of a workgroup's 8 waves, W share NT tiles of 16 columns and take
+// the steps of 256 k's (whole 128-byte lines of each row) of every chunk of K in turn; they join through LDS.  A wave keeps
+// the next chunk's weights in flight while it works on one.  x passes through LDS, two chunks of it: straight from the
+// caches, a lane's 16 bytes lie a row away from its neighbour's, 64 accesses a load, and these bound the kernel (eight
+// rows through 28,672 columns of 3,584: 30 us against 13).
 constexpr int kW4Waves = 8;
-template <int NT, int W, int GROUP>
-__global__ __launch_bounds__(64 * kW4Waves) void gemm_w4_few(const W4Params p) {
-  constexpr int STEP = 256, GB = 128 / GROUP, SPG = 4 / GB;      // groups per 128 k's, products per group
+template <int NT, int W, int GROUP, int MR>
+__global__ __launch_bounds__(64 * kW4Waves, 2) void gemm_w4_few(const W4Params p) {
+  constexpr int STEP = 256, SC = MR == 8 ? 8 : 4, CHUNK = STEP * SC, PW = SC / W;   // steps of a chunk, and of a wave in it
+  constexpr int GB = 128 / GROUP, SPG = 4 / GB, GS = 2 * GB, GC = CHUNK / GROUP;    // groups per 128 k's, step, chunk
+  constexpr int PIECES = CHUNK / 8, LROW = PIECES + 1, NX = MR * PIECES / (64 * kW4Waves);
+  static_assert(W <= SC, "a wave needs a step in every chunk");
+  __shared__ uint4 xt[2][MR * LROW];
+  __shared__ float xs[2][GC][MR];
   __shared__ float join[kW4Waves / W][W > 1 ? W / 2 : 1][NT * 4][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int w = wave % W, set = wave / W;
   const int n0 = (remap_block_id(blockIdx.x, gridDim.x) * (kW4Waves / W) + set) * 16 * NT;
-  const int steps = (p.K + STEP - 1) / STEP, s0 = steps * w / W, s1 = steps * (w + 1) / W, groups = p.K / GROUP;
+  const int steps = (p.K + STEP - 1) / STEP, chunks = (steps + SC - 1) / SC, groups = p.K / GROUP;
 
   // lane constants beside a base that only the step moves (every operand is under 2 GiB)
   unsigned woff[NT], row[NT];
@@ -116,79 +139,96 @@ __global__ __launch_bounds__(64 * kW4Waves) void gemm_w4_few(const W4Params p) {
     woff[t] = n * (p.K / 2) + 16 * g;
     row[t] = n * groups;
   }
-  const unsigned xoff = (r < p.M ? r : p.M - 1) * p.K + 8 * g;
+  const int xr = r < MR ? r : MR - 1;                  // rows past p.M hold anything: they are not stored
 
-  uint4 wq[NT][2], xf[2][4];
-  Groups<2 * GB> gq[NT];
-  const auto load_step = [&](int s, auto tail) {
-    constexpr bool TAIL = decltype(tail)::value;
+  u32x4 wq[PW][NT][2];
+  Groups<GS> gq[PW][NT];
+  uint4 xq[NX];
+  const auto load_w = [&](int s, u32x4 (&to)[NT][2], Groups<GS> (&gt)[NT]) {
     const uint8_t* wb = p.w + static_cast<size_t>(s) * (STEP / 2);
-    const uint16_t* xb = p.x + static_cast<size_t>(s) * STEP;
+    const bool whole = (s + 1) * STEP <= p.K;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+    for (int t = 0; t < NT; ++t) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
+      for (int u = 0; u < 2; ++u) {
         // past the end: the row's first block again, for x's zeros there
-        const bool in = !TAIL || s * STEP + 128 * u + 32 * g < p.K;
-        const u32x4 y = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>((in ? wb + 64 * u : p.w) + woff[t]));
-        wq[t][u] = make_uint4(y.x, y.y, y.z, y.w);
+        const bool in = whole || s * STEP + 128 * u + 32 * g < p.K;
+        to[t][u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>((in ? wb + 64 * u : p.w) + woff[t]));
       }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        xf[u][q] = make_uint4(0, 0, 0, 0);
-        if (!TAIL || s * STEP + 128 * u + 32 * q + 8 * g < p.K)
-          xf[u][q] = *reinterpret_cast<const uint4*>(xb + 128 * u + 32 * q + xoff);
-      }
+      if (whole) gt[t].template load<false>(p, row[t], s * GS, groups);
+      else gt[t].template load<true>(p, row[t], s * GS, groups);
     }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) gq[t].template load<TAIL>(p, row[t], s * 2 * GB, groups);
   };
-  const auto load = [&](int s) {
-    if ((s + 1) * STEP <= p.K) load_step(s, std::false_type());
-    else load_step(s, std::true_type());
+  const auto load_x = [&](int c) {
+#pragma unroll
+    for (int i = 0; i < NX; ++i) {
+      const int at = i * 64 * kW4Waves + threadIdx.x, m = at / PIECES, k = c * CHUNK + at % PIECES * 8;
+      xq[i] = make_uint4(0, 0, 0, 0);
+      if (m < p.M && k < p.K) xq[i] = *reinterpret_cast<const uint4*>(p.x + static_cast<size_t>(m) * p.K + k);
+    }
+  };
+  const auto store_x = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < NX; ++i) {
+      const int at = i * 64 * kW4Waves + threadIdx.x, m = at / PIECES, piece = at % PIECES;
+      stage_x<GROUP>(xq[i], piece, &xt[buf][m * LROW + piece], &xs[buf][piece / (GROUP / 8)][m]);
+    }
   };
 
   f32x4 acc[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const uint4 ones = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
 
-  if (s0 < s1) load(s0);
-  for (int s = s0; s < s1; ++s) {
-    uint32_t d[NT][2][4];
-    uint4 xa[2][4];
-    Groups<2 * GB> gc[NT];
+  load_x(0);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+  for (int j = 0; j < PW; ++j)
+    if (w * PW + j < steps) load_w(w * PW + j, wq[j], gq[j]);
+  store_x(0);
+  __syncthreads();
+  for (int c = 0; c < chunks; ++c) {
+    const int buf = c & 1;
+    if (c + 1 < chunks) load_x(c + 1);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) { d[t][u][0] = wq[t][u].x; d[t][u][1] = wq[t][u].y; d[t][u][2] = wq[t][u].z; d[t][u][3] = wq[t][u].w; }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) xa[u][q] = nibble_order(xf[u][q]);
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) gc[t] = gq[t];
-    if (s + 1 < s1) load(s + 1);
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      f32x4 xs[GB];
-#pragma unroll
-      for (int q = 0; q < GB; ++q) xs[q] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int q = 0; q < 4; ++q) xs[q / SPG] = mfma16(xa[u][q], ones, xs[q / SPG]);
+    for (int j = 0; j < PW; ++j) {
+      const int s = c * SC + w * PW + j;
+      if (s >= steps) break;
+      uint32_t d[NT][2][4];
+      Groups<GS> gc[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        transpose_groups(d[t][u]);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) d[t][u][q] = wq[j][t][u][q];
+        gc[t] = gq[j][t];
+      }
+      if (s + SC < steps) load_w(s + SC, wq[j], gq[j]);
+      const uint4* xl = &xt[buf][xr * LROW + (w * PW + j) * (STEP / 8) + g];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        uint4 xa[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) xa[q] = xl[16 * u + 4 * q];
 #pragma unroll
         for (int q = 0; q < GB; ++q) {
-          f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
+          const float4 x = *reinterpret_cast<const float4*>(&xs[buf][(w * PW + j) * GS + GB * u + q][(4 * g) % MR]);
 #pragma unroll
-          for (int e = q * SPG; e < (q + 1) * SPG; ++e) sum = mfma16(xa[u][e], nibbles(d[t][u][e]), sum);
-          const float sg = gc[t].scale(GB * u + q), zg = gc[t].zero(p, GB * u + q);
+          for (int t = 0; t < NT; ++t) {
+            if (q == 0) transpose_groups(d[t][u]);
+            f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[t][i] = fmaf(sg, fmaf(-zg, xs[q][i], sum[i]), acc[t][i]);
+            for (int e = q * SPG; e < (q + 1) * SPG; ++e) sum = mfma16(xa[e], nibbles(d[t][u][e]), sum);
+            const float sg = gc[t].scale(GB * u + q), zg = gc[t].zero(p, GB * u + q);
+            acc[t][0] = fmaf(sg, fmaf(-zg, x.x, sum[0]), acc[t][0]);
+            acc[t][1] = fmaf(sg, fmaf(-zg, x.y, sum[1]), acc[t][1]);
+            acc[t][2] = fmaf(sg, fmaf(-zg, x.z, sum[2]), acc[t][2]);
+            acc[t][3] = fmaf(sg, fmaf(-zg, x.w, sum[3]), acc[t][3]);
+          }
         }
       }
     }
+    if (c + 1 < chunks) store_x(buf ^ 1);
+    __syncthreads();
   }
 
 #pragma unroll
@@ -224,13 +264,14 @@ __global__ __launch_bounds__(64 * kW4Waves) void gemm_w4_few(const W4Params p) {
 }
 
 // More rows (16 MT at a time): here x would be read far more often than the weights, so the 4 waves of a workgroup take 32
-// columns each and share x through LDS, 128 k's at a time (in the nibbles' order, with its sums over every 32 k's);
-// workgroups split K where the columns give too few, and w4_join adds their sums.
+// columns each and share x through LDS, 256 k's at a time; workgroups split K where the columns give too few, and w4_join
+// adds their sums.
 template <int MT, int GROUP>
-__global__ __launch_bounds__(256) void gemm_w4_rows(const W4Params p) {
-  constexpr int NT = 2, STEP = 128, GB = STEP / GROUP, SPG = 4 / GB, ROWS = 16 * MT, LROW = 17;
-  __shared__ uint4 xt[2][ROWS * LROW];                 // [row][16 pieces of 8 k's]
-  __shared__ float xs[2][4][ROWS];                     // [32 k's][row]
+__global__ __launch_bounds__(256, 2) void gemm_w4_rows(const W4Params p) {
+  constexpr int NT = 2, STEP = 256, GB = 128 / GROUP, SPG = 4 / GB, GS = 2 * GB, ROWS = 16 * MT;
+  constexpr int PIECES = STEP / 8, LROW = PIECES + 1, NX = ROWS * PIECES / 256;
+  __shared__ uint4 xt[2][ROWS * LROW];                 // [row][pieces of 8 k's]
+  __shared__ float xs[2][GS][ROWS];                    // [group][row]
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int id = remap_block_id(blockIdx.x, gridDim.x);
   const int n0 = (id % p.ntiles * 4 + w) * 16 * NT, split = id / p.ntiles, m0 = blockIdx.y * ROWS;
@@ -245,51 +286,38 @@ __global__ __launch_bounds__(256) void gemm_w4_rows(const W4Params p) {
     woff[t] = n * (p.K / 2) + 16 * g;
     row[t] = n * groups;
   }
-  // x: thread t stages piece t % 16 of rows t / 16 + 16 i
-  const int piece = threadIdx.x & 15, xr = threadIdx.x >> 4;
-  unsigned xoff[MT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int m = m0 + xr + 16 * i;
-    xoff[i] = static_cast<unsigned>(m < p.M ? m : p.M - 1) * p.K + 8 * piece;
-  }
+  // x: thread t stages piece t % 32 of rows t / 32 + 8 i
+  const int piece = threadIdx.x % PIECES, xr = threadIdx.x / PIECES;
 
-  uint4 wq[NT], xq[MT];
-  Groups<GB> gq[NT];
-  const auto load_step = [&](int s, auto tail) {
-    constexpr bool TAIL = decltype(tail)::value;
+  u32x4 wq[NT][2];
+  uint4 xq[NX];
+  Groups<GS> gq[NT];
+  const auto load = [&](int s) {
     const uint8_t* wb = p.w + static_cast<size_t>(s) * (STEP / 2);
-    const uint16_t* xb = p.x + static_cast<size_t>(s) * STEP;
+    const bool whole = (s + 1) * STEP <= p.K;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const bool in = !TAIL || s * STEP + 32 * g < p.K;
-      const u32x4 y = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>((in ? wb : p.w) + woff[t]));
-      wq[t] = make_uint4(y.x, y.y, y.z, y.w);
-      gq[t].template load<TAIL>(p, row[t], s * GB, groups);
-    }
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      xq[i] = make_uint4(0, 0, 0, 0);
-      if (!TAIL || s * STEP + 8 * piece < p.K) xq[i] = *reinterpret_cast<const uint4*>(xb + xoff[i]);
+      for (int u = 0; u < 2; ++u) {
+        // past the end: the row's first block again, for x's zeros there
+        const bool in = whole || s * STEP + 128 * u + 32 * g < p.K;
+        wq[t][u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>((in ? wb + 64 * u : p.w) + woff[t]));
+      }
+      if (whole) gq[t].template load<false>(p, row[t], s * GS, groups);
+      else gq[t].template load<true>(p, row[t], s * GS, groups);
     }
-  };
-  const auto load = [&](int s) {
-    if ((s + 1) * STEP <= p.K) load_step(s, std::false_type());
-    else load_step(s, std::true_type());
+    const int k = s * STEP + 8 * piece;
+#pragma unroll
+    for (int i = 0; i < NX; ++i) {
+      const int m = m0 + xr + 8 * i;
+      xq[i] = make_uint4(0, 0, 0, 0);
+      if (m < p.M && k < p.K) xq[i] = *reinterpret_cast<const uint4*>(p.x + static_cast<size_t>(m) * p.K + k);
+    }
   };
   const auto stage = [&](int buf) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const uint4 u = xq[i];
-      float sum = 0.f;
-      const uint32_t v[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum += __uint_as_float(v[e] << 16) + __uint_as_float(v[e] & 0xffff0000u);
-      sum += dpp_f32<kDppQuadXor1>(sum);
-      sum += dpp_f32<kDppQuadXor2>(sum);
-      xt[buf][(xr + 16 * i) * LROW + piece] = nibble_order(u);
-      if ((piece & 3) == 0) xs[buf][piece >> 2][xr + 16 * i] = sum;
-    }
+    for (int i = 0; i < NX; ++i)
+      stage_x<GROUP>(xq[i], piece, &xt[buf][(xr + 8 * i) * LROW + piece], &xs[buf][piece / (GROUP / 8)][xr + 8 * i]);
   };
 
   f32x4 acc[MT][NT];
@@ -302,51 +330,52 @@ __global__ __launch_bounds__(256) void gemm_w4_rows(const W4Params p) {
   for (int s = s0; s < s1; ++s) {
     const int buf = (s - s0) & 1;
     stage(buf);
-    uint32_t d[NT][4];
-    Groups<GB> gc[NT];
+    uint32_t d[NT][2][4];
+    Groups<GS> gc[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      d[t][0] = wq[t].x; d[t][1] = wq[t].y; d[t][2] = wq[t].z; d[t][3] = wq[t].w;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) d[t][u][q] = wq[t][u][q];
       gc[t] = gq[t];
     }
     if (s + 1 < s1) load(s + 1);
-#pragma unroll
-    for (int t = 0; t < NT; ++t) transpose_groups(d[t]);
     __syncthreads();                                   // the buffer is written again two steps on, past the next barrier
 #pragma unroll
-    for (int q = 0; q < GB; ++q) {
-      f32x4 sum[MT][NT];
+    for (int u = 0; u < 2; ++u) {
 #pragma unroll
-      for (int a = 0; a < MT; ++a)
+      for (int t = 0; t < NT; ++t) transpose_groups(d[t][u]);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) sum[a][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int q = 0; q < GB; ++q) {
+        f32x4 sum[MT][NT];
 #pragma unroll
-      for (int e = q * SPG; e < (q + 1) * SPG; ++e) {
-        uint4 b[NT];
+        for (int a = 0; a < MT; ++a)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) b[t] = nibbles(d[t][e]);
-#pragma unroll
-        for (int a = 0; a < MT; ++a) {
-          const uint4 x = xt[buf][(16 * a + r) * LROW + 4 * e + g];
-#pragma unroll
-          for (int t = 0; t < NT; ++t) sum[a][t] = mfma16(x, b[t], sum[a][t]);
-        }
-      }
-#pragma unroll
-      for (int a = 0; a < MT; ++a) {
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int t = 0; t < NT; ++t) sum[a][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int e = q * SPG; e < (q + 1) * SPG; ++e) {
-          const float4 y = *reinterpret_cast<const float4*>(&xs[buf][e][16 * a + 4 * g]);
-          x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+          uint4 b[NT];
+#pragma unroll
+          for (int t = 0; t < NT; ++t) b[t] = nibbles(d[t][u][e]);
+#pragma unroll
+          for (int a = 0; a < MT; ++a) {
+            const uint4 x = xt[buf][(16 * a + r) * LROW + 16 * u + 4 * e + g];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) sum[a][t] = mfma16(x, b[t], sum[a][t]);
+          }
         }
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const float sg = gc[t].scale(q), zg = gc[t].zero(p, q);
-          acc[a][t][0] = fmaf(sg, fmaf(-zg, x.x, sum[a][t][0]), acc[a][t][0]);
-          acc[a][t][1] = fmaf(sg, fmaf(-zg, x.y, sum[a][t][1]), acc[a][t][1]);
-          acc[a][t][2] = fmaf(sg, fmaf(-zg, x.z, sum[a][t][2]), acc[a][t][2]);
-          acc[a][t][3] = fmaf(sg, fmaf(-zg, x.w, sum[a][t][3]), acc[a][t][3]);
+        for (int a = 0; a < MT; ++a) {
+          const float4 x = *reinterpret_cast<const float4*>(&xs[buf][GB * u + q][16 * a + 4 * g]);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const float sg = gc[t].scale(GB * u + q), zg = gc[t].zero(p, GB * u + q);
+            acc[a][t][0] = fmaf(sg, fmaf(-zg, x.x, sum[a][t][0]), acc[a][t][0]);
+            acc[a][t][1] = fmaf(sg, fmaf(-zg, x.y, sum[a][t][1]), acc[a][t][1]);
+            acc[a][t][2] = fmaf(sg, fmaf(-zg, x.z, sum[a][t][2]), acc[a][t][2]);
+            acc[a][t][3] = fmaf(sg, fmaf(-zg, x.w, sum[a][t][3]), acc[a][t][3]);
+          }
         }
       }
     }
@@ -376,8 +405,16 @@ __global__ __launch_bounds__(256) void w4_join(const W4Params p) {
   if (n >= p.N) return;
   float y[2];
   for (int c = 0; c < per; ++c) {
+    const float* from = p.part + static_cast<long long>(m) * p.N + n + c;
+    const long long step = static_cast<long long>(p.M) * p.N;
     float s = 0.f;
-    for (int k = 0; k < p.splits; ++k) s += p.part[(static_cast<long long>(k) * p.M + m) * p.N + n + c];
+    for (int k = 0; k < p.splits; k += 8) {
+      float v[8];                                      // loads in flight together, summed in order
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = k + u < p.splits ? from[(k + u) * step] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += v[u];
+    }
     y[c] = s + (p.bias ? p.bias[n + c] : 0.f);
   }
   w4_store(p, m, n, y[0], y[per - 1]);
@@ -386,49 +423,55 @@ __global__ __launch_bounds__(256) void w4_join(const W4Params p) {
 struct W4Plan {
   int mt, nt, waves, ntiles, splits;   // ntiles: workgroups along the columns
 };
-#ifndef VW4
-#define VW4 512
-#endif
-#ifndef VNT4
-#define VNT4 100000
-#endif
-#ifndef VWV
-#define VWV 4096
-#endif
-W4Plan plan_w4(int M, int N, int K) {
+W4Plan plan_w4(int M, int N, int K, int group) {
   W4Plan a;
   a.splits = 1;
   if (M <= 16) {
     a.mt = 1;
     const int tiles = (N + 15) / 16;
-    a.nt = tiles >= VNT4 ? 2 : 1;
-    a.waves = 8;
-    while (a.waves > 1 && tiles / a.nt * a.waves > VWV) a.waves /= 2;
+    // From 16,384 columns on two tiles a wave (eight rows, 28,672 x 3584: 23.8 us against 25.4), and about 2,000 waves in
+    // all: fewer leave CUs idle (one row, 4608 x 3584: 1,152 waves 11.0 us, 2,304 7.9), more only join more (the wide one:
+    // 23.7 us with 2,048 waves, 30.2 with 7,168).
+    a.nt = tiles >= 1024 && group > 32 ? 2 : 1;
+    a.waves = M <= 8 ? 8 : 4;
+    while (a.waves > 2 && tiles / a.nt * a.waves > 2560) a.waves /= 2;
     a.ntiles = ((tiles + a.nt - 1) / a.nt * a.waves + kW4Waves - 1) / kW4Waves;
     return a;
   }
   a.mt = M <= 32 ? 2 : M <= 48 ? 3 : 4;
   a.nt = 2;
   a.ntiles = (N + 127) / 128;
-  const int steps = (K + 127) / 128, rows = (M + 63) / 64;
-  const int s = VW4 / (a.ntiles * rows), most = (steps + 3) / 4;       // at least four steps each
+  const int steps = (K + 255) / 256, rows = (M + 63) / 64;
+  // two workgroups on every CU (48 rows, 3584 x 14336: 27.6 us; 256 workgroups 29.0, 768 31.8)
+  const int s = 512 / (a.ntiles * rows), most = (steps + 1) / 2;       // at least two steps each
   a.splits = s < 1 ? 1 : s < most ? s : most;
   return a;
 }
 
-template <int NT, int W>
+template <int NT, int W, int MR>
 void launch_few(const W4Params& p, int group, hipStream_t stream) {
   const dim3 g(p.ntiles), th(64 * kW4Waves);
-  if (group == 32) hipLaunchKernelGGL((gemm_w4_few<NT, W, 32>), g, th, 0, stream, p);
-  else if (group == 64) hipLaunchKernelGGL((gemm_w4_few<NT, W, 64>), g, th, 0, stream, p);
-  else hipLaunchKernelGGL((gemm_w4_few<NT, W, 128>), g, th, 0, stream, p);
+  if constexpr (NT == 1) {                             // groups of 32: their scales leave no registers for two tiles
+    if (group == 32) {
+      hipLaunchKernelGGL((gemm_w4_few<NT, W, 32, MR>), g, th, 0, stream, p);
+      return;
+    }
+  }
+  if (group == 64) hipLaunchKernelGGL((gemm_w4_few<NT, W, 64, MR>), g, th, 0, stream, p);
+  else hipLaunchKernelGGL((gemm_w4_few<NT, W, 128, MR>), g, th, 0, stream, p);
 }
 template <int NT>
 void launch_few(const W4Params& p, int waves, int group, hipStream_t stream) {
-  if (waves == 8) launch_few<NT, 8>(p, group, stream);
-  else if (waves == 4) launch_few<NT, 4>(p, group, stream);
-  else if (waves == 2) launch_few<NT, 2>(p, group, stream);
-  else launch_few<NT, 1>(p, group, stream);
+  if (p.M > 8) {
+    if (waves == 4) launch_few<NT, 4, 16>(p, group, stream);
+    else launch_few<NT, 2, 16>(p, group, stream);
+  } else if (waves == 8) {
+    launch_few<NT, 8, 8>(p, group, stream);
+  } else if (waves == 4) {
+    launch_few<NT, 4, 8>(p, group, stream);
+  } else {
+    launch_few<NT, 2, 8>(p, group, stream);
+  }
 }
 template <int MT>
 void launch_rows(const W4Params& p, int group, hipStream_t stream) {
@@ -447,7 +490,7 @@ extern "C" {
 
 size_t pace_gemm_w4_workspace_size(int M, int N, int K) {
   if (M < 1 || N < 1 || K < 1) return 0;
-  const W4Plan a = plan_w4(M, N, K);
+  const W4Plan a = plan_w4(M, N, K, 128);         // the group changes no split
   return a.splits == 1 ? 0 : static_cast<size_t>(a.splits) * M * N * sizeof(float);
 }
 
@@ -466,7 +509,7 @@ pace_status_t pace_gemm_w4(const uint16_t* x, const uint8_t* w, const uint16_t* 
   PACE_REQUIRE(2ll * M * K < lim && static_cast<long long>(N) * K / 2 < lim && 2ll * N * (K / group) < lim &&
                    2ll * M * N < lim && M <= 65535,
                "pace_gemm_w4: an operand reaches 2 GiB, or M=%d is past 65,535", M);
-  const W4Plan a = plan_w4(M, N, K);
+  const W4Plan a = plan_w4(M, N, K, group);
   const size_t need = pace_gemm_w4_workspace_size(M, N, K);
   if (need) {
     if (workspace == nullptr || workspace_bytes < need)
