@@ -248,6 +248,15 @@ ATTEND = [
     (16, 64, (8, 2), 80, [150, 9], [400, 9], 130, 70),
     (16, 64, (8, 2), 128, [90], [90], 1000, 4),                            # a window longer than the context
     (16, 64, (8, 2), 128, [6], [200], 50, 500),                            # sinks past the end: all keys
+    (8, 16, (4, 2), 128, [50], [77], 0, 0),                                # 33 to 128 rows of a KV head
+    (8, 32, (16, 4), 80, [20, 11], [100, 300], 0, 0),
+    (16, 128, (2, 1), 128, [60], [61], 0, 0),
+    (16, 16, (3, 1), 80, [33], [500], 40, 20),
+    (16, 64, (4, 2), 128, [40], [2500], 0, 0),                             # split keys, joined
+    (8, 128, (8, 2), 128, [40], [1700], 0, 0),
+    (8, 16, (4, 2), 80, [1, 2], [3000, 1500], 0, 0),
+    (16, 32, (2, 2), 128, [1], [4097], 3000, 100),
+    (8, 64, (4, 1), 128, [1] * 70, list(range(70)), 0, 0),                 # many sequences, lengths from 0
 ]
 
 
@@ -392,7 +401,11 @@ def test_attention_large_scores():
 # ---------------------------------------------------------------- 4-bit weights
 W4 = [(1, 1, 32, 32, 0, 0), (1, 64, 128, 128, 1, 0), (3, 17, 96, 32, 1, 1), (1, 4608, 3584, 128, 0, 0), (5, 130, 1280, 64, 1, 2),
       (16, 100, 448, 64, 0, 1), (17, 33, 320, 64, 1, 0), (33, 250, 256, 128, 0, 2), (64, 77, 3424, 32, 1, 1),
-      (65, 48, 640, 128, 1, 0), (150, 34, 192, 64, 0, 2), (2, 31, 14336, 128, 1, 0), (8, 2, 288, 32, 0, 2)]
+      (65, 48, 640, 128, 1, 0), (150, 34, 192, 64, 0, 2), (2, 31, 14336, 128, 1, 0), (8, 2, 288, 32, 0, 2),
+      # wider: two tiles a wave, fewer waves per column; odd widths; 9 to 16 rows; many splits
+      (8, 8001, 512, 64, 1, 0), (12, 6000, 1056, 32, 0, 1), (16, 20002, 288, 32, 1, 2), (2, 28680, 384, 128, 0, 2),
+      (11, 24593, 640, 64, 1, 0), (9, 16400, 128, 128, 0, 1), (5, 32784, 96, 32, 1, 0), (7, 200, 2080, 32, 1, 0),
+      (40, 64, 14336, 64, 0, 1), (17, 130, 2016, 32, 1, 2), (64, 3000, 1152, 128, 1, 0), (128, 130, 1024, 128, 0, 2)]
 
 
 @pytest.mark.parametrize("M,N,K,group,zero,epilogue", W4)
