@@ -1121,7 +1121,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
         const int o = 8 * (c & 1);
         const float y = max3(max3(st[c >> 1][o], st[c >> 1][o + 1], st[c >> 1][o + 2]),
                              max3(st[c >> 1][o + 3], st[c >> 1][o + 4], st[c >> 1][o + 5]), fmaxf(st[c >> 1][o + 6], st[c >> 1][o + 7]));
-        top = fmaxf(top, (full_cur || ok_cur[c % NP]) ? y * f[c % NP] : -INFINITY);
+        top = fmaxf(top, full_cur || y != -INFINITY ? y * f[c % NP] : -INFINITY);   // see below
       }
       if (__any(top > m + 8.f)) {
         top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -1143,7 +1143,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
         for (int i = 0; i < 8; ++i) {
           const float s = st[c >> 1][8 * (c & 1) + i];
           e[i] = exp2_fast(fmaf(s, f[c % NP], -mz));
-          // the scales of pages that hold hidden keys alone may be anything
+          // the scales of pages that hold hidden keys alone may be anything, NaN and negative numbers among it
           if constexpr (BITS == 8) e[i] = full_cur || s != -INFINITY ? e[i] : 0.f;
           sum += e[i];
           if constexpr (BITS == 8) e[i] = full_cur || s != -INFINITY ? e[i] * vs[c % NP] : 0.f;
@@ -1399,7 +1399,7 @@ pace_status_t check_cache(const pace_kv_cache* c, const int32_t* table, int max_
                "%s: page=%d not 16, 32, 64, 128 or 256", what, c->page);
   if (c->dim != 80 && c->dim != 128)
     return set_error(PACE_ERR_UNSUPPORTED, "%s: head dim %d not in {80, 128}", what, c->dim);
-  PACE_REQUIRE(static_cast<long long>(max_pages) * c->page < (1ll << 31), "%s: max_pages * page past 2^31", what);
+  PACE_REQUIRE(static_cast<long long>(max_pages) * c->page <= (1ll << 31) - 1024, "%s: max_pages * page past 2^31 - 1024", what);
   out->k = c->k; out->v = c->v; out->k_scale = c->k_scale; out->v_scale = c->v_scale;
   out->table = table;
   out->num_pages = c->num_pages; out->max_pages = max_pages; out->heads = c->heads; out->page = c->page;

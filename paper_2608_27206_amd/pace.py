@@ -559,15 +559,18 @@ def _gpu_of(t: torch.Tensor) -> int:
     return device
 
 
+# the current stream's address without a Stream object around it, where torch has it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _call(name: str, device: int, *args):
     """A library call on the current stream of GPU number `device`, made current for it if it is not."""
     L = _lib or lib()
     if device != torch.cuda.current_device():
         with torch.cuda.device(device):
-            st = getattr(L, name)(*args, torch.cuda.current_stream(device).cuda_stream)
+            st = getattr(L, name)(*args, _raw_stream(device))
     else:
-        # the stream's address without a Stream object around it
-        st = getattr(L, name)(*args, torch._C._cuda_getCurrentRawStream(device))
+        st = getattr(L, name)(*args, _raw_stream(device))
     if st:
         _check(st, name)
 
@@ -630,6 +633,8 @@ def cache_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, ca
         qp, qs = _rows_arg(q, hq, dim, n_src, gpu, "q")
         if q_out is None:
             q_out = torch.empty((n_new, hq, dim), dtype=_BF16, device=q.device)
+    if n_new == 0:
+        return q_out
     axes, sec = 1, None
     if positions is not None:
         axes = 1 if positions.dim() == 1 else positions.shape[0]
@@ -663,6 +668,8 @@ def cache_attention(q: torch.Tensor, cache: KvCache, cu_q: torch.Tensor, seq_len
         lse = None
     elif lse is None:
         lse = torch.empty((hq, n_q), dtype=_F32, device=q.device)
+    if n_q == 0:
+        return o, lse
     if workspace is None:
         need = (_lib or lib()).pace_cache_attention_workspace_size(n_q, hq, cache.heads, dim, cache.bits, B, max_q, max_len,
                                                                    window, sinks)

@@ -330,6 +330,43 @@ def test_attention_bad_pages_count_as_unseen(bits, nq):
     assert np.all(f64(o)[nq] == 0) and np.all(f64(lse)[:, nq] == -np.inf)
 
 
+@pytest.mark.parametrize("nq", [1, 4, 20, 60])
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), -1.0, 0.0])
+def test_attention_does_not_use_scales_past_the_end(nq, scale):
+    """Table entries behind a sequence's last page that name a page of NaN with a scale of anything."""
+    import torch
+    from paper_2608_27206_amd import pace
+    rs = np.random.default_rng(nq)
+    lens = [nq + 49, 17 + nq, nq]
+    pages, table, kc, vc, ks, vs, q, cu = _attend_inputs((8, 16, (4, 2), 128, [nq] * 3, lens, 0, 0), rs)
+    ref = oc.attention(wl.bf16_bits_to_f64(q), f64(kc), f64(vc), f64(ks), f64(vs), cu, lens, np.where(table < 0, 0, table), 16, 128 ** -0.5)
+    used = set(table[table >= 0])
+    dead = next(p for p in range(pages) if p not in used)
+    table[table < 0] = dead
+    kc.view(torch.uint8)[dead], vc.view(torch.uint8)[dead] = 0x7F, 0x7F
+    ks[dead], vs[dead] = scale, scale
+    o, lse = pace.cache_attention(dev_bf16(q[:3 * nq]), pace.KvCache(kc, vc, ks, vs), dev_i32(cu), dev_i32(lens), dev_i32(table), nq, max(lens))
+    torch.cuda.synchronize()
+    n = 3 * nq
+    check_attention(f64(o), f64(lse), [ref[0][:n], ref[1][:, :n], ref[2][:n], ref[3][:, :n]], 128, n)
+
+
+def test_nothing_to_do():
+    import torch
+    from paper_2608_27206_amd import pace
+    c = pace.KvCache(*make_pool(np.random.default_rng(1), 2, 2, 16, 128, 16))
+    x = torch.empty((0, 2, 128), dtype=torch.bfloat16, device="cuda")
+    out = pace.cache_append(x, x, x, c, dev_i32([0, 0]), dev_i32([0]), dev_i32([[0]]), 0)
+    o, lse = pace.cache_attention(x, c, dev_i32([0, 0]), dev_i32([0]), dev_i32([[0]]), 0, 0)
+    assert out.shape == o.shape == (0, 2, 128) and lse.shape == (2, 0)
+    # a sequence without tokens or queries next to one with both
+    y = dev_bf16(wl.random_bf16(3, (1, 2, 128)))
+    pace.cache_append(None, y, y, c, dev_i32([0, 0, 1]), dev_i32([7, 0]), dev_i32([[1], [0]]), 1)
+    o, lse = pace.cache_attention(y, c, dev_i32([0, 0, 1]), dev_i32([0, 1]), dev_i32([[1], [0]]), 1, 16)
+    torch.cuda.synchronize()
+    assert np.array_equal(f64(o), f64(y))          # one key: its value
+
+
 @pytest.mark.parametrize("window,sinks", [(0, 0), (20, 3)])
 @pytest.mark.parametrize("bits,nq", [(16, 6), (8, 6), (16, 90), (8, 200)])
 def test_hidden_keys_do_not_matter(bits, nq, window, sinks):
