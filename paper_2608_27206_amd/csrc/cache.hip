@@ -4,6 +4,7 @@
 #include <math.h>
 
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "pace_internal.h"
@@ -421,13 +422,12 @@ __device__ __forceinline__ int page_of(const AttendParams& p, int entry, int key
 //  O^T = V^T P^T: a lane loads 8 values of each of its 8 keys (8 r .. 8 r + 7 of a row) and turns the 8 x 8
 //    block in registers (one v_perm for two values), so that row m of product c is d = 8 m + c, and a lane
 //    ends with 8 consecutive d of each of four blocks.
-// A row's maximum is only raised when a score passes it by 2^8 (a wave-wide vote), so most tiles need no
-// exchange between lanes; probabilities of up to 256 round like others.
-#ifndef VMIN
-#define VMIN 3
-#endif
+// A row's maximum is only raised when a score passes it by 2^8 (the lanes exchange scores when any row's does), so most
+// tiles need no exchange; probabilities of up to 256 round like others.
+// Three waves per SIMD for 16 rows: 48 ragged sequences of up to 16,384 tokens in 8 bits take 104 us with three and
+// 117 with two (the registers that two would have are not needed); 32 rows do not fit in three's.
 template <int D, int BITS, int R, int W>
-__global__ __launch_bounds__(64 * W, R == 1 ? VMIN : 2) void attend_few(const AttendParams p) {
+__global__ __launch_bounds__(64 * W, R == 1 ? 3 : 2) void attend_few(const AttendParams p) {
   constexpr int T = tile_keys(BITS), U = T / 32;      // keys per step, in blocks of 32
   constexpr int KS = (D + 31) / 32;                   // products along d
   constexpr int KW = BITS == 16 ? 4 : 2;              // dwords of 8 values
@@ -649,7 +649,7 @@ __global__ __launch_bounds__(64 * W, R == 1 ? VMIN : 2) void attend_few(const At
       if (__any(top > m[t] + 8.f)) {
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float mn = fmaxf(m[t], top);
+        const float mn = top > m[t] + 8.f ? top : m[t];   // a row's own scores alone decide about its sums
         const float k = mn == m[t] ? 1.f : exp2_fast(m[t] - mn);
         m[t] = mn;
         l[t] *= k;
@@ -891,9 +891,10 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
   const int slot_mask = p.pool.page - 1;
   const int dg = lane % DG, vkey = (64 / DG) * 4 * w + 4 * (lane / DG);   // V: this thread's VD d's and 4 keys
   const int vpart = NP == 1 ? 0 : w * 4 / WAVES;       // the part of the tile that they lie in
-  uint32_t kr[NK][4], vr[4][VW];
-  int entry[NP], pg[NP], pg_v = -1;                    // the next tile's entries, the staged tile's pages
-  float ks[NP], vs[NP], ks_n[NP], vs_n[NP];
+  constexpr int SETS = G == 1 ? 2 : 1;                 // tiles in flight; two groups have registers for one
+  uint32_t kr[SETS][NK][4], vr[SETS][4][VW];
+  int entry[NP], pg[SETS][NP], pg_v[SETS];             // the next tile's entries, the pages of those in flight
+  float ks[NP], vs[NP], ks_n[SETS][NP], vs_n[SETS][NP];
 
   const auto look_up = [&](int base) {
 #pragma unroll
@@ -912,20 +913,21 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
     koff[i] = (row % KEYS) * D * E + at % CPR * 16;
   }
   const int voff = (vkey % KEYS * D + (VD * dg < D ? VD * dg : 0)) * E;
-  const auto load = [&](int base) {
+  const auto load = [&](int base, auto set) {
+    constexpr int S = decltype(set)::value;
     const char *kb[NP], *vb = nullptr;                 // the same for all lanes
 #pragma unroll
     for (int h = 0; h < NP; ++h) {
-      pg[h] = page_of(p, entry[h], base + KEYS * h);
-      kb[h] = row_of(p.pool.k, base + KEYS * h, pg[h]);
+      pg[S][h] = page_of(p, entry[h], base + KEYS * h);
+      kb[h] = row_of(p.pool.k, base + KEYS * h, pg[S][h]);
       if (h == vpart) {
-        vb = row_of(p.pool.v, base + KEYS * h, pg[h]);
-        pg_v = pg[h];
+        vb = row_of(p.pool.v, base + KEYS * h, pg[S][h]);
+        pg_v[S] = pg[S][h];
       }
       if constexpr (BITS == 8) {
-        const long long ph = static_cast<long long>(pg[h] < 0 ? 0 : pg[h]) * p.pool.heads + hk;
-        ks_n[h] = p.pool.k_scale[ph];
-        vs_n[h] = p.pool.v_scale[ph];
+        const long long ph = static_cast<long long>(pg[S][h] < 0 ? 0 : pg[S][h]) * p.pool.heads + hk;
+        ks_n[S][h] = p.pool.k_scale[ph];
+        vs_n[S][h] = p.pool.v_scale[ph];
       }
     }
 #pragma unroll
@@ -937,56 +939,57 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
         from = part < 2 ? (part == 0 ? kb[0] : kb[1]) : (part == 2 ? kb[2] : kb[3]);
       }
       const u32x4 y = *reinterpret_cast<const u32x4*>(from + koff[i]);
-      kr[i][0] = y.x; kr[i][1] = y.y; kr[i][2] = y.z; kr[i][3] = y.w;
+      kr[S][i][0] = y.x; kr[S][i][1] = y.y; kr[S][i][2] = y.z; kr[S][i][3] = y.w;
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const char* from = vb + voff + j * D * E;
       if constexpr (VW == 4) {
         const u32x4 y = *reinterpret_cast<const u32x4*>(from);
-        vr[j][0] = y.x; vr[j][1] = y.y; vr[j][2] = y.z; vr[j][3] = y.w;
+        vr[S][j][0] = y.x; vr[S][j][1] = y.y; vr[S][j][2] = y.z; vr[S][j][3] = y.w;
       } else if constexpr (VW == 2) {
         const u32x2 y = *reinterpret_cast<const u32x2*>(from);
-        vr[j][0] = y.x; vr[j][1] = y.y;
+        vr[S][j][0] = y.x; vr[S][j][1] = y.y;
       } else {
-        vr[j][0] = *reinterpret_cast<const uint32_t*>(from);
+        vr[S][j][0] = *reinterpret_cast<const uint32_t*>(from);
       }
     }
   };
   // every row of the workgroup sees every key of the tile (whose pages are in pg)
-  const auto is_full = [&](int base) {
+  const auto is_full = [&](int base, int s) {
     bool ok = base + T - 1 <= sp.p_lo && (p.window == 0 || base > sp.p_hi - p.window || base + T <= p.sinks);
 #pragma unroll
-    for (int h = 0; h < NP; ++h) ok = ok && pg[h] >= 0;
+    for (int h = 0; h < NP; ++h) ok = ok && pg[s][h] >= 0;
     return ok;
   };
-  const auto store = [&](int base, int buf) {
+  const auto store = [&](int base, int buf, auto set) {
+    constexpr int S = decltype(set)::value;
     uint4* kl = kt[gr][buf];
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
       const int at = i * NT + tid, row = at / CPR, piece = at % CPR;
       if (T * CPR % NT != 0 && row >= T) continue;
       if constexpr (BITS == 16) {
-        kl[row * KROW + piece] = make_uint4(kr[i][0], kr[i][1], kr[i][2], kr[i][3]);
+        kl[row * KROW + piece] = make_uint4(kr[S][i][0], kr[S][i][1], kr[S][i][2], kr[S][i][3]);
       } else {
-        kl[row * KROW + 2 * piece] = e4m3_bf16x8(kr[i][0], kr[i][1]);
-        kl[row * KROW + 2 * piece + 1] = e4m3_bf16x8(kr[i][2], kr[i][3]);
+        kl[row * KROW + 2 * piece] = e4m3_bf16x8(kr[S][i][0], kr[S][i][1]);
+        kl[row * KROW + 2 * piece + 1] = e4m3_bf16x8(kr[S][i][2], kr[S][i][3]);
       }
     }
-    if (!is_full(base)) {
+    if (!is_full(base, S)) {
       // V rows that no row sees become 0 (0 * NaN is NaN); where the rows differ, values that are not finite too, and
       // `poison` notes which results get a +inf or -inf instead (1, 2; a NaN counts as both)
       uint32_t wild = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int key = base + vkey + j;
-        const bool sees = pg_v >= 0 && key <= sp.p_hi && (p.window == 0 || key > sp.p_lo - p.window || key < p.sinks);
+        const bool sees = pg_v[S] >= 0 && key <= sp.p_hi && (p.window == 0 || key > sp.p_lo - p.window || key < p.sinks);
 #pragma unroll
         for (int d = 0; d < VW; ++d) {
-          vr[j][d] = sees ? vr[j][d] : 0u;
-          const uint32_t m = not_finite<BITS>(vr[j][d]);
+          vr[S][j][d] = sees ? vr[S][j][d] : 0u;
+          const uint32_t m = not_finite<BITS>(vr[S][j][d]);
           wild |= m;
-          if (sp.p_lo != sp.p_hi) vr[j][d] &= ~(BITS == 16 ? (m >> 15) * 0xffffu : (m >> 7) * 0xffu);
+          if (sp.p_lo != sp.p_hi) vr[S][j][d] &= ~(BITS == 16 ? (m >> 15) * 0xffffu : (m >> 7) * 0xffu);
         }
       }
       if (sp.p_lo != sp.p_hi && __any(wild != 0)) {
@@ -1026,12 +1029,12 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
       for (int c = 0; c < VD; ++c) {
         uint2 y;
         if constexpr (BITS == 8) {
-          const uint32_t lo = __builtin_amdgcn_perm(vr[1][c >> 2], vr[0][c >> 2], (c & 2) ? 0x07030602u : 0x05010400u);
-          const uint32_t hi = __builtin_amdgcn_perm(vr[3][c >> 2], vr[2][c >> 2], (c & 2) ? 0x07030602u : 0x05010400u);
+          const uint32_t lo = __builtin_amdgcn_perm(vr[S][1][c >> 2], vr[S][0][c >> 2], (c & 2) ? 0x07030602u : 0x05010400u);
+          const uint32_t hi = __builtin_amdgcn_perm(vr[S][3][c >> 2], vr[S][2][c >> 2], (c & 2) ? 0x07030602u : 0x05010400u);
           y = (c & 1) ? make_uint2(e4m3_bf16<true>(lo), e4m3_bf16<true>(hi)) : make_uint2(e4m3_bf16<false>(lo), e4m3_bf16<false>(hi));
         } else {
           const uint32_t sel = (c & 1) ? 0x07060302u : 0x05040100u;
-          y = make_uint2(__builtin_amdgcn_perm(vr[1][c >> 1], vr[0][c >> 1], sel), __builtin_amdgcn_perm(vr[3][c >> 1], vr[2][c >> 1], sel));
+          y = make_uint2(__builtin_amdgcn_perm(vr[S][1][c >> 1], vr[S][0][c >> 1], sel), __builtin_amdgcn_perm(vr[S][3][c >> 1], vr[S][2][c >> 1], sel));
         }
         const int d = VD * dg + c;
         vl[d * 16 + (((unit >> 1) ^ ((d ^ (d >> 3)) & 7)) << 1 | (unit & 1))] = y;
@@ -1050,30 +1053,36 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
 #pragma unroll
   for (int h = 0; h < NP; ++h) ok_cur[h] = false;
   const auto tile_base = [&](int i) { return T * sp.tile(t0 + gr + G * i); };
-  const auto took = [&](int base) {
-    full_cur = is_full(base);
+  const auto took = [&](int base, int s) {
+    full_cur = is_full(base, s);
 #pragma unroll
     for (int h = 0; h < NP; ++h) {
-      ok_cur[h] = pg[h] >= 0;
-      if constexpr (BITS == 8) { ks[h] = ks_n[h]; vs[h] = vs_n[h]; }
+      ok_cur[h] = pg[s][h] >= 0;
+      if constexpr (BITS == 8) { ks[h] = ks_n[s][h]; vs[h] = vs_n[s][h]; }
     }
   };
+  constexpr std::integral_constant<int, 0> S0;
+  constexpr std::integral_constant<int, SETS - 1> S1;
   __syncthreads();                                     // poison is clear
   if (mine > 0) {
     look_up(tile_base(0));
-    load(tile_base(0));
-    store(tile_base(0), 0);
-    took(tile_base(0));
+    load(tile_base(0), S0);
+    store(tile_base(0), 0, S0);
+    took(tile_base(0), 0);
     if (mine > 1) look_up(tile_base(1));
+    if (SETS == 2 && mine > 1) {
+      load(tile_base(1), S1);
+      if (mine > 2) look_up(tile_base(2));
+    }
   }
   // the queries have arrived: or the loop's first product waits, in every step, for whatever was loaded last
 #pragma unroll
   for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[s]));
   __syncthreads();
-  for (int it = 0; it < most; ++it) {
-    const bool more = it + 1 < mine;
-    if (more) load(tile_base(it + 1));
-    if (it + 2 < mine) look_up(tile_base(it + 2));
+  // One step: tile `it` lies in LDS, the next one in set `next` (SETS = 2: set `free` takes the one after) or on its way
+  const auto step = [&](int it, auto free, auto next) {
+    if (it + SETS < mine) load(tile_base(it + SETS), free);
+    if (it + SETS + 1 < mine) look_up(tile_base(it + SETS + 1));
     if (it < mine) {
       const int base = tile_base(it), buf = it & 1;
       const uint4* kl = kt[gr][buf] + c32 * KROW + g;
@@ -1125,7 +1134,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
       }
       if (__any(top > m + 8.f)) {
         top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float mn = fmaxf(m, top), k = mn == m ? 1.f : exp2_fast(m - mn);
+        const float mn = top > m + 8.f ? top : m, k = mn == m ? 1.f : exp2_fast(m - mn);
         m = mn;
         l *= k;
 #pragma unroll
@@ -1160,11 +1169,19 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    if (more) {
-      store(tile_base(it + 1), (it + 1) & 1);
-      took(tile_base(it + 1));
+    if (it + 1 < mine) {
+      store(tile_base(it + 1), (it + 1) & 1, next);
+      took(tile_base(it + 1), decltype(next)::value);
     }
     __syncthreads();
+  };
+  if constexpr (SETS == 1) {
+    for (int it = 0; it < most; ++it) step(it, S0, S0);
+  } else {
+    for (int it = 0; it < most; it += 2) {
+      step(it, S0, S1);
+      if (it + 1 < most) step(it + 1, S1, S0);
+    }
   }
 
   if constexpr (G == 2) {
@@ -1322,17 +1339,19 @@ struct AttendPlan {
   int rows, row_blocks, splits, chunk;
   long long blocks;
 };
-#ifndef VMANY2
-#define VMANY2 128
-#endif
-#ifndef VMANY
-#define VMANY 32
-#endif
 constexpr int kWaves = 4;
+// Up to 32 rows go to attend_few: 8 sequences of 5 rows x 4 heads take 46 us there and 80 in attend_many, which keeps a
+// tile for rows that are not there.  Beyond 128 rows attend_many takes 256 per workgroup (G = 1) where that leaves 32
+// workgroups before any split: 1,024 tokens x 7 heads over 10,677 take 200 us against 211 with 128 rows, 4,096 tokens
+// over 8,000 474 against 556, 40 tokens x 4 heads of 8 sequences 113 against 128.  Fewer blocks of 256 rows would need
+// twice the parts of 128-row ones, and joining them costs more than reading the keys once less: 48 tokens (8 blocks)
+// take 38 us with 256 rows and 32 with 128, 200 tokens (24 blocks) 74 and 62.
+constexpr int kManyBlocks = 32;
 AttendPlan plan_attention(int Hq, int heads, int bits, int B, int max_q, int max_len, int window, int sinks) {
   AttendPlan a;
   const long long rows = static_cast<long long>(max_q) * (Hq / heads);
-  a.rows = rows > VMANY2 ? many_rows(1) : rows > VMANY ? many_rows(2) : rows > 16 ? 32 : 16;
+  const long long wide = (rows + many_rows(1) - 1) / many_rows(1) * heads * B;
+  a.rows = rows > many_rows(2) && wide >= kManyBlocks ? many_rows(1) : rows > 32 ? many_rows(2) : rows > 16 ? 32 : 16;
   a.row_blocks = static_cast<int>((rows + a.rows - 1) / a.rows);
   const long long base = static_cast<long long>(B) * heads * a.row_blocks;
   if (window >= max_len) window = 0;                  // such a window hides nothing

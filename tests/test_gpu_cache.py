@@ -257,6 +257,15 @@ ATTEND = [
     (8, 16, (4, 2), 80, [1, 2], [3000, 1500], 0, 0),
     (16, 32, (2, 2), 128, [1], [4097], 3000, 100),
     (8, 64, (4, 1), 128, [1] * 70, list(range(70)), 0, 0),                 # many sequences, lengths from 0
+    # more than 128 rows of 32 KV heads in all: 256 rows per workgroup
+    (16, 64, (64, 32), 128, [70, 3], [300, 200], 0, 0),
+    (8, 64, (64, 32), 128, [129], [1500], 0, 0),                           # split keys, joined
+    (16, 16, (32, 32), 80, [140], [150], 0, 0),
+    (8, 32, (16, 8), 80, [150, 0, 1, 70], [700, 9, 300, 70], 0, 0),
+    (16, 128, (16, 8), 128, [0, 133, 200, 66], [0, 133, 100, 260], 0, 0),  # one with queries before the first token
+    (8, 16, (28, 4), 128, [40] * 8, [50, 40, 64, 65, 300, 41, 129, 77], 33, 5),
+    (16, 64, (64, 32), 80, [100], [1400], 700, 70),
+    (8, 256, (64, 32), 128, [65], [65], 20, 0),
 ]
 
 
@@ -313,12 +322,12 @@ def test_attention(case):
 
 
 @pytest.mark.parametrize("bits", [16, 8])
-@pytest.mark.parametrize("nq", [1, 3, 40, 200])
-def test_attention_bad_pages_count_as_unseen(bits, nq):
+@pytest.mark.parametrize("nq,heads", [(1, (4, 2)), (3, (4, 2)), (40, (4, 2)), (200, (4, 2)), (130, (32, 16))])
+def test_attention_bad_pages_count_as_unseen(bits, nq, heads):
     import torch
     from paper_2608_27206_amd import pace
     rs = np.random.default_rng(11 * nq + bits)
-    case = (bits, 16, (4, 2), 128, [nq, 1], [210, 40], 0, 0)
+    case = (bits, 16, heads, 128, [nq, 1], [210, 40], 0, 0)
     pages, table, kc, vc, ks, vs, q, cu = _attend_inputs(case, rs)
     table[0, [1, 5, 6]], table[1] = [-1, pages, 2 ** 31 - 1], -1          # the second sequence sees nothing
     ref = oc.attention(wl.bf16_bits_to_f64(q), f64(kc), f64(vc), None if ks is None else f64(ks),
@@ -330,15 +339,15 @@ def test_attention_bad_pages_count_as_unseen(bits, nq):
     assert np.all(f64(o)[nq] == 0) and np.all(f64(lse)[:, nq] == -np.inf)
 
 
-@pytest.mark.parametrize("nq", [1, 4, 20, 60])
+@pytest.mark.parametrize("nq,heads", [(1, (4, 2)), (4, (4, 2)), (20, (4, 2)), (60, (4, 2)), (70, (22, 11))])
 @pytest.mark.parametrize("scale", [float("nan"), float("inf"), -1.0, 0.0])
-def test_attention_does_not_use_scales_past_the_end(nq, scale):
+def test_attention_does_not_use_scales_past_the_end(nq, heads, scale):
     """Table entries behind a sequence's last page that name a page of NaN with a scale of anything."""
     import torch
     from paper_2608_27206_amd import pace
     rs = np.random.default_rng(nq)
     lens = [nq + 49, 17 + nq, nq]
-    pages, table, kc, vc, ks, vs, q, cu = _attend_inputs((8, 16, (4, 2), 128, [nq] * 3, lens, 0, 0), rs)
+    pages, table, kc, vc, ks, vs, q, cu = _attend_inputs((8, 16, heads, 128, [nq] * 3, lens, 0, 0), rs)
     ref = oc.attention(wl.bf16_bits_to_f64(q), f64(kc), f64(vc), f64(ks), f64(vs), cu, lens, np.where(table < 0, 0, table), 16, 128 ** -0.5)
     used = set(table[table >= 0])
     dead = next(p for p in range(pages) if p not in used)
@@ -368,15 +377,16 @@ def test_nothing_to_do():
 
 
 @pytest.mark.parametrize("window,sinks", [(0, 0), (20, 3)])
-@pytest.mark.parametrize("bits,nq", [(16, 6), (8, 6), (16, 90), (8, 200)])
-def test_hidden_keys_do_not_matter(bits, nq, window, sinks):
+@pytest.mark.parametrize("bits,nq,heads", [(16, 6, (4, 2)), (8, 6, (4, 2)), (16, 90, (4, 2)), (8, 200, (4, 2)),
+                                           (16, 200, (64, 32)), (8, 150, (32, 32))])
+def test_hidden_keys_do_not_matter(bits, nq, heads, window, sinks):
     """NaN and infinities in the K and V of a token reach exactly the queries that see it: all others keep
     their bits."""
     import torch
     from paper_2608_27206_amd import pace
     rs = np.random.default_rng(nq + window)
     L = nq + 130
-    case = (bits, 32, (4, 2), 128, [nq], [L], window, sinks)
+    case = (bits, 32, heads, 128, [nq], [L], window, sinks)
     pages, table, kc, vc, ks, vs, q, cu = _attend_inputs(case, rs)
     args = (dev_i32(cu), dev_i32([L]), dev_i32(table), nq, L)
     dq = dev_bf16(q[:nq])
