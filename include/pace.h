@@ -499,7 +499,7 @@ pace_status_t pace_cache_attention(const uint16_t* q, int n_q, int Hq, const pac
                                    uint16_t* o, float* lse, void* workspace, size_t workspace_bytes,
                                    hipStream_t stream);
 
-/* Workspace bytes for pace_gemm_w4 (partial sums where K is split over workgroups; 0 for M <= 16). */
+/* Workspace bytes for pace_gemm_w4 (partial sums where K is split over workgroups; 0 where it is not). */
 size_t pace_gemm_w4_workspace_size(int M, int N, int K);
 
 /*
@@ -511,8 +511,8 @@ size_t pace_gemm_w4_workspace_size(int M, int N, int K);
  *   x         bf16 [M, K] row-major; x and w 16-byte aligned.  1 <= M <= 65,535; the weights are read once for
  *             every 64 rows.
  *   bias, residual, epilogue, C  as in pace_gemm_bf16.
- * Products accumulate in fp32, in an order fixed by the shape.  x must be finite (a row with an infinity comes out as
- * NaN).  Each operand under 2 GiB.  The workspace must be 16-byte aligned; calls that may run at the same time need
+ * Products accumulate in fp32, in an order fixed by the shape.  x must be finite and should stay under 2^100 (a row with
+ * an infinity comes out as NaN).  Each operand under 2 GiB.  The workspace must be 16-byte aligned; calls that may run at the same time need
  * one each.
  */
 pace_status_t pace_gemm_w4(const uint16_t* x, const uint8_t* w, const uint16_t* scale, const uint8_t* zero,

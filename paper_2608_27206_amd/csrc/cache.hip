@@ -91,7 +91,7 @@ __device__ __forceinline__ int new_tokens(const AppendParams& p, int b, int* fir
   n = n > p.max_new ? p.max_new : n;
   *first = r0;
   if (r0 < 0) return 0;
-  return r0 + n > p.n_new ? p.n_new - r0 : n;
+  return n > p.n_new - r0 ? p.n_new - r0 : n;
 }
 
 constexpr int kAppendThreads = 256;
@@ -382,7 +382,7 @@ __device__ __forceinline__ Span queries_of(const AttendParams& p, int b) {
   if (s.row0 < 0 || s.nq < 0) s.nq = 0;
   if (s.nq > p.n_q - s.row0) s.nq = p.n_q - s.row0;
   s.len = p.len[b];
-  s.len = s.len > p.max_len ? p.max_len : s.len;
+  s.len = s.len > p.max_len ? p.max_len : s.len < 0 ? 0 : s.len;
   return s;
 }
 template <int T>
@@ -1364,7 +1364,7 @@ AttendPlan plan_attention(int Hq, int heads, int bits, int B, int max_q, int max
   // alike, and more of them cost more to join), or four where lengths differ.
   const long long aim = a.rows > 32 ? 256 : a.rows == 32 || B == 1 ? 512 : 1024;
   const long long want = aim / base < 1 ? 1 : aim / base, chunk = (tiles + want - 1) / want;
-  const int least = a.rows > 32 ? 8 : kWaves;
+  const int least = 4;
   a.chunk = static_cast<int>(chunk < least ? least : chunk);
   a.splits = static_cast<int>((tiles + a.chunk - 1) / a.chunk);
   if (a.splits < 1) a.splits = 1;

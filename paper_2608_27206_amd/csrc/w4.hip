@@ -115,7 +115,7 @@ __device__ __forceinline__ void stage_x(uint4 u, int piece, uint4* to, float* su
 // the steps of 256 k's (whole 128-byte lines of each row) of every chunk of K in turn; they join through LDS.  A wave keeps
 // the next chunk's weights in flight while it works on one.  x passes through LDS, two chunks of it: straight from the
 // caches, a lane's 16 bytes lie a row away from its neighbour's, 64 accesses a load, and these bound the kernel (eight
-// rows through 28,672 columns of 3,584: 30 us against 13).
+// rows through 28,672 columns of 3,584: 30 us against 24).
 constexpr int kW4Waves = 8;
 template <int NT, int W, int GROUP, int MR>
 __global__ __launch_bounds__(64 * kW4Waves, 2) void gemm_w4_few(const W4Params p) {
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(64 * kW4Waves, 2) void gemm_w4_few(const W4Params p
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const unsigned n = n0 + 16 * t + r < p.N ? n0 + 16 * t + r : p.N - 1;
-    woff[t] = n * (p.K / 2) + 16 * g;
+    woff[t] = n * (p.K / 2) + (32 * g < p.K ? 16 * g : 0);     // K under 128: a lane past the row's end stays inside it
     row[t] = n * groups;
   }
   const int xr = r < MR ? r : MR - 1;                  // rows past p.M hold anything: they are not stored
@@ -263,7 +263,7 @@ __global__ __launch_bounds__(64 * kW4Waves, 2) void gemm_w4_few(const W4Params p
   }
 }
 
-// More rows (16 MT at a time): here x would be read far more often than the weights, so the 4 waves of a workgroup take 32
+// More rows (16 MT at a time), or long rows of few columns: here x would be read far more often than the weights, so the 4 waves of a workgroup take 32
 // columns each and share x through LDS, 256 k's at a time; workgroups split K where the columns give too few, and w4_join
 // adds their sums.
 template <int MT, int GROUP>
@@ -283,7 +283,7 @@ __global__ __launch_bounds__(256, 2) void gemm_w4_rows(const W4Params p) {
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const unsigned n = n0 + 16 * t + r < p.N ? n0 + 16 * t + r : p.N - 1;
-    woff[t] = n * (p.K / 2) + 16 * g;
+    woff[t] = n * (p.K / 2) + (32 * g < p.K ? 16 * g : 0);     // K under 128: a lane past the row's end stays inside it
     row[t] = n * groups;
   }
   // x: thread t stages piece t % 32 of rows t / 32 + 8 i
@@ -421,27 +421,34 @@ __global__ __launch_bounds__(256) void w4_join(const W4Params p) {
 }
 
 struct W4Plan {
-  int mt, nt, waves, ntiles, splits;   // ntiles: workgroups along the columns
+  int mt, nt, waves, ntiles, splits;   // mt = 0: gemm_w4_few; ntiles: workgroups along the columns
 };
 W4Plan plan_w4(int M, int N, int K, int group) {
   W4Plan a;
   a.splits = 1;
+  const int tiles = (N + 15) / 16, steps = (K + 255) / 256;
   if (M <= 16) {
-    a.mt = 1;
-    const int tiles = (N + 15) / 16;
+    a.mt = 0;
     // From 16,384 columns on two tiles a wave (eight rows, 28,672 x 3584: 23.8 us against 25.4), and about 2,000 waves in
-    // all: fewer leave CUs idle (one row, 4608 x 3584: 1,152 waves 11.0 us, 2,304 7.9), more only join more (the wide one:
+    // all: fewer leave CUs idle (one row, 4608 x 3584: 1,152 waves 11.0 us, 2,304 7.8), more only join more (the wide one:
     // 23.7 us with 2,048 waves, 30.2 with 7,168).
     a.nt = tiles >= 1024 && group > 32 ? 2 : 1;
-    a.waves = M <= 8 ? 8 : 4;
+    const int most = M <= 8 ? 8 : 4;
+    a.waves = most;
     while (a.waves > 2 && tiles / a.nt * a.waves > 2560) a.waves /= 2;
     a.ntiles = ((tiles + a.nt - 1) / a.nt * a.waves + kW4Waves - 1) / kW4Waves;
-    return a;
+    // Where all the waves that a column can have take four steps or more one after the other, gemm_w4_rows splits K over
+    // workgroups instead (8 rows: 3584 x 14336 16.4 us against 20.4, 4096 x 8192 12.4 and 12.7; 16 rows: 18.0 against
+    // 35.3, 4608 x 3584 9.8 and 11.1).  With fewer steps its join costs more than it saves (8 rows: 4608 x 3584 9.2 us
+    // there and 8.8 here, 4096 x 4096 9.3 and 7.6), and where there are columns enough nothing needs a split (16 rows,
+    // 16,000 x 8192: 30.0 and 27.9).
+    if (a.waves < most || (steps + most - 1) / most < 4) return a;
   }
-  a.mt = M <= 32 ? 2 : M <= 48 ? 3 : 4;
+  // rows at a time: no more than there are (17 rows, 3584 x 14336: 20.5 us with 32, 25.2 with 64)
+  a.mt = M <= 16 ? 1 : M <= 32 ? 2 : M <= 48 ? 3 : 4;
   a.nt = 2;
   a.ntiles = (N + 127) / 128;
-  const int steps = (K + 255) / 256, rows = (M + 63) / 64;
+  const int rows = (M + 63) / 64;
   // two workgroups on every CU (48 rows, 3584 x 14336: 27.6 us; 256 workgroups 29.0, 768 31.8)
   const int s = 512 / (a.ntiles * rows), most = (steps + 1) / 2;       // at least two steps each
   a.splits = s < 1 ? 1 : s < most ? s : most;
@@ -517,8 +524,9 @@ pace_status_t pace_gemm_w4(const uint16_t* x, const uint8_t* w, const uint16_t* 
     PACE_REQUIRE(aligned16(workspace), "pace_gemm_w4: workspace must be 16-byte aligned");
   }
   const W4Params p{x, w, scale, zero, bias, residual, C, static_cast<float*>(workspace), M, N, K, epilogue, a.splits, a.ntiles};
-  if (a.mt == 1 && a.nt == 1) launch_few<1>(p, a.waves, group, stream);
-  else if (a.mt == 1) launch_few<2>(p, a.waves, group, stream);
+  if (a.mt == 0 && a.nt == 1) launch_few<1>(p, a.waves, group, stream);
+  else if (a.mt == 0) launch_few<2>(p, a.waves, group, stream);
+  else if (a.mt == 1) launch_rows<1>(p, group, stream);
   else if (a.mt == 2) launch_rows<2>(p, group, stream);
   else if (a.mt == 3) launch_rows<3>(p, group, stream);
   else launch_rows<4>(p, group, stream);

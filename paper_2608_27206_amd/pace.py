@@ -699,7 +699,7 @@ def gemm_w4(x: torch.Tensor, w: torch.Tensor, scale: torch.Tensor, zero: Optiona
     cols = N // 2 if epilogue == 2 else N
     if out is None:
         out = torch.empty((M, cols), dtype=_BF16, device=x.device)
-    if workspace is None and M > 16:
+    if workspace is None:
         need = (_lib or lib()).pace_gemm_w4_workspace_size(M, N, K)
         if need:
             workspace = torch.empty(need, dtype=_U8, device=x.device)

@@ -111,13 +111,14 @@ def test_w4(bad, word):
 
 def test_w4_workspace():
     size = pace.lib().pace_gemm_w4_workspace_size
-    assert size(16, 3584, 14336) == 0 and size(0, 8, 128) == 0 and size(1, -8, 128) == 0
-    need = size(48, 64, 14336)
-    if need:
+    assert size(1, 4608, 3584) == 0 and size(8, 28672, 3584) == 0 and size(0, 8, 128) == 0 and size(1, -8, 128) == 0
+    for M in (1, 48):                              # long rows of few columns: K is split
+        need = size(M, 64, 14336)
+        assert need > 0 and need % (M * 64 * 4) == 0
         for ws, wsb in ((None, 0), (P, need - 1)):
-            st, msg = w4(M=48, N=64, K=14336, ws=ws, wsb=wsb)
+            st, msg = w4(M=M, N=64, K=14336, ws=ws, wsb=wsb)
             assert st == 3 and "workspace" in msg
-        st, msg = w4(M=48, N=64, K=14336, ws=ODD, wsb=need)
+        st, msg = w4(M=M, N=64, K=14336, ws=ODD, wsb=need)
         assert st == 1 and "aligned" in msg
 
 

@@ -452,7 +452,11 @@ W4 = [(1, 1, 32, 32, 0, 0), (1, 64, 128, 128, 1, 0), (3, 17, 96, 32, 1, 1), (1, 
       # wider: two tiles a wave, fewer waves per column; odd widths; 9 to 16 rows; many splits
       (8, 8001, 512, 64, 1, 0), (12, 6000, 1056, 32, 0, 1), (16, 20002, 288, 32, 1, 2), (2, 28680, 384, 128, 0, 2),
       (11, 24593, 640, 64, 1, 0), (9, 16400, 128, 128, 0, 1), (5, 32784, 96, 32, 1, 0), (7, 200, 2080, 32, 1, 0),
-      (40, 64, 14336, 64, 0, 1), (17, 130, 2016, 32, 1, 2), (64, 3000, 1152, 128, 1, 0), (128, 130, 1024, 128, 0, 2)]
+      (40, 64, 14336, 64, 0, 1), (17, 130, 2016, 32, 1, 2), (64, 3000, 1152, 128, 1, 0), (128, 130, 1024, 128, 0, 2),
+      # K in several chunks of x, with few and many columns; split K with up to 16 rows; K under 128
+      (8, 5000, 4672, 64, 1, 1), (4, 300, 5152, 32, 0, 0), (13, 16400, 2304, 128, 1, 2), (16, 10000, 2080, 32, 0, 0),
+      (10, 130, 8224, 32, 1, 2), (16, 4000, 4096, 128, 0, 1), (1, 77, 14336, 64, 1, 0), (8, 258, 8192, 128, 0, 2),
+      (16, 31, 64, 64, 1, 0), (20, 31, 32, 32, 0, 0), (20, 30, 96, 32, 1, 2)]
 
 
 @pytest.mark.parametrize("M,N,K,group,zero,epilogue", W4)
