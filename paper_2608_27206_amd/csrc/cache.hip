@@ -99,7 +99,8 @@ constexpr int kAppendTokens = 8;   // most tokens per workgroup
 
 // Queries, and keys and values of bf16 pages.  A workgroup takes some tokens of one sequence: their
 // angles' cos and sin go to LDS once (all heads share them), then every thread moves 16 values of one
-// head (8 of each half, so that a pair meets in one thread) per step.
+// head (8 of each half, so that a pair meets in one thread) per step.  Short calls are one chain of loads (offsets,
+// source row, position, table entry, values) behind a launch: one token 3.3 us.
 template <int D, bool KV>
 __device__ __forceinline__ void append_rows(const AppendParams& p, int block) {
   constexpr int HALF = D / 2, CH = D / 16;
@@ -188,7 +189,8 @@ __device__ __forceinline__ float page_scale(float top) {
 
 // Keys or values of 8-bit pages: one workgroup owns one (sequence, page, head) of k or v, so the page's
 // scale needs no atomics and one launch is enough.  The new values stay in registers between the
-// maximum and the store.
+// maximum and the store.  With the queries' rows beside it bound by memory: 10,677 tokens, 28/4 heads of 128, move 186 MB
+// in 43.5 us (4.3 TB/s; a copy of them takes 33.8); one token of each of 64 sequences takes 5.4 us.
 template <int D, int ITEMS>
 __device__ __forceinline__ void append_pages(const AppendParams& p, int block) {
   constexpr int HALF = D / 2, CH = D / 16;
@@ -347,7 +349,8 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // Cached keys and values are read once: loads that do not ask the caches to keep them (attention over 131,071
-// tokens 56.6 us against 61.2, 48 sequences in 8 bits 106 against 112).
+// tokens 52 us against 58, 48 sequences in 8 bits 104 against 111; short ragged batches lose a little, 8 sequences of 20
+// rows take 47 us instead of 45).
 __device__ __forceinline__ u32x4 stream16(const void* p) { return __builtin_nontemporal_load(static_cast<const u32x4*>(p)); }
 __device__ __forceinline__ u32x2 stream8(const void* p) { return __builtin_nontemporal_load(static_cast<const u32x2*>(p)); }
 
@@ -424,6 +427,9 @@ __device__ __forceinline__ int page_of(const AttendParams& p, int entry, int key
 //    ends with 8 consecutive d of each of four blocks.
 // A row's maximum is only raised when a score passes it by 2^8 (the lanes exchange scores when any row's does), so most
 // tiles need no exchange; probabilities of up to 256 round like others.
+// 131,071 bf16 tokens of 4 KV heads (268 MB): 45 us, the rate at which memory is read; 48 sequences of up to 16,384 tokens
+// in 8 bits (484 MB) 96 us, 5.0 TB/s, the last parts of unequal lengths.  Short contexts wait for the chain of offsets,
+// table entry, page and first tile: 1,183 tokens 7 us.
 // Three waves per SIMD for 16 rows: 48 ragged sequences of up to 16,384 tokens in 8 bits take 104 us with three and
 // 117 with two (the registers that two would have are not needed); 32 rows do not fit in three's.
 template <int D, int BITS, int R, int W>
@@ -836,6 +842,11 @@ __global__ __launch_bounds__(64 * W, R == 1 ? 3 : 2) void attend_few(const Atten
 //    swizzled by d.
 // Operands are read from LDS four products ahead: one at a time, each product waited out its read (253 us against 211;
 // eight ahead do not fit the registers, 239).
+// With 256 rows the registers hold two tiles on their way, which hides most of their arrival (1,024 tokens x 7 heads
+// over 10,677: 203 us against 214 with one); with 128 rows a thread stages twice as much, and they hold one.
+// That case runs its 149 GFLOP at 750 TFLOP/s, its join included: the matrix units are busy for 30% of it; two waves
+// on a SIMD leave their waits (a third), the exponentials and the staging partly uncovered, and LDS and registers
+// have no room for a third.
 // NP: the pages of a tile, 1 (64 or more tokens a page) or 4 (one for each 16 keys).
 constexpr int kManyTile = 64, kManyThreads = 512;
 constexpr int many_rows(int groups) { return 256 / groups; }
@@ -1261,7 +1272,9 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
 }
 
 // Joins the parts of the rows whose keys were split.  W = 8: a workgroup per row, its waves take the parts in turn;
-// W = 1: a wave per row, for up to 8 parts.
+// W = 1: a wave per row, for up to 8 parts (two parts of 28,672 rows: 83 us with their attention, 152 with a workgroup a
+// row; 128 parts of 28 rows: 52 us with a workgroup, 70 with a wave).  Bound by its chain of launch, lengths and parts (3
+// to 5 us); 28,672 rows by their 37 MB (17 us).
 constexpr int kJoinWaves = 8;
 template <int D, int T, int W>
 __global__ __launch_bounds__(64 * kJoinWaves) void attend_join(const AttendParams p, int block_rows) {
@@ -1360,10 +1373,17 @@ AttendPlan plan_attention(int Hq, int heads, int bits, int B, int max_q, int max
   // tiles that a row block may see at most: sinks and window each begin inside one
   const int tile = a.rows > 32 ? kManyTile : tile_keys(bits);
   const long long tiles = (keys + tile - 1) / tile + (window > 0 ? 2 : 0);
-  // Workgroups to aim at.  Many rows: one on every CU.  Few: two (32 rows: all that fit; one sequence: its parts are
-  // alike, and more of them cost more to join), or four where lengths differ.
-  const long long aim = a.rows > 32 ? 256 : a.rows == 32 || B == 1 ? 512 : 1024;
+  // Workgroups to aim at.  Many rows: one on every CU, all that its registers hold (40 tokens x 4 heads of 8 sequences
+  // 119 us; 512 in all 124, 1,024 155).  Few: two a CU where that is all that fits (32 rows: 8 sequences of 20 rows 47 us,
+  // with four 54) or the sequences' parts are alike, whose number only costs in the join (one sequence of 131,071: 52 us,
+  // with four 56; 24 that a window of 4,096 bounds: 30.7 and 33.2), else four: 48 sequences of up to 16,384 take 104 us,
+  // with two 140.
+  const bool alike = B == 1 || 2 * keys <= max_len;
+  const long long aim = a.rows > 32 ? 256 : a.rows == 32 || alike ? 512 : 1024;
   const long long want = aim / base < 1 ? 1 : aim / base, chunk = (tiles + want - 1) / want;
+  // A part of fewer than four tiles costs more to join than it saves (64 tokens x 7 heads over 1,183: 18.5 us, parts of
+  // two tiles 23.9; one token over 5,000: 11.2 us, parts of one 12.1); more leave CUs idle (32 tokens over 1,183: 17.5 us,
+  // parts of eight 20.4).
   const int least = 4;
   a.chunk = static_cast<int>(chunk < least ? least : chunk);
   a.splits = static_cast<int>((tiles + a.chunk - 1) / a.chunk);

@@ -115,7 +115,10 @@ __device__ __forceinline__ void stage_x(uint4 u, int piece, uint4* to, float* su
 // the steps of 256 k's (whole 128-byte lines of each row) of every chunk of K in turn; they join through LDS.  A wave keeps
 // the next chunk's weights in flight while it works on one.  x passes through LDS, two chunks of it: straight from the
 // caches, a lane's 16 bytes lie a row away from its neighbour's, 64 accesses a load, and these bound the kernel (eight
-// rows through 28,672 columns of 3,584: 30 us against 24).
+// rows through 28,672 columns of 3,584: 30 us against 23).
+// What is left there, with a floor of 10 us for 55 MB of weights, scales and zeros: the first loads arrive after about 10
+// us, and from then on instructions bound it (a wave issues VALU work for a quarter of its time, two of them on a SIMD);
+// one row of 4608 x 3584 takes 7.8 us, launch, chain and the join of 8 waves, against 1.6 for its bytes.
 constexpr int kW4Waves = 8;
 template <int NT, int W, int GROUP, int MR>
 __global__ __launch_bounds__(64 * kW4Waves, 2) void gemm_w4_few(const W4Params p) {
@@ -263,9 +266,11 @@ __global__ __launch_bounds__(64 * kW4Waves, 2) void gemm_w4_few(const W4Params p
   }
 }
 
-// More rows (16 MT at a time), or long rows of few columns: here x would be read far more often than the weights, so the 4 waves of a workgroup take 32
-// columns each and share x through LDS, 256 k's at a time; workgroups split K where the columns give too few, and w4_join
-// adds their sums.
+// More rows (16 MT at a time), or long rows of few columns: here x would be read far more often than the weights, so the 4
+// waves of a workgroup take 32 columns each and share x through LDS, 256 k's at a time; workgroups split K where the
+// columns give too few, and w4_join adds their sums.  48 rows of 3584 x 14336 take 27 us, 4 to 5 of them the join, against
+// 5.3 for 29 MB: a part is three or four steps of load, stage, barrier and products, one after the other, and two
+// workgroups on a CU cover a third of that.  Two steps in flight gave nothing (29.4 us).
 template <int MT, int GROUP>
 __global__ __launch_bounds__(256, 2) void gemm_w4_rows(const W4Params p) {
   constexpr int NT = 2, STEP = 256, GB = 128 / GROUP, SPG = 4 / GB, GS = 2 * GB, ROWS = 16 * MT;
