@@ -843,7 +843,7 @@ __global__ __launch_bounds__(64 * W, R == 1 ? 3 : 2) void attend_few(const Atten
 // Operands are read from LDS four products ahead: one at a time, each product waited out its read (253 us against 211;
 // eight ahead do not fit the registers, 239).
 // With 256 rows the registers hold two tiles on their way, which hides most of their arrival (1,024 tokens x 7 heads
-// over 10,677: 203 us against 214 with one); with 128 rows a thread stages twice as much, and they hold one.
+// over 10,677: 200 us against 212 with one); with 128 rows a thread stages twice as much, and they hold one.
 // That case runs its 149 GFLOP at 750 TFLOP/s, its join included: the matrix units are busy for 30% of it; two waves
 // on a SIMD leave their waits (a third), the exponentials and the staging partly uncovered, and LDS and registers
 // have no room for a third.
@@ -1272,15 +1272,16 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
 }
 
 // Joins the parts of the rows whose keys were split.  W = 8: a workgroup per row, its waves take the parts in turn;
-// W = 1: a wave per row, for up to 8 parts (two parts of 28,672 rows: 83 us with their attention, 152 with a workgroup a
-// row; 128 parts of 28 rows: 52 us with a workgroup, 70 with a wave).  Bound by its chain of launch, lengths and parts (3
-// to 5 us); 28,672 rows by their 37 MB (17 us).
-constexpr int kJoinWaves = 8;
+// W = 1: half a wave per row, for up to 8 parts (two parts of 28,672 rows: 75 us with their attention, 80 with a wave a
+// row, 152 with a workgroup; 128 parts of 28 rows: 52 us with a workgroup, 70 with a wave).  Bound by its chain of launch,
+// lengths and parts (3 to 5 us), which the waves of 28,672 rows go through four times over: 10.5 us for 37 MB.
+constexpr int kJoinWaves = 8, kJoinLanes = 32;
 template <int D, int T, int W>
 __global__ __launch_bounds__(64 * kJoinWaves) void attend_join(const AttendParams p, int block_rows) {
-  __shared__ float part[W][3][64];
-  const int lane = threadIdx.x & 63, w = W == 1 ? 0 : threadIdx.x >> 6;
-  int id = W == 1 ? blockIdx.x * kJoinWaves + (threadIdx.x >> 6) : blockIdx.x;
+  constexpr int L = W == 1 ? kJoinLanes : 64, V = 128 / L;     // lanes of a row, and values of each
+  __shared__ float part[W][V + 1][64];
+  const int lane = threadIdx.x & (L - 1), w = W == 1 ? 0 : threadIdx.x >> 6;
+  int id = W == 1 ? blockIdx.x * (64 * kJoinWaves / L) + threadIdx.x / L : blockIdx.x;
   const int h = id % p.Hq;
   id /= p.Hq;
   const int i = id % p.max_q, b = id / p.max_q;
@@ -1295,10 +1296,12 @@ __global__ __launch_bounds__(64 * kJoinWaves) void attend_join(const AttendParam
   if (splits == 1) return;
   const int n = sp.row0 + i;
   const long long row = static_cast<long long>(n) * p.Hq + h, all = static_cast<long long>(p.n_q) * p.Hq;
-  float m = -INFINITY, sum = 0.f, y0 = 0.f, y1 = 0.f;
+  float m = -INFINITY, sum = 0.f, y[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) y[e] = 0.f;
   for (int s0 = w; s0 < splits; s0 += 4 * W) {
     float ms[4], ls[4];
-    float2 v[4];
+    float v[4][V];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int s = s0 + u * W;
@@ -1306,44 +1309,55 @@ __global__ __launch_bounds__(64 * kJoinWaves) void attend_join(const AttendParam
       const float2 ml = *reinterpret_cast<const float2*>(from + D);
       ms[u] = s < splits ? ml.x : -INFINITY;
       ls[u] = s < splits ? ml.y : 0.f;
-      v[u] = make_float2(0.f, 0.f);
-      if (s < splits && 2 * lane < D) v[u] = *reinterpret_cast<const float2*>(from + 2 * lane);
+#pragma unroll
+      for (int e = 0; e < V; e += 2) {
+        float2 z = make_float2(0.f, 0.f);
+        if (s < splits && V * lane < D) z = *reinterpret_cast<const float2*>(from + V * lane + e);
+        v[u][e] = z.x;
+        v[u][e + 1] = z.y;
+      }
     }
     const float mn = fmaxf(m, fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3])));
     const float k = m == mn ? 1.f : exp2_fast(m - mn);
     m = mn;
     sum *= k;
-    y0 *= k;
-    y1 *= k;
+#pragma unroll
+    for (int e = 0; e < V; ++e) y[e] *= k;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const float f = ms[u] == mn ? 1.f : exp2_fast(ms[u] - mn);
       sum += ls[u] * f;
-      y0 += v[u].x * f;
-      y1 += v[u].y * f;
+#pragma unroll
+      for (int e = 0; e < V; ++e) y[e] += v[u][e] * f;
     }
   }
   float top = m;
   if constexpr (W > 1) {
-    part[w][0][lane] = y0;
-    part[w][1][lane] = y1;
-    part[w][2][lane] = lane == 0 ? m : sum;
+#pragma unroll
+    for (int e = 0; e < V; ++e) part[w][e][lane] = y[e];
+    part[w][V][lane] = lane == 0 ? m : sum;
     __syncthreads();
     if (w != 0) return;
-    top = part[0][2][0];
+    top = part[0][V][0];
 #pragma unroll
-    for (int u = 1; u < W; ++u) top = fmaxf(top, part[u][2][0]);
-    sum = y0 = y1 = 0.f;
+    for (int u = 1; u < W; ++u) top = fmaxf(top, part[u][V][0]);
+    sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < V; ++e) y[e] = 0.f;
 #pragma unroll
     for (int u = 0; u < W; ++u) {
-      const float f = part[u][2][0] == top ? 1.f : exp2_fast(part[u][2][0] - top);
-      sum += part[u][2][1] * f;
-      y0 += part[u][0][lane] * f;
-      y1 += part[u][1][lane] * f;
+      const float f = part[u][V][0] == top ? 1.f : exp2_fast(part[u][V][0] - top);
+      sum += part[u][V][1] * f;
+#pragma unroll
+      for (int e = 0; e < V; ++e) y[e] += part[u][e][lane] * f;
     }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  if (2 * lane < D) *reinterpret_cast<uint32_t*>(p.o + row * D + 2 * lane) = pack_bf16x2(y0 * inv, y1 * inv);
+  if (V * lane < D) {
+#pragma unroll
+    for (int e = 0; e < V; e += 2)
+      *reinterpret_cast<uint32_t*>(p.o + row * D + V * lane + e) = pack_bf16x2(y[e] * inv, y[e + 1] * inv);
+  }
   if (lane == 0 && p.lse) p.lse[static_cast<long long>(h) * p.n_q + n] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
@@ -1404,9 +1418,10 @@ void launch_many(const AttendParams& p, dim3 grid, hipStream_t stream) {
 template <int D, int T>
 void launch_join(const AttendParams& p, const AttendPlan& a, hipStream_t stream) {
   const long long rows = static_cast<long long>(p.B) * p.max_q * p.Hq;
+  constexpr int per = 64 * kJoinWaves / kJoinLanes;    // rows of a workgroup, for few parts
   const dim3 th(64 * kJoinWaves);
   if (a.splits <= 8)
-    hipLaunchKernelGGL((attend_join<D, T, 1>), dim3(static_cast<unsigned>((rows + kJoinWaves - 1) / kJoinWaves)), th, 0, stream, p, a.rows);
+    hipLaunchKernelGGL((attend_join<D, T, 1>), dim3(static_cast<unsigned>((rows + per - 1) / per)), th, 0, stream, p, a.rows);
   else
     hipLaunchKernelGGL((attend_join<D, T, kJoinWaves>), dim3(static_cast<unsigned>(rows)), th, 0, stream, p, a.rows);
 }
