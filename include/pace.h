@@ -459,7 +459,7 @@ typedef struct pace_kv_cache {
  * between powers of two, except where a code becomes subnormal).  Values that are not finite are
  * stored as NaN.
  * A source row outside [0, n_src), a place past the table and a page outside [0, num_pages) are not
- * written.  Asynchronous on `stream`; no workspace.
+ * written.  q_out and the cache must not overlap q, k and v.  Asynchronous on `stream`; no workspace.
  */
 pace_status_t pace_cache_append(const uint16_t* q, long long q_stride, const uint16_t* k, long long k_stride,
                                 const uint16_t* v, long long v_stride, int n_src, int Hq, const int32_t* rows,
@@ -489,8 +489,9 @@ size_t pace_cache_attention_workspace_size(int n_q, int Hq, int heads, int dim, 
  *   o         bf16 [n_q, Hq, dim]; lse fp32 [Hq, n_q], natural log, or NULL.  A query that sees no key (or
  *             whose scores are all -inf) gets o = 0 and lse = -inf.  Rows at or past cu_q[B] are left as they were.
  * Keys that a query does not see have no effect on it, whatever their K, V and scales hold.  A page outside
- * [0, num_pages) counts as unseen.  Results do not depend on the order in which workgroups run.  Scores and sums are
- * fp32, probabilities are rounded to bf16; sums are divided at the end, so values of V should stay under 2^100.
+ * [0, num_pages) counts as unseen; entries of pages that no query sees may be anything.  Results do not
+ * depend on the order in which workgroups run.  Scores and sums are fp32, probabilities are rounded to bf16;
+ * sums are divided at the end, so values of V should stay under 2^100.
  * The workspace must be 16-byte aligned; calls that may run at the same time need one each.
  */
 pace_status_t pace_cache_attention(const uint16_t* q, int n_q, int Hq, const pace_kv_cache* cache,

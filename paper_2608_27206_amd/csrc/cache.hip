@@ -1509,10 +1509,20 @@ pace_status_t debug_attention(const AttendParams& p, hipStream_t stream) {
   pace_status_t st = check_offsets(p.cu, p.B, p.n_q, p.max_q, "pace_cache_attention: cu_q", stream);
   if (st != PACE_OK) return st;
   if ((st = check_values(p.len, p.B, nullptr, 0, p.max_len, "pace_cache_attention: seq_len", stream)) != PACE_OK) return st;
-  std::vector<int32_t> len(p.B);
-  if ((st = copy_to_host(len.data(), p.len, p.B, stream)) != PACE_OK) return st;
-  std::vector<int> first(p.B, 0), last(p.B);
-  for (int b = 0; b < p.B; ++b) last[b] = (len[b] + p.pool.page - 1) >> p.pool.shift;
+  std::vector<int32_t> len(p.B), cu(p.B + 1);
+  if ((st = copy_to_host(len.data(), p.len, p.B, stream)) != PACE_OK ||
+      (st = copy_to_host(cu.data(), p.cu, p.B + 1, stream)) != PACE_OK)
+    return st;
+  // the pages that some query sees: those of the sinks, and from the first query's window on
+  std::vector<int> zero(p.B, 0), sinks(p.B), first(p.B), last(p.B);
+  for (int b = 0; b < p.B; ++b) {
+    const bool none = cu[b + 1] == cu[b];
+    const int from = p.window == 0 ? 0 : len[b] - (cu[b + 1] - cu[b]) - p.window + 1;
+    first[b] = from <= 0 ? 0 : from >> p.pool.shift;
+    last[b] = none ? 0 : (len[b] + p.pool.page - 1) >> p.pool.shift;
+    sinks[b] = none ? 0 : ((p.sinks < len[b] ? p.sinks : len[b]) + p.pool.page - 1) >> p.pool.shift;
+  }
+  if ((st = check_pages(p.pool, p.B, zero, sinks, false, what, stream)) != PACE_OK) return st;
   return check_pages(p.pool, p.B, first, last, false, what, stream);
 }
 

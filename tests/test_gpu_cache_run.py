@@ -293,3 +293,36 @@ def test_debug_checks(debug_env):
     # entries past a sequence's pages are not looked at
     pace.cache_attention(q, cache, dev_i32([0, 1, 2]), dev_i32([16, 25]), dev_i32([[0, 99], [2, 3]]), 1, 32)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_pages_that_left_the_window(debug_env, bits):
+    """A caller that streams gives back the pages behind the window: their entries are -1, the results stay, and
+    PACE_DEBUG complains about the pages that are still seen alone."""
+    import torch
+    from paper_2608_27206_amd import pace
+    rs = np.random.default_rng(9 + bits)
+    page, n, window, sinks = 16, 400, 60, 20
+    kc, vc, ks, vs = make_pool(rs, 27, 2, page, 128, bits)
+    cache = pace.KvCache(kc, vc, ks, vs)
+    q = dev_bf16(wl.random_bf16(3, (4, 8, 128)))
+    table = rs.permutation(27)[:25].astype(np.int32)[None]
+    first = (n - 3 - window + 1) // page                                # seen by the first of three queries
+    gone = table.copy()
+    gone[0, 2:first] = -1
+    for nq in (1, 3):
+        say(f"pages behind the window: bits {bits}, {nq} queries")
+        cu, lens = dev_i32([0, nq]), dev_i32([n])
+        want = pace.cache_attention(q[:nq], cache, cu, lens, dev_i32(table), nq, n, window=window, sinks=sinks)
+        got = pace.cache_attention(q[:nq], cache, cu, lens, dev_i32(gone), nq, n, window=window, sinks=sinks)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0].view(torch.int16), want[0].view(torch.int16)) and torch.equal(got[1], want[1])
+    for j in (1, first):
+        bad = gone.copy()
+        bad[0, j] = -1
+        with pytest.raises(pace.PaceError, match="block_table"):
+            pace.cache_attention(q[:3], cache, cu, lens, dev_i32(bad), 3, n, window=window, sinks=sinks)
+    # a sequence without queries is not looked at
+    pace.cache_attention(q[:1], cache, dev_i32([0, 1, 1]), dev_i32([n, n]), dev_i32(np.concatenate([gone, 0 * gone - 1])), 1, n,
+                         window=window, sinks=sinks)
+    torch.cuda.synchronize()
