@@ -340,12 +340,10 @@ __device__ __forceinline__ f32x4 mfma16(uint4 a, uint4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-// Maximum of three in one instruction.  fmaxf would first canonicalise values fresh from a matrix product; a NaN loses
-// either way.
+// Maximum of three in one instruction (fmaxf would first canonicalise values fresh from a matrix product).  A NaN wins: its
+// row is NaN whatever its maximum is, and no comparison with it raises one.
 __device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
 
 // Cached keys and values are read once: loads that do not ask the caches to keep them (attention over 131,071
