@@ -120,9 +120,9 @@ __device__ __forceinline__ void stage_x(uint4 u, int piece, uint4* to, float* su
 // the steps of 256 k's (whole 128-byte lines of each row) of every chunk of K in turn; they join through LDS.  A wave keeps
 // the next chunk's weights in flight while it works on one.  x passes through LDS, two chunks of it: straight from the
 // caches, a lane's 16 bytes lie a row away from its neighbour's, 64 accesses a load, and these bound the kernel (eight
-// rows through 28,672 columns of 3,584: 30 us against 23).
+// rows through 28,672 columns of 3,584: 30 us against 24; 22.5 today).
 // What is left there, with a floor of 10 us for 55 MB of weights, scales and zeros: the first loads arrive after about 10
-// us, and from then on instructions bound it (a wave issues VALU work for a quarter of its time, two of them on a SIMD);
+// us, and from then on instructions bound it (a wave issues VALU work for a fifth of its time, two of them on a SIMD);
 // one row of 4608 x 3584 takes 7.8 us, launch, chain and the join of 8 waves, against 1.6 for its bytes.
 constexpr int kW4Waves = 8;
 template <int NT, int W, int GROUP, int MR>
