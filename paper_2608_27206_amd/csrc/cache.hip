@@ -1403,6 +1403,11 @@ AttendPlan plan_attention(int Hq, int heads, int bits, int B, int max_q, int max
   a.blocks = base * a.splits;
   return a;
 }
+// Whether B sequences of max_q queries and Hq heads stay under 2^31 rows, as the plan and the kernels' numbers assume.
+bool rows_fit(int B, int max_q, int Hq) {
+  const long long lim = 1ll << 31, q = static_cast<long long>(B) * max_q;
+  return q < lim && q * Hq < lim && static_cast<long long>(B) * Hq < lim;
+}
 size_t attend_bytes(const AttendPlan& a, int n_q, int Hq, int dim) {
   return a.splits == 1 ? 0 : static_cast<size_t>(a.splits) * n_q * Hq * (dim + 4) * sizeof(float);
 }
@@ -1564,6 +1569,9 @@ pace_status_t pace_cache_append(const uint16_t* q, long long q_stride, const uin
       p.end1 = sections[0] + sections[1];
     }
   }
+  const char* many = "pace_cache_append: too many sequences, tokens or heads";
+  const long long lim = 1ll << 31;
+  PACE_REQUIRE(n_new < lim - 1024 && static_cast<long long>(B) * max_new < lim, "%s", many);
   if (max_new == 0) return PACE_OK;
   p.q = q; p.k = k; p.v = v; p.qs = q_stride; p.ks = k_stride; p.vs = v_stride;
   p.rows = rows; p.cu = cu_new; p.ctx = ctx_len; p.pos = positions; p.freq = inv_freq; p.q_out = q_out;
@@ -1573,10 +1581,10 @@ pace_status_t pace_cache_append(const uint16_t* q, long long q_stride, const uin
   p.tiles = (max_new + p.tokens - 1) / p.tokens;
   p.pages = (max_new - 1 + cache->page - 1) / cache->page + 1;
   const long long row_blocks = static_cast<long long>(B) * p.tiles;
-  const long long page_blocks = 2ll * B * p.pages * hkv;
-  PACE_REQUIRE(row_blocks + page_blocks < (1ll << 31) &&
-                   static_cast<long long>(kAppendTokens) * (static_cast<long long>(Hq) + 2 * hkv) * d < (1ll << 31),
-               "pace_cache_append: too many sequences, tokens or heads");
+  const long long held = static_cast<long long>(B) * p.pages;
+  PACE_REQUIRE(held < lim, "%s", many);
+  const long long page_blocks = 2 * held * hkv;
+  PACE_REQUIRE(row_blocks + page_blocks < lim && kAppendTokens * (static_cast<long long>(q ? Hq : 0) + 2ll * hkv) * d < lim, "%s", many);
   if (debug_checks()) {
     try {
       if ((st = debug_append(p, stream)) != PACE_OK) return st;
@@ -1591,7 +1599,7 @@ pace_status_t pace_cache_append(const uint16_t* q, long long q_stride, const uin
 size_t pace_cache_attention_workspace_size(int n_q, int Hq, int heads, int dim, int bits, int B, int max_q, int max_len,
                                            int window, int sinks) {
   if (n_q < 1 || heads < 1 || Hq < heads || Hq % heads != 0 || dim < 1 || (bits != 16 && bits != 8) || B < 1 || max_q < 1 || max_len < 0 ||
-      window < 0 || sinks < 0)
+      window < 0 || sinks < 0 || !rows_fit(B, max_q, Hq))
     return 0;
   const AttendPlan a = plan_attention(Hq, heads, bits, B, max_q, max_len, window, sinks);
   return attend_bytes(a, n_q, Hq, dim);
@@ -1614,14 +1622,14 @@ pace_status_t pace_cache_attention(const uint16_t* q, int n_q, int Hq, const pac
                "pace_cache_attention: n_q=%d max_q=%d max_len=%d (at most max_pages * page)", n_q, max_q, max_len);
   PACE_REQUIRE(window >= 0 && sinks >= 0, "pace_cache_attention: window=%d sinks=%d", window, sinks);
   PACE_REQUIRE(isfinite(scale) && scale > 0.f, "pace_cache_attention: scale must be positive");
+  PACE_REQUIRE(rows_fit(B, max_q, Hq), "pace_cache_attention: too many queries and heads");
   if (max_q == 0) return PACE_OK;
   p.q = q; p.cu = cu_q; p.len = seq_len; p.o = o; p.lse = lse;
   p.n_q = n_q; p.Hq = Hq; p.group = Hq / cache->heads; p.B = B; p.max_q = max_q; p.max_len = max_len;
   p.window = window >= max_len ? 0 : window;
   p.sinks = sinks; p.scale_log2 = scale * kLog2e;
   const AttendPlan a = plan_attention(Hq, cache->heads, cache->bits, B, max_q, max_len, window, sinks);
-  PACE_REQUIRE(a.blocks < (1ll << 31) && static_cast<long long>(B) * max_q * Hq < (1ll << 31),
-               "pace_cache_attention: too many queries and heads");
+  PACE_REQUIRE(a.blocks < (1ll << 31), "pace_cache_attention: too many queries and heads");
   p.row_blocks = a.row_blocks;
   p.splits = a.splits;
   p.chunk = a.chunk;

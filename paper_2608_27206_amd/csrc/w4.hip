@@ -510,7 +510,8 @@ using namespace pace;
 extern "C" {
 
 size_t pace_gemm_w4_workspace_size(int M, int N, int K) {
-  if (M < 1 || N < 1 || K < 1) return 0;
+  const long long lim = 1ll << 31;
+  if (M < 1 || N < 1 || K < 1 || 2ll * M * K >= lim || 2ll * M * N >= lim || static_cast<long long>(N) * K / 2 >= lim) return 0;
   const W4Plan a = plan_w4(M, N, K, 128);         // the group changes no split
   return a.splits == 1 ? 0 : static_cast<size_t>(a.splits) * M * N * sizeof(float);
 }

@@ -139,3 +139,26 @@ def test_binding_refuses_what_it_cannot_pass_on():
     x, w = torch.zeros((1, 128), dtype=torch.bfloat16), torch.zeros((4, 64), dtype=torch.uint8)
     with pytest.raises(pace.PaceError, match="GPU"):
         pace.gemm_w4(x, w, torch.ones((4, 2), dtype=torch.bfloat16))
+
+
+BIG = 2 ** 31 - 1
+
+
+def test_sizes_past_32_bits_are_refused():
+    """Products of counts that pass 2^31, or wrap to something small: an error, no division by what is left."""
+    for bad in (dict(n_src=BIG, n_new=BIG, max_new=1), dict(n_src=BIG, n_new=BIG, max_new=BIG), dict(B=BIG, n_src=1 << 20, n_new=1 << 20, max_new=1 << 20),
+                dict(B=1 << 30, max_new=4), dict(Hq=1 << 24, qs=1 << 31)):
+        st, msg = append(**bad)
+        assert st == 1 and "too many" in msg, bad
+    st, msg = append(c=cache(heads=1 << 24), ks=1 << 31, vs=1 << 31)
+    assert st == 1 and "too many" in msg
+    for bad in (dict(n_q=BIG, max_q=BIG), dict(n_q=BIG, max_q=1 << 29, Hq=4), dict(B=BIG), dict(B=1 << 29, max_q=0), dict(n_q=1 << 30, max_q=1 << 30, Hq=BIG - 1),
+                dict(B=BIG, n_q=BIG, max_q=BIG, Hq=BIG - 1)):
+        st, msg = attend(**bad)
+        assert st == 1 and "too many" in msg, bad
+    size = pace.lib().pace_cache_attention_workspace_size
+    for B, n, hq, heads in ((BIG, 1, 4, 4), (1, BIG, 4, 4), (1, 1 << 30, 1 << 20, 1 << 10), (1 << 16, 1 << 16, 1 << 30, 1), (BIG, BIG, BIG, 1), (1, 1, BIG, BIG)):
+        assert size(n, hq, heads, 128, 16, B, n, 4096, 0, 0) >= 0
+    size = pace.lib().pace_gemm_w4_workspace_size
+    for M, N, K in ((1 << 30, 1 << 30, 128), (BIG, BIG, BIG), (1, BIG, 128), (1 << 24, 128, 128), (17, BIG, 1), (BIG, 1, 1)):
+        assert size(M, N, K) == 0
