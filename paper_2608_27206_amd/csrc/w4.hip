@@ -437,42 +437,60 @@ __global__ __launch_bounds__(256) void w4_join(const W4Params p) {
 struct W4Plan {
   int mt, nt, waves, ntiles, splits;   // mt = 0: gemm_w4_few; ntiles: workgroups along the columns
 };
+// Only tiles and waves depend on the group: the parts' workspace is sized without it.  Times are of calls whose weights come from
+// memory, groups of 128 where nothing else is said.
 W4Plan plan_w4(int M, int N, int K, int group) {
   W4Plan a;
   a.splits = 1;
   const int tiles = (N + 15) / 16, steps = (K + 255) / 256;
   if (M <= 16) {
     a.mt = 0;
-    // From 16,384 columns on two tiles a wave (eight rows, 28,672 x 3584: 23.8 us against 25.4), and about 2,000 waves in
-    // all: fewer leave CUs idle (one row, 4608 x 3584: 1,152 waves 11.0 us, 2,304 7.8), more only join more (the wide one:
-    // 23.7 us with 2,048 waves, 30.2 with 7,168).
-    a.nt = tiles >= 1024 && group > 32 ? 2 : 1;
+    // All the waves that share a chunk where columns are few (eight rows, 4096 x 8192: 12.2 us with eight, 14.5 with four; 16
+    // rows, 5120 x 5120: 14.2 with four, 17.4 with two), half of them where there are columns enough (eight rows,
+    // 18,944 x 3584: 16.6 us with four, 19.8 with eight; 16 rows: 19.7 with two, 21.8 with four).  Groups of 32 keep them all: what
+    // their scales take of a wave outweighs the join (eight rows, 18,944 x 3584: 21.6 us with eight, 27.5 with four; 16
+    // rows: 24.2 with four, 31.7 with two).
     const int most = M <= 8 ? 8 : 4;
-    a.waves = most;
-    while (a.waves > 2 && tiles / a.nt * a.waves > 2560) a.waves /= 2;
+    a.waves = group == 32 || tiles <= (M <= 8 ? 384 : 1024) ? most : most / 2;
+    // Two tiles a wave, and two waves, where that leaves a little less than a workgroup for every CU (eight rows, 32,768 x
+    // 3584: 20.8 us against 22.1, 26,640 x 3584: 20.4 and 21.1, 24,592 x 3584: 20.3 and 19.7; one row, 27,648 x 8192 in
+    // groups of 64: 40.6 and 37.3).
+    const bool wide = M > 4 && M <= 8 && group > 32 && tiles > 1664 && tiles <= 2048;
+    a.nt = wide ? 2 : 1;
+    if (wide) a.waves = 2;
     a.ntiles = ((tiles + a.nt - 1) / a.nt * a.waves + kW4Waves - 1) / kW4Waves;
-    // Where all the waves that a column can have take four steps or more one after the other, gemm_w4_rows splits K over
-    // workgroups instead (8 rows: 3584 x 14336 16.4 us against 20.4, 4096 x 8192 12.4 and 12.7; 16 rows: 18.0 against
-    // 35.3, 4608 x 3584 9.8 and 11.1).  With fewer steps its join costs more than it saves (8 rows: 4608 x 3584 9.2 us
-    // there and 8.8 here, 4096 x 4096 9.3 and 7.6), and where there are columns enough nothing needs a split (16 rows,
-    // 16,000 x 8192: 30.0 and 27.9).
-    if (a.waves < most || (steps + most - 1) / most < 4) return a;
+    // gemm_w4_rows splits K over workgroups instead where all the waves that a column can have take four steps or more one
+    // after the other, and K is long beside the columns (eight rows, 4096 x 14336: 16.4 us against 19.2, 6144 x 14336: 22.3
+    // and 22.2, 6144 x 8192: 15.3 and 14.2; 16 rows, 8192 x 8192: 18.4 and 21.8, x 5120: 16.3 and 14.5, 12,800 x 14336: 39.4
+    // and 41.1, 16,384 x 14336: 46.2 and 43.8).  With fewer steps its join costs more than it saves (eight rows, 4096 x
+    // 5120: 11.8 against 8.8).
+    const bool split = (steps + most - 1) / most >= 4 && tiles <= (M <= 8 ? 7 : 24) * steps && tiles <= (M <= 8 ? 384 : 800);
+    // 257 to 340 workgroups of 9 to 16 rows are a second round for a few CUs, while three parts of gemm_w4_rows fit one: worth
+    // it from 20 steps on (16 rows, 18,944 x 8192: 36.1 us against 41.7, 20,480 x 5120: 27.5 and 28.4, x 3584: 20.2 and
+    // 19.9; 24,576 x 8192, two parts: 47.0 and 42.6).
+    const bool round = M > 8 && tiles > 1024 && tiles <= 1360 && steps >= 20;
+    if (!split && !round) return a;
   }
   // rows at a time: no more than there are (17 rows, 3584 x 14336: 20.5 us with 32, 25.2 with 64)
   a.mt = M <= 16 ? 1 : M <= 32 ? 2 : M <= 48 ? 3 : 4;
   a.nt = 2;
   a.ntiles = (N + 127) / 128;
   const int rows = (M + 63) / 64;
-  // two workgroups on every CU (48 rows, 3584 x 14336: 27.6 us; 256 workgroups 29.0, 768 31.8)
-  const int s = 512 / (a.ntiles * rows), most = (steps + 1) / 2;       // at least two steps each
-  a.splits = s < 1 ? 1 : s < most ? s : most;
+  // two workgroups on every CU (48 rows, 3584 x 14336: 27.6 us; 256 workgroups 29.0, 768 31.8), of two steps each (of an
+  // odd number of steps, one part has a single one)
+  const int s = 512 / (a.ntiles * rows), parts = (steps + 1) / 2;
+  a.splits = s < 1 ? 1 : s < parts ? s : parts;
   return a;
+}
+
+size_t w4_bytes(const W4Plan& a, int M, int N) {
+  return a.splits == 1 ? 0 : static_cast<size_t>(a.splits) * M * N * sizeof(float);
 }
 
 template <int NT, int W, int MR>
 void launch_few(const W4Params& p, int group, hipStream_t stream) {
   const dim3 g(p.ntiles), th(64 * kW4Waves);
-  if constexpr (NT == 1) {                             // groups of 32: their scales leave no registers for two tiles
+  if constexpr (W == (MR == 8 ? 8 : 4)) {
     if (group == 32) {
       hipLaunchKernelGGL((gemm_w4_few<NT, W, 32, MR>), g, th, 0, stream, p);
       return;
@@ -481,18 +499,10 @@ void launch_few(const W4Params& p, int group, hipStream_t stream) {
   if (group == 64) hipLaunchKernelGGL((gemm_w4_few<NT, W, 64, MR>), g, th, 0, stream, p);
   else hipLaunchKernelGGL((gemm_w4_few<NT, W, 128, MR>), g, th, 0, stream, p);
 }
-template <int NT>
-void launch_few(const W4Params& p, int waves, int group, hipStream_t stream) {
-  if (p.M > 8) {
-    if (waves == 4) launch_few<NT, 4, 16>(p, group, stream);
-    else launch_few<NT, 2, 16>(p, group, stream);
-  } else if (waves == 8) {
-    launch_few<NT, 8, 8>(p, group, stream);
-  } else if (waves == 4) {
-    launch_few<NT, 4, 8>(p, group, stream);
-  } else {
-    launch_few<NT, 2, 8>(p, group, stream);
-  }
+void launch_few(const W4Params& p, const W4Plan& a, int group, hipStream_t stream) {
+  if (p.M > 8) a.waves == 4 ? launch_few<1, 4, 16>(p, group, stream) : launch_few<1, 2, 16>(p, group, stream);
+  else if (a.nt == 2) launch_few<2, 2, 8>(p, group, stream);
+  else a.waves == 8 ? launch_few<1, 8, 8>(p, group, stream) : launch_few<1, 4, 8>(p, group, stream);
 }
 template <int MT>
 void launch_rows(const W4Params& p, int group, hipStream_t stream) {
@@ -512,8 +522,7 @@ extern "C" {
 size_t pace_gemm_w4_workspace_size(int M, int N, int K) {
   const long long lim = 1ll << 31;
   if (M < 1 || N < 1 || K < 1 || 2ll * M * K >= lim || 2ll * M * N >= lim || static_cast<long long>(N) * K / 2 >= lim) return 0;
-  const W4Plan a = plan_w4(M, N, K, 128);         // the group changes no split
-  return a.splits == 1 ? 0 : static_cast<size_t>(a.splits) * M * N * sizeof(float);
+  return w4_bytes(plan_w4(M, N, K, 128), M, N);
 }
 
 pace_status_t pace_gemm_w4(const uint16_t* x, const uint8_t* w, const uint16_t* scale, const uint8_t* zero,
@@ -532,15 +541,14 @@ pace_status_t pace_gemm_w4(const uint16_t* x, const uint8_t* w, const uint16_t* 
                    2ll * M * N < lim && M <= 65535,
                "pace_gemm_w4: an operand reaches 2 GiB, or M=%d is past 65,535", M);
   const W4Plan a = plan_w4(M, N, K, group);
-  const size_t need = pace_gemm_w4_workspace_size(M, N, K);
+  const size_t need = w4_bytes(a, M, N);
   if (need) {
     if (workspace == nullptr || workspace_bytes < need)
       return set_error(PACE_ERR_WORKSPACE, "pace_gemm_w4: workspace %zu < %zu bytes", workspace_bytes, need);
     PACE_REQUIRE(aligned16(workspace), "pace_gemm_w4: workspace must be 16-byte aligned");
   }
   const W4Params p{x, w, scale, zero, bias, residual, C, static_cast<float*>(workspace), M, N, K, epilogue, a.splits, a.ntiles};
-  if (a.mt == 0 && a.nt == 1) launch_few<1>(p, a.waves, group, stream);
-  else if (a.mt == 0) launch_few<2>(p, a.waves, group, stream);
+  if (a.mt == 0) launch_few(p, a, group, stream);
   else if (a.mt == 1) launch_rows<1>(p, group, stream);
   else if (a.mt == 2) launch_rows<2>(p, group, stream);
   else if (a.mt == 3) launch_rows<3>(p, group, stream);
