@@ -490,7 +490,10 @@ size_t pace_cache_attention_workspace_size(int n_q, int Hq, int heads, int dim, 
  *             whose scores are all -inf) gets o = 0 and lse = -inf.  Rows at or past cu_q[B] are left as they were.
  * Keys that a query does not see have no effect on it, whatever their K, V and scales hold.  A page outside
  * [0, num_pages) counts as unseen; entries of pages that no query sees may be anything.  Results do not
- * depend on the order in which workgroups run.  Scores and sums are fp32, probabilities are rounded to bf16;
+ * depend on the order in which workgroups run; how keys are split for them follows the longest of seq_len, so max_len
+ * may be as large as a captured step needs.  A batch is laid out for max_q queries a sequence and for like
+ * lengths: a prompt's chunk among single tokens, or one sequence many times longer than the others of a large
+ * batch, is faster in a call of its own.  Scores and sums are fp32, probabilities are rounded to bf16;
  * sums are divided at the end, so values of V should stay under 2^100.
  * The workspace must be 16-byte aligned; calls that may run at the same time need one each.
  */

@@ -326,7 +326,8 @@ struct AttendParams {
   float* part;               // partial results [splits, n_q * Hq, D + 4]: D values, maximum, sum
   Pool pool;
   int n_q, Hq, group, B, max_q, max_len, window, sinks;
-  int row_blocks, splits, chunk;   // row blocks of a KV head, most parts of its keys, tiles per part
+  int row_blocks, splits;    // row blocks of a KV head, most parts of its keys
+  int want, size;            // parts that the longest should make; tiles of a part, 0: as many as that takes
   float scale_log2;
 };
 
@@ -398,10 +399,44 @@ __device__ __forceinline__ void tiles_of(const AttendParams& p, int i_lo, int i_
   if (s->tail0 <= s->head_tiles) { s->tail0 = 0; s->head_tiles = 0; }
   s->tiles = end - s->tail0 + s->head_tiles;
 }
-// How many parts a row block's tiles are split into: parts of one size over all sequences, so that workgroups are
-// alike where lengths are not.
-__device__ __forceinline__ int splits_of(const AttendParams& p, int tiles) {
-  const int s = (tiles + p.chunk - 1) / p.chunk;
+// Tiles of T keys that a row block may see at most in a sequence of up to `len` tokens: sinks and window each begin inside one.
+__host__ __device__ __forceinline__ int most_tiles(int len, int T, int window, int sinks, int max_q) {
+  const long long seen = static_cast<long long>(window) + sinks + max_q;
+  const int keys = window > 0 && seen < len ? static_cast<int>(seen) : len;    // len <= 2^31 - 1,024
+  return (keys + T - 1) / T + (window > 0 ? 2 : 0);
+}
+// Tiles of a part, where the longest sequence's should make `want`.  A part of fewer than four tiles costs more to join than
+// it saves (64 tokens x 7 heads over 1,183: 18.5 us, parts of two tiles 23.9; one token over 5,000: 11.2 us, parts of one
+// 12.1); more leave CUs idle (32 tokens over 1,183: 17.5 us, parts of eight 20.4).
+constexpr int kLeastTiles = 4;
+__device__ __forceinline__ int part_tiles(int tiles, int want) {
+  const int part = (tiles + want - 1) / want;
+  return part < kLeastTiles ? kLeastTiles : part;
+}
+// Tiles of a row block's parts: one size over all sequences, so that workgroups are alike where lengths are not.  The
+// longest sequence sets it, not the caller's bound, in which a captured step leaves room: under a bound of 131,072, 48
+// sequences of up to 16,384 tokens in 8 bits take 106 us (233 with parts cut from the bound; 105 under 16,384), 1,024
+// tokens x 7 heads over 10,677 194 (362), 8 sequences of up to 1,183 16 (53).  Reading the lengths costs a few tenths of a
+// microsecond in each of the two launches.  All the lanes of a wave call it.
+template <int T>
+__device__ __forceinline__ int part_of(const AttendParams& p) {
+  if (p.size != 0) return p.size;
+  int longest = p.len[0];
+  if (p.B > 1) {
+    int m = 0;
+    for (int i = threadIdx.x & 63; i < p.B; i += 64) m = p.len[i] > m ? p.len[i] : m;
+    const auto larger = [&](int y) { m = y > m ? y : m; };
+    larger(dpp_u32<kDppQuadXor1>(m));
+    larger(dpp_u32<kDppQuadXor2>(m));
+    larger(dpp_u32<kDppRowHalfMirror>(m));
+    larger(dpp_u32<kDppRowMirror>(m));
+    for (int r = 0; r < 64; r += 16) longest = __builtin_amdgcn_readlane(m, r) > longest ? __builtin_amdgcn_readlane(m, r) : longest;
+  }
+  longest = longest < 0 ? 0 : longest < p.max_len ? longest : p.max_len;
+  return part_tiles(most_tiles(longest, T, p.window, p.sinks, p.max_q), p.want);
+}
+__device__ __forceinline__ int splits_of(const AttendParams& p, int tiles, int part) {
+  const int s = (tiles + part - 1) / part;
   return s < 1 ? 1 : s < p.splits ? s : p.splits;
 }
 
@@ -446,12 +481,13 @@ __global__ __launch_bounds__(64 * W, R == 1 ? 3 : 2) void attend_few(const Atten
   const int rb = id % p.row_blocks;
   id /= p.row_blocks;
   const int hk = id % p.pool.heads, b = id / p.pool.heads;
+  const int part = part_of<T>(p);
   Span sp = queries_of(p, b);
   const int rows = sp.nq * p.group, x0 = rb * 16 * R;
   if (x0 >= rows) return;
   const int x1 = x0 + 16 * R < rows ? x0 + 16 * R - 1 : rows - 1;
   tiles_of<T>(p, x0 / p.group, x1 / p.group, &sp);
-  const int splits = splits_of(p, sp.tiles);
+  const int splits = splits_of(p, sp.tiles, part);
   if (split >= splits) return;
   const int t0 = static_cast<int>(static_cast<long long>(sp.tiles) * split / splits);
   const int t1 = static_cast<int>(static_cast<long long>(sp.tiles) * (split + 1) / splits);
@@ -874,12 +910,13 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many(const AttendParam
   const int split = id % p.splits;
   id /= p.splits;
   const int hk = id % p.pool.heads, b = id / p.pool.heads;
+  const int part = part_of<T>(p);
   Span sp = queries_of(p, b);
   const int rows = sp.nq * p.group, x0 = rb * ROWS;
   if (x0 >= rows) return;
   const int x1 = x0 + ROWS < rows ? x0 + ROWS - 1 : rows - 1;
   tiles_of<T>(p, x0 / p.group, x1 / p.group, &sp);
-  const int splits = splits_of(p, sp.tiles);
+  const int splits = splits_of(p, sp.tiles, part);
   if (split >= splits) return;
   const int t0 = static_cast<int>(static_cast<long long>(sp.tiles) * split / splits);
   const int t1 = static_cast<int>(static_cast<long long>(sp.tiles) * (split + 1) / splits);
@@ -1283,6 +1320,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void attend_join(const AttendParam
   const int h = id % p.Hq;
   id /= p.Hq;
   const int i = id % p.max_q, b = id / p.max_q;
+  const int tiles_part = part_of<T>(p);
   if (W == 1 && b >= p.B) return;
   Span sp = queries_of(p, b);
   if (i >= sp.nq) return;
@@ -1290,7 +1328,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void attend_join(const AttendParam
   const int rows = sp.nq * p.group, x = i * p.group + h % p.group, x0 = x / block_rows * block_rows;
   const int x1 = x0 + block_rows < rows ? x0 + block_rows - 1 : rows - 1;
   tiles_of<T>(p, x0 / p.group, x1 / p.group, &sp);
-  const int splits = splits_of(p, sp.tiles);
+  const int splits = splits_of(p, sp.tiles, tiles_part);
   if (splits == 1) return;
   const int n = sp.row0 + i;
   const long long row = static_cast<long long>(n) * p.Hq + h, all = static_cast<long long>(p.n_q) * p.Hq;
@@ -1361,7 +1399,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void attend_join(const AttendParam
 
 // How a call is laid out: rows of a KV head per workgroup, and the parts that a row block's keys are split into.
 struct AttendPlan {
-  int rows, row_blocks, splits, chunk;
+  int rows, row_blocks, splits, want, size;
   long long blocks;
 };
 constexpr int kWaves = 4;
@@ -1380,26 +1418,24 @@ AttendPlan plan_attention(int Hq, int heads, int bits, int B, int max_q, int max
   a.row_blocks = static_cast<int>((rows + a.rows - 1) / a.rows);
   const long long base = static_cast<long long>(B) * heads * a.row_blocks;
   if (window >= max_len) window = 0;                  // such a window hides nothing
-  long long keys = max_len;
-  if (window > 0 && static_cast<long long>(window) + sinks + max_q < keys) keys = static_cast<long long>(window) + sinks + max_q;
-  // tiles that a row block may see at most: sinks and window each begin inside one
   const int tile = a.rows > 32 ? kManyTile : tile_keys(bits);
-  const long long tiles = (keys + tile - 1) / tile + (window > 0 ? 2 : 0);
   // Workgroups to aim at.  Many rows: one on every CU, all that its registers hold (40 tokens x 4 heads of 8 sequences
   // 119 us; 512 in all 124, 1,024 155).  Few: two a CU where that is all that fits (32 rows: 8 sequences of 20 rows 47 us,
   // with four 54) or the sequences' parts are alike, whose number only costs in the join (one sequence of 131,071: 52 us,
   // with four 56; 24 that a window of 4,096 bounds: 30.7 and 33.2), else four: 48 sequences of up to 16,384 take 104 us,
   // with two 140.
-  const bool alike = B == 1 || 2 * keys <= max_len;
+  // Where sequences and heads alone give that many workgroups nothing is split, and a sequence far longer than the others
+  // takes its own time: 256 sequences x 4 heads, one of 131,072 tokens and 255 of 1,000, 1,770 us (the long one in a call of
+  // its own 54, the others 90).  Parts of at most 4,096 keys whatever the batch is make that 380 us, but their empty
+  // workgroups cost a batch under a loose bound more than it has to lose (512 sequences x 8 heads of up to 2,048 tokens under
+  // 131,072: 433 us, with such parts 645).
+  const bool alike = B == 1 || (window > 0 && 2 * (static_cast<long long>(window) + sinks + max_q) <= max_len);
   const long long aim = a.rows > 32 ? 256 : a.rows == 32 || alike ? 512 : 1024;
-  const long long want = aim / base < 1 ? 1 : aim / base, chunk = (tiles + want - 1) / want;
-  // A part of fewer than four tiles costs more to join than it saves (64 tokens x 7 heads over 1,183: 18.5 us, parts of
-  // two tiles 23.9; one token over 5,000: 11.2 us, parts of one 12.1); more leave CUs idle (32 tokens over 1,183: 17.5 us,
-  // parts of eight 20.4).
-  const int least = 4;
-  a.chunk = static_cast<int>(chunk < least ? least : chunk);
-  a.splits = static_cast<int>((tiles + a.chunk - 1) / a.chunk);
+  a.want = static_cast<int>(aim / base < 1 ? 1 : aim / base);
+  const int least = (most_tiles(max_len, tile, window, sinks, max_q) + kLeastTiles - 1) / kLeastTiles;
+  a.splits = least < a.want ? least : a.want;          // no length up to max_len makes more
   if (a.splits < 1) a.splits = 1;
+  a.size = least <= a.want ? kLeastTiles : 0;          // then every length makes parts of the least size
   a.blocks = base * a.splits;
   return a;
 }
@@ -1632,7 +1668,8 @@ pace_status_t pace_cache_attention(const uint16_t* q, int n_q, int Hq, const pac
   PACE_REQUIRE(a.blocks < (1ll << 31), "pace_cache_attention: too many queries and heads");
   p.row_blocks = a.row_blocks;
   p.splits = a.splits;
-  p.chunk = a.chunk;
+  p.want = a.want;
+  p.size = a.size;
   const size_t need = attend_bytes(a, n_q, Hq, cache->dim);
   if (need) {
     if (workspace == nullptr || workspace_bytes < need)
