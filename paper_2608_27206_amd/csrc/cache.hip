@@ -392,8 +392,7 @@ __device__ __forceinline__ void tiles_of(const AttendParams& p, int i_lo, int i_
   s->p_lo = s->len - s->nq + i_lo;
   s->p_hi = s->len - s->nq + i_hi;
   const int end = s->p_hi < 0 ? 0 : s->p_hi / T + 1;
-  const int first = p.window == 0 ? 0 : s->p_lo - p.window + 1;      // p_lo < 2^31 and window >= 0: no overflow
-  s->tail0 = first <= 0 ? 0 : first / T;
+  s->tail0 = p.window == 0 || s->p_lo < p.window ? 0 : (s->p_lo - p.window + 1) / T;   // p_lo may be as low as -nq
   const int sinks = p.sinks < s->p_hi + 1 ? p.sinks : s->p_hi + 1;
   s->head_tiles = sinks <= 0 ? 0 : (sinks + T - 1) / T;
   if (s->tail0 <= s->head_tiles) { s->tail0 = 0; s->head_tiles = 0; }
@@ -1556,8 +1555,8 @@ pace_status_t debug_attention(const AttendParams& p, hipStream_t stream) {
   std::vector<int> zero(p.B, 0), sinks(p.B), first(p.B), last(p.B);
   for (int b = 0; b < p.B; ++b) {
     const bool none = cu[b + 1] == cu[b];
-    const int from = p.window == 0 ? 0 : len[b] - (cu[b + 1] - cu[b]) - p.window + 1;
-    first[b] = from <= 0 ? 0 : from >> p.pool.shift;
+    const long long from = p.window == 0 ? 0 : static_cast<long long>(len[b]) - (cu[b + 1] - cu[b]) - p.window + 1;
+    first[b] = from <= 0 ? 0 : static_cast<int>(from >> p.pool.shift);
     last[b] = none ? 0 : (len[b] + p.pool.page - 1) >> p.pool.shift;
     sinks[b] = none ? 0 : ((p.sinks < len[b] ? p.sinks : len[b]) + p.pool.page - 1) >> p.pool.shift;
   }

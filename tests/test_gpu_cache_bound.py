@@ -1,11 +1,11 @@
-"""Cache attention under a bound max_len that is not the longest length, as a captured step has it."""
+"""Cache attention under a bound max_len that is not the longest length, as a captured step has it, and at the largest sizes."""
 import numpy as np
 import pytest
 
 from oracle import cache as oc
 from paper_2608_27206_amd import workloads as wl
 from tests.gpu_util import dev_bf16, dev_i32, say
-from tests.test_gpu_cache import _attend_inputs, check_attention, f64
+from tests.test_gpu_cache import _attend_inputs, check_attention, f64, make_pool
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +55,27 @@ def test_a_loose_bound_changes_nothing(case):
         check_attention(f64(o), f64(lse), (ref[0][:n], ref[1][:, :n], ref[2][:n], ref[3][:, :n]), dim, n)
     if window == 0:
         assert got[0][2].max() > 1 and torch.equal(got[0][2], got[1][2])
+
+
+@pytest.mark.parametrize("debug", [False, True])
+@pytest.mark.parametrize("nq", [3, 40, 2100])
+def test_a_window_near_the_largest_length(nq, debug, monkeypatch):
+    """A table of 2^31 - 1,024 tokens, a window one short of that, and queries before the first token: p - window passes -2^31
+    for the earliest of 2,100 (they see nothing), and the others see all their keys."""
+    import torch
+    from paper_2608_27206_amd import pace
+    if debug:
+        monkeypatch.setenv("PACE_DEBUG", "1")
+    rs = np.random.default_rng(nq)
+    page, dim, n = 256, 80, 30
+    kc, vc, ks, vs = make_pool(rs, 3, 1, page, dim, 16)
+    q = wl.random_bf16(nq, (nq, 1, dim))
+    pages = (2 ** 31 - 1024) // page
+    table = torch.full((1, pages), -1, dtype=torch.int32, device="cuda")
+    table[0, 0] = 2
+    say(f"window of {pages * page - 1}, {nq} queries of {n} tokens")
+    o, lse = pace.cache_attention(dev_bf16(q), pace.KvCache(kc, vc), dev_i32([0, nq]), dev_i32([n]), table, nq, pages * page,
+                                  window=pages * page - 1, sinks=5)
+    torch.cuda.synchronize()
+    ref = oc.attention(wl.bf16_bits_to_f64(q), f64(kc), f64(vc), None, None, [0, nq], [n], np.array([[2]]), page, dim ** -0.5)
+    check_attention(f64(o), f64(lse), ref, dim, nq)
