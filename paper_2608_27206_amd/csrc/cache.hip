@@ -1479,6 +1479,8 @@ pace_status_t launch_attend(const AttendParams& p, const AttendPlan& a, hipStrea
 }
 
 // ---------------------------------------------------------------- host checks
+constexpr long long kMostThreads = (1ll << 32) - 64 * kJoinWaves;    // of a launch; a grid may round up to a workgroup more
+
 pace_status_t check_cache(const pace_kv_cache* c, const int32_t* table, int max_pages, int B, const char* what,
                           Pool* out) {
   PACE_REQUIRE(c != nullptr && c->k && c->v && table, "%s: null cache or block_table", what);
@@ -1619,7 +1621,7 @@ pace_status_t pace_cache_append(const uint16_t* q, long long q_stride, const uin
   const long long held = static_cast<long long>(B) * p.pages;
   PACE_REQUIRE(held < lim, "%s", many);
   const long long page_blocks = 2 * held * hkv;
-  PACE_REQUIRE(row_blocks + page_blocks < lim && kAppendTokens * (static_cast<long long>(q ? Hq : 0) + 2ll * hkv) * d < lim, "%s", many);
+  PACE_REQUIRE(row_blocks + page_blocks < kMostThreads / kAppendThreads && kAppendTokens * (static_cast<long long>(q ? Hq : 0) + 2ll * hkv) * d < lim, "%s", many);
   if (debug_checks()) {
     try {
       if ((st = debug_append(p, stream)) != PACE_OK) return st;
@@ -1664,7 +1666,9 @@ pace_status_t pace_cache_attention(const uint16_t* q, int n_q, int Hq, const pac
   p.window = window >= max_len ? 0 : window;
   p.sinks = sinks; p.scale_log2 = scale * kLog2e;
   const AttendPlan a = plan_attention(Hq, cache->heads, cache->bits, B, max_q, max_len, window, sinks);
-  PACE_REQUIRE(a.blocks < (1ll << 31), "pace_cache_attention: too many queries and heads");
+  const long long joins = a.splits == 1 ? 0 : static_cast<long long>(B) * max_q * Hq * (a.splits <= 8 ? kJoinLanes : 64 * kJoinWaves);
+  PACE_REQUIRE(a.blocks * (a.rows > 32 ? kManyThreads : 64 * kWaves) < kMostThreads && joins < kMostThreads,
+               "pace_cache_attention: too many queries and heads");
   p.row_blocks = a.row_blocks;
   p.splits = a.splits;
   p.want = a.want;

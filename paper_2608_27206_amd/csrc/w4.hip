@@ -521,7 +521,7 @@ extern "C" {
 
 size_t pace_gemm_w4_workspace_size(int M, int N, int K) {
   const long long lim = 1ll << 31;
-  if (M < 1 || N < 1 || K < 1 || 2ll * M * K >= lim || 2ll * M * N >= lim || static_cast<long long>(N) * K / 2 >= lim) return 0;
+  if (M < 1 || N < 1 || K < 1 || 2ll * M * K >= lim || 2ll * M * N >= lim || (N + 15ll) / 16 * 16 * K / 2 >= lim) return 0;
   return w4_bytes(plan_w4(M, N, K, 128), M, N);
 }
 
@@ -537,7 +537,8 @@ pace_status_t pace_gemm_w4(const uint16_t* x, const uint8_t* w, const uint16_t* 
                "pace_gemm_w4: M=%d N=%d K=%d (K a positive multiple of group=%d)", M, N, K, group);
   PACE_REQUIRE(aligned16(x) && aligned16(w), "pace_gemm_w4: x and w must be 16-byte aligned");
   const long long lim = 1ll << 31;
-  PACE_REQUIRE(2ll * M * K < lim && static_cast<long long>(N) * K / 2 < lim && 2ll * N * (K / group) < lim &&
+  // whole tiles of columns: a launch of one workgroup each then stays under 2^32 threads
+  PACE_REQUIRE(2ll * M * K < lim && (N + 15ll) / 16 * 16 * K / 2 < lim && 2ll * N * (K / group) < lim &&
                    2ll * M * N < lim && M <= 65535,
                "pace_gemm_w4: an operand reaches 2 GiB, or M=%d is past 65,535", M);
   const W4Plan a = plan_w4(M, N, K, group);
