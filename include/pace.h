@@ -459,7 +459,8 @@ typedef struct pace_kv_cache {
  * between powers of two, except where a code becomes subnormal).  Values that are not finite are
  * stored as NaN.
  * A source row outside [0, n_src), a place past the table and a page outside [0, num_pages) are not
- * written.  q_out and the cache must not overlap q, k and v.  Asynchronous on `stream`; no workspace.
+ * written.  q_out and the cache must not overlap q, k and v.  Batches padded so far that a launch would take 2^32
+ * threads are refused.  Asynchronous on `stream`; no workspace.
  */
 pace_status_t pace_cache_append(const uint16_t* q, long long q_stride, const uint16_t* k, long long k_stride,
                                 const uint16_t* v, long long v_stride, int n_src, int Hq, const int32_t* rows,
@@ -493,8 +494,8 @@ size_t pace_cache_attention_workspace_size(int n_q, int Hq, int heads, int dim, 
  * depend on the order in which workgroups run; how keys are split for them follows the longest of seq_len, so max_len
  * may be as large as a captured step needs.  A batch is laid out for max_q queries a sequence and for like
  * lengths: a prompt's chunk among single tokens, or one sequence many times longer than the others of a large
- * batch, is faster in a call of its own.  Scores and sums are fp32, probabilities are rounded to bf16;
- * sums are divided at the end, so values of V should stay under 2^100.
+ * batch, is faster in a call of its own; one whose launch would take 2^32 threads is refused.  Scores and sums
+ * are fp32, probabilities are rounded to bf16; sums are divided at the end, so values of V should stay under 2^100.
  * The workspace must be 16-byte aligned; calls that may run at the same time need one each.
  */
 pace_status_t pace_cache_attention(const uint16_t* q, int n_q, int Hq, const pace_kv_cache* cache,
@@ -513,7 +514,7 @@ size_t pace_gemm_w4_workspace_size(int M, int N, int K);
  *   scale     bf16 [N, K / group]; zero uint8 [N, K / group] with values 0..15, or NULL (8 everywhere).
  *   group     32, 64 or 128; K a positive multiple of group.
  *   x         bf16 [M, K] row-major; x and w 16-byte aligned.  1 <= M <= 65,535; the weights are read once for
- *             every 64 rows.
+ *             every 64 rows.  For the rows of a prompt pace_gemm_bf16 on the same weights in bf16 is up to twice as fast.
  *   bias, residual, epilogue, C  as in pace_gemm_bf16.
  * Products accumulate in fp32, in an order fixed by the shape.  x must be finite and should stay under 2^100 (a row with
  * an infinity comes out as NaN).  Each operand under 2 GiB.  The workspace must be 16-byte aligned; calls that may run at the same time need

@@ -877,9 +877,9 @@ __global__ __launch_bounds__(64 * W, R == 1 ? 3 : 2) void attend_few(const Atten
 // eight ahead do not fit the registers, 239).
 // With 256 rows the registers hold two tiles on their way, which hides most of their arrival (1,024 tokens x 7 heads
 // over 10,677: 200 us against 212 with one); with 128 rows a thread stages twice as much, and they hold one.
-// That case runs its 149 GFLOP at 750 TFLOP/s, its join included: the matrix units are busy for 30% of it; two waves
-// on a SIMD leave their waits (a third), the exponentials and the staging partly uncovered, and LDS and registers
-// have no room for a third.
+// That case runs its 149 GFLOP at 760 TFLOP/s, its join included: its 112 row blocks in two parts are 224 workgroups, which
+// leave 32 CUs without one; on the others two waves on a SIMD leave their waits (a third), the exponentials and the
+// staging partly uncovered, and LDS and registers have no room for a third.
 // NP: the pages of a tile, 1 (64 or more tokens a page) or 4 (one for each 16 keys).
 constexpr int kManyTile = 64, kManyThreads = 512;
 constexpr int many_rows(int groups) { return 256 / groups; }

@@ -120,10 +120,12 @@ __device__ __forceinline__ void stage_x(uint4 u, int piece, uint4* to, float* su
 // the steps of 256 k's (whole 128-byte lines of each row) of every chunk of K in turn; they join through LDS.  A wave keeps
 // the next chunk's weights in flight while it works on one.  x passes through LDS, two chunks of it: straight from the
 // caches, a lane's 16 bytes lie a row away from its neighbour's, 64 accesses a load, and these bound the kernel (eight
-// rows through 28,672 columns of 3,584: 30 us against 24; 22.5 today).
-// What is left there, with a floor of 10 us for 55 MB of weights, scales and zeros: the first loads arrive after about 10
-// us, and from then on instructions bound it (a wave issues VALU work for a fifth of its time, two of them on a SIMD);
-// one row of 4608 x 3584 takes 7.8 us, launch, chain and the join of 8 waves, against 1.6 for its bytes.
+// rows through 28,672 columns of 3,584: 30 us against 24; 22 today).
+// What is left there, with a floor of 10 us for 55 MB of weights, scales and zeros: 224 workgroups leave 32 CUs without
+// one, the two waves of a column take eight and six of its 14 steps, and the four steps that each asks for before its
+// first product (57% of the weights) arrive behind a barrier for x, so loads and products hardly overlap.  One row of 4608 x
+// 3584 takes 7.8 us against 1.6 for its bytes: of eight waves two take one step and the others two, the second chunk's
+// x is staged behind a barrier after the first one's products, and seven rows of zeros are staged beside the one.
 constexpr int kW4Waves = 8;
 template <int NT, int W, int GROUP, int MR>
 __global__ __launch_bounds__(64 * kW4Waves, 2) void gemm_w4_few(const W4Params p) {
@@ -276,9 +278,13 @@ __global__ __launch_bounds__(64 * kW4Waves, 2) void gemm_w4_few(const W4Params p
 
 // More rows (16 MT at a time), or long rows of few columns: here x would be read far more often than the weights, so the 4
 // waves of a workgroup take 32 columns each and share x through LDS, 256 k's at a time; workgroups split K where the
-// columns give too few, and w4_join adds their sums.  48 rows of 3584 x 14336 take 27 us, 4 to 5 of them the join, against
-// 5.3 for 29 MB: a part is three or four steps of load, stage, barrier and products, one after the other, and two
-// workgroups on a CU cover a third of that.  Two steps in flight gave nothing (29.4 us).
+// columns give too few, and w4_join adds their sums.  48 rows of 3584 x 14336 take 27 us, 4 of them the join, against 5.3
+// for 29 MB: 18 parts write 12.4 MB of sums and the join reads them again, some parts have four of the 56 steps and some three,
+// and a step's load, stage, barrier and products come one after the other, about 6 us; two workgroups on a CU cover a
+// third of that.  Two steps in flight gave nothing (29.4 us).
+// Many rows are served, not meant: each 64 of them turn the weights into pairs again, 1,183 through 28,672 columns of 3,584
+// run at 460 TFLOP/s, 10,677 at 520, where the bf16 product of such weights reaches 970 and 1,165; it is faster from
+// about 32 rows on there, from 100 for 4608 x 3584 and from 256 for 3584 x 14336.
 template <int MT, int GROUP>
 __global__ __launch_bounds__(256, 2) void gemm_w4_rows(const W4Params p) {
   const Nibbles nibbles;
