@@ -1434,7 +1434,8 @@ AttendPlan plan_attention(int Hq, int heads, int bits, int B, int max_q, int max
   const int least = (most_tiles(max_len, tile, window, sinks, max_q) + kLeastTiles - 1) / kLeastTiles;
   a.splits = least < a.want ? least : a.want;          // no length up to max_len makes more
   if (a.splits < 1) a.splits = 1;
-  a.size = least <= a.want ? kLeastTiles : 0;          // then every length makes parts of the least size
+  // nothing to split, or parts of the least size whatever the lengths are: nobody reads those of the other sequences
+  a.size = a.splits == 1 || least <= a.want ? kLeastTiles : 0;
   a.blocks = base * a.splits;
   return a;
 }

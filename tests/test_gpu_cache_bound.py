@@ -79,3 +79,24 @@ def test_a_window_near_the_largest_length(nq, debug, monkeypatch):
     torch.cuda.synchronize()
     ref = oc.attention(wl.bf16_bits_to_f64(q), f64(kc), f64(vc), None, None, [0, nq], [n], np.array([[2]]), page, dim ** -0.5)
     check_attention(f64(o), f64(lse), ref, dim, nq)
+
+
+@pytest.mark.parametrize("heads,dim,bits", [(1, 128, 16), (2, 80, 8)])
+def test_many_sequences_under_a_loose_bound(heads, dim, bits):
+    """30,000 sequences of one query, lengths from 0, a table much wider than they are: nothing is split, and no sequence's call
+    depends on how many others there are."""
+    import torch
+    from paper_2608_27206_amd import pace
+    rs = np.random.default_rng(heads)
+    B, page = 30000, 16
+    lens = rs.integers(0, 33, size=B).astype(np.int32)
+    kc, vc, ks, vs = make_pool(rs, 64, heads, page, dim, bits)
+    table = rs.integers(0, 64, size=(B, 64)).astype(np.int32)             # sequences may share what they read
+    q = wl.random_bf16(5, (B, heads, dim))
+    some = rs.permutation(B)[:200]
+    say(f"{B} sequences, {heads} heads of {dim}, {bits} bits")
+    o, lse = pace.cache_attention(dev_bf16(q), pace.KvCache(kc, vc, ks, vs), dev_i32(np.arange(B + 1)), dev_i32(lens), dev_i32(table), 1, 1024)
+    torch.cuda.synchronize()
+    ref = oc.attention(wl.bf16_bits_to_f64(q[some]), f64(kc), f64(vc), None if ks is None else f64(ks), None if vs is None else f64(vs),
+                       np.arange(201), lens[some], table[some], page, dim ** -0.5)
+    check_attention(f64(o)[some], f64(lse)[:, some], ref, dim, 200)
