@@ -7,6 +7,7 @@ from oracle import cache as oc
 from paper_2608_27206_amd import workloads as wl
 from tests.gpu_util import dev_bf16, dev_f32, say
 from tests.test_gpu_cache import f64
+from tests.test_gpu_cache import test_w4 as check_w4
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +45,11 @@ def test_workspace_is_asked_for_where_it_is_used(M, N, K):
         ref, tol = oc.w4(wl.bf16_bits_to_f64(x), w[some], wl.bf16_bits_to_f64(s[some]), None, group, bias[some],
                          wl.bf16_bits_to_f64(res[:, some]), 1)
         assert np.all(np.abs(got[:, some] - ref) <= 2.0 ** -8 * np.abs(ref) + tol)
+
+
+# two tiles a wave (5 to 8 rows of about 26,700 to 32,768 columns, groups of 64 and 128), and their neighbours on every side
+@pytest.mark.parametrize("M,N,K,group,zero,epilogue", [
+    (8, 28680, 384, 128, 1, 2), (5, 32768, 640, 64, 0, 1), (6, 26641, 2432, 128, 0, 0), (7, 30002, 192, 64, 1, 2), (8, 26640, 2240, 64, 1, 1),
+    (8, 26624, 384, 128, 1, 2), (8, 32770, 256, 64, 1, 2), (4, 30000, 384, 128, 1, 1), (9, 30002, 384, 64, 1, 2), (8, 30000, 288, 32, 1, 2)])
+def test_two_tiles_a_wave(M, N, K, group, zero, epilogue):
+    check_w4(M, N, K, group, zero, epilogue)
