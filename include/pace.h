@@ -524,6 +524,66 @@ pace_status_t pace_gemm_w4(const uint16_t* x, const uint8_t* w, const uint16_t* 
                            const float* bias, const uint16_t* residual, uint16_t* C, int M, int N, int K, int group,
                            int epilogue, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
+/* ---------------------------------------------------------------- a layer in 8 bits */
+
+/*
+ * The operators of a layer whose products run in 8 bits: OCP e4m3 codes with an fp32 scale for each block, value =
+ * code * scale.  Activations have a scale for each 128 neighbouring values of a row, K / 128 rows of M scales
+ * ([ceil(K / 128), M]); weights one for each 128 x 128 ([ceil(N / 128), ceil(K / 128)]).  The last block of a row
+ * or column may be shorter.  Widths are multiples of 16.
+ */
+
+/*
+ * Quantises rows or weights: scale = max(largest finite |x| of the block / 448, 2^-120), code = x / scale, rounded to
+ * nearest even; values that are not finite become NaN.
+ *   x       bf16 [M, K], row i at x + i * x_stride (in elements, a multiple of 8, at least K); 16-byte aligned, K a
+ *           multiple of 16, at most 2^20.
+ *   rows    1: activations, scale fp32 [ceil(K / 128), M]; 128: weights, scale fp32 [ceil(M / 128), ceil(K / 128)].
+ *   q       codes [M, K], 16-byte aligned.
+ * M = 0 is a no-op.  q must not overlap x.  Asynchronous on `stream`; no workspace.
+ */
+pace_status_t pace_quantize_fp8(const uint16_t* x, long long x_stride, int M, int K, int rows, uint8_t* q, float* scale,
+                                hipStream_t stream);
+
+/*
+ * RMS norm with the residual's addition in front of it: h = x + residual, y = h / sqrt(mean(h^2) + eps) * gamma, in fp32
+ * with one rounding of each output.
+ *   x, residual  bf16 [M, K], rows x_stride and residual_stride apart (in elements, multiples of 8, at least K); residual
+ *           may be NULL (h = x; its stride is not read then).
+ *   gamma   fp32 [K]; eps > 0.  K a multiple of 16, at most 65,536.
+ *   sum     bf16 [M, K] = h, or NULL.  It may be the memory of x or residual (with rows K apart).
+ *   y       bf16 [M, K], or NULL and instead of it
+ *   q, scale  codes [M, K] and scales [ceil(K / 128), M] of y, as pace_quantize_fp8 (rows = 1) makes them of y's fp32 values.
+ * Tensors are 16-byte aligned (scale: 4).  Squares are summed in fp32: |h| should stay under 2^60.  A row that holds a
+ * NaN becomes NaN.  M = 0 is a no-op.  y may be the memory of x or residual (with rows K apart), but not sum's.
+ * Asynchronous on `stream`; no workspace.
+ */
+pace_status_t pace_rmsnorm(const uint16_t* x, long long x_stride, const uint16_t* residual, long long residual_stride,
+                           const float* gamma, float eps, int M, int K, uint16_t* sum, uint16_t* y, uint8_t* q, float* scale,
+                           hipStream_t stream);
+
+/* Workspace bytes for pace_gemm_fp8 (partial sums; 0 where none are needed).  bits: of the output, 16 or 8. */
+size_t pace_gemm_fp8_workspace_size(int M, int N, int K, int bits);
+
+/*
+ * C = x W^T of 8-bit rows and weights: C[m, n] = sum over blocks b of x_scale[b, m] * w_scale[n / 128, b] *
+ * (sum over the k's of b of x[m, k] w[n, k]), with pace_gemm_bf16's epilogues.
+ *   x       codes [M, K]; x_scale fp32: the scale of row m and block b at x_scale[b * x_scale_stride + m], x_scale_stride at
+ *           least M (rows a .. b - 1 of a larger batch: x + a * K, x_scale + a, the same stride).
+ *   w       codes [N, K]; w_scale fp32 [ceil(N / 128), ceil(K / 128)].  x and w 16-byte aligned, K a multiple of 16, at
+ *           most 2^20.
+ *   bias, residual, epilogue  as in pace_gemm_bf16 (bias fp32 [N] or NULL; 1: + residual bf16 [M, N]; 2: SwiGLU of
+ *           columns 2f and 2f + 1, N even).
+ *   C       bf16 [M, N], or [M, N / 2] with SwiGLU; or, with c_scale, SwiGLU and N a multiple of 32, codes [M, N / 2]
+ *           (16-byte aligned) with c_scale fp32 [ceil(N / 256), M], quantised from fp32 as by pace_quantize_fp8 (rows = 1).
+ * The products of a block are summed by the matrix cores, the blocks in fp32, in an order fixed by the shape.  A NaN in x makes its row of C NaN, one in
+ * w its column.  C may be the residual's memory.  M = 0 is a no-op.  The workspace must be 16-byte aligned; calls that may
+ * run at the same time need one each.
+ */
+pace_status_t pace_gemm_fp8(const uint8_t* x, const float* x_scale, long long x_scale_stride, const uint8_t* w, const float* w_scale,
+                            const float* bias, const uint16_t* residual, void* C, float* c_scale, int M, int N, int K, int epilogue,
+                            void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -83,6 +83,11 @@ _PROTOS = {
     "pace_gemm_w4_workspace_size": (c_size, [c_int, c_int, c_int]),
     "pace_gemm_w4": (c_int, [c_void, c_void, c_void, c_void, c_void, c_void, c_void, c_int, c_int, c_int, c_int, c_int,
                              c_void, c_size, c_void]),
+    "pace_quantize_fp8": (c_int, [c_void, c_ll, c_int, c_int, c_int, c_void, c_void, c_void]),
+    "pace_rmsnorm": (c_int, [c_void, c_ll, c_void, c_ll, c_void, c_float, c_int, c_int, c_void, c_void, c_void, c_void, c_void]),
+    "pace_gemm_fp8_workspace_size": (c_size, [c_int, c_int, c_int, c_int]),
+    "pace_gemm_fp8": (c_int, [c_void, c_void, c_ll, c_void, c_void, c_void, c_void, c_void, c_void, c_int, c_int, c_int, c_int,
+                              c_void, c_size, c_void]),
 }
 
 EXPORTED = tuple(_PROTOS.keys())
@@ -709,3 +714,101 @@ def gemm_w4(x: torch.Tensor, w: torch.Tensor, scale: torch.Tensor, zero: Optiona
           _arg(out, _BF16, (M, cols), gpu, "out"), M, N, K, K // groups, epilogue,
           *_scratch(workspace, gpu))
     return out
+
+
+# ---------------------------------------------------------------- a layer in 8 bits
+def _matrix_arg(t: torch.Tensor, dtype, shape: tuple, device: int, name: str):
+    """Address and row stride of a matrix whose rows are contiguous and may lie further apart."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or (shape[1] > 1 and t.stride(1) != 1):
+        raise PaceError(f"{name} must be a {dtype} matrix {list(shape)} of contiguous rows on GPU {device}, not {t.dtype} "
+                        f"{list(t.shape)} (strides {t.stride()}) on {t.device}")
+    return t.data_ptr(), (t.stride(0) if shape[0] > 1 else shape[1])
+
+
+def quantize_fp8(x: torch.Tensor, rows: int = 1, out: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
+    """x bf16 [M, K] (rows of any stride) to e4m3 codes [M, K] with a scale for each 128 neighbouring values of a row (rows=1:
+    scale fp32 [ceil(K / 128), M], what gemm_fp8 takes for x) or for each 128 x 128 (rows=128: [ceil(M / 128), ceil(K / 128)],
+    what it takes for w).  Returns (codes, scale)."""
+    gpu = _gpu_of(x)
+    if x.dim() != 2:
+        raise PaceError("x must be 2-D")
+    M, K = x.shape
+    kb = (K + 127) // 128
+    shape = (kb, M) if rows == 1 else ((M + 127) // 128, kb)
+    if out is None:
+        out = torch.empty((M, K), dtype=_E4M3, device=x.device)
+    if scale is None:
+        scale = torch.empty(shape, dtype=_F32, device=x.device)
+    xp, xs = _matrix_arg(x, _BF16, (M, K), gpu, "x")
+    _call("pace_quantize_fp8", gpu, xp, xs, M, K, rows, _arg(out, _E4M3, (M, K), gpu, "out"),
+          _arg(scale, _F32, shape, gpu, "scale"))
+    return out, scale
+
+
+def rmsnorm(x: torch.Tensor, gamma: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6, bits: int = 16,
+            out: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None):
+    """RMS norm of x bf16 [M, K], or of x + residual, times gamma fp32 [K]; x and residual may have rows of any stride.
+    Returns (y, scale, sum): y bf16 and scale None (bits=16), or e4m3 codes and their scales fp32 [ceil(K / 128), M]
+    (bits=8); sum bf16 = x + residual, None without a residual.  sum_out may be the residual itself."""
+    gpu = _gpu_of(x)
+    if x.dim() != 2:
+        raise PaceError("x must be 2-D")
+    if bits != 8 and bits != 16:
+        raise PaceError(f"bits={bits} is not 8 or 16")
+    M, K = x.shape
+    kb = (K + 127) // 128
+    xp, xs = _matrix_arg(x, _BF16, (M, K), gpu, "x")
+    rp, rs = None, 0
+    if residual is None:
+        sum_out = None
+    else:
+        rp, rs = _matrix_arg(residual, _BF16, (M, K), gpu, "residual")
+        if sum_out is None:
+            sum_out = torch.empty((M, K), dtype=_BF16, device=x.device)
+    kind = _E4M3 if bits == 8 else _BF16
+    if out is None:
+        out = torch.empty((M, K), dtype=kind, device=x.device)
+    y = _arg(out, kind, (M, K), gpu, "out")
+    if bits == 16:
+        scale = None
+    elif scale is None:
+        scale = torch.empty((kb, M), dtype=_F32, device=x.device)
+    _call("pace_rmsnorm", gpu, xp, xs, rp, rs, _arg(gamma, _F32, (K,), gpu, "gamma"), eps, M, K,
+          _arg(sum_out, _BF16, (M, K), gpu, "sum_out"), y if bits == 16 else None, y if bits == 8 else None,
+          _arg(scale, _F32, (kb, M), gpu, "scale"))
+    return out, scale, sum_out
+
+
+def gemm_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
+             residual: Optional[torch.Tensor] = None, epilogue: int = 0, bits: int = 16, out: Optional[torch.Tensor] = None,
+             out_scale: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """C = x W^T of e4m3 codes x [M, K] with x_scale fp32 [ceil(K / 128), M] (rows of any stride: a slice of rows is x[a:b],
+    x_scale[:, a:b]) and w [N, K] with w_scale fp32 [ceil(N / 128), ceil(K / 128)]; bias, residual and epilogue as in
+    gemm_bf16.  Returns (C, None), or with bits=8 and SwiGLU (codes [M, N / 2], their scales [ceil(N / 256), M]), ready for
+    the next product."""
+    gpu = _gpu_of(x)
+    if x.dim() != 2 or w.dim() != 2:
+        raise PaceError("x and w must be 2-D")
+    if bits != 8 and bits != 16:
+        raise PaceError(f"bits={bits} is not 8 or 16")
+    M, K = x.shape
+    N = w.shape[0]
+    kb = (K + 127) // 128
+    cols = N // 2 if epilogue == 2 else N
+    kind = _E4M3 if bits == 8 else _BF16
+    xsp, xss = _matrix_arg(x_scale, _F32, (kb, M), gpu, "x_scale")
+    if out is None:
+        out = torch.empty((M, cols), dtype=kind, device=x.device)
+    if bits == 16:
+        out_scale = None
+    elif out_scale is None:
+        out_scale = torch.empty(((cols + 127) // 128, M), dtype=_F32, device=x.device)
+    if workspace is None:
+        need = (_lib or lib()).pace_gemm_fp8_workspace_size(M, N, K, bits)
+        if need:
+            workspace = torch.empty(need, dtype=_U8, device=x.device)
+    _call("pace_gemm_fp8", gpu, _arg(x, _E4M3, (M, K), gpu, "x"), xsp, xss, _arg(w, _E4M3, (N, K), gpu, "w"),
+          _arg(w_scale, _F32, ((N + 127) // 128, kb), gpu, "w_scale"), _arg(bias, _F32, (N,), gpu, "bias"),
+          _arg(residual, _BF16, (M, cols), gpu, "residual"), _arg(out, kind, (M, cols), gpu, "out"),
+          _arg(out_scale, _F32, ((cols + 127) // 128, M), gpu, "out_scale"), M, N, K, epilogue, *_scratch(workspace, gpu))
+    return out, out_scale

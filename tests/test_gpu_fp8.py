@@ -1,0 +1,261 @@
+"""The 8-bit operators of a layer against the float64 oracle.  A rounding is off by at most half a step (bf16: 2^-8 of the value,
+e4m3: oracle.fp8.half_step); what 32-bit arithmetic adds comes with the oracle's results."""
+import numpy as np
+import pytest
+
+from oracle import fp8 as o8
+from paper_2608_27206_amd import workloads as wl
+from tests.gpu_util import dev_bf16, dev_f32, host, say
+from tests.test_gpu_cache import f64
+
+pytestmark = pytest.mark.gpu
+
+
+def bits_of(x):
+    return wl.f32_to_bf16_bits(np.asarray(x, np.float32))
+
+
+def rows_of(rs, M, K):
+    """Rows with an outlying channel in a hundred, as bf16 bits."""
+    return bits_of(rs.standard_normal((M, K)) * (1 + 9 * (rs.random(K) < 0.01)))
+
+
+def wide(bits, stride):
+    """A device matrix [M, K] whose rows lie `stride` apart, NaN between them."""
+    import torch
+    M, K = bits.shape
+    t = torch.full((M, stride), float("nan"), dtype=torch.bfloat16, device="cuda")
+    t[:, :K] = dev_bf16(bits)
+    return t[:, :K]
+
+
+def code_values(q):
+    import torch
+    return q.to(torch.float32).cpu().numpy().astype(np.float64)
+
+
+def make_codes(rs, M, K, rows):
+    """Random codes with positive scales: (device codes, device scales, values, scales)."""
+    import torch
+    x = rs.standard_normal((M, K)).astype(np.float32) * 40
+    q = torch.from_numpy(x).cuda().to(torch.float8_e4m3fn)
+    shape = (o8.blocks(K), M) if rows == 1 else (o8.blocks(M), o8.blocks(K))
+    s = (0.02 * np.exp(rs.uniform(-2, 2, shape)) / (1 if rows == 1 else np.sqrt(K))).astype(np.float32)
+    return q, dev_f32(s), code_values(q), s.astype(np.float64)
+
+
+# ---------------------------------------------------------------- quantisation
+@pytest.mark.parametrize("rows", [1, 128])
+@pytest.mark.parametrize("M,K,pad", [(1, 16, 0), (1, 3584, 0), (3, 128, 8), (5, 144, 0), (127, 112, 24), (128, 256, 0), (129, 272, 8), (300, 1280, 0),
+                                     (17, 3424, 16), (2, 20000, 0)])
+def test_quantize(M, K, pad, rows):
+    import torch
+    from paper_2608_27206_amd import pace
+    rs = np.random.default_rng(M * 7 + K + rows)
+    x = rows_of(rs, M, K)
+    say(f"quantize M={M} K={K} rows={rows}")
+    q, s = pace.quantize_fp8(wide(x, K + pad) if pad else dev_bf16(x), rows=rows)
+    torch.cuda.synchronize()
+    X, S = wl.bf16_bits_to_f64(x), host(s).astype(np.float64)
+    ref = o8.scales(X, rows)
+    assert S.shape == ref.shape and np.all(np.abs(S - ref) <= 2.0 ** -23 * ref)
+    assert o8.codes_ok(code_values(q), X, S, rows, 0.0).all()
+
+
+@pytest.mark.parametrize("rows", [1, 128])
+def test_quantize_values_that_are_not_finite_zeros_and_extremes(rows):
+    import torch
+    from paper_2608_27206_amd import pace
+    rs = np.random.default_rng(5)
+    x = rs.standard_normal((260, 400)).astype(np.float32)
+    x[0, 3], x[0, 200], x[1, 7], x[140, 399] = np.nan, np.inf, -np.inf, np.nan
+    x[2, :128] = 0
+    x[3, 128:256] = np.nan                       # a block of a row without a finite value
+    x[4, :128] = -0.0
+    x[128:256, :128] = 0                         # a block of weights
+    x[5, 256:384] = 3.3e38                       # near the largest bf16
+    x[6, 256:384] *= np.float32(1e-38)
+    x[256:, :] *= np.float32(1e-39)              # bf16's subnormals: under the least scale
+    b = bits_of(x)
+    q, s = pace.quantize_fp8(dev_bf16(b), rows=rows)
+    torch.cuda.synchronize()
+    X, S = wl.bf16_bits_to_f64(b), host(s).astype(np.float64)
+    ref = o8.scales(X, rows)
+    assert np.all(np.abs(S - ref) <= 2.0 ** -23 * ref)
+    got = code_values(q)
+    assert o8.codes_ok(got, X, S, rows, 0.0).all()
+    assert np.isnan(got[0, 3]) and np.isnan(got[0, 200]) and np.isnan(got[1, 7]) and np.isnan(got[3, 128:256]).all()
+    assert np.all(got[2, :128] == 0)
+
+
+# ---------------------------------------------------------------- norm
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("M,K,residual,pad", [(1, 16, True, 0), (1, 3584, True, 0), (2, 144, False, 0), (4, 512, True, 8), (5, 528, True, 0), (7, 1024, False, 16), (33, 1040, True, 0),
+                                              (131, 1280, True, 0), (3, 4096, True, 0), (3, 4112, True, 8), (2, 16384, False, 0), (2, 16400, True, 0),
+                                              (1, 65536, True, 0)])
+def test_rmsnorm(M, K, residual, pad, bits):
+    import torch
+    from paper_2608_27206_amd import pace
+    rs = np.random.default_rng(M + 3 * K + bits)
+    x, r = rows_of(rs, M, K), rows_of(rs, M, K)
+    g = (1 + 0.1 * rs.standard_normal(K)).astype(np.float32)
+    place = (lambda b: wide(b, K + pad)) if pad else dev_bf16
+    say(f"rmsnorm M={M} K={K} residual={residual} bits={bits}")
+    y, s, h = pace.rmsnorm(place(x), dev_f32(g), place(r) if residual else None, eps=1e-5, bits=bits)
+    torch.cuda.synchronize()
+    H, Y, tol = o8.norm(wl.bf16_bits_to_f64(x), wl.bf16_bits_to_f64(r) if residual else None, g.astype(np.float64), float(np.float32(1e-5)))
+    check_norm(y, s, h, H, Y, tol, residual, bits)
+
+
+def check_norm(y, s, h, H, Y, tol, residual, bits):
+    if residual:
+        assert np.all(np.abs(f64(h) - H) <= (2.0 ** -8 + 2.0 ** -24) * np.abs(H))
+    else:
+        assert h is None
+    if bits == 16:
+        assert s is None and np.all(np.abs(f64(y) - Y) <= 2.0 ** -8 * (np.abs(Y) + tol) + tol)
+        return
+    S, ref = host(s).astype(np.float64), o8.scales(Y, 1)
+    assert np.all(np.abs(S - ref) <= o8.scales(tol, 1) + 2.0 ** -23 * ref)
+    assert o8.codes_ok(code_values(y), Y, S, 1, tol).all()
+
+
+@pytest.mark.parametrize("M,K", [(5, 272), (3, 5008)])
+def test_rmsnorm_in_place(M, K):
+    """The sum over the residual's memory, the output over x's."""
+    import torch
+    from paper_2608_27206_amd import pace
+    rs = np.random.default_rng(K)
+    x, r, g = rows_of(rs, M, K), rows_of(rs, M, K), np.ones(K, np.float32)
+    dx, dr = dev_bf16(x), dev_bf16(r)
+    y, s, h = pace.rmsnorm(dx, dev_f32(g), dr, out=dx, sum_out=dr)
+    torch.cuda.synchronize()
+    assert y.data_ptr() == dx.data_ptr() and h.data_ptr() == dr.data_ptr()
+    H, Y, tol = o8.norm(wl.bf16_bits_to_f64(x), wl.bf16_bits_to_f64(r), g.astype(np.float64), float(np.float32(1e-6)))
+    check_norm(y, s, h, H, Y, tol, True, 16)
+
+
+def test_rmsnorm_of_zeros_and_of_values_that_are_not_finite():
+    import torch
+    from paper_2608_27206_amd import pace
+    rs = np.random.default_rng(9)
+    x = rs.standard_normal((5, 400)).astype(np.float32)
+    x[1] = 0
+    x[2, 5], x[3, 390] = np.nan, np.inf
+    b = bits_of(x)
+    for bits in (8, 16):
+        y, s, _ = pace.rmsnorm(dev_bf16(b), dev_f32(np.ones(400)), bits=bits)
+        torch.cuda.synchronize()
+        got = code_values(y)
+        assert np.all(got[1] == 0) and np.isnan(got[2]).all()
+        assert np.isnan(got[3, 390]) and np.all(np.delete(got[3], 390) == 0)       # x / infinity
+        keep = [0, 4]
+        X = wl.bf16_bits_to_f64(b)[keep]
+        H, Y, tol = o8.norm(X, None, np.ones(400), float(np.float32(1e-6)))
+        check_norm(y[keep], None if s is None else s[:, keep], None, H, Y, tol, False, bits)
+
+
+# ---------------------------------------------------------------- product
+SHAPES = [(1, 1, 16), (1, 64, 128), (2, 33, 144), (1, 4608, 3584), (8, 256, 272), (13, 1000, 1280), (16, 130, 4096), (17, 514, 400), (48, 384, 2064), (64, 128, 128),
+          (65, 1026, 640), (129, 257, 528), (200, 640, 3424), (257, 300, 256), (300, 2050, 1008), (1183, 512, 384)]
+
+
+def run_product(rs, M, N, K, epilogue, bits, workspace_extra=None):
+    import torch
+    from paper_2608_27206_amd import pace
+    x, xs, X, XS = make_codes(rs, M, K, 1)
+    w, ws, W, WS = make_codes(rs, N, K, 128)
+    bias = rs.standard_normal(N).astype(np.float32) if epilogue != 1 else None
+    res = bits_of(rs.standard_normal((M, N))) if epilogue == 1 else None
+    say(f"gemm_fp8 M={M} N={N} K={K} epilogue={epilogue} bits={bits}")
+    y, s = pace.gemm_fp8(x, xs, w, ws, None if bias is None else dev_f32(bias), None if res is None else dev_bf16(res), epilogue, bits)
+    torch.cuda.synchronize()
+    ref, tol = o8.product(X, XS, W, WS, bias, None if res is None else wl.bf16_bits_to_f64(res), epilogue)
+    check_product(y, s, ref, tol, bits)
+    return y, s
+
+
+def check_product(y, s, ref, tol, bits):
+    if bits == 16:
+        assert s is None and np.all(np.abs(f64(y) - ref) <= 2.0 ** -8 * (np.abs(ref) + tol) + tol)
+        return
+    S, want = host(s).astype(np.float64), o8.scales(ref, 1)
+    assert S.shape == want.shape and np.all(np.abs(S - want) <= o8.scales(tol, 1) + 2.0 ** -23 * want)
+    assert o8.codes_ok(code_values(y), ref, S, 1, tol).all()
+
+
+@pytest.mark.parametrize("epilogue", [0, 1])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_gemm_fp8(M, N, K, epilogue):
+    run_product(np.random.default_rng(M + N + K + epilogue), M, N, K, epilogue, 16)
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_gemm_fp8_swiglu(M, N, K, bits):
+    N += N % 2 if bits == 16 else -N % 32
+    run_product(np.random.default_rng(M + N + K + bits), M, N, K, 2, bits)
+
+
+@pytest.mark.parametrize("M", [3, 40, 300])
+def test_rows_of_a_larger_batch(M):
+    """A slice of rows: the codes x[a:b] and the scales x_scale[:, a:b], whose blocks lie the whole batch apart."""
+    import torch
+    from paper_2608_27206_amd import pace
+    rs = np.random.default_rng(M)
+    N, K, a = 260, 400, 5
+    x, xs, X, XS = make_codes(rs, M + 9, K, 1)
+    w, ws, W, WS = make_codes(rs, N, K, 128)
+    y, _ = pace.gemm_fp8(x[a:a + M], xs[:, a:a + M], w, ws)
+    torch.cuda.synchronize()
+    ref, tol = o8.product(X[a:a + M], XS[:, a:a + M], W, WS)
+    check_product(y, None, ref, tol, 16)
+
+
+@pytest.mark.parametrize("M,N", [(1, 70), (12, 300), (50, 520), (300, 260), (600, 520)])
+def test_nan_stays_in_its_row_and_column(M, N):
+    import torch
+    from paper_2608_27206_amd import pace
+    rs = np.random.default_rng(M + N)
+    K = 656
+    x, xs, X, XS = make_codes(rs, M, K, 1)
+    w, ws, W, WS = make_codes(rs, N, K, 128)
+    ref, tol = o8.product(X, XS, W, WS)
+    m, n = M // 2, N - 1
+    x.view(torch.uint8)[m, K - 1] = 0x7F
+    w.view(torch.uint8)[n, 130] = 0xFF
+    y, _ = pace.gemm_fp8(x, xs, w, ws)
+    torch.cuda.synchronize()
+    got = f64(y)
+    assert np.isnan(got[m]).all() and np.isnan(got[:, n]).all()
+    keep = np.ix_([i for i in range(M) if i != m], [j for j in range(N) if j != n])
+    assert np.all(np.abs(got[keep] - ref[keep]) <= 2.0 ** -8 * (np.abs(ref[keep]) + tol[keep]) + tol[keep])
+
+
+@pytest.mark.parametrize("M", [3, 40, 300])
+def test_output_over_the_residual(M):
+    import torch
+    from paper_2608_27206_amd import pace
+    rs = np.random.default_rng(M)
+    N, K = 392, 528
+    x, xs, X, XS = make_codes(rs, M, K, 1)
+    w, ws, W, WS = make_codes(rs, N, K, 128)
+    res = bits_of(rs.standard_normal((M, N)))
+    dr = dev_bf16(res)
+    y, _ = pace.gemm_fp8(x, xs, w, ws, residual=dr, epilogue=1, out=dr)
+    torch.cuda.synchronize()
+    ref, tol = o8.product(X, XS, W, WS, None, wl.bf16_bits_to_f64(res), 1)
+    check_product(y, None, ref, tol, 16)
+
+
+def test_no_rows():
+    import torch
+    from paper_2608_27206_amd import pace
+    z = torch.empty((0, 256), dtype=torch.bfloat16, device="cuda")
+    q, s = pace.quantize_fp8(z)
+    assert q.shape == (0, 256) and s.shape == (2, 0)
+    y, s2, h = pace.rmsnorm(z, torch.ones(256, device="cuda"), z, bits=8)
+    assert y.shape == (0, 256) and s2.shape == (2, 0) and h.shape == (0, 256)
+    w, ws = pace.quantize_fp8(torch.ones((64, 256), dtype=torch.bfloat16, device="cuda"), rows=128)
+    c, _ = pace.gemm_fp8(q, s, w, ws)
+    assert c.shape == (0, 64)
