@@ -25,7 +25,7 @@ def blocks(n: int) -> int:
     return -(-n // BLOCK)
 
 
-def spread(scale: np.ndarray, shape, rows: int) -> np.ndarray:
+def per_value(scale: np.ndarray, shape, rows: int) -> np.ndarray:
     """The scale of every value: scale [K blocks, M] for rows = 1, [row blocks, K blocks] for 128."""
     s = scale.T if rows == 1 else np.repeat(scale, rows, 0)
     return np.repeat(s, BLOCK, 1)[:shape[0], :shape[1]]
@@ -45,7 +45,7 @@ def scales(x: np.ndarray, rows: int) -> np.ndarray:
 def codes_ok(got: np.ndarray, y: np.ndarray, scale: np.ndarray, rows: int, tol) -> np.ndarray:
     """Which codes (as values) lie within half a step of y / scale, for the scales that came with them; y known to `tol`,
     and quantised through the scale's reciprocal in 32 bits (three roundings: 2^-22)."""
-    s = spread(scale, y.shape, rows)
+    s = per_value(scale, y.shape, rows)
     with np.errstate(invalid="ignore"):
         v, t = y / s, tol / s
         near = np.abs(got - v) <= half_step(np.abs(v) * (1 + 2.0 ** -22) + t) + t + 2.0 ** -22 * np.abs(v)
@@ -60,13 +60,26 @@ def norm(x: np.ndarray, residual, gamma: np.ndarray, eps: float):
     return h, y, (0.5 * 80 + 8) * 2.0 ** -24 * np.abs(y)
 
 
-def product(x, xs, w, ws, bias=None, residual=None, epilogue: int = 0):
-    """(C, tol) of code values x [M, K], w [N, K] with their scales.  A block's 128 products are exact and summed by the
-    matrix cores: at most 128 steps that each lose less than 2^-23 of the magnitudes' sum; blocks, their scales' product, up to 64
-    parts of K and bias or residual round once each (2^-24)."""
-    X, W = x * spread(xs, x.shape, 1), w * spread(ws, w.shape, BLOCK)
+def eight_max(x: np.ndarray) -> np.ndarray:
+    """The largest magnitude of each 8 neighbouring values of a row."""
+    return np.abs(x).reshape(x.shape[0], -1, 8).max(2)
+
+
+def product(x, xs, w, ws, bias=None, residual=None, epilogue: int = 0, wide: bool = True):
+    """(C, tol, spread) of code values x [M, K], w [N, K] with their scales.
+    tol bounds what the sums may be off.  Products of two codes are exact (8 bits).  wide: 128 steps of a block that each lose less
+    than 2^-23 of the magnitudes' sum.  Not wide: the matrix cores put the products of 8 neighbouring k's on a grid of 2^-13 of
+    the largest of them, so that each of the other 7 loses less than that; the eights are added in 32 bits as above.  Blocks, their
+    scales' product, up to 64 parts of K and bias or residual round once each (2^-24).
+    spread: the eights' part of tol as if they were off in signs of their own, the root of the sum of their squares (0 where wide)."""
+    X, W = x * per_value(xs, x.shape, 1), w * per_value(ws, w.shape, BLOCK)
     y = X @ W.T
     t = (128 * 2.0 ** -23 + (blocks(x.shape[1]) + 68) * 2.0 ** -24) * (np.abs(X) @ np.abs(W).T)
+    off = np.zeros_like(y)
+    if not wide:
+        a, b = eight_max(X) * 7 * 2.0 ** -13, eight_max(W)
+        t = t + a @ b.T
+        off = np.sqrt((a * a) @ (b * b).T)
     if bias is not None:
         y = y + bias
         t = t + 2.0 ** -24 * np.abs(y)
@@ -78,5 +91,6 @@ def product(x, xs, w, ws, bias=None, residual=None, epilogue: int = 0):
         with np.errstate(over="ignore"):
             silu = g / (1 + np.exp(-g))
         # |silu'| <= 1.1; the sigmoid's own arithmetic is a few roundings
-        return silu * u, 1.1 * tg * np.abs(u) + np.abs(silu) * tu + 1.1 * tg * tu + 2.0 ** -20 * np.abs(silu * u)
-    return y, t
+        through = lambda a, b: 1.1 * a * np.abs(u) + np.abs(silu) * b + 1.1 * a * b   # noqa: E731
+        return silu * u, through(tg, tu) + 2.0 ** -20 * np.abs(silu * u), through(off[:, 0::2], off[:, 1::2])
+    return y, t, off

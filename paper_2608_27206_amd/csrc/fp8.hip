@@ -11,7 +11,11 @@ namespace pace {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kBlock = 128;                    // values that share a scale
 constexpr float kE4m3Max = 448.f;
@@ -32,7 +36,16 @@ __device__ __forceinline__ void unpack8(uint4 u, float (&x)[8]) {
     x[2 * i + 1] = hi_bf16(v[i]);
   }
 }
-__device__ __forceinline__ float silu(float x) { return x / (1.f + expf(-x)); }
+// x / (1 + e^-x).  The exponent x log2(e) is taken to twice 24 bits (its rounding alone would cost 2^-18 at x = -20), the
+// exponential and reciprocal units round once each: within 2^-21 of the value, and half the time of expf and a division.
+__device__ __forceinline__ float silu(float x) {
+  constexpr float kL = 1.44269504f, kLo = 1.92596303e-8f, kLn2 = 0.693147181f;   // log2(e) = kL + kLo
+  const float c = __builtin_amdgcn_fmed3f(x, -200.f, 200.f);
+  const float t = c * -kL, lo = fmaf(c, -kL, -t) - c * kLo;
+  float e = __builtin_amdgcn_exp2f(t);
+  e = fmaf(e, lo * kLn2, e);
+  return x * __builtin_amdgcn_rcpf(1.f + e);
+}
 
 // What a value adds to its block's maximum: its magnitude, 0 where it is not finite.
 __device__ __forceinline__ float magnitude(float x) { return fabsf(x) <= FLT_MAX ? fabsf(x) : 0.f; }
@@ -197,101 +210,743 @@ struct Fp8Params {
   const uint16_t* R;
   void* C;
   float* cs;                   // scales of 8-bit outputs
-  float* part;                 // [splits, M, N]
-  long long xs_stride;
-  int M, N, K, kb, mode, splits;
+  float* part;                 // [splits, M, N] sums for fp8_join, or null: the kernel finishes the output
+  long long xs_stride, cs_stride;
+  int M, N, K, kb, mode, splits, tiles_m, tiles_n;
+  int width;                   // elements per access to C and R: 8, 4, 2 or 1 as their alignment allows
 };
+
+enum { kEpiBias = 0, kEpiResidual = 1, kEpiSwiglu = 2 };
 
 __device__ __forceinline__ f32x4 mfma128(i32x8 a, i32x8 b) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
 }
+__device__ __forceinline__ f32x4 mfma32(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// One output value of 16 bits (or a SwiGLU pair's) from its finished sum.
-__device__ __forceinline__ void fp8_store(const Fp8Params& p, int m, int n, float y, float y_pair) {
-  const long long at = static_cast<long long>(m) * (p.mode == 2 ? p.N / 2 : p.N) + (p.mode == 2 ? n / 2 : n);
-  if (p.mode == 1) y += bf16_f32(p.R[at]);
-  if (p.mode == 2) y = silu(y) * y_pair;
-  static_cast<uint16_t*>(p.C)[at] = f32_bf16(y);
+// A lane's 32 codes of a row and block: as they are, or as bf16 values, exactly.
+struct Codes {
+  i32x8 v;
+};
+struct Values {
+  bf16x8 v[4];
+};
+__device__ __forceinline__ bf16x8 widen8(uint32_t a, uint32_t b) {
+  const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true);
+  const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false), s = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true);
+  return bf16x8{p.x, p.y, q.x, q.y, r.x, r.y, s.x, s.y};
+}
+__device__ __forceinline__ Codes lift(i32x8 u, Codes*) { return {u}; }
+__device__ __forceinline__ Values lift(i32x8 u, Values*) {
+  Values o;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) o.v[q] = widen8(static_cast<uint32_t>(u[2 * q]), static_cast<uint32_t>(u[2 * q + 1]));
+  return o;
+}
+// The sums of a block's 128 products, of N rows of x with columns of W.
+template <int N>
+__device__ __forceinline__ void dot_block(const Codes& w, const Codes (&x)[N], f32x4 (&d)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) d[i] = mfma128(w.v, x[i].v);
+}
+template <int N>
+__device__ __forceinline__ void dot_block(const Values& w, const Values (&x)[N], f32x4 (&d)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) d[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int i = 0; i < N; ++i) d[i] = mfma32(w.v[q], x[i].v[q], d[i]);
 }
 
-// 64 x 64 of C by four waves, operands straight from memory.  W is the products' A operand: a lane then holds four
-// neighbouring columns n of one row m, whose block of 128 has one scale for the lane.
-__global__ __launch_bounds__(256) void gemm_fp8_direct(const Fp8Params p) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-  const int tiles = (p.N + 63) / 64, tm = blockIdx.x / tiles;
-  const int n0 = (blockIdx.x - tm * tiles) * 64 + (w & 1) * 32, m0 = tm * 64 + (w >> 1) * 32;
-  f32x4 acc[2][2] = {};
-  const auto load = [&](const uint8_t* base, int row, int rows, int k) {
-    uint4 u[2] = {};
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (row < rows && k + 64 * h < p.K) u[h] = *reinterpret_cast<const uint4*>(base + static_cast<long long>(row) * p.K + k + 64 * h);
-    return i32x8{static_cast<int>(u[0].x), static_cast<int>(u[0].y), static_cast<int>(u[0].z), static_cast<int>(u[0].w),
-                 static_cast<int>(u[1].x), static_cast<int>(u[1].y), static_cast<int>(u[1].z), static_cast<int>(u[1].w)};
+typedef __attribute__((address_space(3))) const char lds_char;
+constexpr unsigned kOut = 0x7FFFFFF0u;   // an offset past every range: reads as zeros
+
+__device__ __forceinline__ i32x4 rsrc_of(const void* base, unsigned bytes) {
+  const unsigned long long a = reinterpret_cast<unsigned long long>(base);
+  i32x4 r;
+  r.x = __builtin_amdgcn_readfirstlane(static_cast<int>(a & 0xffffffffull));
+  r.y = __builtin_amdgcn_readfirstlane(static_cast<int>((a >> 32) & 0xffffull));   // stride 0
+  r.z = __builtin_amdgcn_readfirstlane(static_cast<int>(bytes));
+  r.w = 0x00020000;
+  return r;
+}
+// 64 lanes x 16 (4) bytes from the buffer to lds .. lds + 1023 (255); untracked by the compiler, awaited with wait_loads.
+__device__ __forceinline__ void dma16(i32x4 r, unsigned lds, unsigned voff) {
+  const unsigned m0 = __builtin_amdgcn_readfirstlane(lds);
+  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(r), "{m0}"(m0) : "memory");
+}
+__device__ __forceinline__ void dma4(i32x4 r, unsigned lds, unsigned voff) {
+  const unsigned m0 = __builtin_amdgcn_readfirstlane(lds);
+  asm volatile("s_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(voff), "s"(r), "{m0}"(m0) : "memory");
+}
+// all but the last N of the wave's loads have arrived, and its LDS reads have returned
+template <int N>
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
+
+template <int W> struct Unit;
+template <> struct Unit<8> { typedef uint4 type; };
+template <> struct Unit<4> { typedef uint2 type; };
+template <> struct Unit<2> { typedef uint32_t type; };
+template <> struct Unit<1> { typedef uint16_t type; };
+template <typename F>
+__device__ __forceinline__ void with_width(int width, F f) {
+  if (width == 8) f(std::integral_constant<int, 8>{});
+  else if (width == 4) f(std::integral_constant<int, 4>{});
+  else if (width == 2) f(std::integral_constant<int, 2>{});
+  else f(std::integral_constant<int, 1>{});
+}
+
+template <typename T, int MI, int NI, int WM, int WN, int ST, int G>
+__global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Params p) {
+  constexpr int BM = 16 * MI * WM, BN = 16 * NI * WN, NW = WM * WN, TH = 64 * NW * G;
+  constexpr int kScales = BM < 64 ? 64 : BM;                     // floats of a stage
+  constexpr int kStage = (BM + BN) * kBlock;                     // bytes of a stage
+  constexpr int kScaleSlots = ST + 1;
+  constexpr int MP = MI < 2 ? 1 : 2, Q = MI / MP;                // tiles of a step, steps of a stage
+  // DMAs of a wave and stage, 8 rows each: the first part (w's rows, those of x that the first half of the steps reads, and the
+  // scales) is asked for in mid-stage, the second at the end
+  constexpr bool kTwo = Q % 4 == 0, kWide = sizeof(T) != sizeof(Codes);
+  constexpr int kWD = BN / 8 / NW, kXD = BM / 8 / NW, kLate = kTwo ? kXD / 2 : 0, kEarly = kWD + kXD - kLate + 1;
+  static_assert(kWD * 8 * NW == BN && kXD * 8 * NW == BM && (!kTwo || kXD % 2 == 0) && NW % 2 == 0 && (Q == 1 || Q % 2 == 0) && kBlock % (16 * NI) == 0, "tile");
+  constexpr int kRing = ST * G * kStage, kTile = BM * BN * 2, kJoin = (G - 1) * BM * BN * 4, kBoth = kTile > kJoin ? kTile : kJoin;
+  __shared__ __align__(16) char lds[kRing > kBoth ? kRing : kBoth];
+  __shared__ float scales[kScaleSlots * G][kScales];
+  __shared__ float top_of[WN][BM];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), w = wave % NW, kg = wave / NW;
+  const int r = lane & 15, g = lane >> 4;
+  const int wm = (w / WN) * 16 * MI, wn = (w % WN) * 16 * NI;
+  // XCD-contiguous order; groups of eight row tiles column by column, so that the workgroups that run together on an XCD
+  // share a few rows of x and a few of w in its L2
+  const int per = p.tiles_m * p.tiles_n;
+  const int lb = remap_block_id(blockIdx.x, gridDim.x);
+  const int split = lb / per, tl = lb - split * per;
+  const int gsz = 8 * p.tiles_n, grp = tl / gsz, in = tl - grp * gsz;
+  const int gm = min(8, p.tiles_m - 8 * grp);
+  const int tn = in / gm, tm = 8 * grp + (in - tn * gm);
+  const int bm = tm * BM, bn = tn * BN;
+  const int t0 = static_cast<int>(static_cast<long long>(p.kb) * split / p.splits);
+  const int t1 = static_cast<int>(static_cast<long long>(p.kb) * (split + 1) / p.splits);
+  const int nk = (t1 - t0 + G - 1) / G;                // stages; a group of waves takes block t0 + G * stage + its number
+  const auto block_of = [&](int stage) { return t0 + G * stage + kg; };
+  const int rows_m = min(BM, p.M - bm), rows_n = min(BN, p.N - bn);
+  const i32x4 ra = rsrc_of(p.x + static_cast<long long>(bm) * p.K, static_cast<unsigned>(rows_m) * p.K);
+  const i32x4 rb = rsrc_of(p.w + static_cast<long long>(bn) * p.K, static_cast<unsigned>(rows_n) * p.K);
+  const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<unsigned long long>((lds_char*)(const void*)lds));
+
+  // A DMA brings 8 rows; chunk c (16 bytes) of row r lies in slot c ^ ((r >> 1) & 7)
+  const int r8 = lane >> 3, kc = ((lane & 7) ^ (4 * (w & 1) + (r8 >> 1))) * 16;
+  const unsigned off0 = static_cast<unsigned>(r8) * p.K + kc;
+  const int k_end = min(p.K, t1 * kBlock);
+  const auto rows8 = [&](const i32x4& rs, int row, int lds_row, int t, int buf, bool in_k) __attribute__((always_inline)) {
+    // rows past the end lie past the buffer's range
+    dma16(rs, lds0 + (buf * G + kg) * kStage + lds_row * kBlock, in_k ? off0 + static_cast<unsigned>(row) * p.K + t * kBlock : kOut);
   };
-  for (int b = 0; b < p.kb; ++b) {
-    i32x8 wf[2], xf[2];
-    float s[2];
-    const float sw = n0 < p.N ? p.ws[static_cast<long long>(n0 / kBlock) * p.kb + b] : 0.f;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int m = m0 + 16 * i + r;
-      wf[i] = load(p.w, n0 + 16 * i + r, p.N, b * kBlock + 16 * g);
-      xf[i] = load(p.x, m, p.M, b * kBlock + 16 * g);
-      s[i] = m < p.M ? p.xs[b * p.xs_stride + m] * sw : 0.f;
+  // x's rows of 8 that wave w brings as its u-th: the first half of them is what the first half of the steps reads
+  const auto x_row = [&](int u) __attribute__((always_inline)) {
+    if constexpr (kTwo) {
+      const int i = w + NW * (u % (kXD / 2));            // of BM / 16; a half of a wave's rows are MI of them
+      return i / MI * (16 * MI) + u / (kXD / 2) * (8 * MI) + i % MI * 8;
+    } else {
+      return 8 * (w + NW * u);
     }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const f32x4 d = mfma128(wf[j], xf[i]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(s[i], d[e], acc[i][j][e]);
-      }
-  }
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int m = m0 + 16 * i + r;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int n = n0 + 16 * j + 4 * g + e;
-        if (m >= p.M || n >= p.N) continue;
-        if (p.part) p.part[static_cast<long long>(m) * p.N + n] = acc[i][j][e];
-        else if (p.mode != 2) fp8_store(p, m, n, acc[i][j][e] + (p.bias ? p.bias[n] : 0.f), 0.f);
-        else if (e % 2 == 0)
-          fp8_store(p, m, n, acc[i][j][e] + (p.bias ? p.bias[n] : 0.f), acc[i][j][(e + 1) & 3] + (p.bias ? p.bias[n + 1] : 0.f));
-      }
+  };
+  // DMA u of the stage's first part, and of its second
+  const auto load_early = [&](int u, int t, int buf, int slot) __attribute__((always_inline)) {
+    const bool in_k = t * kBlock + kc < k_end;             // past the end of K, or of the part: zeros
+    if (u < kWD) {
+      rows8(rb, 8 * (w + NW * u), BM + 8 * (w + NW * u), t, buf, in_k);
+    } else if (u < kEarly - 1) {
+      rows8(ra, x_row(u - kWD), x_row(u - kWD), t, buf, in_k);
+    } else {
+      const int s = w % (kScales / 64) * 64;            // more waves than pieces: the same again
+      dma4(rsrc_of(p.xs + t * p.xs_stride + bm, static_cast<unsigned>(rows_m) * 4),
+           static_cast<unsigned>(reinterpret_cast<unsigned long long>((lds_char*)(const void*)&scales[0][0])) + ((slot * G + kg) * kScales + s) * 4,
+           t < t1 ? static_cast<unsigned>(s + lane) * 4 : kOut);
     }
-}
+  };
+  const auto load_late = [&](int u, int t, int buf) __attribute__((always_inline)) {
+    rows8(ra, x_row(kXD - kLate + u), x_row(kXD - kLate + u), t, buf, t * kBlock + kc < k_end);
+  };
+  // fragments: a lane has chunks g and g + 4 of row r
+  const int at0 = r * kBlock + ((g ^ (r >> 1)) & 7) * 16, at1 = at0 ^ 64;
+  const auto frag = [&](int buf, int row) __attribute__((always_inline)) {
+    const char* st = lds + (buf * G + kg) * kStage + row * kBlock;
+    const i32x4 a = *reinterpret_cast<const i32x4*>(st + at0), b = *reinterpret_cast<const i32x4*>(st + at1);
+    return i32x8{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  };
+  const auto x_scale = [&](int slot, int i) __attribute__((always_inline)) { return scales[slot * G + kg][wm + 16 * i + r]; };
+  // w's scales: one for the wave and block, 64 blocks in a register's lanes
+  const int nb = min(bn + wn, p.N - 1) / kBlock;
+  float wscales = 0.f;
 
-// Adds the parts of a split K in their order and finishes the output.  With 8 bits a wave has the 256 columns of a block.
-__global__ __launch_bounds__(256) void fp8_join(const Fp8Params p) {
-  const int per = p.cs ? 4 : p.mode == 2 ? 2 : 1;
-  const int cols = (p.N + 256 * per - 1) / (256 * per);
-  const int m = blockIdx.x / cols, n = ((blockIdx.x - m * cols) * 256 + threadIdx.x) * per;
-  float y[4] = {};
+  f32x4 acc[MI][NI];
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    if (c >= per || n >= p.N) break;
-    for (int k = 0; k < p.splits; ++k) y[c] += p.part[(static_cast<long long>(k) * p.M + m) * p.N + n + c];
-    if (p.bias) y[c] += p.bias[n + c];
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  const auto scales_from = [&](int stage) __attribute__((always_inline)) {
+    const int b = block_of(stage + lane);
+    wscales = b < p.kb ? p.ws[static_cast<long long>(nb) * p.kb + b] : 0.f;
+    asm volatile("s_waitcnt vmcnt(0)" : "+v"(wscales));   // now, and not at every use for all loads in flight
+  };
+  scales_from(0);
+#pragma unroll
+  for (int s = 0; s < ST; ++s) {
+#pragma unroll
+    for (int u = 0; u < kEarly; ++u) load_early(u, block_of(s), s, s);
+#pragma unroll
+    for (int u = 0; u < kLate; ++u) load_late(u, block_of(s), s);
   }
-  if (!p.cs) {
-    if (n < p.N) fp8_store(p, m, n, y[0], y[1]);
+  wait_loads<(ST - 1) * (kEarly + kLate)>();
+  barrier();
+
+  T wf[NI];
+  i32x8 xr[2][MP];
+  float xsc[2][MP];
+#pragma unroll
+  for (int j = 0; j < NI; ++j) wf[j] = lift(frag(0, BM + wn + 16 * j), static_cast<T*>(nullptr));
+#pragma unroll
+  for (int i = 0; i < MP; ++i) {
+    xr[0][i] = frag(0, wm + 16 * i);
+    xsc[0][i] = x_scale(0, i);
+  }
+  int cur = 0, cs = 0;                                 // the stage's buffer and scales
+  // What a step has formed goes into acc in the next one, under its products.
+  f32x4 d[MP];
+  float ds[MP];
+#pragma unroll
+  for (int i = 0; i < MP; ++i) {
+    d[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    ds[i] = 0.f;
+  }
+  const auto add = [&](int q, int j) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < MP; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[q * MP + i][j][e] = fmaf(ds[i], d[i][e], acc[q * MP + i][j][e]);
+#pragma unroll
+    for (int i = 0; i < MP; ++i) asm volatile("" : "+v"(acc[q * MP + i][j]));   // here, not behind the stage's branches
+  };
+  // Stage k: its first fragments are in registers.  Before its last step a wave, which then holds the last fragments, meets
+  // the others; what is left of the stage's buffer takes stage k + ST, and the last products run under the first reads of
+  // stage k + 1.  With four steps they meet in mid-stage too: then every wave holds w's rows and has read half of x's.
+  for (int k = 0; k < nk; ++k) {
+    const int nxt = cur == ST - 1 ? 0 : cur + 1, ns = cs == kScaleSlots - 1 ? 0 : cs + 1, far = cs == 0 ? kScaleSlots - 1 : cs - 1;
+    const float sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wscales), k & 63));
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int slot = Q == 1 ? 0 : q & 1, next_slot = Q == 1 ? 0 : (q + 1) & 1;
+      T x[MP];
+      float s[MP];
+      const bool last = q == Q - 1;
+      if (kTwo && q == Q / 2 - 1) {
+        // this stage's second part has come; in flight are the stages after it
+        wait_loads<(ST - 1) * (kEarly + kLate)>();
+        barrier();
+      }
+      if (last) {
+        // the next stage's first part has come
+        wait_loads<(ST - 2) * (kEarly + kLate) + (kTwo ? kLate + kEarly : 0)>();
+        barrier();
+      }
+#pragma unroll
+      for (int i = 0; i < MP; ++i) {
+        x[i] = lift(xr[slot][i], static_cast<T*>(nullptr));
+        s[i] = xsc[slot][i] * sw;
+      }
+      // past the end of K the reads bring anything, and nothing uses it
+#pragma unroll
+      for (int i = 0; i < MP; ++i) {
+        xr[next_slot][i] = frag(last ? nxt : cur, wm + 16 * (last ? i : (q + 1) * MP + i));
+        xsc[next_slot][i] = x_scale(last ? ns : cs, last ? i : (q + 1) * MP + i);
+      }
+      i32x8 wr[2];
+      if (last && kWide) wr[0] = frag(nxt, BM + wn);
+#pragma unroll
+      for (int j = 0; j < NI; ++j) {
+        f32x4 c[MP];
+        dot_block(wf[j], x, c);
+        if (last && kWide && j + 1 < NI) wr[(j + 1) & 1] = frag(nxt, BM + wn + 16 * (j + 1));
+        if (j) add(q, j - 1);
+        else add(q ? q - 1 : Q - 1, NI - 1);
+        // what the barriers have freed is asked for a piece at a time, behind the step's reads and under its products
+        constexpr int kSlots = kTwo ? (Q / 2) * NI : NI, kFirst = kTwo ? Q / 2 - 1 : Q - 1;
+        const int at = (q - kFirst) * NI + j;
+        if (at >= 0 && at < kSlots) {
+#pragma unroll
+          for (int u = 0; u < kEarly; ++u)
+            if (u * kSlots / kEarly == at) load_early(u, block_of(k + ST), cur, far);
+        }
+        if (last) {
+#pragma unroll
+          for (int u = 0; u < kLate; ++u)
+            if (u * NI / kLate == j) load_late(u, block_of(k + ST), cur);
+        }
+        if (last) {
+          if constexpr (kWide) {
+            wf[j] = lift(wr[j & 1], static_cast<T*>(nullptr));
+#pragma unroll
+            for (int u = 0; u < 4; ++u) asm volatile("" : "+v"(wf[j].v[u]));   // here, under the products
+          } else {
+            wf[j] = lift(frag(nxt, BM + wn + 16 * j), static_cast<T*>(nullptr));
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < MP; ++i) {
+          d[i] = c[i];
+          ds[i] = s[i];
+        }
+        if constexpr (kWide) {
+#pragma unroll
+          for (int u = 0; u < 4 * MP; ++u) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+          }
+        } else {
+          __builtin_amdgcn_sched_group_barrier(0x008, MP, 0);          // this step's products first,
+          __builtin_amdgcn_sched_group_barrier(0x002, 4 * MP, 0);      // the sums of the one before under them
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if ((k & 63) == 63 && k + 1 < nk) scales_from(k + 1);
+    cur = nxt;
+    cs = ns;
+  }
+  add(Q - 1, NI - 1);
+  wait_loads<0>();                                     // those past the end: the epilogue uses the same LDS
+  if constexpr (G > 1) {
+    __syncthreads();
+    f32x4* from = reinterpret_cast<f32x4*>(lds) + w * (MI * NI * 64) + lane;   // each group's tile after the other's
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NI; ++j)
+        if (kg) from[(kg - 1) * (BM * BN / 4) + (i * NI + j) * 64] = acc[i][j];
+    __syncthreads();
+#pragma unroll
+    for (int o = 0; o < G - 1; ++o)
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+          if (!kg) acc[i][j] += from[o * (BM * BN / 4) + (i * NI + j) * 64];
+  }
+
+  // epilogue: element e of tile (i, j) is row wm + 16 i + r, column wn + 16 j + 4 g + e
+  if (p.part) {
+    if (kg) return;
+    float* part = p.part + static_cast<long long>(split) * p.M * p.N;
+    const bool whole = p.N % 4 == 0;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int m = bm + wm + 16 * i + r;
+#pragma unroll
+      for (int j = 0; j < NI; ++j) {
+        const int n = bn + wn + 16 * j + 4 * g;
+        if (m >= p.M || n >= p.N) continue;
+        float* to = part + static_cast<long long>(m) * p.N + n;
+        if (whole) *reinterpret_cast<f32x4*>(to) = acc[i][j];
+        else
+          for (int e = 0; e < 4; ++e)
+            if (n + e < p.N) to[e] = acc[i][j][e];
+      }
+    }
     return;
   }
+  if (p.bias) {
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int n = bn + wn + 16 * j + 4 * g;
+      f32x4 b;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) b[e] = n + e < p.N ? p.bias[n + e] : 0.f;
+#pragma unroll
+      for (int i = 0; i < MI; ++i) acc[i][j] += b;
+    }
+  }
+  __syncthreads();                                     // every wave has read its last stage
+  const int mode = p.mode;
+  if constexpr (BN == 256 && G == 1) {
+    if (p.cs) {
+      // SwiGLU to 8 bits: the tile's 128 outputs of a row are a block
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        float top = 0.f;
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+          acc[i][j][0] = silu(acc[i][j][0]) * acc[i][j][1];
+          acc[i][j][1] = silu(acc[i][j][2]) * acc[i][j][3];
+          top = fmaxf(top, fmaxf(magnitude(acc[i][j][0]), magnitude(acc[i][j][1])));
+        }
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        if (g == 0) top_of[w % WN][wm + 16 * i + r] = top;
+      }
+      __syncthreads();
+      const auto row_scale = [&](int row) {
+        float top = top_of[0][row];
+#pragma unroll
+        for (int c = 1; c < WN; ++c) top = fmaxf(top, top_of[c][row]);
+        return scale_of(top);
+      };
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        const int row = wm + 16 * i + r;
+        const float inv = 1.f / row_scale(row);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+          const int c = (wn + 16 * j + 4 * g) / 2;
+          *reinterpret_cast<uint16_t*>(lds + row * 128 + (((c >> 4) ^ (row & 7)) << 4) + (c & 15)) =
+              static_cast<uint16_t>(to_e4m3(acc[i][j][0], acc[i][j][1], 0.f, 0.f, inv));
+        }
+      }
+      __syncthreads();
+      const int cols = p.N / 2;
+      uint8_t* C = static_cast<uint8_t*>(p.C);
+      for (int c = tid; c < BM * 8; c += TH) {
+        const int row = c >> 3, ch = c & 7, m = bm + row, n = bn / 2 + 16 * ch;
+        if (m < p.M && n < cols)
+          *reinterpret_cast<uint4*>(C + static_cast<long long>(m) * cols + n) = *reinterpret_cast<const uint4*>(lds + row * 128 + ((ch ^ (row & 7)) << 4));
+      }
+      for (int row = tid; row < rows_m; row += TH) p.cs[bn / 256 * p.cs_stride + bm + row] = row_scale(row);
+      return;
+    }
+  }
+  // 16 bits: the tile goes through LDS, 16-byte chunk ch of row i in slot ch ^ (i mod the chunks of a row), so that rows leave
+  // in whole lines; a residual tile comes in the same way first
+  uint16_t* tile = reinterpret_cast<uint16_t*>(lds);
+  constexpr int kCh = BN / 8;
+  if (mode == kEpiResidual) {
+    with_width(p.width, [&](auto WC) __attribute__((always_inline)) {
+      constexpr int W = decltype(WC)::value, kUnits = BN / W;
+      typedef typename Unit<W>::type U;
+#pragma unroll 8
+      for (int c = tid; c < BM * kUnits; c += TH) {
+        const int row = c / kUnits, cl = c % kUnits * W;
+        U v{};
+        if (bm + row < p.M && bn + cl < p.N)
+          v = *reinterpret_cast<const U*>(p.R + static_cast<long long>(bm + row) * p.N + bn + cl);
+        *reinterpret_cast<U*>(&tile[row * BN + (((cl >> 3) ^ (row & (kCh - 1))) << 3) + (cl & 7)]) = v;
+      }
+    });
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    if (kg) break;
+    const int row = wm + 16 * i + r;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int cl = wn + 16 * j + 4 * g;
+      if (mode == kEpiSwiglu) {
+        const int cg = cl >> 1;
+        *reinterpret_cast<uint32_t*>(&tile[row * (BN / 2) + (((cg >> 3) ^ (row & (kCh / 2 - 1))) << 3) + (cg & 7)]) =
+            pack2(silu(acc[i][j][0]) * acc[i][j][1], silu(acc[i][j][2]) * acc[i][j][3]);
+      } else {
+        uint2* at = reinterpret_cast<uint2*>(&tile[row * BN + (((cl >> 3) ^ (row & (kCh - 1))) << 3) + (cl & 7)]);
+        f32x4 v = acc[i][j];
+        if (mode == kEpiResidual) {
+          const uint2 u = *at;
+          v += f32x4{lo_bf16(u.x), hi_bf16(u.x), lo_bf16(u.y), hi_bf16(u.y)};
+        }
+        *at = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+      }
+    }
+  }
+  __syncthreads();
+  const bool glu = mode == kEpiSwiglu;
+  const int cols = glu ? p.N / 2 : p.N, c0 = glu ? bn / 2 : bn;
+  const int cpr = glu ? kCh / 2 : kCh, cbits = __builtin_ctz(cpr);
+  uint16_t* C = static_cast<uint16_t*>(p.C);
+  with_width(p.width, [&](auto WC) __attribute__((always_inline)) {
+    constexpr int W = decltype(WC)::value, kLog = W == 8 ? 0 : W == 4 ? 1 : W == 2 ? 2 : 3;   // log2 of 8 / W
+    typedef typename Unit<W>::type U;
+    const int ubits = cbits + kLog;
+    for (int c = tid; c < BM << ubits; c += TH) {
+      const int row = c >> ubits, u = c & ((1 << ubits) - 1), ch = u >> kLog;
+      const int m = bm + row, n = c0 + u * W;
+      if (m >= p.M || n >= cols) continue;
+      *reinterpret_cast<U*>(C + static_cast<long long>(m) * cols + n) =
+          *reinterpret_cast<const U*>(&tile[(row * cpr + (ch ^ (row & (cpr - 1)))) * 8 + (u & (8 / W - 1)) * W]);
+    }
+  });
+}
+
+// Four neighbouring columns (fewer at the row's end) of a row from their finished sums: bias, residual or SwiGLU, 16 bits.
+__device__ __forceinline__ void finish4(const Fp8Params& p, int m, int n, f32x4 y) {
+  const bool whole = p.N % 4 == 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (p.bias && n + e < p.N) y[e] += p.bias[n + e];
+  uint16_t* C = static_cast<uint16_t*>(p.C);
+  if (p.mode == kEpiSwiglu) {
+    uint16_t* to = C + static_cast<long long>(m) * (p.N / 2) + n / 2;
+    to[0] = f32_bf16(silu(y[0]) * y[1]);
+    if (n + 2 < p.N) to[1] = f32_bf16(silu(y[2]) * y[3]);
+    return;
+  }
+  const long long at = static_cast<long long>(m) * p.N + n;
+  if (whole && p.width >= 4) {
+    if (p.mode == kEpiResidual) {
+      const uint2 u = *reinterpret_cast<const uint2*>(p.R + at);
+      y += f32x4{lo_bf16(u.x), hi_bf16(u.x), lo_bf16(u.y), hi_bf16(u.y)};
+    }
+    *reinterpret_cast<uint2*>(C + at) = make_uint2(pack2(y[0], y[1]), pack2(y[2], y[3]));
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (n + e < p.N) C[at + e] = f32_bf16(p.mode == kEpiResidual ? y[e] + bf16_f32(p.R[at + e]) : y[e]);
+}
+__device__ __forceinline__ void store4(const Fp8Params& p, float* to, int n, f32x4 y) {
+  if (p.N % 4 == 0) *reinterpret_cast<f32x4*>(to) = y;
+  else
+    for (int e = 0; e < 4; ++e)
+      if (n + e < p.N) to[e] = y[e];
+}
+
+// Up to 16 rows: bound by the weights' bytes.  W of a workgroup's 8 waves share 16 columns and take the blocks of K in turn; a
+// wave keeps D blocks in flight.  The codes become bf16 values, whose products the matrix cores sum in 32 bits.
+constexpr int kFewWaves = 8;
+template <int W, int D>
+__global__ __launch_bounds__(64 * kFewWaves, 2) void gemm_fp8_few(const Fp8Params p) {
+  constexpr int SETS = kFewWaves / W;
+  __shared__ f32x4 join[SETS][W > 1 ? W - 1 : 1][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  const int w = wave % W, set = wave / W;
+  const int n0 = (remap_block_id(blockIdx.x, gridDim.x) * SETS + set) * 16;
+  const int n = n0 + r < p.N ? n0 + r : p.N - 1;
+  const uint8_t* wrow = p.w + static_cast<long long>(n) * p.K + 16 * g;
+  const uint8_t* xrow = p.x + static_cast<long long>(r < p.M ? r : 0) * p.K + 16 * g;
+  const float* ws = p.ws + static_cast<long long>(min(n0, p.N - 1) / kBlock) * p.kb;
+  struct {
+    u32x4 w[2], x[2];
+    float xs, ws;
+  } in[D];
+  const auto load = [&](int i, int b) __attribute__((always_inline)) {
+    const int k = b * kBlock;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      in[i].w[u] = in[i].x[u] = u32x4{0, 0, 0, 0};
+      if (k + 64 * u + 16 * g >= p.K) continue;
+      in[i].w[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(wrow + k + 64 * u));
+      if (r < p.M) in[i].x[u] = *reinterpret_cast<const u32x4*>(xrow + k + 64 * u);
+    }
+    in[i].xs = r < p.M ? p.xs[b * p.xs_stride + r] : 0.f;
+    in[i].ws = ws[b];
+  };
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < D; ++i)
+    if (w + i * W < p.kb) load(i, w + i * W);
+  for (int b0 = w; b0 < p.kb; b0 += D * W) {
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+      const int b = b0 + i * W;
+      if (b >= p.kb) break;
+      f32x4 d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          d = mfma32(widen8(in[i].w[u][2 * h], in[i].w[u][2 * h + 1]), widen8(in[i].x[u][2 * h], in[i].x[u][2 * h + 1]), d);
+      const float s = in[i].xs * in[i].ws;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = fmaf(s, d[e], acc[e]);
+      if (b + D * W < p.kb) load(i, b + D * W);
+    }
+  }
+  if constexpr (W > 1) {
+    if (w) join[set][w - 1][lane] = acc;
+    __syncthreads();
+    if (w) return;
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i) acc += join[set][i][lane];
+  }
+  const int at = n0 + 4 * g;
+  if (r >= p.M || at >= p.N) return;
+  if (p.part) store4(p, p.part + static_cast<long long>(r) * p.N + at, at, acc);
+  else finish4(p, r, at, acc);
+}
+
+// Adds the parts of a split K in their order and finishes the output, four columns a thread.  With 8 bits a wave has the 256
+// columns of a block.
+__global__ __launch_bounds__(256) void fp8_join(const Fp8Params p) {
+  const int cols = (p.N + 1023) / 1024;
+  const int m = blockIdx.x / cols, n = ((blockIdx.x - m * cols) * 256 + threadIdx.x) * 4;
+  if (n >= p.N && !p.cs) return;
+  const float* from = p.part + static_cast<long long>(m) * p.N + n;
+  const long long step = static_cast<long long>(p.M) * p.N;
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  if (n < p.N) {
+    if (p.N % 4 == 0) {
+      for (int k = 0; k < p.splits; k += 4) {
+        f32x4 v[4];                                    // loads in flight together, summed in order
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = k + u < p.splits ? *reinterpret_cast<const f32x4*>(from + (k + u) * step) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) y += v[u];
+      }
+    } else {
+      for (int k = 0; k < p.splits; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (n + e < p.N) y[e] += from[k * step + e];
+    }
+  }
+  if (!p.cs) {
+    finish4(p, m, n, y);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (p.bias && n < p.N) y[e] += p.bias[n + e];
   const float a = silu(y[0]) * y[1], b = silu(y[2]) * y[3];
   const float scale = scale_of(wave_reduce_dpp(fmaxf(magnitude(a), magnitude(b)), [](float u, float v) { return fmaxf(u, v); }));
   if (n >= p.N) return;
   static_cast<uint16_t*>(p.C)[(static_cast<long long>(m) * (p.N / 2) + n / 2) / 2] = static_cast<uint16_t>(to_e4m3(a, b, 0.f, 0.f, 1.f / scale));
-  if ((threadIdx.x & 63) == 0) p.cs[static_cast<long long>(n / 256) * p.M + m] = scale;
+  if ((threadIdx.x & 63) == 0) p.cs[n / 256 * p.cs_stride + m] = scale;
+}
+
+// Elements that an access to C and R may move at once.
+int width_of(const Fp8Params& p) {
+  const uintptr_t bits = 2 * static_cast<uintptr_t>(p.mode == kEpiSwiglu ? p.N / 2 : p.N) | reinterpret_cast<uintptr_t>(p.C) |
+                         (p.mode == kEpiResidual ? reinterpret_cast<uintptr_t>(p.R) : 0);
+  return bits % 16 == 0 ? 8 : bits % 8 == 0 ? 4 : bits % 4 == 0 ? 2 : 1;
+}
+template <int W, int D>
+void launch_few(const Fp8Params& p, hipStream_t stream) {
+  const int sets = kFewWaves / W, tiles = (p.N + 15) / 16;
+  hipLaunchKernelGGL((gemm_fp8_few<W, D>), dim3((tiles + sets - 1) / sets), dim3(64 * kFewWaves), 0, stream, p);
+}
+void launch_join(const Fp8Params& p, hipStream_t stream) {
+  hipLaunchKernelGGL(fp8_join, dim3((p.N + 1023) / 1024 * p.M), dim3(256), 0, stream, p);
+}
+template <typename T, int MI, int NI, int WM, int WN, int ST, int G = 1>
+void launch_tile(Fp8Params p, int splits, hipStream_t stream) {
+  if (p.cs && !p.part && (16 * NI * WN != 256 || G > 1)) return;   // no tile of these widths finishes 8 bits: the plan never asks for it
+  p.tiles_m = (p.M + 16 * MI * WM - 1) / (16 * MI * WM);
+  p.tiles_n = (p.N + 16 * NI * WN - 1) / (16 * NI * WN);
+  p.splits = splits;
+  hipLaunchKernelGGL((gemm_fp8_tile<T, MI, NI, WM, WN, ST, G>), dim3(static_cast<unsigned>(p.tiles_m) * p.tiles_n * splits), dim3(64 * WM * WN * G), 0, stream, p);
 }
 
 bool too_many_threads(long long groups, int threads) { return groups * threads >= (1ll << 32); }
 
-size_t fp8_bytes(int M, int N, int bits) { return bits == 8 ? static_cast<size_t>(M) * N * sizeof(float) : 0; }
+// What a product of M rows is made of: one launch or two (whole rounds of the largest tiles, and the rows that are left),
+// each of one kernel with K in `splits` parts.
+struct Fp8Launch {
+  int tile, m0, rows, splits;          // tile: of kTiles, -1: gemm_fp8_few
+  bool part;                           // sums go through the workspace and fp8_join
+};
+struct Fp8Plan {
+  Fp8Launch run[2];
+  int runs;
+  size_t bytes;
+};
+
+// The tiles' times in us: a workgroup's start and end, its stage of 128 k's (for each group of waves) alone on a CU and for every
+// further one there, the end of a round.  Fitted to 5,500 timings over 160 shapes (1 to 10,677 rows, 64 to 28,672 columns, K 128
+// to 14,336, K in 1 to 12 parts, weights from memory): what the plan picks takes 1.03 times the best that was measured, in the mean.
+struct Fp8Tile {
+  int bm, bn, groups, per_cu;
+  bool wide;
+  float fixed, stage, shared, round;
+  void (*launch)(Fp8Params, int, hipStream_t);
+};
+const Fp8Tile kTiles[] = {
+    {256, 256, 1, 1, false, 9.13f, 1.466f, 0.000f, 2.98f, launch_tile<Codes, 8, 4, 2, 4, 2>},
+    {128, 128, 1, 2, false, 4.76f, 0.783f, 0.325f, 2.32f, launch_tile<Codes, 4, 4, 2, 2, 2>},
+    {64, 128, 1, 2, false, 4.35f, 0.419f, 0.326f, 1.87f, launch_tile<Codes, 4, 2, 1, 4, 3>},
+    {64, 128, 2, 1, false, 3.07f, 0.783f, 0.000f, 3.55f, launch_tile<Codes, 4, 2, 1, 4, 3, 2>},
+    {64, 64, 2, 1, false, 2.29f, 0.520f, 0.000f, 3.08f, launch_tile<Codes, 4, 1, 1, 4, 3, 2>},
+    {32, 64, 2, 2, false, 2.01f, 0.421f, 0.328f, 2.99f, launch_tile<Codes, 2, 1, 1, 4, 3, 2>},
+    {128, 256, 1, 1, true, 5.42f, 1.698f, 0.000f, 2.46f, launch_tile<Values, 4, 4, 2, 4, 2>},
+    {128, 128, 1, 2, true, 6.08f, 1.009f, 0.737f, 0.00f, launch_tile<Values, 4, 4, 2, 2, 2>},
+    {32, 64, 2, 2, true, 2.15f, 0.510f, 0.428f, 2.61f, launch_tile<Values, 2, 1, 1, 4, 3, 2>},
+};
+constexpr int kNumTiles = sizeof(kTiles) / sizeof(kTiles[0]);
+constexpr float kMemory = 4.1e6f;      // bytes per us of operands that come from memory once
+constexpr int kMostSplits = 12, kMostRows = 1 << 26;
+constexpr double kMostSums = 5e7;      // of the parts of K together
+
+long long tiles_of(const Fp8Tile& t, int rows, int N) { return (rows + t.bm - 1ll) / t.bm * ((N + t.bn - 1ll) / t.bn); }
+float join_time(int rows, int N, int splits) { return 2.9f + 1.4e-6f * splits * rows * static_cast<float>(N); }
+float tile_time(const Fp8Tile& t, int rows, int N, int K, int splits) {
+  const int kb = (K + kBlock - 1) / kBlock, stages = ((kb + splits - 1) / splits + t.groups - 1) / t.groups;
+  const long long n = tiles_of(t, rows, N) * splits, round = 256ll * t.per_cu;
+  const long long full = n / round;
+  const int left = static_cast<int>((n - full * round + 255) / 256);      // workgroups of a CU in the last round
+  const auto turn = [&](int there) { return stages * (t.stage + t.shared * (there - 1)) + t.round; };
+  const float work = t.fixed + full * turn(t.per_cu) + (left ? turn(left) : 0.f);
+  const float bytes = 3.9f + (static_cast<float>(rows) * K + static_cast<float>(N) * K + 2.f * rows * N) / kMemory;
+  return work > bytes ? work : bytes;
+}
+// gemm_fp8_few: a column's 8 waves take kb / 8 blocks one after the other; over many columns they read memory less well than the
+// tiles (one row of 28,672 columns of 3,584: 28 us against 22.6; of 3,584 columns 6.4 against 9.4 with parts and their join).
+float few_time(int rows, int N, int K) {
+  const int kb = (K + kBlock - 1) / kBlock, blocks = (kb + kFewWaves - 1) / kFewWaves;
+  const float n = (N + 15) / 16 / 256.f, work = 2.2f + (n > 1.f ? n : 1.f) * blocks * (0.854f + 0.0267f * rows);
+  const float bytes = 2.5f + static_cast<float>(N) * K / 2.9e6f;
+  return work > bytes ? work : bytes;
+}
+
+// The quickest single launch for these rows.
+float plan_rows(int rows, int N, int K, bool eight, bool wide, Fp8Launch* out) {
+  const int kb = (K + kBlock - 1) / kBlock;
+  float best = 1e30f;
+  if (rows <= 16) {
+    best = few_time(rows, N, K) + (eight ? join_time(rows, N, 1) : 0.f);
+    *out = {-1, 0, rows, 1, eight};
+  }
+  for (int i = 0; i < kNumTiles; ++i) {
+    const Fp8Tile& t = kTiles[i];
+    if (t.wide != wide || (t.bm > 32 && t.bm >= 2 * rows)) continue;
+    for (int s = 1; s <= kMostSplits; ++s) {
+      if (s > 1 && (2 * s > kb || static_cast<double>(s) * rows * N > kMostSums)) break;
+      const bool part = s > 1 || (eight && (t.bn != 256 || t.groups != 1));
+      const float time = tile_time(t, rows, N, K, s) + (part ? join_time(rows, N, s) : 0.f);
+      if (time < best) {
+        best = time;
+        *out = {i, 0, rows, s, part};
+      }
+    }
+  }
+  return best;
+}
+
+Fp8Plan plan_fp8(int M, int N, int K, bool eight, bool wide) {
+  Fp8Plan a{};
+  a.runs = 1;
+  const float one = plan_rows(M, N, K, eight, wide, &a.run[0]);
+  // The largest tiles come in rounds of 256; rows that would fill a small part of a last round may be quicker in a launch of
+  // their own.
+  for (int i = 0; i < kNumTiles; ++i) {
+    const Fp8Tile& t = kTiles[i];
+    if (t.wide != wide || t.per_cu != 1 || t.groups != 1) continue;
+    const long long across = (N + t.bn - 1ll) / t.bn, rounds = tiles_of(t, M, N) / 256, down = rounds * 256 / across;
+    const int rows = static_cast<int>(down * t.bm < M ? down * t.bm : M);
+    if (rounds < 1 || rows < 1 || rows >= M) continue;
+    Fp8Launch rest;
+    const float two = tile_time(t, rows, N, K, 1) + plan_rows(M - rows, N, K, eight, wide, &rest);
+    if (two < 0.98f * one) {
+      rest.m0 = rows;
+      a.run[0] = {i, 0, rows, 1, false};
+      a.run[1] = rest;
+      a.runs = 2;
+    }
+  }
+  for (int i = 0; i < a.runs; ++i) {
+    const size_t need = a.run[i].part ? static_cast<size_t>(a.run[i].splits) * a.run[i].rows * N * sizeof(float) : 0;
+    if (need > a.bytes) a.bytes = need;
+  }
+  return a;
+}
+
+bool fp8_wide(int sums, bool eight) { return sums == PACE_SUMS_AUTO ? eight : sums == PACE_SUMS_WIDE; }
 
 }  // namespace
 }  // namespace pace
@@ -340,15 +995,16 @@ pace_status_t pace_rmsnorm(const uint16_t* x, long long x_stride, const uint16_t
   return check_launch("pace_rmsnorm");
 }
 
-size_t pace_gemm_fp8_workspace_size(int M, int N, int K, int bits) {
-  if (M < 1 || N < 1 || K < 1) return 0;
-  return fp8_bytes(M, N, bits);
+size_t pace_gemm_fp8_workspace_size(int M, int N, int K, int bits, int sums) {
+  if (M < 1 || N < 1 || K < 1 || M > kMostRows || N > (1 << 30) || K > (1 << 20)) return 0;
+  return plan_fp8(M, N, K, bits == 8, fp8_wide(sums, bits == 8)).bytes;
 }
 
 pace_status_t pace_gemm_fp8(const uint8_t* x, const float* x_scale, long long x_scale_stride, const uint8_t* w, const float* w_scale,
                             const float* bias, const uint16_t* residual, void* C, float* c_scale, int M, int N, int K, int epilogue,
-                            void* workspace, size_t workspace_bytes, hipStream_t stream) {
+                            int sums, void* workspace, size_t workspace_bytes, hipStream_t stream) {
   PACE_REQUIRE(epilogue >= 0 && epilogue <= 2, "pace_gemm_fp8: epilogue %d not in {0, 1, 2}", epilogue);
+  PACE_REQUIRE(sums >= PACE_SUMS_AUTO && sums <= PACE_SUMS_WIDE, "pace_gemm_fp8: sums %d not in {0, 1, 2}", sums);
   PACE_REQUIRE(M >= 0 && N >= 1 && K >= 16 && K % 16 == 0 && K <= (1 << 20), "pace_gemm_fp8: M=%d N=%d K=%d (K a positive multiple of 16, at most 2^20)", M, N, K);
   PACE_REQUIRE(epilogue != 2 || N % 2 == 0, "pace_gemm_fp8: SwiGLU needs an even N");
   PACE_REQUIRE(!c_scale || (epilogue == 2 && N % 32 == 0), "pace_gemm_fp8: 8-bit output needs SwiGLU and N=%d a multiple of 32", N);
@@ -357,19 +1013,43 @@ pace_status_t pace_gemm_fp8(const uint8_t* x, const float* x_scale, long long x_
   PACE_REQUIRE(epilogue != 1 || residual != nullptr, "pace_gemm_fp8: residual epilogue without residual");
   PACE_REQUIRE(aligned16(x) && aligned16(w), "pace_gemm_fp8: x and w must be 16-byte aligned");
   PACE_REQUIRE(!c_scale || aligned16(C), "pace_gemm_fp8: codes of the output must be 16-byte aligned");
-  PACE_REQUIRE(x_scale_stride >= M, "pace_gemm_fp8: x_scale_stride %lld < M=%d", x_scale_stride, M);
-  PACE_REQUIRE(N <= (1 << 30) && !too_many_threads((M + 63ll) / 64 * ((N + 63) / 64), 256), "pace_gemm_fp8: too many rows or columns (M=%d N=%d)", M, N);
-  PACE_REQUIRE(!c_scale || !too_many_threads((N + 1023ll) / 1024 * M, 256), "pace_gemm_fp8: too many rows or columns (M=%d N=%d)", M, N);
-  const size_t need = fp8_bytes(M, N, c_scale ? 8 : 16);
-  if (need) {
-    if (workspace == nullptr || workspace_bytes < need)
-      return set_error(PACE_ERR_WORKSPACE, "pace_gemm_fp8: workspace %zu < %zu bytes", workspace_bytes, need);
+  PACE_REQUIRE(x_scale_stride >= M && x_scale_stride < (1ll << 40), "pace_gemm_fp8: x_scale_stride %lld < M=%d, or past 2^40", x_scale_stride, M);
+  // the smallest tile's workgroups, the join's and the parts' sums
+  PACE_REQUIRE(M <= kMostRows && N <= (1 << 30) && (M + 31ll) / 32 * ((N + 63ll) / 64) * 512 * kMostSplits < (1ll << 32) &&
+                   static_cast<long long>(M) * ((N + 1023ll) / 1024) * 256 < (1ll << 32),
+               "pace_gemm_fp8: too many rows or columns (M=%d N=%d)", M, N);
+  const Fp8Plan a = plan_fp8(M, N, K, c_scale != nullptr, fp8_wide(sums, c_scale != nullptr));
+  if (a.bytes) {
+    if (workspace == nullptr || workspace_bytes < a.bytes)
+      return set_error(PACE_ERR_WORKSPACE, "pace_gemm_fp8: workspace %zu < %zu bytes", workspace_bytes, a.bytes);
     PACE_REQUIRE(aligned16(workspace), "pace_gemm_fp8: workspace must be 16-byte aligned");
   }
-  const Fp8Params p{x, x_scale, w, w_scale, bias, residual, C, c_scale, need ? static_cast<float*>(workspace) : nullptr, x_scale_stride,
-                    M, N, K, (K + kBlock - 1) / kBlock, epilogue, 1};
-  hipLaunchKernelGGL(gemm_fp8_direct, dim3((N + 63) / 64 * ((M + 63) / 64)), dim3(256), 0, stream, p);
-  if (need) hipLaunchKernelGGL(fp8_join, dim3((N + 1023) / 1024 * M), dim3(256), 0, stream, p);
+  const int cols = epilogue == 2 ? N / 2 : N;
+  for (int i = 0; i < a.runs; ++i) {
+    const Fp8Launch& l = a.run[i];
+    Fp8Params p{};
+    p.x = x + static_cast<long long>(l.m0) * K;
+    p.xs = x_scale + l.m0;
+    p.w = w;
+    p.ws = w_scale;
+    p.bias = bias;
+    p.R = epilogue == 1 ? residual + static_cast<long long>(l.m0) * cols : nullptr;
+    p.C = static_cast<char*>(C) + static_cast<long long>(l.m0) * cols * (c_scale ? 1 : 2);
+    p.cs = c_scale ? c_scale + l.m0 : nullptr;
+    p.part = l.part ? static_cast<float*>(workspace) : nullptr;
+    p.xs_stride = x_scale_stride;
+    p.cs_stride = M;
+    p.M = l.rows;
+    p.N = N;
+    p.K = K;
+    p.kb = (K + kBlock - 1) / kBlock;
+    p.mode = epilogue;
+    p.splits = l.splits;
+    p.width = width_of(p);
+    if (l.tile < 0) launch_few<8, 2>(p, stream);
+    else kTiles[l.tile].launch(p, l.splits, stream);
+    if (l.part) launch_join(p, stream);
+  }
   return check_launch("pace_gemm_fp8");
 }
 

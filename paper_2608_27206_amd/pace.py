@@ -85,9 +85,9 @@ _PROTOS = {
                              c_void, c_size, c_void]),
     "pace_quantize_fp8": (c_int, [c_void, c_ll, c_int, c_int, c_int, c_void, c_void, c_void]),
     "pace_rmsnorm": (c_int, [c_void, c_ll, c_void, c_ll, c_void, c_float, c_int, c_int, c_void, c_void, c_void, c_void, c_void]),
-    "pace_gemm_fp8_workspace_size": (c_size, [c_int, c_int, c_int, c_int]),
+    "pace_gemm_fp8_workspace_size": (c_size, [c_int] * 5),
     "pace_gemm_fp8": (c_int, [c_void, c_void, c_ll, c_void, c_void, c_void, c_void, c_void, c_void, c_int, c_int, c_int, c_int,
-                              c_void, c_size, c_void]),
+                              c_int, c_void, c_size, c_void]),
 }
 
 EXPORTED = tuple(_PROTOS.keys())
@@ -717,6 +717,9 @@ def gemm_w4(x: torch.Tensor, w: torch.Tensor, scale: torch.Tensor, zero: Optiona
 
 
 # ---------------------------------------------------------------- a layer in 8 bits
+SUMS_AUTO, SUMS_FAST, SUMS_WIDE = 0, 1, 2            # PACE_SUMS_* of include/pace.h
+
+
 def _matrix_arg(t: torch.Tensor, dtype, shape: tuple, device: int, name: str):
     """Address and row stride of a matrix whose rows are contiguous and may lie further apart."""
     if t.dtype is not dtype or t.shape != shape or t.get_device() != device or (shape[1] > 1 and t.stride(1) != 1):
@@ -780,12 +783,14 @@ def rmsnorm(x: torch.Tensor, gamma: torch.Tensor, residual: Optional[torch.Tenso
 
 
 def gemm_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
-             residual: Optional[torch.Tensor] = None, epilogue: int = 0, bits: int = 16, out: Optional[torch.Tensor] = None,
-             out_scale: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+             residual: Optional[torch.Tensor] = None, epilogue: int = 0, bits: int = 16, sums: int = SUMS_AUTO,
+             out: Optional[torch.Tensor] = None, out_scale: Optional[torch.Tensor] = None,
+             workspace: Optional[torch.Tensor] = None):
     """C = x W^T of e4m3 codes x [M, K] with x_scale fp32 [ceil(K / 128), M] (rows of any stride: a slice of rows is x[a:b],
     x_scale[:, a:b]) and w [N, K] with w_scale fp32 [ceil(N / 128), ceil(K / 128)]; bias, residual and epilogue as in
     gemm_bf16.  Returns (C, None), or with bits=8 and SwiGLU (codes [M, N / 2], their scales [ceil(N / 256), M]), ready for
-    the next product."""
+    the next product.  sums: SUMS_FAST adds the products of a block as the matrix cores do (8 at a time on a grid of 2^-13 of
+    the largest), SUMS_WIDE in 32 bits at half the matrix rate; SUMS_AUTO is wide for bits=8 alone."""
     gpu = _gpu_of(x)
     if x.dim() != 2 or w.dim() != 2:
         raise PaceError("x and w must be 2-D")
@@ -804,11 +809,12 @@ def gemm_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: t
     elif out_scale is None:
         out_scale = torch.empty(((cols + 127) // 128, M), dtype=_F32, device=x.device)
     if workspace is None:
-        need = (_lib or lib()).pace_gemm_fp8_workspace_size(M, N, K, bits)
+        need = (_lib or lib()).pace_gemm_fp8_workspace_size(M, N, K, bits, sums)
         if need:
             workspace = torch.empty(need, dtype=_U8, device=x.device)
     _call("pace_gemm_fp8", gpu, _arg(x, _E4M3, (M, K), gpu, "x"), xsp, xss, _arg(w, _E4M3, (N, K), gpu, "w"),
           _arg(w_scale, _F32, ((N + 127) // 128, kb), gpu, "w_scale"), _arg(bias, _F32, (N,), gpu, "bias"),
           _arg(residual, _BF16, (M, cols), gpu, "residual"), _arg(out, kind, (M, cols), gpu, "out"),
-          _arg(out_scale, _F32, ((cols + 127) // 128, M), gpu, "out_scale"), M, N, K, epilogue, *_scratch(workspace, gpu))
+          _arg(out_scale, _F32, ((cols + 127) // 128, M), gpu, "out_scale"), M, N, K, epilogue, sums,
+          *_scratch(workspace, gpu))
     return out, out_scale

@@ -21,7 +21,7 @@ def norm(**kw):
 
 
 def gemm(**kw):
-    a = dict(x=P, xs=P, xss=4, w=P, ws=P, bias=None, residual=None, C=P, cs=None, M=4, N=64, K=256, epilogue=0, wsp=None, wsb=0, stream=None)
+    a = dict(x=P, xs=P, xss=4, w=P, ws=P, bias=None, residual=None, C=P, cs=None, M=4, N=64, K=256, epilogue=0, sums=0, wsp=None, wsb=0, stream=None)
     a.update(kw)
     return pace.lib().pace_gemm_fp8(*a.values()), pace.lib().pace_last_error().decode()
 
@@ -50,7 +50,7 @@ def test_norm(bad, word):
 
 @pytest.mark.parametrize("bad,word", [
     (dict(x=None), "null"), (dict(xs=None), "null"), (dict(w=None), "null"), (dict(ws=None), "null"), (dict(C=None), "null"), (dict(x=ODD), "aligned"),
-    (dict(w=ODD), "aligned"), (dict(epilogue=3), "epilogue"), (dict(epilogue=-1), "epilogue"), (dict(epilogue=1), "residual"), (dict(epilogue=2, N=63), "even"),
+    (dict(w=ODD), "aligned"), (dict(epilogue=3), "epilogue"), (dict(epilogue=-1), "epilogue"), (dict(sums=3), "sums"), (dict(sums=-1), "sums"), (dict(epilogue=1), "residual"), (dict(epilogue=2, N=63), "even"),
     (dict(M=-1), "M=-1"), (dict(N=0), "N=0"), (dict(K=0), "K=0"), (dict(K=264), "K=264"), (dict(K=(1 << 20) + 16), "2^20"), (dict(xss=3), "stride"),
     (dict(cs=P), "SwiGLU"), (dict(cs=P, epilogue=1, residual=P), "SwiGLU"), (dict(cs=P, epilogue=2, N=48), "32"), (dict(cs=P, epilogue=2, C=ODD), "aligned"),
     (dict(N=(1 << 30) + 1), "too many"), (dict(M=1 << 22, xss=1 << 22, N=1 << 22), "too many")])
@@ -67,8 +67,8 @@ def test_no_rows_are_no_error():
 
 @pytest.mark.parametrize("M,N,K,bits", [(8, 28672, 3584, 8), (48, 3584, 14336, 16), (300, 640, 1280, 8)])
 def test_gemm_workspace(M, N, K, bits):
-    need = pace.lib().pace_gemm_fp8_workspace_size(M, N, K, bits)
-    assert pace.lib().pace_gemm_fp8_workspace_size(0, N, K, bits) == 0 and pace.lib().pace_gemm_fp8_workspace_size(M, -N, K, bits) == 0
+    need = pace.lib().pace_gemm_fp8_workspace_size(M, N, K, bits, 0)
+    assert pace.lib().pace_gemm_fp8_workspace_size(0, N, K, bits, 0) == 0 and pace.lib().pace_gemm_fp8_workspace_size(M, -N, K, bits, 0) == 0
     if need:
         kw = dict(M=M, N=N, K=K, xss=M, epilogue=2 if bits == 8 else 0, cs=P if bits == 8 else None)
         for ws, wsb, st, word in ((None, 0, 3, "workspace"), (P, need - 1, 3, "workspace"), (ODD, need, 1, "aligned")):

@@ -20,7 +20,7 @@ def test_scales_by_hand():
     tiny = 2.0 ** -120
     assert np.array_equal(o8.scales(x, 1), [[1, 14 / 448, tiny], [7 / 448, tiny, tiny]])
     assert np.array_equal(o8.scales(x, 128), [[1, 7 / 448]])
-    assert np.array_equal(o8.spread(np.array([[1.0, 2, 3], [4, 5, 6]]), (3, 144), 1)[:, [0, 127, 128, 143]],
+    assert np.array_equal(o8.per_value(np.array([[1.0, 2, 3], [4, 5, 6]]), (3, 144), 1)[:, [0, 127, 128, 143]],
                           [[1, 1, 4, 4], [2, 2, 5, 5], [3, 3, 6, 6]])
 
 
@@ -42,9 +42,22 @@ def test_product_by_a_triple_loop():
     v = v[np.isfinite(v)]
     x, w = rs.choice(v, (3, 144)), rs.choice(v, (130, 144))
     xs, ws = rs.random((2, 3)), rs.random((2, 2))
-    y, tol = o8.product(x, xs, w, ws)
+    y, tol, off = o8.product(x, xs, w, ws)
+    assert np.all(off == 0)
     for m, n in ((0, 0), (2, 127), (1, 128), (2, 129)):
         ref = sum(x[m, k] * xs[k // 128, m] * w[n, k] * ws[n // 128, k // 128] for k in range(144))
         assert abs(y[m, n] - ref) <= 1e-9 * tol[m, n] / 2.0 ** -24
-    g, _ = o8.product(x, xs, w, ws, epilogue=2)
-    assert np.allclose(g[:, 3], y[:, 6] / (1 + np.exp(-y[:, 6])) * y[:, 7])
+    g, _, _ = o8.product(x, xs, w, ws, epilogue=2)
+    with np.errstate(over="ignore"):
+        assert np.allclose(g[:, 3], y[:, 6] / (1 + np.exp(-y[:, 6])) * y[:, 7])
+
+
+def test_what_eights_on_a_grid_may_lose():
+    """One eight with products 2^10, 1 and six zeros: on a grid of 2^-13 of the largest the 1 may be lost up to 2^-3."""
+    x, w = np.zeros((1, 16)), np.ones((1, 16))
+    x[0, 0], x[0, 1] = 2.0 ** 8, 1
+    w[0, 0] = 4
+    one = np.ones((1, 1))
+    y, tol, off = o8.product(x, one, w, one, wide=False)
+    _, tight, _ = o8.product(x, one, w, one)
+    assert y[0, 0] == 1025 and np.isclose(tol[0, 0] - tight[0, 0], 7 * 2.0 ** -3) and np.isclose(off[0, 0], 7 * 2.0 ** -3)
