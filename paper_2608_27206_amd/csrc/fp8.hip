@@ -242,20 +242,30 @@ __device__ __forceinline__ Values lift(i32x8 u, Values*) {
   for (int q = 0; q < 4; ++q) o.v[q] = widen8(static_cast<uint32_t>(u[2 * q]), static_cast<uint32_t>(u[2 * q + 1]));
   return o;
 }
-// The sums of a block's 128 products, of N rows of x with columns of W.
-template <int N>
-__device__ __forceinline__ void dot_block(const Codes& w, const Codes (&x)[N], f32x4 (&d)[N]) {
+// The sums of a block's 128 products: N rows of x (16 each) with N2 columns of w.
+template <int N2, int N>
+__device__ __forceinline__ void dot_block(const Codes* w, const Codes (&x)[N], f32x4 (&d)[N2 * N]) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) d[i] = mfma128(w.v, x[i].v);
+  for (int j = 0; j < N2; ++j)
+#pragma unroll
+    for (int i = 0; i < N; ++i) d[j * N + i] = mfma128(w[j].v, x[i].v);
 }
-template <int N>
-__device__ __forceinline__ void dot_block(const Values& w, const Values (&x)[N], f32x4 (&d)[N]) {
+template <int N2, int N>
+__device__ __forceinline__ void dot_block(const Values* w, const Values (&x)[N], f32x4 (&d)[N2 * N]) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) d[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int t = 0; t < N2 * N; ++t) d[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int q = 0; q < 4; ++q)
 #pragma unroll
-    for (int i = 0; i < N; ++i) d[i] = mfma32(w.v[q], x[i].v[q], d[i]);
+    for (int j = 0; j < N2; ++j)
+#pragma unroll
+      for (int i = 0; i < N; ++i) d[j * N + i] = mfma32(w[j].v[q], x[i].v[q], d[j * N + i]);
+}
+// keeps what has been computed where it stands, between the products of the same step
+__device__ __forceinline__ void pin(Codes&) {}
+__device__ __forceinline__ void pin(Values& o) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) asm volatile("" : "+v"(o.v[q]));
 }
 
 typedef __attribute__((address_space(3))) const char lds_char;
@@ -300,15 +310,17 @@ __device__ __forceinline__ void with_width(int width, F f) {
 template <typename T, int MI, int NI, int WM, int WN, int ST, int G>
 __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Params p) {
   constexpr int BM = 16 * MI * WM, BN = 16 * NI * WN, NW = WM * WN, TH = 64 * NW * G;
-  constexpr int kScales = BM < 64 ? 64 : BM;                     // floats of a stage
+  constexpr int kScales = (BM + 63) / 64 * 64;                   // floats of a stage, whole DMAs of them
   constexpr int kStage = (BM + BN) * kBlock;                     // bytes of a stage
   constexpr int kScaleSlots = ST + 1;
-  constexpr int MP = MI < 2 ? 1 : 2, Q = MI / MP;                // tiles of a step, steps of a stage
+  constexpr bool kWide = sizeof(T) != sizeof(Codes), kAhead = kWide && NI % 2 == 0 && MI % 2 == 0;
+  constexpr int MP = MI % 2 || kAhead ? 1 : 2, Q = MI / MP;      // tiles of x in a step, steps of a stage
+  constexpr int JP = MP == 1 && NI % 2 == 0 ? 2 : 1, NU = NI / JP;   // tiles of w in a unit, units of a step
   // DMAs of a wave and stage, 8 rows each: the first part (w's rows, those of x that the first half of the steps reads, and the
   // scales) is asked for in mid-stage, the second at the end
-  constexpr bool kTwo = Q % 4 == 0, kWide = sizeof(T) != sizeof(Codes);
+  constexpr bool kTwo = Q % 4 == 0;
   constexpr int kWD = BN / 8 / NW, kXD = BM / 8 / NW, kLate = kTwo ? kXD / 2 : 0, kEarly = kWD + kXD - kLate + 1;
-  static_assert(kWD * 8 * NW == BN && kXD * 8 * NW == BM && (!kTwo || kXD % 2 == 0) && NW % 2 == 0 && (Q == 1 || Q % 2 == 0) && kBlock % (16 * NI) == 0, "tile");
+  static_assert(kWD * 8 * NW == BN && kXD * 8 * NW == BM && (!kTwo || kXD % 2 == 0) && NW % 2 == 0 && kBlock % (16 * NI) == 0 && kScales / 64 <= NW, "tile");
   constexpr int kRing = ST * G * kStage, kTile = BM * BN * 2, kJoin = (G - 1) * BM * BN * 4, kBoth = kTile > kJoin ? kTile : kJoin;
   __shared__ __align__(16) char lds[kRing > kBoth ? kRing : kBoth];
   __shared__ float scales[kScaleSlots * G][kScales];
@@ -402,32 +414,36 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
   wait_loads<(ST - 1) * (kEarly + kLate)>();
   barrier();
 
-  T wf[NI];
+  T* const kind = nullptr;
+  T wf[NI], xa[MP];
   i32x8 xr[2][MP];
   float xsc[2][MP];
 #pragma unroll
-  for (int j = 0; j < NI; ++j) wf[j] = lift(frag(0, BM + wn + 16 * j), static_cast<T*>(nullptr));
+  for (int j = 0; j < NI; ++j) wf[j] = lift(frag(0, BM + wn + 16 * j), kind);
 #pragma unroll
   for (int i = 0; i < MP; ++i) {
     xr[0][i] = frag(0, wm + 16 * i);
     xsc[0][i] = x_scale(0, i);
+    if (kAhead) xa[i] = lift(xr[0][i], kind);
   }
   int cur = 0, cs = 0;                                 // the stage's buffer and scales
-  // What a step has formed goes into acc in the next one, under its products.
-  f32x4 d[MP];
+  // What a unit of products has formed goes into acc in the next one, under its products.
+  f32x4 d[JP * MP];
   float ds[MP];
 #pragma unroll
-  for (int i = 0; i < MP; ++i) {
-    d[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    ds[i] = 0.f;
-  }
-  const auto add = [&](int q, int j) __attribute__((always_inline)) {
+  for (int i = 0; i < MP; ++i) ds[i] = 0.f;
 #pragma unroll
-    for (int i = 0; i < MP; ++i)
+  for (int t = 0; t < JP * MP; ++t) d[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const auto add = [&](int q, int u) __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[q * MP + i][j][e] = fmaf(ds[i], d[i][e], acc[q * MP + i][j][e]);
+    for (int j = 0; j < JP; ++j)
 #pragma unroll
-    for (int i = 0; i < MP; ++i) asm volatile("" : "+v"(acc[q * MP + i][j]));   // here, not behind the stage's branches
+      for (int i = 0; i < MP; ++i) {
+        f32x4& to = acc[q * MP + i][u * JP + j];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[e] = fmaf(ds[i], d[j * MP + i][e], to[e]);
+        asm volatile("" : "+v"(to));                   // here, not behind the stage's branches
+      }
   };
   // Stage k: its first fragments are in registers.  Before its last step a wave, which then holds the last fragments, meets
   // the others; what is left of the stage's buffer takes stage k + ST, and the last products run under the first reads of
@@ -437,10 +453,9 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
     const float sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wscales), k & 63));
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-      const int slot = Q == 1 ? 0 : q & 1, next_slot = Q == 1 ? 0 : (q + 1) & 1;
-      T x[MP];
-      float s[MP];
       const bool last = q == Q - 1;
+      const int slot = q & 1, next_slot = last ? 0 : (q + 1) & 1;
+      float s[MP];
       if (kTwo && q == Q / 2 - 1) {
         // this stage's second part has come; in flight are the stages after it
         wait_loads<(ST - 1) * (kEarly + kLate)>();
@@ -453,7 +468,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
       }
 #pragma unroll
       for (int i = 0; i < MP; ++i) {
-        x[i] = lift(xr[slot][i], static_cast<T*>(nullptr));
+        if (!kAhead) xa[i] = lift(xr[slot][i], kind);
         s[i] = xsc[slot][i] * sw;
       }
       // past the end of K the reads bring anything, and nothing uses it
@@ -462,60 +477,82 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
         xr[next_slot][i] = frag(last ? nxt : cur, wm + 16 * (last ? i : (q + 1) * MP + i));
         xsc[next_slot][i] = x_scale(last ? ns : cs, last ? i : (q + 1) * MP + i);
       }
-      i32x8 wr[2];
-      if (last && kWide) wr[0] = frag(nxt, BM + wn);
+      i32x8 wr[2 * JP];                                // the next stage's w before it is widened
+      T xn[MP];
+      if (last && kWide) {
 #pragma unroll
-      for (int j = 0; j < NI; ++j) {
-        f32x4 c[MP];
-        dot_block(wf[j], x, c);
-        if (last && kWide && j + 1 < NI) wr[(j + 1) & 1] = frag(nxt, BM + wn + 16 * (j + 1));
-        if (j) add(q, j - 1);
-        else add(q ? q - 1 : Q - 1, NI - 1);
+        for (int j = 0; j < JP; ++j) wr[j] = frag(nxt, BM + wn + 16 * j);
+      }
+#pragma unroll
+      for (int u = 0; u < NU; ++u) {
+        f32x4 c[JP * MP];
+        dot_block<JP>(&wf[u * JP], xa, c);
+        if (last && kWide && u + 1 < NU) {
+#pragma unroll
+          for (int j = 0; j < JP; ++j) wr[((u + 1) & 1) * JP + j] = frag(nxt, BM + wn + 16 * ((u + 1) * JP + j));
+        }
+        if (u) add(q, u - 1);
+        else add(q ? q - 1 : Q - 1, NU - 1);
         // what the barriers have freed is asked for a piece at a time, behind the step's reads and under its products
-        constexpr int kSlots = kTwo ? (Q / 2) * NI : NI, kFirst = kTwo ? Q / 2 - 1 : Q - 1;
-        const int at = (q - kFirst) * NI + j;
+        constexpr int kSlots = kTwo ? (Q / 2) * NU : NU, kFirst = kTwo ? Q / 2 - 1 : Q - 1;
+        const int at = (q - kFirst) * NU + u;
         if (at >= 0 && at < kSlots) {
 #pragma unroll
-          for (int u = 0; u < kEarly; ++u)
-            if (u * kSlots / kEarly == at) load_early(u, block_of(k + ST), cur, far);
+          for (int l = 0; l < kEarly; ++l)
+            if (l * kSlots / kEarly == at) load_early(l, block_of(k + ST), cur, far);
         }
         if (last) {
 #pragma unroll
-          for (int u = 0; u < kLate; ++u)
-            if (u * NI / kLate == j) load_late(u, block_of(k + ST), cur);
+          for (int l = 0; l < kLate; ++l)
+            if (l * NU / kLate == u) load_late(l, block_of(k + ST), cur);
+        }
+        // the next step's x and the next stage's w are widened under the products, too
+        if (kAhead && u == NU - 1) {
+#pragma unroll
+          for (int i = 0; i < MP; ++i) {
+            xn[i] = lift(xr[next_slot][i], kind);
+            pin(xn[i]);
+          }
         }
         if (last) {
-          if constexpr (kWide) {
-            wf[j] = lift(wr[j & 1], static_cast<T*>(nullptr));
 #pragma unroll
-            for (int u = 0; u < 4; ++u) asm volatile("" : "+v"(wf[j].v[u]));   // here, under the products
-          } else {
-            wf[j] = lift(frag(nxt, BM + wn + 16 * j), static_cast<T*>(nullptr));
+          for (int j = 0; j < JP; ++j) {
+            T& to = wf[u * JP + j];
+            if constexpr (kWide) to = lift(wr[(u & 1) * JP + j], kind);
+            else to = lift(frag(nxt, BM + wn + 16 * (u * JP + j)), kind);
+            pin(to);
           }
         }
 #pragma unroll
-        for (int i = 0; i < MP; ++i) {
-          d[i] = c[i];
-          ds[i] = s[i];
-        }
-        if constexpr (kWide) {
+        for (int t = 0; t < JP * MP; ++t) d[t] = c[t];
 #pragma unroll
-          for (int u = 0; u < 4 * MP; ++u) {
+        for (int i = 0; i < MP; ++i) ds[i] = s[i];
+        if constexpr (kWide) {
+          const int each = 1 + (kAhead && u == NU - 1 ? 2 : 0) + (last ? 4 : 0) + (kAhead ? 0 : 2);   // VALU work for each product
+#pragma unroll
+          for (int t = 0; t < 4 * JP * MP; ++t) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+            if (each == 1) __builtin_amdgcn_sched_group_barrier(0x002, 1, 0);
+            else if (each == 3) __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+            else if (each == 5) __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+            else __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
           }
         } else {
-          __builtin_amdgcn_sched_group_barrier(0x008, MP, 0);          // this step's products first,
-          __builtin_amdgcn_sched_group_barrier(0x002, 4 * MP, 0);      // the sums of the one before under them
+          __builtin_amdgcn_sched_group_barrier(0x008, JP * MP, 0);     // this unit's products first,
+          __builtin_amdgcn_sched_group_barrier(0x002, 4 * JP * MP, 0); // the sums of the one before under them
         }
         __builtin_amdgcn_sched_barrier(0);
+      }
+      if (kAhead) {
+#pragma unroll
+        for (int i = 0; i < MP; ++i) xa[i] = xn[i];
       }
     }
     if ((k & 63) == 63 && k + 1 < nk) scales_from(k + 1);
     cur = nxt;
     cs = ns;
   }
-  add(Q - 1, NI - 1);
+  add(Q - 1, NU - 1);
   wait_loads<0>();                                     // those past the end: the epilogue uses the same LDS
   if constexpr (G > 1) {
     __syncthreads();
@@ -848,9 +885,10 @@ struct Fp8Plan {
   size_t bytes;
 };
 
-// The tiles' times in us: a workgroup's start and end, its stage of 128 k's (for each group of waves) alone on a CU and for every
-// further one there, the end of a round.  Fitted to 5,500 timings over 160 shapes (1 to 10,677 rows, 64 to 28,672 columns, K 128
-// to 14,336, K in 1 to 12 parts, weights from memory): what the plan picks takes 1.03 times the best that was measured, in the mean.
+// The tiles' times in us: a launch's start and end, a stage of 128 k's (for each group of waves) alone on a CU and what every further
+// workgroup there adds to it, a round's end.  Fitted to 10,800 timings over 210 shapes (1 to 10,677 rows, 64 to 28,672 columns, K 128
+// to 14,336, K in 1 to 12 parts, weights from memory): what the plan picks takes 1.03 times the best that was measured in the
+// mean, at most 1.26 times.  Of 21 tiles tried these are the ones without which that grows by half a percent or more.
 struct Fp8Tile {
   int bm, bn, groups, per_cu;
   bool wide;
@@ -858,23 +896,26 @@ struct Fp8Tile {
   void (*launch)(Fp8Params, int, hipStream_t);
 };
 const Fp8Tile kTiles[] = {
-    {256, 256, 1, 1, false, 9.13f, 1.466f, 0.000f, 2.98f, launch_tile<Codes, 8, 4, 2, 4, 2>},
-    {128, 128, 1, 2, false, 4.76f, 0.783f, 0.325f, 2.32f, launch_tile<Codes, 4, 4, 2, 2, 2>},
-    {64, 128, 1, 2, false, 4.35f, 0.419f, 0.326f, 1.87f, launch_tile<Codes, 4, 2, 1, 4, 3>},
-    {64, 128, 2, 1, false, 3.07f, 0.783f, 0.000f, 3.55f, launch_tile<Codes, 4, 2, 1, 4, 3, 2>},
-    {64, 64, 2, 1, false, 2.29f, 0.520f, 0.000f, 3.08f, launch_tile<Codes, 4, 1, 1, 4, 3, 2>},
-    {32, 64, 2, 2, false, 2.01f, 0.421f, 0.328f, 2.99f, launch_tile<Codes, 2, 1, 1, 4, 3, 2>},
-    {128, 256, 1, 1, true, 5.42f, 1.698f, 0.000f, 2.46f, launch_tile<Values, 4, 4, 2, 4, 2>},
-    {128, 128, 1, 2, true, 6.08f, 1.009f, 0.737f, 0.00f, launch_tile<Values, 4, 4, 2, 2, 2>},
-    {32, 64, 2, 2, true, 2.15f, 0.510f, 0.428f, 2.61f, launch_tile<Values, 2, 1, 1, 4, 3, 2>},
+    {256, 256, 1, 1, false, 3.92f, 1.481f, 0.000f, 8.72f, launch_tile<Codes, 8, 4, 2, 4, 2>},
+    {192, 128, 1, 1, false, 3.56f, 0.779f, 0.000f, 5.06f, launch_tile<Codes, 6, 2, 2, 4, 3>},
+    {160, 128, 1, 2, false, 1.04f, 0.835f, 0.424f, 7.23f, launch_tile<Codes, 5, 4, 2, 2, 2>},
+    {128, 128, 2, 1, false, 2.70f, 1.256f, 0.000f, 5.66f, launch_tile<Codes, 4, 4, 2, 2, 2, 2>},
+    {96, 128, 2, 1, false, 2.39f, 1.136f, 0.000f, 4.69f, launch_tile<Codes, 3, 4, 2, 2, 2, 2>},
+    {64, 128, 2, 1, false, 2.25f, 0.779f, 0.000f, 4.49f, launch_tile<Codes, 4, 2, 1, 4, 3, 2>},
+    {64, 64, 2, 1, false, 2.13f, 0.524f, 0.000f, 3.33f, launch_tile<Codes, 4, 1, 1, 4, 3, 2>},
+    {32, 64, 2, 2, false, 2.02f, 0.442f, 0.345f, 2.97f, launch_tile<Codes, 2, 1, 1, 4, 3, 2>},
+    {192, 256, 1, 1, true, 4.23f, 2.113f, 0.000f, 5.08f, launch_tile<Values, 6, 4, 2, 4, 2>},
+    {128, 256, 1, 1, true, 3.40f, 1.624f, 0.000f, 4.72f, launch_tile<Values, 4, 4, 2, 4, 2>},
+    {128, 128, 1, 2, true, 4.88f, 0.943f, 0.793f, 1.40f, launch_tile<Values, 4, 4, 2, 2, 2>},
+    {32, 64, 2, 2, true, 2.05f, 0.534f, 0.458f, 2.68f, launch_tile<Values, 2, 1, 1, 4, 3, 2>},
 };
 constexpr int kNumTiles = sizeof(kTiles) / sizeof(kTiles[0]);
-constexpr float kMemory = 4.1e6f;      // bytes per us of operands that come from memory once
+constexpr float kMemory = 4.0e6f;      // bytes per us of operands that come from memory once
 constexpr int kMostSplits = 12, kMostRows = 1 << 26;
 constexpr double kMostSums = 5e7;      // of the parts of K together
 
 long long tiles_of(const Fp8Tile& t, int rows, int N) { return (rows + t.bm - 1ll) / t.bm * ((N + t.bn - 1ll) / t.bn); }
-float join_time(int rows, int N, int splits) { return 2.9f + 1.4e-6f * splits * rows * static_cast<float>(N); }
+float join_time(int rows, int N, int splits) { return 2.8f + 1.3e-6f * splits * rows * static_cast<float>(N); }
 float tile_time(const Fp8Tile& t, int rows, int N, int K, int splits) {
   const int kb = (K + kBlock - 1) / kBlock, stages = ((kb + splits - 1) / splits + t.groups - 1) / t.groups;
   const long long n = tiles_of(t, rows, N) * splits, round = 256ll * t.per_cu;
