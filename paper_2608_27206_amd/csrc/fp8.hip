@@ -92,8 +92,8 @@ struct QuantParams {
 
 // Rows: 16 lanes per block of 128, blocks of a row after one another.
 __global__ __launch_bounds__(256) void quantize_rows(const QuantParams p) {
-  const long long block = static_cast<long long>(blockIdx.x) * 16 + (threadIdx.x >> 4);
-  const int row = static_cast<int>(block / p.kb), kb = static_cast<int>(block - static_cast<long long>(row) * p.kb);
+  const unsigned block = blockIdx.x * 16 + (threadIdx.x >> 4);   // under 2^28: a launch has fewer than 2^32 threads
+  const int row = static_cast<int>(block / static_cast<unsigned>(p.kb)), kb = static_cast<int>(block - static_cast<unsigned>(row) * p.kb);
   if (row >= p.M) return;                              // whole groups of 16 lanes
   const int k = kb * kBlock + (threadIdx.x & 15) * 8;
   float x[8] = {};
@@ -139,7 +139,9 @@ struct NormParams {
 
 // h = x + residual, y = h / sqrt(mean(h^2) + eps) * gamma: T threads a row, which stays in registers (NC pieces of 8
 // values a thread), so it is read once; 16 neighbouring lanes hold a block of 128, whose scale needs no more than them.
-template <int T, int NC>
+// Bound by memory: 42,196 rows of 1,280 with the residual to 8 bits move 380 MB in 83 us (4.6 TB/s; a copy 5.1).  Few rows are
+// bound by the chain loads -> sum -> norm -> maximum -> store: they take 256 threads each, and gamma comes with the row (GAMMA).
+template <int T, int NC, bool GAMMA>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_rows(const NormParams p) {
   constexpr int ROWS = T < 256 ? 256 / T : 1;
   __shared__ float red[T / 64];
@@ -148,19 +150,28 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_rows(const NormPara
   const int pieces = p.K / 8;
   const uint4* x = reinterpret_cast<const uint4*>(p.x + row * p.stride);
   const uint4* r = reinterpret_cast<const uint4*>(p.residual + row * p.rstride);
+  uint4 xv[NC], rv[NC];
+  float4 gv[GAMMA ? NC : 1][2];
+#pragma unroll
+  for (int i = 0; i < NC; ++i) {
+    const int c = i * T + t;
+    xv[i] = rv[i] = make_uint4(0, 0, 0, 0);
+    if (c < pieces) {
+      xv[i] = x[c];
+      if (p.residual) rv[i] = r[c];
+      if constexpr (GAMMA) {
+        gv[i][0] = reinterpret_cast<const float4*>(p.gamma)[2 * c];
+        gv[i][1] = reinterpret_cast<const float4*>(p.gamma)[2 * c + 1];
+      }
+    }
+  }
   float h[NC][8];
   float ss = 0.f;
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
-    const int c = i * T + t;
-    uint4 u = make_uint4(0, 0, 0, 0), v = u;
-    if (c < pieces) {
-      u = x[c];
-      if (p.residual) v = r[c];
-    }
     float add[8];
-    unpack8(u, h[i]);
-    unpack8(v, add);
+    unpack8(xv[i], h[i]);
+    unpack8(rv[i], add);
 #pragma unroll
     for (int e = 0; e < 8; ++e) h[i][e] += add[e];
   }
@@ -181,7 +192,8 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_rows(const NormPara
           make_uint4(pack2(h[i][0], h[i][1]), pack2(h[i][2], h[i][3]), pack2(h[i][4], h[i][5]), pack2(h[i][6], h[i][7]));
     float y[8] = {};
     if (in) {
-      const float4 g0 = reinterpret_cast<const float4*>(p.gamma)[2 * c], g1 = reinterpret_cast<const float4*>(p.gamma)[2 * c + 1];
+      const float4 g0 = GAMMA ? gv[GAMMA ? i : 0][0] : reinterpret_cast<const float4*>(p.gamma)[2 * c];
+      const float4 g1 = GAMMA ? gv[GAMMA ? i : 0][1] : reinterpret_cast<const float4*>(p.gamma)[2 * c + 1];
       const float g[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] = h[i][e] * inv * g[e];
@@ -198,6 +210,13 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_rows(const NormPara
       if ((t & 15) == 0) p.scale[static_cast<long long>(c / 16) * p.M + row] = scale;
     }
   }
+}
+// A wave a row where there are rows enough to fill the card.
+constexpr int kManyRows = 1024;
+template <int T, int NC, bool GAMMA>
+void launch_norm(const NormParams& p, hipStream_t stream) {
+  constexpr int rows = T < 256 ? 256 / T : 1;
+  hipLaunchKernelGGL((rmsnorm_rows<T, NC, GAMMA>), dim3((p.M + rows - 1ll) / rows), dim3(T < 256 ? 256 : T), 0, stream, p);
 }
 
 // ---------------------------------------------------------------- product
@@ -350,7 +369,23 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
   const int r8 = lane >> 3, kc = ((lane & 7) ^ (4 * (w & 1) + (r8 >> 1))) * 16;
   const unsigned off0 = static_cast<unsigned>(r8) * p.K + kc;
   const int k_end = min(p.K, t1 * kBlock);
-  const auto rows8 = [&](const i32x4& rs, int row, int lds_row, int t, int buf, bool in_k) __attribute__((always_inline)) {
+  // A residual tile takes the place of the blocks after the last one: it is in LDS, laid out as the epilogue reads it, when
+  // the last products are done (read there it cost a round of 256 x 256 tiles 15 us).
+  const bool ring_r = G == 1 && p.mode == kEpiResidual && !p.part && p.width == 8 && p.N < (1 << 20) && nk >= ST;
+  constexpr int kCh = BN / 8;                                    // chunks of 8 values of a tile's row of 16 bits
+  const i32x4 rr = ring_r ? rsrc_of(p.R + static_cast<long long>(bm) * p.N, static_cast<unsigned>(rows_m) * p.N * 2) : ra;
+  const auto residual8 = [&](int lds_row, int buf) __attribute__((always_inline)) {
+    const int at = buf * kStage + lds_row * kBlock, row = at / (BN * 2) + lane / kCh;      // 1,024 bytes: 512 / BN rows
+    const int n = bn + ((lane % kCh) ^ (row & (kCh - 1))) * 8;
+    dma16(rr, lds0 + at, at < kTile && row < rows_m && n < p.N ? (static_cast<unsigned>(row) * p.N + n) * 2u : kOut);
+  };
+  const auto rows8 = [&](const i32x4& rs, int row, int lds_row, int t, int buf, bool in_k, auto tail) __attribute__((always_inline)) {
+    if constexpr (decltype(tail)::value) {
+      if (ring_r) {
+        residual8(lds_row, buf);
+        return;
+      }
+    }
     // rows past the end lie past the buffer's range
     dma16(rs, lds0 + (buf * G + kg) * kStage + lds_row * kBlock, in_k ? off0 + static_cast<unsigned>(row) * p.K + t * kBlock : kOut);
   };
@@ -364,12 +399,12 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
     }
   };
   // DMA u of the stage's first part, and of its second
-  const auto load_early = [&](int u, int t, int buf, int slot) __attribute__((always_inline)) {
+  const auto load_early = [&](int u, int t, int buf, int slot, auto tail) __attribute__((always_inline)) {
     const bool in_k = t * kBlock + kc < k_end;             // past the end of K, or of the part: zeros
     if (u < kWD) {
-      rows8(rb, 8 * (w + NW * u), BM + 8 * (w + NW * u), t, buf, in_k);
+      rows8(rb, 8 * (w + NW * u), BM + 8 * (w + NW * u), t, buf, in_k, tail);
     } else if (u < kEarly - 1) {
-      rows8(ra, x_row(u - kWD), x_row(u - kWD), t, buf, in_k);
+      rows8(ra, x_row(u - kWD), x_row(u - kWD), t, buf, in_k, tail);
     } else {
       const int s = w % (kScales / 64) * 64;            // more waves than pieces: the same again
       dma4(rsrc_of(p.xs + t * p.xs_stride + bm, static_cast<unsigned>(rows_m) * 4),
@@ -377,8 +412,8 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
            t < t1 ? static_cast<unsigned>(s + lane) * 4 : kOut);
     }
   };
-  const auto load_late = [&](int u, int t, int buf) __attribute__((always_inline)) {
-    rows8(ra, x_row(kXD - kLate + u), x_row(kXD - kLate + u), t, buf, t * kBlock + kc < k_end);
+  const auto load_late = [&](int u, int t, int buf, auto tail) __attribute__((always_inline)) {
+    rows8(ra, x_row(kXD - kLate + u), x_row(kXD - kLate + u), t, buf, t * kBlock + kc < k_end, tail);
   };
   // fragments: a lane has chunks g and g + 4 of row r
   const int at0 = r * kBlock + ((g ^ (r >> 1)) & 7) * 16, at1 = at0 ^ 64;
@@ -407,9 +442,9 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
 #pragma unroll
   for (int s = 0; s < ST; ++s) {
 #pragma unroll
-    for (int u = 0; u < kEarly; ++u) load_early(u, block_of(s), s, s);
+    for (int u = 0; u < kEarly; ++u) load_early(u, block_of(s), s, s, std::false_type{});
 #pragma unroll
-    for (int u = 0; u < kLate; ++u) load_late(u, block_of(s), s);
+    for (int u = 0; u < kLate; ++u) load_late(u, block_of(s), s, std::false_type{});
   }
   wait_loads<(ST - 1) * (kEarly + kLate)>();
   barrier();
@@ -448,7 +483,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
   // Stage k: its first fragments are in registers.  Before its last step a wave, which then holds the last fragments, meets
   // the others; what is left of the stage's buffer takes stage k + ST, and the last products run under the first reads of
   // stage k + 1.  With four steps they meet in mid-stage too: then every wave holds w's rows and has read half of x's.
-  for (int k = 0; k < nk; ++k) {
+  const auto stage = [&](int k, auto tail) __attribute__((always_inline)) {
     const int nxt = cur == ST - 1 ? 0 : cur + 1, ns = cs == kScaleSlots - 1 ? 0 : cs + 1, far = cs == 0 ? kScaleSlots - 1 : cs - 1;
     const float sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wscales), k & 63));
 #pragma unroll
@@ -499,12 +534,12 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
         if (at >= 0 && at < kSlots) {
 #pragma unroll
           for (int l = 0; l < kEarly; ++l)
-            if (l * kSlots / kEarly == at) load_early(l, block_of(k + ST), cur, far);
+            if (l * kSlots / kEarly == at) load_early(l, block_of(k + ST), cur, far, tail);
         }
         if (last) {
 #pragma unroll
           for (int l = 0; l < kLate; ++l)
-            if (l * NU / kLate == u) load_late(l, block_of(k + ST), cur);
+            if (l * NU / kLate == u) load_late(l, block_of(k + ST), cur, tail);
         }
         // the next step's x and the next stage's w are widened under the products, too
         if (kAhead && u == NU - 1) {
@@ -551,6 +586,13 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
     if ((k & 63) == 63 && k + 1 < nk) scales_from(k + 1);
     cur = nxt;
     cs = ns;
+  };
+  int k = 0;
+  if constexpr (G == 1) {
+    for (; k < nk - ST; ++k) stage(k, std::false_type{});
+    for (; k < nk; ++k) stage(k, std::true_type{});
+  } else {
+    for (; k < nk; ++k) stage(k, std::false_type{});
   }
   add(Q - 1, NU - 1);
   wait_loads<0>();                                     // those past the end: the epilogue uses the same LDS
@@ -655,8 +697,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
   // 16 bits: the tile goes through LDS, 16-byte chunk ch of row i in slot ch ^ (i mod the chunks of a row), so that rows leave
   // in whole lines; a residual tile comes in the same way first
   uint16_t* tile = reinterpret_cast<uint16_t*>(lds);
-  constexpr int kCh = BN / 8;
-  if (mode == kEpiResidual) {
+  if (mode == kEpiResidual && !ring_r) {
     with_width(p.width, [&](auto WC) __attribute__((always_inline)) {
       constexpr int W = decltype(WC)::value, kUnits = BN / W;
       typedef typename Unit<W>::type U;
@@ -1027,12 +1068,17 @@ pace_status_t pace_rmsnorm(const uint16_t* x, long long x_stride, const uint16_t
   PACE_REQUIRE(x_stride >= K && x_stride % 8 == 0 && x_stride < (1ll << 31), "pace_rmsnorm: row stride %lld (a multiple of 8, at least K=%d)", x_stride, K);
   PACE_REQUIRE(!residual || (residual_stride >= K && residual_stride % 8 == 0 && residual_stride < (1ll << 31)),
                "pace_rmsnorm: residual's row stride %lld (a multiple of 8, at least K=%d)", residual_stride, K);
-  PACE_REQUIRE(!too_many_threads(M, K <= 4096 ? 64 : K <= 16384 ? 256 : 1024), "pace_rmsnorm: too many rows (M=%d)", M);
+  PACE_REQUIRE(!too_many_threads(M, M >= kManyRows && K <= 4096 ? 64 : K <= 16384 ? 256 : 1024), "pace_rmsnorm: too many rows (M=%d)", M);
   const NormParams p{x, residual, gamma, sum, y, q, scale, x_stride, residual_stride, eps, M, K};
-  if (K <= 1024) hipLaunchKernelGGL((rmsnorm_rows<64, 2>), dim3((M + 3ll) / 4), dim3(256), 0, stream, p);
-  else if (K <= 4096) hipLaunchKernelGGL((rmsnorm_rows<64, 8>), dim3((M + 3ll) / 4), dim3(256), 0, stream, p);
-  else if (K <= 16384) hipLaunchKernelGGL((rmsnorm_rows<256, 8>), dim3(M), dim3(256), 0, stream, p);
-  else hipLaunchKernelGGL((rmsnorm_rows<1024, 8>), dim3(M), dim3(1024), 0, stream, p);
+  const bool many = M >= kManyRows;
+  if (many && K <= 1024) launch_norm<64, 2, false>(p, stream);
+  else if (many && K <= 2048) launch_norm<64, 4, false>(p, stream);
+  else if (many && K <= 4096) launch_norm<64, 8, false>(p, stream);
+  else if (K <= 2048) launch_norm<256, 1, true>(p, stream);
+  else if (K <= 4096) launch_norm<256, 2, true>(p, stream);
+  else if (K <= 8192) launch_norm<256, 4, false>(p, stream);
+  else if (K <= 16384) launch_norm<256, 8, false>(p, stream);
+  else launch_norm<1024, 8, false>(p, stream);
   return check_launch("pace_rmsnorm");
 }
 

@@ -728,6 +728,14 @@ def _matrix_arg(t: torch.Tensor, dtype, shape: tuple, device: int, name: str):
     return t.data_ptr(), (t.stride(0) if shape[0] > 1 else shape[1])
 
 
+def _output(t: Optional[torch.Tensor], like: torch.Tensor, dtype, shape: tuple, device: int, name: str):
+    """The caller's output tensor, or a new one beside `like`, and its address."""
+    if t is None:
+        t = like.new_empty(shape, dtype=dtype)
+        return t, t.data_ptr()
+    return t, _arg(t, dtype, shape, device, name)
+
+
 def quantize_fp8(x: torch.Tensor, rows: int = 1, out: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
     """x bf16 [M, K] (rows of any stride) to e4m3 codes [M, K] with a scale for each 128 neighbouring values of a row (rows=1:
     scale fp32 [ceil(K / 128), M], what gemm_fp8 takes for x) or for each 128 x 128 (rows=128: [ceil(M / 128), ceil(K / 128)],
@@ -738,13 +746,10 @@ def quantize_fp8(x: torch.Tensor, rows: int = 1, out: Optional[torch.Tensor] = N
     M, K = x.shape
     kb = (K + 127) // 128
     shape = (kb, M) if rows == 1 else ((M + 127) // 128, kb)
-    if out is None:
-        out = torch.empty((M, K), dtype=_E4M3, device=x.device)
-    if scale is None:
-        scale = torch.empty(shape, dtype=_F32, device=x.device)
     xp, xs = _matrix_arg(x, _BF16, (M, K), gpu, "x")
-    _call("pace_quantize_fp8", gpu, xp, xs, M, K, rows, _arg(out, _E4M3, (M, K), gpu, "out"),
-          _arg(scale, _F32, shape, gpu, "scale"))
+    out, op = _output(out, x, _E4M3, (M, K), gpu, "out")
+    scale, sp = _output(scale, x, _F32, shape, gpu, "scale")
+    _call("pace_quantize_fp8", gpu, xp, xs, M, K, rows, op, sp)
     return out, scale
 
 
@@ -761,24 +766,20 @@ def rmsnorm(x: torch.Tensor, gamma: torch.Tensor, residual: Optional[torch.Tenso
     M, K = x.shape
     kb = (K + 127) // 128
     xp, xs = _matrix_arg(x, _BF16, (M, K), gpu, "x")
-    rp, rs = None, 0
+    rp, rs, hp = None, 0, None
     if residual is None:
         sum_out = None
     else:
         rp, rs = _matrix_arg(residual, _BF16, (M, K), gpu, "residual")
-        if sum_out is None:
-            sum_out = torch.empty((M, K), dtype=_BF16, device=x.device)
-    kind = _E4M3 if bits == 8 else _BF16
-    if out is None:
-        out = torch.empty((M, K), dtype=kind, device=x.device)
-    y = _arg(out, kind, (M, K), gpu, "out")
+        sum_out, hp = _output(sum_out, x, _BF16, (M, K), gpu, "sum_out")
     if bits == 16:
-        scale = None
-    elif scale is None:
-        scale = torch.empty((kb, M), dtype=_F32, device=x.device)
-    _call("pace_rmsnorm", gpu, xp, xs, rp, rs, _arg(gamma, _F32, (K,), gpu, "gamma"), eps, M, K,
-          _arg(sum_out, _BF16, (M, K), gpu, "sum_out"), y if bits == 16 else None, y if bits == 8 else None,
-          _arg(scale, _F32, (kb, M), gpu, "scale"))
+        scale = qp = sp = None
+        out, yp = _output(out, x, _BF16, (M, K), gpu, "out")
+    else:
+        yp = None
+        out, qp = _output(out, x, _E4M3, (M, K), gpu, "out")
+        scale, sp = _output(scale, x, _F32, (kb, M), gpu, "scale")
+    _call("pace_rmsnorm", gpu, xp, xs, rp, rs, _arg(gamma, _F32, (K,), gpu, "gamma"), eps, M, K, hp, yp, qp, sp)
     return out, scale, sum_out
 
 
@@ -800,21 +801,17 @@ def gemm_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: t
     N = w.shape[0]
     kb = (K + 127) // 128
     cols = N // 2 if epilogue == 2 else N
-    kind = _E4M3 if bits == 8 else _BF16
     xsp, xss = _matrix_arg(x_scale, _F32, (kb, M), gpu, "x_scale")
-    if out is None:
-        out = torch.empty((M, cols), dtype=kind, device=x.device)
+    out, op = _output(out, x, _E4M3 if bits == 8 else _BF16, (M, cols), gpu, "out")
     if bits == 16:
-        out_scale = None
-    elif out_scale is None:
-        out_scale = torch.empty(((cols + 127) // 128, M), dtype=_F32, device=x.device)
+        out_scale = sp = None
+    else:
+        out_scale, sp = _output(out_scale, x, _F32, ((cols + 127) // 128, M), gpu, "out_scale")
     if workspace is None:
         need = (_lib or lib()).pace_gemm_fp8_workspace_size(M, N, K, bits, sums)
         if need:
-            workspace = torch.empty(need, dtype=_U8, device=x.device)
+            workspace = x.new_empty((need,), dtype=_U8)
     _call("pace_gemm_fp8", gpu, _arg(x, _E4M3, (M, K), gpu, "x"), xsp, xss, _arg(w, _E4M3, (N, K), gpu, "w"),
           _arg(w_scale, _F32, ((N + 127) // 128, kb), gpu, "w_scale"), _arg(bias, _F32, (N,), gpu, "bias"),
-          _arg(residual, _BF16, (M, cols), gpu, "residual"), _arg(out, kind, (M, cols), gpu, "out"),
-          _arg(out_scale, _F32, ((cols + 127) // 128, M), gpu, "out_scale"), M, N, K, epilogue, sums,
-          *_scratch(workspace, gpu))
+          _arg(residual, _BF16, (M, cols), gpu, "residual"), op, sp, M, N, K, epilogue, sums, *_scratch(workspace, gpu))
     return out, out_scale
