@@ -40,11 +40,9 @@ __device__ __forceinline__ void unpack8(uint4 u, float (&x)[8]) {
 // exponential and reciprocal units round once each: within 2^-21 of the value, and half the time of expf and a division.
 __device__ __forceinline__ float silu(float x) {
   constexpr float kL = 1.44269504f, kLo = 1.92596303e-8f, kLn2 = 0.693147181f;   // log2(e) = kL + kLo
-  const float c = __builtin_amdgcn_fmed3f(x, -200.f, 200.f);
+  const float c = __builtin_amdgcn_fmed3f(x, -200.f, 200.f);                     // past them e^-x is infinite, or 0 beside 1
   const float t = c * -kL, lo = fmaf(c, -kL, -t) - c * kLo;
-  float e = __builtin_amdgcn_exp2f(t);
-  e = fmaf(e, lo * kLn2, e);
-  return x * __builtin_amdgcn_rcpf(1.f + e);
+  return x * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(t), fmaf(lo, kLn2, 1.f), 1.f));
 }
 
 // What a value adds to its block's maximum: its magnitude, 0 where it is not finite.
@@ -80,6 +78,9 @@ __device__ __forceinline__ float max16(float x) {
   x = fmaxf(x, dpp_f32<kDppRowHalfMirror>(x));
   return fmaxf(x, dpp_f32<kDppRowMirror>(x));
 }
+
+// A launch has fewer than 2^32 threads.
+bool fits(long long groups, int threads) { return groups * threads < (1ll << 32); }
 
 // ---------------------------------------------------------------- quantisation
 struct QuantParams {
@@ -905,14 +906,11 @@ void launch_join(const Fp8Params& p, hipStream_t stream) {
 }
 template <typename T, int MI, int NI, int WM, int WN, int ST, int G = 1>
 void launch_tile(Fp8Params p, int splits, hipStream_t stream) {
-  if (p.cs && !p.part && (16 * NI * WN != 256 || G > 1)) return;   // no tile of these widths finishes 8 bits: the plan never asks for it
   p.tiles_m = (p.M + 16 * MI * WM - 1) / (16 * MI * WM);
   p.tiles_n = (p.N + 16 * NI * WN - 1) / (16 * NI * WN);
   p.splits = splits;
   hipLaunchKernelGGL((gemm_fp8_tile<T, MI, NI, WM, WN, ST, G>), dim3(static_cast<unsigned>(p.tiles_m) * p.tiles_n * splits), dim3(64 * WM * WN * G), 0, stream, p);
 }
-
-bool too_many_threads(long long groups, int threads) { return groups * threads >= (1ll << 32); }
 
 // What a product of M rows is made of: one launch or two (whole rounds of the largest tiles, and the rows that are left),
 // each of one kernel with K in `splits` parts.
@@ -931,24 +929,24 @@ struct Fp8Plan {
 // to 14,336, K in 1 to 12 parts, weights from memory): what the plan picks takes 1.03 times the best that was measured in the
 // mean, at most 1.26 times.  Of 21 tiles tried these are the ones without which that grows by half a percent or more.
 struct Fp8Tile {
-  int bm, bn, groups, per_cu;
+  int bm, bn, groups, per_cu, threads;
   bool wide;
   float fixed, stage, shared, round;
   void (*launch)(Fp8Params, int, hipStream_t);
 };
 const Fp8Tile kTiles[] = {
-    {256, 256, 1, 1, false, 3.92f, 1.481f, 0.000f, 8.72f, launch_tile<Codes, 8, 4, 2, 4, 2>},
-    {192, 128, 1, 1, false, 3.56f, 0.779f, 0.000f, 5.06f, launch_tile<Codes, 6, 2, 2, 4, 3>},
-    {160, 128, 1, 2, false, 1.04f, 0.835f, 0.424f, 7.23f, launch_tile<Codes, 5, 4, 2, 2, 2>},
-    {128, 128, 2, 1, false, 2.70f, 1.256f, 0.000f, 5.66f, launch_tile<Codes, 4, 4, 2, 2, 2, 2>},
-    {96, 128, 2, 1, false, 2.39f, 1.136f, 0.000f, 4.69f, launch_tile<Codes, 3, 4, 2, 2, 2, 2>},
-    {64, 128, 2, 1, false, 2.25f, 0.779f, 0.000f, 4.49f, launch_tile<Codes, 4, 2, 1, 4, 3, 2>},
-    {64, 64, 2, 1, false, 2.13f, 0.524f, 0.000f, 3.33f, launch_tile<Codes, 4, 1, 1, 4, 3, 2>},
-    {32, 64, 2, 2, false, 2.02f, 0.442f, 0.345f, 2.97f, launch_tile<Codes, 2, 1, 1, 4, 3, 2>},
-    {192, 256, 1, 1, true, 4.23f, 2.113f, 0.000f, 5.08f, launch_tile<Values, 6, 4, 2, 4, 2>},
-    {128, 256, 1, 1, true, 3.40f, 1.624f, 0.000f, 4.72f, launch_tile<Values, 4, 4, 2, 4, 2>},
-    {128, 128, 1, 2, true, 4.88f, 0.943f, 0.793f, 1.40f, launch_tile<Values, 4, 4, 2, 2, 2>},
-    {32, 64, 2, 2, true, 2.05f, 0.534f, 0.458f, 2.68f, launch_tile<Values, 2, 1, 1, 4, 3, 2>},
+    {256, 256, 1, 1, 512, false, 3.92f, 1.481f, 0.000f, 8.72f, launch_tile<Codes, 8, 4, 2, 4, 2>},
+    {192, 128, 1, 1, 512, false, 3.56f, 0.779f, 0.000f, 5.06f, launch_tile<Codes, 6, 2, 2, 4, 3>},
+    {160, 128, 1, 2, 256, false, 1.04f, 0.835f, 0.424f, 7.23f, launch_tile<Codes, 5, 4, 2, 2, 2>},
+    {128, 128, 2, 1, 512, false, 2.70f, 1.256f, 0.000f, 5.66f, launch_tile<Codes, 4, 4, 2, 2, 2, 2>},
+    {96, 128, 2, 1, 512, false, 2.39f, 1.136f, 0.000f, 4.69f, launch_tile<Codes, 3, 4, 2, 2, 2, 2>},
+    {64, 128, 2, 1, 512, false, 2.25f, 0.779f, 0.000f, 4.49f, launch_tile<Codes, 4, 2, 1, 4, 3, 2>},
+    {64, 64, 2, 1, 512, false, 2.13f, 0.524f, 0.000f, 3.33f, launch_tile<Codes, 4, 1, 1, 4, 3, 2>},
+    {32, 64, 2, 2, 512, false, 2.02f, 0.442f, 0.345f, 2.97f, launch_tile<Codes, 2, 1, 1, 4, 3, 2>},
+    {192, 256, 1, 1, 512, true, 4.23f, 2.113f, 0.000f, 5.08f, launch_tile<Values, 6, 4, 2, 4, 2>},
+    {128, 256, 1, 1, 512, true, 3.40f, 1.624f, 0.000f, 4.72f, launch_tile<Values, 4, 4, 2, 4, 2>},
+    {128, 128, 1, 2, 256, true, 4.88f, 0.943f, 0.793f, 1.40f, launch_tile<Values, 4, 4, 2, 2, 2>},
+    {32, 64, 2, 2, 512, true, 2.05f, 0.534f, 0.458f, 2.68f, launch_tile<Values, 2, 1, 1, 4, 3, 2>},
 };
 constexpr int kNumTiles = sizeof(kTiles) / sizeof(kTiles[0]);
 constexpr float kMemory = 4.0e6f;      // bytes per us of operands that come from memory once
@@ -969,6 +967,7 @@ float tile_time(const Fp8Tile& t, int rows, int N, int K, int splits) {
 }
 // gemm_fp8_few: a column's 8 waves take kb / 8 blocks one after the other; over many columns they read memory less well than the
 // tiles (one row of 28,672 columns of 3,584: 28 us against 22.6; of 3,584 columns 6.4 against 9.4 with parts and their join).
+bool join_fits(int rows, int N) { return fits((N + 1023ll) / 1024 * rows, 256); }
 float few_time(int rows, int N, int K) {
   const int kb = (K + kBlock - 1) / kBlock, blocks = (kb + kFewWaves - 1) / kFewWaves;
   const float n = (N + 15) / 16 / 256.f, work = 2.2f + (n > 1.f ? n : 1.f) * blocks * (0.854f + 0.0267f * rows);
@@ -976,11 +975,14 @@ float few_time(int rows, int N, int K) {
   return work > bytes ? work : bytes;
 }
 
-// The quickest single launch for these rows.
+// A tile whose columns hold whole blocks of 128 SwiGLU outputs quantises them itself.
+bool finishes_eight(const Fp8Tile& t) { return t.bn == 256 && t.groups == 1; }
+
+// The quickest single launch for these rows; 1e30: every one would take 2^32 threads.
 float plan_rows(int rows, int N, int K, bool eight, bool wide, Fp8Launch* out) {
   const int kb = (K + kBlock - 1) / kBlock;
   float best = 1e30f;
-  if (rows <= 16) {
+  if (rows <= 16 && fits((N + 15ll) / 16, 64 * kFewWaves) && (!eight || join_fits(rows, N))) {
     best = few_time(rows, N, K) + (eight ? join_time(rows, N, 1) : 0.f);
     *out = {-1, 0, rows, 1, eight};
   }
@@ -989,7 +991,8 @@ float plan_rows(int rows, int N, int K, bool eight, bool wide, Fp8Launch* out) {
     if (t.wide != wide || (t.bm > 32 && t.bm >= 2 * rows)) continue;
     for (int s = 1; s <= kMostSplits; ++s) {
       if (s > 1 && (2 * s > kb || static_cast<double>(s) * rows * N > kMostSums)) break;
-      const bool part = s > 1 || (eight && (t.bn != 256 || t.groups != 1));
+      const bool part = s > 1 || (eight && !finishes_eight(t));
+      if (!fits(tiles_of(t, rows, N) * s, t.threads) || (part && !join_fits(rows, N))) break;
       const float time = tile_time(t, rows, N, K, s) + (part ? join_time(rows, N, s) : 0.f);
       if (time < best) {
         best = time;
@@ -1002,19 +1005,21 @@ float plan_rows(int rows, int N, int K, bool eight, bool wide, Fp8Launch* out) {
 
 Fp8Plan plan_fp8(int M, int N, int K, bool eight, bool wide) {
   Fp8Plan a{};
-  a.runs = 1;
-  const float one = plan_rows(M, N, K, eight, wide, &a.run[0]);
+  float best = plan_rows(M, N, K, eight, wide, &a.run[0]);
+  a.runs = best < 1e30f ? 1 : 0;
+  best *= 0.98f;                                       // a second launch has to be worth it
   // The largest tiles come in rounds of 256; rows that would fill a small part of a last round may be quicker in a launch of
   // their own.
   for (int i = 0; i < kNumTiles; ++i) {
     const Fp8Tile& t = kTiles[i];
-    if (t.wide != wide || t.per_cu != 1 || t.groups != 1) continue;
+    if (t.wide != wide || t.per_cu != 1 || t.groups != 1 || (eight && !finishes_eight(t))) continue;
     const long long across = (N + t.bn - 1ll) / t.bn, rounds = tiles_of(t, M, N) / 256, down = rounds * 256 / across;
     const int rows = static_cast<int>(down * t.bm < M ? down * t.bm : M);
-    if (rounds < 1 || rows < 1 || rows >= M) continue;
+    if (rounds < 1 || rows < 1 || rows >= M || a.runs == 0 || !fits(rounds * 256, t.threads)) continue;
     Fp8Launch rest;
     const float two = tile_time(t, rows, N, K, 1) + plan_rows(M - rows, N, K, eight, wide, &rest);
-    if (two < 0.98f * one) {
+    if (two < best) {
+      best = two;
       rest.m0 = rows;
       a.run[0] = {i, 0, rows, 1, false};
       a.run[1] = rest;
@@ -1047,7 +1052,7 @@ pace_status_t pace_quantize_fp8(const uint16_t* x, long long x_stride, int M, in
   PACE_REQUIRE(x_stride >= K && x_stride % 8 == 0 && x_stride < (1ll << 31), "pace_quantize_fp8: row stride %lld (a multiple of 8, at least K=%d)", x_stride, K);
   const int kb = (K + kBlock - 1) / kBlock;
   const long long blocks = static_cast<long long>(rows == 1 ? M : (M + 127ll) / kBlock) * kb, groups = rows == 1 ? (blocks + 15) / 16 : blocks;
-  PACE_REQUIRE(!too_many_threads(groups, 256), "pace_quantize_fp8: too many blocks (M=%d K=%d)", M, K);
+  PACE_REQUIRE(fits(groups, 256), "pace_quantize_fp8: too many blocks (M=%d K=%d)", M, K);
   const QuantParams p{x, q, scale, x_stride, M, K, kb};
   const dim3 grid(static_cast<unsigned>(groups)), th(256);
   if (rows == 1) hipLaunchKernelGGL(quantize_rows, grid, th, 0, stream, p);
@@ -1068,7 +1073,7 @@ pace_status_t pace_rmsnorm(const uint16_t* x, long long x_stride, const uint16_t
   PACE_REQUIRE(x_stride >= K && x_stride % 8 == 0 && x_stride < (1ll << 31), "pace_rmsnorm: row stride %lld (a multiple of 8, at least K=%d)", x_stride, K);
   PACE_REQUIRE(!residual || (residual_stride >= K && residual_stride % 8 == 0 && residual_stride < (1ll << 31)),
                "pace_rmsnorm: residual's row stride %lld (a multiple of 8, at least K=%d)", residual_stride, K);
-  PACE_REQUIRE(!too_many_threads(M, M >= kManyRows && K <= 4096 ? 64 : K <= 16384 ? 256 : 1024), "pace_rmsnorm: too many rows (M=%d)", M);
+  PACE_REQUIRE(fits(M, M >= kManyRows && K <= 4096 ? 64 : K <= 16384 ? 256 : 1024), "pace_rmsnorm: too many rows (M=%d)", M);
   const NormParams p{x, residual, gamma, sum, y, q, scale, x_stride, residual_stride, eps, M, K};
   const bool many = M >= kManyRows;
   if (many && K <= 1024) launch_norm<64, 2, false>(p, stream);
@@ -1101,11 +1106,9 @@ pace_status_t pace_gemm_fp8(const uint8_t* x, const float* x_scale, long long x_
   PACE_REQUIRE(aligned16(x) && aligned16(w), "pace_gemm_fp8: x and w must be 16-byte aligned");
   PACE_REQUIRE(!c_scale || aligned16(C), "pace_gemm_fp8: codes of the output must be 16-byte aligned");
   PACE_REQUIRE(x_scale_stride >= M && x_scale_stride < (1ll << 40), "pace_gemm_fp8: x_scale_stride %lld < M=%d, or past 2^40", x_scale_stride, M);
-  // the smallest tile's workgroups, the join's and the parts' sums
-  PACE_REQUIRE(M <= kMostRows && N <= (1 << 30) && (M + 31ll) / 32 * ((N + 63ll) / 64) * 512 * kMostSplits < (1ll << 32) &&
-                   static_cast<long long>(M) * ((N + 1023ll) / 1024) * 256 < (1ll << 32),
-               "pace_gemm_fp8: too many rows or columns (M=%d N=%d)", M, N);
+  PACE_REQUIRE(M <= kMostRows && N <= (1 << 30), "pace_gemm_fp8: too many rows or columns (M=%d N=%d)", M, N);
   const Fp8Plan a = plan_fp8(M, N, K, c_scale != nullptr, fp8_wide(sums, c_scale != nullptr));
+  PACE_REQUIRE(a.runs > 0, "pace_gemm_fp8: too many rows or columns (M=%d N=%d)", M, N);
   if (a.bytes) {
     if (workspace == nullptr || workspace_bytes < a.bytes)
       return set_error(PACE_ERR_WORKSPACE, "pace_gemm_fp8: workspace %zu < %zu bytes", workspace_bytes, a.bytes);
