@@ -339,6 +339,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
   // DMAs of a wave and stage, 8 rows each: the first part (w's rows, those of x that the first half of the steps reads, and the
   // scales) is asked for in mid-stage, the second at the end
   constexpr bool kTwo = Q % 4 == 0;
+  constexpr bool kWhole = !kWide && G > 1 && 16 * (MI + NI) + 4 * MI * NI <= 128;
   constexpr int kWD = BN / 8 / NW, kXD = BM / 8 / NW, kLate = kTwo ? kXD / 2 : 0, kEarly = kWD + kXD - kLate + 1;
   static_assert(kWD * 8 * NW == BN && kXD * 8 * NW == BM && (!kTwo || kXD % 2 == 0) && NW % 2 == 0 && kBlock % (16 * NI) == 0 && kScales / 64 <= NW, "tile");
   constexpr int kRing = ST * G * kStage, kTile = BM * BN * 2, kJoin = (G - 1) * BM * BN * 4, kBoth = kTile > kJoin ? kTile : kJoin;
@@ -382,7 +383,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
   };
   const auto rows8 = [&](const i32x4& rs, int row, int lds_row, int t, int buf, bool in_k, auto tail) __attribute__((always_inline)) {
     if constexpr (decltype(tail)::value) {
-      if (ring_r) {
+      if (ring_r && t >= t1) {
         residual8(lds_row, buf);
         return;
       }
@@ -450,152 +451,239 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
   wait_loads<(ST - 1) * (kEarly + kLate)>();
   barrier();
 
-  T* const kind = nullptr;
-  T wf[NI], xa[MP];
-  i32x8 xr[2][MP];
-  float xsc[2][MP];
-#pragma unroll
-  for (int j = 0; j < NI; ++j) wf[j] = lift(frag(0, BM + wn + 16 * j), kind);
-#pragma unroll
-  for (int i = 0; i < MP; ++i) {
-    xr[0][i] = frag(0, wm + 16 * i);
-    xsc[0][i] = x_scale(0, i);
-    if (kAhead) xa[i] = lift(xr[0][i], kind);
-  }
   int cur = 0, cs = 0;                                 // the stage's buffer and scales
-  // What a unit of products has formed goes into acc in the next one, under its products.
-  f32x4 d[JP * MP];
-  float ds[MP];
+  if constexpr (kWhole) {
+    // Both operands of a stage are in registers before it begins: the next stage's are read under its products, and the stage
+    // opens with the one meeting at which its own buffer is free and the next one full.
+    constexpr int JW = NI % 2 == 0 ? 2 : 1, U = MI * NI / 2, kReads = MI + NI, kReadIn = U > 2 ? U * 3 / 4 : U;
+    T wf[2][NI];
+    T xf[2][MI];
+    float xsc[2][MI];
+    T* const kind = nullptr;
+    const auto read = [&](int l, auto to, int buf, int slot) __attribute__((always_inline)) {
+      constexpr int P = decltype(to)::value;
+      if (l < NI) {
+        wf[P][l] = lift(frag(buf, BM + wn + 16 * l), kind);
+      } else {
+        xf[P][l - NI] = lift(frag(buf, wm + 16 * (l - NI)), kind);
+        xsc[P][l - NI] = x_scale(slot, l - NI);
+      }
+    };
 #pragma unroll
-  for (int i = 0; i < MP; ++i) ds[i] = 0.f;
+    for (int l = 0; l < kReads; ++l) read(l, std::integral_constant<int, 0>{}, 0, 0);
+    // What a unit (two products) has formed goes into acc in the next one, under its products.
+    f32x4 d[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+    float ds[2] = {0.f, 0.f};
+    const auto add = [&](int u) __attribute__((always_inline)) {
 #pragma unroll
-  for (int t = 0; t < JP * MP; ++t) d[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const auto add = [&](int q, int u) __attribute__((always_inline)) {
+      for (int t = 0; t < 2; ++t) {
+        f32x4& to = JW == 2 ? acc[u / (NI / JW)][u % (NI / JW) * 2 + t] : acc[2 * u + t][0];
 #pragma unroll
-    for (int j = 0; j < JP; ++j)
-#pragma unroll
-      for (int i = 0; i < MP; ++i) {
-        f32x4& to = acc[q * MP + i][u * JP + j];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) to[e] = fmaf(ds[i], d[j * MP + i][e], to[e]);
+        for (int e = 0; e < 4; ++e) to[e] = fmaf(ds[t], d[t][e], to[e]);
         asm volatile("" : "+v"(to));                   // here, not behind the stage's branches
       }
-  };
-  // Stage k: its first fragments are in registers.  Before its last step a wave, which then holds the last fragments, meets
-  // the others; what is left of the stage's buffer takes stage k + ST, and the last products run under the first reads of
-  // stage k + 1.  With four steps they meet in mid-stage too: then every wave holds w's rows and has read half of x's.
-  const auto stage = [&](int k, auto tail) __attribute__((always_inline)) {
-    const int nxt = cur == ST - 1 ? 0 : cur + 1, ns = cs == kScaleSlots - 1 ? 0 : cs + 1, far = cs == 0 ? kScaleSlots - 1 : cs - 1;
-    const float sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wscales), k & 63));
+    };
+    const auto stage = [&](int k, auto from, auto tail) __attribute__((always_inline)) {
+      constexpr int P = decltype(from)::value;
+      const int nxt = cur == ST - 1 ? 0 : cur + 1, ns = cs == kScaleSlots - 1 ? 0 : cs + 1, far = cs == 0 ? kScaleSlots - 1 : cs - 1;
+      const float sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wscales), k & 63));
+      wait_loads<(ST - 2) * kEarly>();                 // the next stage has come, and this one's reads
+      barrier();
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
-      const bool last = q == Q - 1;
-      const int slot = q & 1, next_slot = last ? 0 : (q + 1) & 1;
-      float s[MP];
-      if (kTwo && q == Q / 2 - 1) {
-        // this stage's second part has come; in flight are the stages after it
-        wait_loads<(ST - 1) * (kEarly + kLate)>();
-        barrier();
-      }
-      if (last) {
-        // the next stage's first part has come
-        wait_loads<(ST - 2) * (kEarly + kLate) + (kTwo ? kLate + kEarly : 0)>();
-        barrier();
-      }
+      for (int u = 0; u < U; ++u) {
+        f32x4 c[2];
+        float s[2];
 #pragma unroll
-      for (int i = 0; i < MP; ++i) {
-        if (!kAhead) xa[i] = lift(xr[slot][i], kind);
-        s[i] = xsc[slot][i] * sw;
-      }
-      // past the end of K the reads bring anything, and nothing uses it
-#pragma unroll
-      for (int i = 0; i < MP; ++i) {
-        xr[next_slot][i] = frag(last ? nxt : cur, wm + 16 * (last ? i : (q + 1) * MP + i));
-        xsc[next_slot][i] = x_scale(last ? ns : cs, last ? i : (q + 1) * MP + i);
-      }
-      i32x8 wr[2 * JP];                                // the next stage's w before it is widened
-      T xn[MP];
-      if (last && kWide) {
-#pragma unroll
-        for (int j = 0; j < JP; ++j) wr[j] = frag(nxt, BM + wn + 16 * j);
-      }
-#pragma unroll
-      for (int u = 0; u < NU; ++u) {
-        f32x4 c[JP * MP];
-        dot_block<JP>(&wf[u * JP], xa, c);
-        if (last && kWide && u + 1 < NU) {
-#pragma unroll
-          for (int j = 0; j < JP; ++j) wr[((u + 1) & 1) * JP + j] = frag(nxt, BM + wn + 16 * ((u + 1) * JP + j));
+        for (int t = 0; t < 2; ++t) {
+          const int i = JW == 2 ? u / (NI / JW) : 2 * u + t, j = JW == 2 ? u % (NI / JW) * 2 + t : 0;
+          c[t] = mfma128(wf[P][j].v, xf[P][i].v);
+          s[t] = xsc[P][i] * sw;
         }
-        if (u) add(q, u - 1);
-        else add(q ? q - 1 : Q - 1, NU - 1);
-        // what the barriers have freed is asked for a piece at a time, behind the step's reads and under its products
-        constexpr int kSlots = kTwo ? (Q / 2) * NU : NU, kFirst = kTwo ? Q / 2 - 1 : Q - 1;
-        const int at = (q - kFirst) * NU + u;
-        if (at >= 0 && at < kSlots) {
+        add(u ? u - 1 : U - 1);
+        // past the end of K the reads bring anything, and nothing uses it
 #pragma unroll
-          for (int l = 0; l < kEarly; ++l)
-            if (l * kSlots / kEarly == at) load_early(l, block_of(k + ST), cur, far, tail);
+        for (int l = 0; l < kReads; ++l)
+          if (l * kReadIn / kReads == u) read(l, std::integral_constant<int, 1 - P>{}, nxt, ns);
+#pragma unroll
+        for (int l = 0; l < kEarly; ++l)
+          if (l * U / kEarly == u) load_early(l, block_of(k + ST), cur, far, tail);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          d[t] = c[t];
+          ds[t] = s[t];
         }
-        if (last) {
-#pragma unroll
-          for (int l = 0; l < kLate; ++l)
-            if (l * NU / kLate == u) load_late(l, block_of(k + ST), cur, tail);
-        }
-        // the next step's x and the next stage's w are widened under the products, too
-        if (kAhead && u == NU - 1) {
-#pragma unroll
-          for (int i = 0; i < MP; ++i) {
-            xn[i] = lift(xr[next_slot][i], kind);
-            pin(xn[i]);
-          }
-        }
-        if (last) {
-#pragma unroll
-          for (int j = 0; j < JP; ++j) {
-            T& to = wf[u * JP + j];
-            if constexpr (kWide) to = lift(wr[(u & 1) * JP + j], kind);
-            else to = lift(frag(nxt, BM + wn + 16 * (u * JP + j)), kind);
-            pin(to);
-          }
-        }
-#pragma unroll
-        for (int t = 0; t < JP * MP; ++t) d[t] = c[t];
-#pragma unroll
-        for (int i = 0; i < MP; ++i) ds[i] = s[i];
-        if constexpr (kWide) {
-          const int each = 1 + (kAhead && u == NU - 1 ? 2 : 0) + (last ? 4 : 0) + (kAhead ? 0 : 2);   // VALU work for each product
-#pragma unroll
-          for (int t = 0; t < 4 * JP * MP; ++t) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            if (each == 1) __builtin_amdgcn_sched_group_barrier(0x002, 1, 0);
-            else if (each == 3) __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
-            else if (each == 5) __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
-            else __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
-          }
-        } else {
-          __builtin_amdgcn_sched_group_barrier(0x008, JP * MP, 0);     // this unit's products first,
-          __builtin_amdgcn_sched_group_barrier(0x002, 4 * JP * MP, 0); // the sums of the one before under them
-        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);             // this unit's products first,
+        __builtin_amdgcn_sched_group_barrier(0x002, 8, 0);             // the sums of the one before under them
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (kAhead) {
-#pragma unroll
-        for (int i = 0; i < MP; ++i) xa[i] = xn[i];
-      }
+      if ((k & 63) == 63 && k + 1 < nk) scales_from(k + 1);
+      cur = nxt;
+      cs = ns;
+    };
+    const std::integral_constant<int, 0> even;
+    const std::integral_constant<int, 1> odd;
+    int k = 0;
+    const int plain = G == 1 ? nk - ST : nk;             // the stages after them ask for no block of K
+    for (; k + 1 < plain; k += 2) {
+      stage(k, even, std::false_type{});
+      stage(k + 1, odd, std::false_type{});
     }
-    if ((k & 63) == 63 && k + 1 < nk) scales_from(k + 1);
-    cur = nxt;
-    cs = ns;
-  };
-  int k = 0;
-  if constexpr (G == 1) {
-    for (; k < nk - ST; ++k) stage(k, std::false_type{});
-    for (; k < nk; ++k) stage(k, std::true_type{});
+    if constexpr (G == 1) {
+      for (; k < nk; ++k) {
+        if (k & 1) stage(k, odd, std::true_type{});
+        else stage(k, even, std::true_type{});
+      }
+    } else if (k < nk) {
+      stage(k, even, std::false_type{});
+    }
+    add(U - 1);
   } else {
-    for (; k < nk; ++k) stage(k, std::false_type{});
+    T* const kind = nullptr;
+    T wf[NI], xa[MP];
+    i32x8 xr[2][MP];
+    float xsc[2][MP];
+#pragma unroll
+    for (int j = 0; j < NI; ++j) wf[j] = lift(frag(0, BM + wn + 16 * j), kind);
+#pragma unroll
+    for (int i = 0; i < MP; ++i) {
+      xr[0][i] = frag(0, wm + 16 * i);
+      xsc[0][i] = x_scale(0, i);
+      if (kAhead) xa[i] = lift(xr[0][i], kind);
+    }
+    // What a unit of products has formed goes into acc in the next one, under its products.
+    f32x4 d[JP * MP];
+    float ds[MP];
+#pragma unroll
+    for (int i = 0; i < MP; ++i) ds[i] = 0.f;
+#pragma unroll
+    for (int t = 0; t < JP * MP; ++t) d[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const auto add = [&](int q, int u) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < JP; ++j)
+#pragma unroll
+        for (int i = 0; i < MP; ++i) {
+          f32x4& to = acc[q * MP + i][u * JP + j];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) to[e] = fmaf(ds[i], d[j * MP + i][e], to[e]);
+          asm volatile("" : "+v"(to));                   // here, not behind the stage's branches
+        }
+    };
+    // Stage k: its first fragments are in registers.  Before its last step a wave, which then holds the last fragments, meets
+    // the others; what is left of the stage's buffer takes stage k + ST, and the last products run under the first reads of
+    // stage k + 1.  With four steps they meet in mid-stage too: then every wave holds w's rows and has read half of x's.
+    const auto stage = [&](int k, auto tail) __attribute__((always_inline)) {
+      const int nxt = cur == ST - 1 ? 0 : cur + 1, ns = cs == kScaleSlots - 1 ? 0 : cs + 1, far = cs == 0 ? kScaleSlots - 1 : cs - 1;
+      const float sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wscales), k & 63));
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const bool last = q == Q - 1;
+        const int slot = q & 1, next_slot = last ? 0 : (q + 1) & 1;
+        float s[MP];
+        if (kTwo && q == Q / 2 - 1) {
+          // this stage's second part has come; in flight are the stages after it
+          wait_loads<(ST - 1) * (kEarly + kLate)>();
+          barrier();
+        }
+        if (last) {
+          // the next stage's first part has come
+          wait_loads<(ST - 2) * (kEarly + kLate) + (kTwo ? kLate + kEarly : 0)>();
+          barrier();
+        }
+#pragma unroll
+        for (int i = 0; i < MP; ++i) {
+          if (!kAhead) xa[i] = lift(xr[slot][i], kind);
+          s[i] = xsc[slot][i] * sw;
+        }
+        // past the end of K the reads bring anything, and nothing uses it
+#pragma unroll
+        for (int i = 0; i < MP; ++i) {
+          xr[next_slot][i] = frag(last ? nxt : cur, wm + 16 * (last ? i : (q + 1) * MP + i));
+          xsc[next_slot][i] = x_scale(last ? ns : cs, last ? i : (q + 1) * MP + i);
+        }
+        i32x8 wr[2 * JP];                                // the next stage's w before it is widened
+        T xn[MP];
+        if (last && kWide) {
+#pragma unroll
+          for (int j = 0; j < JP; ++j) wr[j] = frag(nxt, BM + wn + 16 * j);
+        }
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+          f32x4 c[JP * MP];
+          dot_block<JP>(&wf[u * JP], xa, c);
+          if (last && kWide && u + 1 < NU) {
+#pragma unroll
+            for (int j = 0; j < JP; ++j) wr[((u + 1) & 1) * JP + j] = frag(nxt, BM + wn + 16 * ((u + 1) * JP + j));
+          }
+          if (u) add(q, u - 1);
+          else add(q ? q - 1 : Q - 1, NU - 1);
+          // what the barriers have freed is asked for a piece at a time, behind the step's reads and under its products
+          constexpr int kSlots = kTwo ? (Q / 2) * NU : NU, kFirst = kTwo ? Q / 2 - 1 : Q - 1;
+          const int at = (q - kFirst) * NU + u;
+          if (at >= 0 && at < kSlots) {
+#pragma unroll
+            for (int l = 0; l < kEarly; ++l)
+              if (l * kSlots / kEarly == at) load_early(l, block_of(k + ST), cur, far, tail);
+          }
+          if (last) {
+#pragma unroll
+            for (int l = 0; l < kLate; ++l)
+              if (l * NU / kLate == u) load_late(l, block_of(k + ST), cur, tail);
+          }
+          // the next step's x and the next stage's w are widened under the products, too
+          if (kAhead && u == NU - 1) {
+#pragma unroll
+            for (int i = 0; i < MP; ++i) {
+              xn[i] = lift(xr[next_slot][i], kind);
+              pin(xn[i]);
+            }
+          }
+          if (last) {
+#pragma unroll
+            for (int j = 0; j < JP; ++j) {
+              T& to = wf[u * JP + j];
+              if constexpr (kWide) to = lift(wr[(u & 1) * JP + j], kind);
+              else to = lift(frag(nxt, BM + wn + 16 * (u * JP + j)), kind);
+              pin(to);
+            }
+          }
+#pragma unroll
+          for (int t = 0; t < JP * MP; ++t) d[t] = c[t];
+#pragma unroll
+          for (int i = 0; i < MP; ++i) ds[i] = s[i];
+          if constexpr (kWide) {
+            const int each = 1 + (kAhead && u == NU - 1 ? 2 : 0) + (last ? 4 : 0) + (kAhead ? 0 : 2);   // VALU work for each product
+#pragma unroll
+            for (int t = 0; t < 4 * JP * MP; ++t) {
+              __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+              if (each == 1) __builtin_amdgcn_sched_group_barrier(0x002, 1, 0);
+              else if (each == 3) __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+              else if (each == 5) __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+              else __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
+            }
+          } else {
+            __builtin_amdgcn_sched_group_barrier(0x008, JP * MP, 0);     // this unit's products first,
+            __builtin_amdgcn_sched_group_barrier(0x002, 4 * JP * MP, 0); // the sums of the one before under them
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (kAhead) {
+#pragma unroll
+          for (int i = 0; i < MP; ++i) xa[i] = xn[i];
+        }
+      }
+      if ((k & 63) == 63 && k + 1 < nk) scales_from(k + 1);
+      cur = nxt;
+      cs = ns;
+    };
+    int k = 0;
+    if constexpr (G == 1) {
+      for (; k < nk - ST; ++k) stage(k, std::false_type{});
+      for (; k < nk; ++k) stage(k, std::true_type{});
+    } else {
+      for (; k < nk; ++k) stage(k, std::false_type{});
+    }
+    add(Q - 1, NU - 1);
   }
-  add(Q - 1, NU - 1);
   wait_loads<0>();                                     // those past the end: the epilogue uses the same LDS
   if constexpr (G > 1) {
     __syncthreads();
@@ -924,10 +1012,10 @@ struct Fp8Plan {
   size_t bytes;
 };
 
-// The tiles' times in us: a launch's start and end, a stage of 128 k's (for each group of waves) alone on a CU and what every further
-// workgroup there adds to it, a round's end.  Fitted to 10,800 timings over 210 shapes (1 to 10,677 rows, 64 to 28,672 columns, K 128
-// to 14,336, K in 1 to 12 parts, weights from memory): what the plan picks takes 1.03 times the best that was measured in the
-// mean, at most 1.26 times.  Of 21 tiles tried these are the ones without which that grows by half a percent or more.
+// The tiles' times in us: a launch's start and end, a stage of 128 k's (for each group of waves) alone on a CU and what a further
+// workgroup there adds to it, a round's end.  Fitted to 8,500 timings over 210 shapes (1 to 10,677 rows, 64 to 28,672 columns, K 128
+// to 14,336, K in 1 to 12 parts, weights from memory): what the plan picks takes 1.02 times the best that was measured in the
+// mean, at most 1.3 times.  Of 26 tiles tried these are the ones that bring it there.
 struct Fp8Tile {
   int bm, bn, groups, per_cu, threads;
   bool wide;
@@ -935,26 +1023,27 @@ struct Fp8Tile {
   void (*launch)(Fp8Params, int, hipStream_t);
 };
 const Fp8Tile kTiles[] = {
-    {256, 256, 1, 1, 512, false, 3.92f, 1.481f, 0.000f, 8.72f, launch_tile<Codes, 8, 4, 2, 4, 2>},
-    {192, 128, 1, 1, 512, false, 3.56f, 0.779f, 0.000f, 5.06f, launch_tile<Codes, 6, 2, 2, 4, 3>},
-    {160, 128, 1, 2, 256, false, 1.04f, 0.835f, 0.424f, 7.23f, launch_tile<Codes, 5, 4, 2, 2, 2>},
-    {128, 128, 2, 1, 512, false, 2.70f, 1.256f, 0.000f, 5.66f, launch_tile<Codes, 4, 4, 2, 2, 2, 2>},
-    {96, 128, 2, 1, 512, false, 2.39f, 1.136f, 0.000f, 4.69f, launch_tile<Codes, 3, 4, 2, 2, 2, 2>},
-    {64, 128, 2, 1, 512, false, 2.25f, 0.779f, 0.000f, 4.49f, launch_tile<Codes, 4, 2, 1, 4, 3, 2>},
-    {64, 64, 2, 1, 512, false, 2.13f, 0.524f, 0.000f, 3.33f, launch_tile<Codes, 4, 1, 1, 4, 3, 2>},
-    {32, 64, 2, 2, 512, false, 2.02f, 0.442f, 0.345f, 2.97f, launch_tile<Codes, 2, 1, 1, 4, 3, 2>},
-    {192, 256, 1, 1, 512, true, 4.23f, 2.113f, 0.000f, 5.08f, launch_tile<Values, 6, 4, 2, 4, 2>},
-    {128, 256, 1, 1, 512, true, 3.40f, 1.624f, 0.000f, 4.72f, launch_tile<Values, 4, 4, 2, 4, 2>},
-    {128, 128, 1, 2, 256, true, 4.88f, 0.943f, 0.793f, 1.40f, launch_tile<Values, 4, 4, 2, 2, 2>},
-    {32, 64, 2, 2, 512, true, 2.05f, 0.534f, 0.458f, 2.68f, launch_tile<Values, 2, 1, 1, 4, 3, 2>},
+    {256, 256, 1, 1, 512, false, 2.73f, 1.426f, 0.000f, 10.52f, launch_tile<Codes, 8, 4, 2, 4, 2>},
+    {192, 256, 1, 1, 512, false, 3.28f, 1.324f, 0.000f, 7.43f, launch_tile<Codes, 6, 4, 2, 4, 2>},
+    {256, 128, 1, 1, 512, false, 3.29f, 0.890f, 0.000f, 7.03f, launch_tile<Codes, 4, 4, 4, 2, 3>},
+    {192, 128, 1, 1, 512, false, 3.02f, 0.734f, 0.000f, 5.73f, launch_tile<Codes, 3, 4, 4, 2, 3>},
+    {160, 128, 1, 2, 256, false, 1.70f, 0.817f, 0.429f, 7.04f, launch_tile<Codes, 5, 4, 2, 2, 2>},
+    {96, 128, 2, 1, 512, false, 2.02f, 1.111f, 0.000f, 4.81f, launch_tile<Codes, 3, 4, 2, 2, 2, 2>},
+    {64, 128, 2, 1, 512, false, 1.61f, 0.697f, 0.000f, 4.58f, launch_tile<Codes, 4, 2, 1, 4, 3, 2>},
+    {64, 64, 2, 1, 512, false, 1.55f, 0.487f, 0.000f, 3.40f, launch_tile<Codes, 4, 1, 1, 4, 3, 2>},
+    {32, 64, 2, 2, 512, false, 1.18f, 0.361f, 0.311f, 3.04f, launch_tile<Codes, 2, 1, 1, 4, 3, 2>},
+    {192, 256, 1, 1, 512, true, 2.65f, 2.048f, 0.000f, 7.06f, launch_tile<Values, 6, 4, 2, 4, 2>},
+    {128, 256, 1, 1, 512, true, 2.34f, 1.583f, 0.000f, 6.10f, launch_tile<Values, 4, 4, 2, 4, 2>},
+    {128, 128, 1, 2, 256, true, 3.93f, 0.903f, 0.823f, 3.05f, launch_tile<Values, 4, 4, 2, 2, 2>},
+    {32, 64, 2, 2, 512, true, 1.32f, 0.538f, 0.417f, 2.84f, launch_tile<Values, 2, 1, 1, 4, 3, 2>},
 };
 constexpr int kNumTiles = sizeof(kTiles) / sizeof(kTiles[0]);
-constexpr float kMemory = 4.0e6f;      // bytes per us of operands that come from memory once
+constexpr float kMemory = 5.0e6f;      // bytes per us of operands that come from memory once
 constexpr int kMostSplits = 12, kMostRows = 1 << 26;
 constexpr double kMostSums = 5e7;      // of the parts of K together
 
 long long tiles_of(const Fp8Tile& t, int rows, int N) { return (rows + t.bm - 1ll) / t.bm * ((N + t.bn - 1ll) / t.bn); }
-float join_time(int rows, int N, int splits) { return 2.8f + 1.3e-6f * splits * rows * static_cast<float>(N); }
+float join_time(int rows, int N, int splits) { return 2.9f + 1.1e-6f * splits * rows * static_cast<float>(N); }
 float tile_time(const Fp8Tile& t, int rows, int N, int K, int splits) {
   const int kb = (K + kBlock - 1) / kBlock, stages = ((kb + splits - 1) / splits + t.groups - 1) / t.groups;
   const long long n = tiles_of(t, rows, N) * splits, round = 256ll * t.per_cu;
@@ -962,8 +1051,8 @@ float tile_time(const Fp8Tile& t, int rows, int N, int K, int splits) {
   const int left = static_cast<int>((n - full * round + 255) / 256);      // workgroups of a CU in the last round
   const auto turn = [&](int there) { return stages * (t.stage + t.shared * (there - 1)) + t.round; };
   const float work = t.fixed + full * turn(t.per_cu) + (left ? turn(left) : 0.f);
-  const float bytes = 3.9f + (static_cast<float>(rows) * K + static_cast<float>(N) * K + 2.f * rows * N) / kMemory;
-  return work > bytes ? work : bytes;
+  const float bytes = 1.8f + (static_cast<float>(rows) * K + static_cast<float>(N) * K + 2.f * rows * N) / kMemory;
+  return sqrtf(work * work + bytes * bytes);
 }
 // gemm_fp8_few: a column's 8 waves take kb / 8 blocks one after the other; over many columns they read memory less well than the
 // tiles (one row of 28,672 columns of 3,584: 28 us against 22.6; of 3,584 columns 6.4 against 9.4 with parts and their join).
