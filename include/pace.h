@@ -31,7 +31,7 @@
  *     the host, synchronises the stream and checks it first, returning
  *     PACE_ERR_INVALID_ARG before any launch when it is inconsistent.
  *   - The library keeps no global mutable state other than the thread-local
- *     error message and, for pace_ddae_select_varlen_noalloc only, a static per-GPU
+ *     error message, the last sizes' plan of pace_gemm_fp8 (thread-local) and, for pace_ddae_select_varlen_noalloc only, a static per-GPU
  *     scratch array and the table of its device addresses, so independent calls (other
  *     than overlapping calls of that entry point on one GPU) may run concurrently on
  *     different streams.
@@ -567,7 +567,8 @@ pace_status_t pace_rmsnorm(const uint16_t* x, long long x_stride, const uint16_t
  * of the largest of them; their sums, and the blocks', are fp32.  PACE_SUMS_FAST takes that: 1.5e-5 of the result's size on
  * normal data, far below an output's rounding to 16 bits.  PACE_SUMS_WIDE turns the codes into 16-bit values first, whose
  * products are summed in fp32: half the matrix rate, the same time where the weights' bytes bound the call.
- * PACE_SUMS_AUTO: wide for 8-bit outputs, whose fp32 scales show the difference, fast for 16-bit ones.
+ * PACE_SUMS_AUTO: wide for 8-bit outputs, whose fp32 scales show the difference, fast for 16-bit ones.  Up to 16 rows may be
+ * summed wide whatever is asked for.
  */
 enum { PACE_SUMS_AUTO = 0, PACE_SUMS_FAST = 1, PACE_SUMS_WIDE = 2 };
 

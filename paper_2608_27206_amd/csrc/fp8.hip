@@ -79,6 +79,8 @@ __device__ __forceinline__ float max16(float x) {
   return fmaxf(x, dpp_f32<kDppRowMirror>(x));
 }
 
+template <typename T>
+bool whole(const T* p) { return reinterpret_cast<uintptr_t>(p) % sizeof(T) == 0; }   // lies at a multiple of its own size
 // A launch has fewer than 2^32 threads.
 bool fits(long long groups, int threads) { return groups * threads < (1ll << 32); }
 
@@ -325,6 +327,15 @@ __device__ __forceinline__ void with_width(int width, F f) {
   else if (width == 4) f(std::integral_constant<int, 4>{});
   else if (width == 2) f(std::integral_constant<int, 2>{});
   else f(std::integral_constant<int, 1>{});
+}
+
+// The bias of four neighbouring columns.
+__device__ __forceinline__ f32x4 bias4(const Fp8Params& p, int n) {
+  f32x4 b = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (p.bias && n + e < p.N) b[e] = p.bias[n + e];
+  return b;
 }
 
 template <typename T, int MI, int NI, int WM, int WN, int ST, int G>
@@ -727,10 +738,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
   if (p.bias) {
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
-      const int n = bn + wn + 16 * j + 4 * g;
-      f32x4 b;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) b[e] = n + e < p.N ? p.bias[n + e] : 0.f;
+      const f32x4 b = bias4(p, bn + wn + 16 * j + 4 * g);
 #pragma unroll
       for (int i = 0; i < MI; ++i) acc[i][j] += b;
     }
@@ -843,11 +851,9 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
 }
 
 // Four neighbouring columns (fewer at the row's end) of a row from their finished sums: bias, residual or SwiGLU, 16 bits.
-__device__ __forceinline__ void finish4(const Fp8Params& p, int m, int n, f32x4 y) {
+__device__ __forceinline__ void finish4(const Fp8Params& p, int m, int n, f32x4 y, f32x4 bias) {
   const bool whole = p.N % 4 == 0;
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (p.bias && n + e < p.N) y[e] += p.bias[n + e];
+  y += bias;
   uint16_t* C = static_cast<uint16_t*>(p.C);
   if (p.mode == kEpiSwiglu) {
     uint16_t* to = C + static_cast<long long>(m) * (p.N / 2) + n / 2;
@@ -899,7 +905,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void gemm_fp8_few(const Fp8Param
     for (int u = 0; u < 2; ++u) {
       in[i].w[u] = in[i].x[u] = u32x4{0, 0, 0, 0};
       if (k + 64 * u + 16 * g >= p.K) continue;
-      in[i].w[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(wrow + k + 64 * u));
+      in[i].w[u] = *reinterpret_cast<const u32x4*>(wrow + k + 64 * u);
       if (r < p.M) in[i].x[u] = *reinterpret_cast<const u32x4*>(xrow + k + 64 * u);
     }
     in[i].xs = r < p.M ? p.xs[b * p.xs_stride + r] : 0.f;
@@ -909,6 +915,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void gemm_fp8_few(const Fp8Param
 #pragma unroll
   for (int i = 0; i < D; ++i)
     if (w + i * W < p.kb) load(i, w + i * W);
+  f32x4 bias = {0.f, 0.f, 0.f, 0.f};                   // beside the weights: behind them it would be a wait of its own
+  if (!p.part && w == 0) bias = bias4(p, n0 + 4 * g);
   for (int b0 = w; b0 < p.kb; b0 += D * W) {
 #pragma unroll
     for (int i = 0; i < D; ++i) {
@@ -936,7 +944,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void gemm_fp8_few(const Fp8Param
   const int at = n0 + 4 * g;
   if (r >= p.M || at >= p.N) return;
   if (p.part) store4(p, p.part + static_cast<long long>(r) * p.N + at, at, acc);
-  else finish4(p, r, at, acc);
+  else finish4(p, r, at, acc, bias);
 }
 
 // Adds the parts of a split K in their order and finishes the output, four columns a thread.  With 8 bits a wave has the 256
@@ -945,6 +953,7 @@ __global__ __launch_bounds__(256) void fp8_join(const Fp8Params p) {
   const int cols = (p.N + 1023) / 1024;
   const int m = blockIdx.x / cols, n = ((blockIdx.x - m * cols) * 256 + threadIdx.x) * 4;
   if (n >= p.N && !p.cs) return;
+  const f32x4 bias = bias4(p, n);
   const float* from = p.part + static_cast<long long>(m) * p.N + n;
   const long long step = static_cast<long long>(p.M) * p.N;
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
@@ -965,12 +974,10 @@ __global__ __launch_bounds__(256) void fp8_join(const Fp8Params p) {
     }
   }
   if (!p.cs) {
-    finish4(p, m, n, y);
+    finish4(p, m, n, y, bias);
     return;
   }
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (p.bias && n < p.N) y[e] += p.bias[n + e];
+  y += bias;
   const float a = silu(y[0]) * y[1], b = silu(y[2]) * y[3];
   const float scale = scale_of(wave_reduce_dpp(fmaxf(magnitude(a), magnitude(b)), [](float u, float v) { return fmaxf(u, v); }));
   if (n >= p.N) return;
@@ -1092,7 +1099,7 @@ float plan_rows(int rows, int N, int K, bool eight, bool wide, Fp8Launch* out) {
   return best;
 }
 
-Fp8Plan plan_fp8(int M, int N, int K, bool eight, bool wide) {
+Fp8Plan make_plan(int M, int N, int K, bool eight, bool wide) {
   Fp8Plan a{};
   float best = plan_rows(M, N, K, eight, wide, &a.run[0]);
   a.runs = best < 1e30f ? 1 : 0;
@@ -1122,6 +1129,17 @@ Fp8Plan plan_fp8(int M, int N, int K, bool eight, bool wide) {
   return a;
 }
 
+// A call asks for the workspace's size and then runs: the plan, which takes 0.3 to 6 us, is made once for both.
+const Fp8Plan& plan_fp8(int M, int N, int K, bool eight, bool wide) {
+  static thread_local struct {
+    int M, N, K;
+    bool eight, wide;
+    Fp8Plan plan;
+  } last = {};
+  if (last.M != M || last.N != N || last.K != K || last.eight != eight || last.wide != wide) last = {M, N, K, eight, wide, make_plan(M, N, K, eight, wide)};
+  return last.plan;
+}
+
 bool fp8_wide(int sums, bool eight) { return sums == PACE_SUMS_AUTO ? eight : sums == PACE_SUMS_WIDE; }
 
 }  // namespace
@@ -1138,6 +1156,7 @@ pace_status_t pace_quantize_fp8(const uint16_t* x, long long x_stride, int M, in
   if (M == 0) return PACE_OK;
   PACE_REQUIRE(x && q && scale, "pace_quantize_fp8: null device pointer");
   PACE_REQUIRE(aligned16(x) && aligned16(q), "pace_quantize_fp8: x and q must be 16-byte aligned");
+  PACE_REQUIRE(whole(scale), "pace_quantize_fp8: scale must be aligned to its type");
   PACE_REQUIRE(x_stride >= K && x_stride % 8 == 0 && x_stride < (1ll << 31), "pace_quantize_fp8: row stride %lld (a multiple of 8, at least K=%d)", x_stride, K);
   const int kb = (K + kBlock - 1) / kBlock;
   const long long blocks = static_cast<long long>(rows == 1 ? M : (M + 127ll) / kBlock) * kb, groups = rows == 1 ? (blocks + 15) / 16 : blocks;
@@ -1159,6 +1178,7 @@ pace_status_t pace_rmsnorm(const uint16_t* x, long long x_stride, const uint16_t
   PACE_REQUIRE(x && gamma, "pace_rmsnorm: null device pointer");
   PACE_REQUIRE(aligned16(x) && aligned16(residual) && aligned16(gamma) && aligned16(sum) && aligned16(y) && aligned16(q),
                "pace_rmsnorm: tensors must be 16-byte aligned");
+  PACE_REQUIRE(whole(scale), "pace_rmsnorm: scale must be aligned to its type");
   PACE_REQUIRE(x_stride >= K && x_stride % 8 == 0 && x_stride < (1ll << 31), "pace_rmsnorm: row stride %lld (a multiple of 8, at least K=%d)", x_stride, K);
   PACE_REQUIRE(!residual || (residual_stride >= K && residual_stride % 8 == 0 && residual_stride < (1ll << 31)),
                "pace_rmsnorm: residual's row stride %lld (a multiple of 8, at least K=%d)", residual_stride, K);
@@ -1194,9 +1214,11 @@ pace_status_t pace_gemm_fp8(const uint8_t* x, const float* x_scale, long long x_
   PACE_REQUIRE(epilogue != 1 || residual != nullptr, "pace_gemm_fp8: residual epilogue without residual");
   PACE_REQUIRE(aligned16(x) && aligned16(w), "pace_gemm_fp8: x and w must be 16-byte aligned");
   PACE_REQUIRE(!c_scale || aligned16(C), "pace_gemm_fp8: codes of the output must be 16-byte aligned");
+  PACE_REQUIRE(whole(x_scale) && whole(w_scale) && whole(bias) && whole(c_scale) && whole(residual) && whole(static_cast<uint16_t*>(C)),
+               "pace_gemm_fp8: scales, bias, residual and C must be aligned to their types");
   PACE_REQUIRE(x_scale_stride >= M && x_scale_stride < (1ll << 40), "pace_gemm_fp8: x_scale_stride %lld < M=%d, or past 2^40", x_scale_stride, M);
   PACE_REQUIRE(M <= kMostRows && N <= (1 << 30), "pace_gemm_fp8: too many rows or columns (M=%d N=%d)", M, N);
-  const Fp8Plan a = plan_fp8(M, N, K, c_scale != nullptr, fp8_wide(sums, c_scale != nullptr));
+  const Fp8Plan& a = plan_fp8(M, N, K, c_scale != nullptr, fp8_wide(sums, c_scale != nullptr));
   PACE_REQUIRE(a.runs > 0, "pace_gemm_fp8: too many rows or columns (M=%d N=%d)", M, N);
   if (a.bytes) {
     if (workspace == nullptr || workspace_bytes < a.bytes)

@@ -157,9 +157,9 @@ def test_rmsnorm_of_zeros_and_of_values_that_are_not_finite():
 
 # ---------------------------------------------------------------- product
 SHAPES = [(1, 1, 16), (1, 64, 128), (2, 33, 144), (1, 4608, 3584), (8, 256, 272), (13, 1000, 1280), (16, 130, 4096), (17, 514, 400), (48, 384, 2064), (64, 128, 128),
-          (65, 1026, 640), (129, 257, 528), (200, 640, 3424), (257, 300, 256), (300, 2050, 1008)]
+          (65, 1026, 640), (129, 257, 528), (200, 640, 3424), (257, 300, 256), (300, 2050, 1008), (3, 100, 8976), (300, 520, 9200), (1100, 264, 8464)]
 LARGE = [(8, 20490, 656), (33, 2050, 1296), (48, 3584, 2576), (100, 4100, 2000), (200, 9000, 400), (300, 3600, 1296), (520, 3330, 4240),
-         (600, 1290, 4368), (700, 16390, 272), (775, 7552, 640), (2300, 4610, 1552), (1183, 512, 384), (1500, 3584, 2064), (1600, 2000, 1040), (3000, 6150, 2064), (4400, 4130, 1296)]
+         (600, 1290, 4368), (700, 16390, 272), (775, 7552, 640), (2300, 4610, 1552), (1183, 512, 384), (1183, 3590, 8720), (1500, 3584, 2064), (1600, 2000, 1040), (3000, 6150, 2064), (4400, 4130, 1296)]
 
 
 FAST, WIDE = 1, 2                                   # pace.SUMS_FAST, pace.SUMS_WIDE
