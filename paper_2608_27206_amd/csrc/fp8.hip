@@ -142,8 +142,9 @@ struct NormParams {
 
 // h = x + residual, y = h / sqrt(mean(h^2) + eps) * gamma: T threads a row, which stays in registers (NC pieces of 8
 // values a thread), so it is read once; 16 neighbouring lanes hold a block of 128, whose scale needs no more than them.
-// Bound by memory: 42,196 rows of 1,280 with the residual to 8 bits move 380 MB in 83 us (4.6 TB/s; a copy 5.1).  Few rows are
-// bound by the chain loads -> sum -> norm -> maximum -> store: they take 256 threads each, and gamma comes with the row (GAMMA).
+// Bound by memory: 42,196 rows of 1,280 with the residual to 8 bits move 380 MB in 74 us (5.1 TB/s, the rate of a copy), 10,677
+// of 3,584 268 MB in 50 (a wave a row, 64 values a lane: 58).  Few rows are bound by the chain loads -> sum -> norm -> maximum ->
+// store (one of 3,584: 3.8 us, 6.6 in a single wave): they take 256 threads each, and gamma comes with the row (GAMMA).
 template <int T, int NC, bool GAMMA>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_rows(const NormParams p) {
   constexpr int ROWS = T < 256 ? 256 / T : 1;
@@ -214,7 +215,9 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_rows(const NormPara
     }
   }
 }
-// A wave a row where there are rows enough to fill the card.
+// A wave a row where it holds few values and there are rows enough to fill the card (42,196 x 1,280: 76.9 us, 78.6 with 256
+// threads a row; 20,000 x 1,024: 28.5 and 34.5; 1,183 x 1,280: 6.9 and 6.3).  5,000 x 8,192: 52.8 us with 512 threads, 58.7 with
+// 256, 60.5 with 1,024.
 constexpr int kManyRows = 1024;
 template <int T, int NC, bool GAMMA>
 void launch_norm(const NormParams& p, hipStream_t stream) {
@@ -745,11 +748,12 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
   }
   __syncthreads();                                     // every wave has read its last stage
   const int mode = p.mode;
-  if constexpr (BN == 256 && G == 1) {
+  if constexpr (BN == 256) {
     if (p.cs) {
       // SwiGLU to 8 bits: the tile's 128 outputs of a row are a block
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
+        if (kg) break;
         float top = 0.f;
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
@@ -770,6 +774,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
       };
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
+        if (kg) break;
         const int row = wm + 16 * i + r;
         const float inv = 1.f / row_scale(row);
 #pragma unroll
@@ -1020,9 +1025,9 @@ struct Fp8Plan {
 };
 
 // The tiles' times in us: a launch's start and end, a stage of 128 k's (for each group of waves) alone on a CU and what a further
-// workgroup there adds to it, a round's end.  Fitted to 8,500 timings over 210 shapes (1 to 10,677 rows, 64 to 28,672 columns, K 128
+// workgroup there adds to it, a round's end.  Fitted to 13,800 timings over 210 shapes (1 to 10,677 rows, 64 to 28,672 columns, K 128
 // to 14,336, K in 1 to 12 parts, weights from memory): what the plan picks takes 1.02 times the best that was measured in the
-// mean, at most 1.3 times.  Of 26 tiles tried these are the ones that bring it there.
+// mean, at most 1.4 times (8-bit outputs 1.2).  Of 29 tiles tried these are the ones that bring it there.
 struct Fp8Tile {
   int bm, bn, groups, per_cu, threads;
   bool wide;
@@ -1039,10 +1044,12 @@ const Fp8Tile kTiles[] = {
     {64, 128, 2, 1, 512, false, 1.61f, 0.697f, 0.000f, 4.58f, launch_tile<Codes, 4, 2, 1, 4, 3, 2>},
     {64, 64, 2, 1, 512, false, 1.55f, 0.487f, 0.000f, 3.40f, launch_tile<Codes, 4, 1, 1, 4, 3, 2>},
     {32, 64, 2, 2, 512, false, 1.18f, 0.361f, 0.311f, 3.04f, launch_tile<Codes, 2, 1, 1, 4, 3, 2>},
-    {192, 256, 1, 1, 512, true, 2.65f, 2.048f, 0.000f, 7.06f, launch_tile<Values, 6, 4, 2, 4, 2>},
-    {128, 256, 1, 1, 512, true, 2.34f, 1.583f, 0.000f, 6.10f, launch_tile<Values, 4, 4, 2, 4, 2>},
-    {128, 128, 1, 2, 256, true, 3.93f, 0.903f, 0.823f, 3.05f, launch_tile<Values, 4, 4, 2, 2, 2>},
-    {32, 64, 2, 2, 512, true, 1.32f, 0.538f, 0.417f, 2.84f, launch_tile<Values, 2, 1, 1, 4, 3, 2>},
+    {192, 256, 1, 1, 512, true, 6.17f, 2.078f, 0.000f, 3.76f, launch_tile<Values, 6, 4, 2, 4, 2>},
+    {128, 256, 1, 1, 512, true, 4.93f, 1.574f, 0.000f, 3.91f, launch_tile<Values, 4, 4, 2, 4, 2>},
+    {64, 256, 1, 1, 256, true, 3.65f, 1.138f, 0.000f, 4.61f, launch_tile<Values, 4, 4, 1, 4, 3>},
+    {32, 256, 2, 1, 512, true, 2.03f, 1.472f, 0.000f, 3.66f, launch_tile<Values, 2, 4, 1, 4, 2, 2>},
+    {128, 128, 1, 2, 256, true, 6.03f, 0.904f, 0.733f, 1.45f, launch_tile<Values, 4, 4, 2, 2, 2>},
+    {32, 64, 2, 2, 512, true, 2.22f, 0.536f, 0.398f, 2.71f, launch_tile<Values, 2, 1, 1, 4, 3, 2>},
 };
 constexpr int kNumTiles = sizeof(kTiles) / sizeof(kTiles[0]);
 constexpr float kMemory = 5.0e6f;      // bytes per us of operands that come from memory once
@@ -1062,17 +1069,17 @@ float tile_time(const Fp8Tile& t, int rows, int N, int K, int splits) {
   return sqrtf(work * work + bytes * bytes);
 }
 // gemm_fp8_few: a column's 8 waves take kb / 8 blocks one after the other; over many columns they read memory less well than the
-// tiles (one row of 28,672 columns of 3,584: 28 us against 22.6; of 3,584 columns 6.4 against 9.4 with parts and their join).
+// tiles (one row of 28,672 columns of 3,584: 26 us against 22.6; of 3,584 columns 6.2 against 9.4 with parts and their join).
 bool join_fits(int rows, int N) { return fits((N + 1023ll) / 1024 * rows, 256); }
 float few_time(int rows, int N, int K) {
   const int kb = (K + kBlock - 1) / kBlock, blocks = (kb + kFewWaves - 1) / kFewWaves;
-  const float n = (N + 15) / 16 / 256.f, work = 2.2f + (n > 1.f ? n : 1.f) * blocks * (0.854f + 0.0267f * rows);
-  const float bytes = 2.5f + static_cast<float>(N) * K / 2.9e6f;
+  const float n = (N + 15) / 16 / 256.f, work = 2.f + (n > 1.f ? n : 1.f) * blocks * (0.77f + 0.024f * rows);
+  const float bytes = 2.5f + static_cast<float>(N) * K / 3.2e6f;
   return work > bytes ? work : bytes;
 }
 
 // A tile whose columns hold whole blocks of 128 SwiGLU outputs quantises them itself.
-bool finishes_eight(const Fp8Tile& t) { return t.bn == 256 && t.groups == 1; }
+bool finishes_eight(const Fp8Tile& t) { return t.bn == 256; }
 
 // The quickest single launch for these rows; 1e30: every one would take 2^32 threads.
 float plan_rows(int rows, int N, int K, bool eight, bool wide, Fp8Launch* out) {
@@ -1182,16 +1189,14 @@ pace_status_t pace_rmsnorm(const uint16_t* x, long long x_stride, const uint16_t
   PACE_REQUIRE(x_stride >= K && x_stride % 8 == 0 && x_stride < (1ll << 31), "pace_rmsnorm: row stride %lld (a multiple of 8, at least K=%d)", x_stride, K);
   PACE_REQUIRE(!residual || (residual_stride >= K && residual_stride % 8 == 0 && residual_stride < (1ll << 31)),
                "pace_rmsnorm: residual's row stride %lld (a multiple of 8, at least K=%d)", residual_stride, K);
-  PACE_REQUIRE(fits(M, M >= kManyRows && K <= 4096 ? 64 : K <= 16384 ? 256 : 1024), "pace_rmsnorm: too many rows (M=%d)", M);
+  PACE_REQUIRE(fits(M, M >= kManyRows && K <= 2048 ? 64 : K <= 4096 ? 256 : K <= 16384 ? 512 : 1024), "pace_rmsnorm: too many rows (M=%d)", M);
   const NormParams p{x, residual, gamma, sum, y, q, scale, x_stride, residual_stride, eps, M, K};
-  const bool many = M >= kManyRows;
-  if (many && K <= 1024) launch_norm<64, 2, false>(p, stream);
-  else if (many && K <= 2048) launch_norm<64, 4, false>(p, stream);
-  else if (many && K <= 4096) launch_norm<64, 8, false>(p, stream);
+  if (M >= kManyRows && K <= 1024) launch_norm<64, 2, false>(p, stream);
+  else if (M >= kManyRows && K <= 2048) launch_norm<64, 4, false>(p, stream);
   else if (K <= 2048) launch_norm<256, 1, true>(p, stream);
   else if (K <= 4096) launch_norm<256, 2, true>(p, stream);
-  else if (K <= 8192) launch_norm<256, 4, false>(p, stream);
-  else if (K <= 16384) launch_norm<256, 8, false>(p, stream);
+  else if (K <= 8192) launch_norm<512, 2, false>(p, stream);
+  else if (K <= 16384) launch_norm<512, 4, false>(p, stream);
   else launch_norm<1024, 8, false>(p, stream);
   return check_launch("pace_rmsnorm");
 }

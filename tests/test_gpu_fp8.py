@@ -91,7 +91,7 @@ def test_quantize_values_that_are_not_finite_zeros_and_extremes(rows):
 # ---------------------------------------------------------------- norm
 @pytest.mark.parametrize("bits", [8, 16])
 @pytest.mark.parametrize("M,K,residual,pad", [(1, 16, True, 0), (1, 3584, True, 0), (2, 144, False, 0), (4, 512, True, 8), (5, 528, True, 0), (7, 1024, False, 16), (33, 1040, True, 0),
-                                              (131, 1280, True, 0), (3, 4096, True, 0), (3, 4112, True, 8), (2, 16384, False, 0), (2, 16400, True, 0),
+                                              (131, 1280, True, 0), (3, 4096, True, 0), (3, 4112, True, 8), (2, 8192, True, 0), (2, 8208, True, 8), (2, 16384, False, 0), (2, 16400, True, 0), (1030, 144, True, 8), (1025, 1040, True, 0), (1026, 2064, False, 0),
                                               (1, 65536, True, 0)])
 def test_rmsnorm(M, K, residual, pad, bits):
     import torch
@@ -158,7 +158,7 @@ def test_rmsnorm_of_zeros_and_of_values_that_are_not_finite():
 # ---------------------------------------------------------------- product
 SHAPES = [(1, 1, 16), (1, 64, 128), (2, 33, 144), (1, 4608, 3584), (8, 256, 272), (13, 1000, 1280), (16, 130, 4096), (17, 514, 400), (48, 384, 2064), (64, 128, 128),
           (65, 1026, 640), (129, 257, 528), (200, 640, 3424), (257, 300, 256), (300, 2050, 1008), (3, 100, 8976), (300, 520, 9200), (1100, 264, 8464)]
-LARGE = [(8, 20490, 656), (33, 2050, 1296), (48, 3584, 2576), (100, 4100, 2000), (200, 9000, 400), (300, 3600, 1296), (520, 3330, 4240),
+LARGE = [(8, 20490, 656), (64, 13690, 1040), (100, 10010, 784), (33, 2050, 1296), (48, 3584, 2576), (100, 4100, 2000), (200, 9000, 400), (300, 3600, 1296), (520, 3330, 4240),
          (600, 1290, 4368), (700, 16390, 272), (775, 7552, 640), (2300, 4610, 1552), (1183, 512, 384), (1183, 3590, 8720), (1500, 3584, 2064), (1600, 2000, 1040), (3000, 6150, 2064), (4400, 4130, 1296)]
 
 
