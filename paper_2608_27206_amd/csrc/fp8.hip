@@ -37,7 +37,8 @@ __device__ __forceinline__ void unpack8(uint4 u, float (&x)[8]) {
   }
 }
 // x / (1 + e^-x).  The exponent x log2(e) is taken to twice 24 bits (its rounding alone would cost 2^-18 at x = -20), the
-// exponential and reciprocal units round once each: within 2^-21 of the value, and half the time of expf and a division.
+// exponential and reciprocal units round once each: within 2^-21 of the value (one under 2^-126 may come as 0), and half the time
+// of expf and a division.
 __device__ __forceinline__ float silu(float x) {
   constexpr float kL = 1.44269504f, kLo = 1.92596303e-8f, kLn2 = 0.693147181f;   // log2(e) = kL + kLo
   const float c = __builtin_amdgcn_fmed3f(x, -200.f, 200.f);                     // past them e^-x is infinite, or 0 beside 1

@@ -768,12 +768,15 @@ def rmsnorm(x: torch.Tensor, gamma: torch.Tensor, residual: Optional[torch.Tenso
     xp, xs = _matrix_arg(x, _BF16, (M, K), gpu, "x")
     rp, rs, hp = None, 0, None
     if residual is None:
-        sum_out = None
+        if sum_out is not None:
+            raise PaceError("sum_out is x + residual: it needs a residual")
     else:
         rp, rs = _matrix_arg(residual, _BF16, (M, K), gpu, "residual")
         sum_out, hp = _output(sum_out, x, _BF16, (M, K), gpu, "sum_out")
     if bits == 16:
-        scale = qp = sp = None
+        if scale is not None:
+            raise PaceError("a 16-bit output has no scale")
+        qp = sp = None
         out, yp = _output(out, x, _BF16, (M, K), gpu, "out")
     else:
         yp = None
@@ -804,7 +807,9 @@ def gemm_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: t
     xsp, xss = _matrix_arg(x_scale, _F32, (kb, M), gpu, "x_scale")
     out, op = _output(out, x, _E4M3 if bits == 8 else _BF16, (M, cols), gpu, "out")
     if bits == 16:
-        out_scale = sp = None
+        if out_scale is not None:
+            raise PaceError("a 16-bit output has no out_scale")
+        sp = None
     else:
         out_scale, sp = _output(out_scale, x, _F32, ((cols + 127) // 128, M), gpu, "out_scale")
     if workspace is None:

@@ -324,3 +324,18 @@ def test_no_rows():
     w, ws = pace.quantize_fp8(torch.ones((64, 256), dtype=torch.bfloat16, device="cuda"), rows=128)
     c, _ = pace.gemm_fp8(q, s, w, ws)
     assert c.shape == (0, 64)
+
+
+def test_outputs_that_nothing_would_fill_are_refused():
+    import torch
+    from paper_2608_27206_amd import pace
+    x = torch.ones((4, 256), dtype=torch.bfloat16, device="cuda")
+    g = torch.ones(256, device="cuda")
+    with pytest.raises(pace.PaceError, match="residual"):
+        pace.rmsnorm(x, g, sum_out=torch.empty_like(x))
+    with pytest.raises(pace.PaceError, match="scale"):
+        pace.rmsnorm(x, g, bits=16, scale=torch.empty((2, 4), device="cuda"))
+    q, s = pace.quantize_fp8(x)
+    w, ws = pace.quantize_fp8(torch.ones((64, 256), dtype=torch.bfloat16, device="cuda"), rows=128)
+    with pytest.raises(pace.PaceError, match="out_scale"):
+        pace.gemm_fp8(q, s, w, ws, epilogue=2, out_scale=torch.empty((1, 4), device="cuda"))
