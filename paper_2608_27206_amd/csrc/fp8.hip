@@ -318,6 +318,7 @@ __device__ __forceinline__ void dma4(i32x4 r, unsigned lds, unsigned voff) {
 // all but the last N of the wave's loads have arrived, and its LDS reads have returned
 template <int N>
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
 
 template <int W> struct Unit;
@@ -342,8 +343,151 @@ __device__ __forceinline__ f32x4 bias4(const Fp8Params& p, int n) {
   return b;
 }
 
-template <typename T, int MI, int NI, int WM, int WN, int ST, int G>
-__global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Params p) {
+// A wave's part of a tile (rows from m, columns from n) to 16 bits, from its registers: lanes trade pieces so that each has 8
+// neighbouring outputs of a row.  Every load that the wave has asked for has come before the first of them is stored.
+__device__ __forceinline__ void trade16(uint32_t& a, uint32_t& b) {
+  const auto y = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  a = y[0];
+  b = y[1];
+}
+__device__ __forceinline__ void trade32(uint32_t& a, uint32_t& b) {
+  const auto y = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  a = y[0];
+  b = y[1];
+}
+// SwiGLU of a lane's part of a row, in elements 0 and 1 of each tile, and the maximum over the wave's part.
+template <int NI>
+__device__ __forceinline__ float swiglu_tops(f32x4 (&y)[NI]) {
+  float top = 0.f;
+#pragma unroll
+  for (int j = 0; j < NI; ++j) {
+    y[j][0] = silu(y[j][0]) * y[j][1];
+    y[j][1] = silu(y[j][2]) * y[j][3];
+    top = fmaxf(top, fmaxf(magnitude(y[j][0]), magnitude(y[j][1])));
+  }
+  top = fmaxf(top, __shfl_xor(top, 16, 64));
+  return fmaxf(top, __shfl_xor(top, 32, 64));
+}
+// 8 bits: the WN waves that share a row hand their maxima on in top_of.
+template <int MI, int NI, int WN, int BM>
+__device__ __forceinline__ void finish_tile(const Fp8Params& p, f32x4 (&acc)[MI][NI], float (&top_of)[WN][BM], int wm, int m, int n, int r, int g, int wave) {
+  if (p.bias) {
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const f32x4 b = bias4(p, n + 16 * j + 4 * g);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) acc[i][j] += b;
+    }
+  }
+  const int rows = p.M - m;                            // N is under 2^20: a tile's offsets hold 32 bits
+  if (p.mode == kEpiSwiglu) {
+    static_assert(NI == 4, "lane group g ends with the 8 outputs of tile g");
+    const int cols = p.N / 2, c = n / 2 + 8 * g;
+    if constexpr (WN * NI == 16) {
+      if (p.cs) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+          const float top = swiglu_tops<NI>(acc[i]);
+          if (g == 0) top_of[wave % WN][wm + 16 * i + r] = top;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        __syncthreads();
+        wait_loads<0>();
+        uint8_t* const C = static_cast<uint8_t*>(p.C) + static_cast<long long>(m) * cols;
+        float* const cs = p.cs + n / 256 * p.cs_stride + m;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+          const int row = 16 * i + r;
+          float top = top_of[0][wm + row];
+#pragma unroll
+          for (int o = 1; o < WN; ++o) top = fmaxf(top, top_of[o][wm + row]);
+          const float scale = scale_of(top), inv = 1.f / scale;
+          uint32_t a = to_e4m3(acc[i][0][0], acc[i][0][1], acc[i][1][0], acc[i][1][1], inv);
+          uint32_t b = to_e4m3(acc[i][2][0], acc[i][2][1], acc[i][3][0], acc[i][3][1], inv);
+          trade32(a, b);
+          uint32_t even = (a & 0xffffu) | b << 16, odd = a >> 16 | (b & 0xffff0000u);
+          trade16(even, odd);
+          const uint2 v = make_uint2((even & 0xffffu) | odd << 16, even >> 16 | (odd & 0xffff0000u));
+          if (row < rows && c < cols) *reinterpret_cast<uint2*>(C + static_cast<unsigned>(row * cols + c)) = v;
+          if (row < rows && wave % WN == 0 && g == 0) cs[row] = scale;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        return;
+      }
+    }
+    uint16_t* const C = static_cast<uint16_t*>(p.C) + static_cast<long long>(m) * cols;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      uint32_t u[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) u[j] = pack2(silu(acc[i][j][0]) * acc[i][j][1], silu(acc[i][j][2]) * acc[i][j][3]);
+      trade16(u[0], u[1]);
+      trade16(u[2], u[3]);
+      trade32(u[0], u[2]);
+      trade32(u[1], u[3]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][0][j] = __uint_as_float(u[j]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    wait_loads<0>();
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int row = 16 * i + r;
+      if (row < rows && c < cols) *reinterpret_cast<f32x4*>(C + static_cast<unsigned>(row * cols + c)) = acc[i][0];
+    }
+    return;
+  }
+  const int c = n + 16 * (g & 1) + 8 * (g >> 1);
+  uint16_t* const C = static_cast<uint16_t*>(p.C) + static_cast<long long>(m) * p.N;
+  const bool with = p.mode == kEpiResidual;
+  const uint16_t* const R = with ? p.R + static_cast<long long>(m) * p.N : nullptr;
+  constexpr int kDeep = MI % 4 == 0 ? 4 : 3;           // rows of tiles whose residual is in flight
+  uint4 res[kDeep][NI / 2];
+  const auto ask = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < NI; j += 2) {
+      const int row = 16 * i + r;
+      uint4 u = make_uint4(0, 0, 0, 0);
+      if (row < rows && c + 16 * j < p.N) u = *reinterpret_cast<const uint4*>(R + static_cast<unsigned>(row * p.N + c + 16 * j));
+      res[i % kDeep][j / 2] = u;
+    }
+  };
+  if (with) {
+#pragma unroll
+    for (int i = 0; i < kDeep && i < MI; ++i) ask(i);
+  }
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+#pragma unroll
+    for (int j = 0; j < NI; j += 2) {
+      if (with) {
+        uint4 u = res[i % kDeep][j / 2];
+        trade16(u.x, u.z);
+        trade16(u.y, u.w);
+        acc[i][j] += f32x4{lo_bf16(u.x), hi_bf16(u.x), lo_bf16(u.y), hi_bf16(u.y)};
+        acc[i][j + 1] += f32x4{lo_bf16(u.z), hi_bf16(u.z), lo_bf16(u.w), hi_bf16(u.w)};
+      }
+      uint4 u = make_uint4(pack2(acc[i][j][0], acc[i][j][1]), pack2(acc[i][j][2], acc[i][j][3]), pack2(acc[i][j + 1][0], acc[i][j + 1][1]),
+                           pack2(acc[i][j + 1][2], acc[i][j + 1][3]));
+      trade16(u.x, u.z);
+      trade16(u.y, u.w);
+      acc[i][j] = f32x4{__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
+    }
+    if (with && i + kDeep < MI) ask(i + kDeep);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  wait_loads<0>();
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; j += 2) {
+      const int row = 16 * i + r;
+      if (row < rows && c + 16 * j < p.N) *reinterpret_cast<f32x4*>(C + static_cast<unsigned>(row * p.N + c + 16 * j)) = acc[i][j];
+    }
+}
+
+template <typename T, int MI, int NI, int WM, int WN, int ST, int G, bool RUN>
+__global__ __launch_bounds__(64 * WM * WN * G, MI * NI > 32 ? 1 : 2) void gemm_fp8_tile(const Fp8Params p) {
   constexpr int BM = 16 * MI * WM, BN = 16 * NI * WN, NW = WM * WN, TH = 64 * NW * G;
   constexpr int kScales = (BM + 63) / 64 * 64;                   // floats of a stage, whole DMAs of them
   constexpr int kStage = (BM + BN) * kBlock;                     // bytes of a stage
@@ -368,27 +512,33 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
   // share a few rows of x and a few of w in its L2
   const int per = p.tiles_m * p.tiles_n;
   const int lb = remap_block_id(blockIdx.x, gridDim.x);
-  const int split = lb / per, tl = lb - split * per;
-  const int gsz = 8 * p.tiles_n, grp = tl / gsz, in = tl - grp * gsz;
-  const int gm = min(8, p.tiles_m - 8 * grp);
-  const int tn = in / gm, tm = 8 * grp + (in - tn * gm);
-  const int bm = tm * BM, bn = tn * BN;
+  const int split = lb / per;
+  int bm, bn, rows_m;                                  // the tile whose operands are asked for
+  i32x4 ra, rb;
+  const auto take = [&](int tl) __attribute__((always_inline)) {
+    const int gsz = 8 * p.tiles_n, grp = tl / gsz, in = tl - grp * gsz;
+    const int gm = min(8, p.tiles_m - 8 * grp);
+    const int tn = in / gm, tm = 8 * grp + (in - tn * gm);
+    bm = tm * BM;
+    bn = tn * BN;
+    rows_m = min(BM, p.M - bm);
+    ra = rsrc_of(p.x + static_cast<long long>(bm) * p.K, static_cast<unsigned>(rows_m) * p.K);
+    rb = rsrc_of(p.w + static_cast<long long>(bn) * p.K, static_cast<unsigned>(min(BN, p.N - bn)) * p.K);
+  };
+  take(lb - split * per);
   const int t0 = static_cast<int>(static_cast<long long>(p.kb) * split / p.splits);
   const int t1 = static_cast<int>(static_cast<long long>(p.kb) * (split + 1) / p.splits);
   const int nk = (t1 - t0 + G - 1) / G;                // stages; a group of waves takes block t0 + G * stage + its number
   const auto block_of = [&](int stage) { return t0 + G * stage + kg; };
-  const int rows_m = min(BM, p.M - bm), rows_n = min(BN, p.N - bn);
-  const i32x4 ra = rsrc_of(p.x + static_cast<long long>(bm) * p.K, static_cast<unsigned>(rows_m) * p.K);
-  const i32x4 rb = rsrc_of(p.w + static_cast<long long>(bn) * p.K, static_cast<unsigned>(rows_n) * p.K);
   const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<unsigned long long>((lds_char*)(const void*)lds));
 
   // A DMA brings 8 rows; chunk c (16 bytes) of row r lies in slot c ^ ((r >> 1) & 7)
   const int r8 = lane >> 3, kc = ((lane & 7) ^ (4 * (w & 1) + (r8 >> 1))) * 16;
-  const unsigned off0 = static_cast<unsigned>(r8) * p.K + kc;
+  unsigned off0 = static_cast<unsigned>(r8) * p.K + kc;
   const int k_end = min(p.K, t1 * kBlock);
   // A residual tile takes the place of the blocks after the last one: it is in LDS, laid out as the epilogue reads it, when
   // the last products are done (read there it cost a round of 256 x 256 tiles 15 us).
-  const bool ring_r = G == 1 && p.mode == kEpiResidual && !p.part && p.width == 8 && p.N < (1 << 20) && nk >= ST;
+  const bool ring_r = G == 1 && !RUN && p.mode == kEpiResidual && !p.part && p.width == 8 && p.N < (1 << 20) && nk >= ST;
   constexpr int kCh = BN / 8;                                    // chunks of 8 values of a tile's row of 16 bits
   const i32x4 rr = ring_r ? rsrc_of(p.R + static_cast<long long>(bm) * p.N, static_cast<unsigned>(rows_m) * p.N * 2) : ra;
   const auto residual8 = [&](int lds_row, int buf) __attribute__((always_inline)) {
@@ -433,15 +583,18 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
     rows8(ra, x_row(kXD - kLate + u), x_row(kXD - kLate + u), t, buf, t * kBlock + kc < k_end, tail);
   };
   // fragments: a lane has chunks g and g + 4 of row r
-  const int at0 = r * kBlock + ((g ^ (r >> 1)) & 7) * 16, at1 = at0 ^ 64;
+  int at0 = r * kBlock + ((g ^ (r >> 1)) & 7) * 16;
   const auto frag = [&](int buf, int row) __attribute__((always_inline)) {
     const char* st = lds + (buf * G + kg) * kStage + row * kBlock;
-    const i32x4 a = *reinterpret_cast<const i32x4*>(st + at0), b = *reinterpret_cast<const i32x4*>(st + at1);
+    const i32x4 a = *reinterpret_cast<const i32x4*>(st + at0), b = *reinterpret_cast<const i32x4*>(st + (at0 ^ 64));
     return i32x8{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
   };
   const auto x_scale = [&](int slot, int i) __attribute__((always_inline)) { return scales[slot * G + kg][wm + 16 * i + r]; };
   // w's scales: one for the wave and block, 64 blocks in a register's lanes
-  const int nb = min(bn + wn, p.N - 1) / kBlock;
+  const auto scales_of = [&](int b) __attribute__((always_inline)) {
+    const int nb = min(bn + wn, p.N - 1) / kBlock;
+    return b < p.kb ? p.ws[static_cast<long long>(nb) * p.kb + b] : 0.f;
+  };
   float wscales = 0.f;
 
   f32x4 acc[MI][NI];
@@ -451,8 +604,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
     for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   const auto scales_from = [&](int stage) __attribute__((always_inline)) {
-    const int b = block_of(stage + lane);
-    wscales = b < p.kb ? p.ws[static_cast<long long>(nb) * p.kb + b] : 0.f;
+    wscales = scales_of(block_of(stage + lane));
     asm volatile("s_waitcnt vmcnt(0)" : "+v"(wscales));   // now, and not at every use for all loads in flight
   };
   scales_from(0);
@@ -463,7 +615,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
 #pragma unroll
     for (int u = 0; u < kLate; ++u) load_late(u, block_of(s), s, std::false_type{});
   }
-  wait_loads<(ST - 1) * (kEarly + kLate)>();
+  wait_loads<RUN ? 0 : (ST - 1) * (kEarly + kLate)>();
   barrier();
 
   int cur = 0, cs = 0;                                 // the stage's buffer and scales
@@ -557,14 +709,17 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
     T wf[NI], xa[MP];
     i32x8 xr[2][MP];
     float xsc[2][MP];
+    const auto begin = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < NI; ++j) wf[j] = lift(frag(0, BM + wn + 16 * j), kind);
+      for (int j = 0; j < NI; ++j) wf[j] = lift(frag(cur, BM + wn + 16 * j), kind);
 #pragma unroll
-    for (int i = 0; i < MP; ++i) {
-      xr[0][i] = frag(0, wm + 16 * i);
-      xsc[0][i] = x_scale(0, i);
-      if (kAhead) xa[i] = lift(xr[0][i], kind);
-    }
+      for (int i = 0; i < MP; ++i) {
+        xr[0][i] = frag(cur, wm + 16 * i);
+        xsc[0][i] = x_scale(cs, i);
+        if (kAhead) xa[i] = lift(xr[0][i], kind);
+      }
+    };
+    begin();
     // What a unit of products has formed goes into acc in the next one, under its products.
     f32x4 d[JP * MP];
     float ds[MP];
@@ -586,7 +741,13 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
     // Stage k: its first fragments are in registers.  Before its last step a wave, which then holds the last fragments, meets
     // the others; what is left of the stage's buffer takes stage k + ST, and the last products run under the first reads of
     // stage k + 1.  With four steps they meet in mid-stage too: then every wave holds w's rows and has read half of x's.
-    const auto stage = [&](int k, auto tail) __attribute__((always_inline)) {
+    // RUN: `ask` is the block that is asked for, perhaps of the next tile, whose first ST stages have come before this one's
+    // output left (FRESH: of the first ST stages, 1 and 2, all but the last know the next stage to be there; the last stage, 3, leaves
+    // the next one's fragments in LDS).
+    int ask = 0;
+    const auto stage = [&](int k, auto tail, auto fresh) __attribute__((always_inline)) {
+      constexpr int FRESH = decltype(fresh)::value;
+      const auto far_block = [&] { return RUN ? ask : block_of(k + ST); };
       const int nxt = cur == ST - 1 ? 0 : cur + 1, ns = cs == kScaleSlots - 1 ? 0 : cs + 1, far = cs == 0 ? kScaleSlots - 1 : cs - 1;
       const float sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wscales), k & 63));
 #pragma unroll
@@ -596,12 +757,14 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
         float s[MP];
         if (kTwo && q == Q / 2 - 1) {
           // this stage's second part has come; in flight are the stages after it
-          wait_loads<(ST - 1) * (kEarly + kLate)>();
+          if constexpr (FRESH == 1 || FRESH == 2) wait_reads();
+          else wait_loads<(ST - 1) * (kEarly + kLate)>();
           barrier();
         }
         if (last) {
           // the next stage's first part has come
-          wait_loads<(ST - 2) * (kEarly + kLate) + (kTwo ? kLate + kEarly : 0)>();
+          if constexpr (FRESH == 1) wait_reads();
+          else wait_loads<(ST - 2) * (kEarly + kLate) + (kTwo ? kLate + kEarly : 0)>();
           barrier();
         }
 #pragma unroll
@@ -612,12 +775,14 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
         // past the end of K the reads bring anything, and nothing uses it
 #pragma unroll
         for (int i = 0; i < MP; ++i) {
+          if (last && FRESH == 3) break;
           xr[next_slot][i] = frag(last ? nxt : cur, wm + 16 * (last ? i : (q + 1) * MP + i));
           xsc[next_slot][i] = x_scale(last ? ns : cs, last ? i : (q + 1) * MP + i);
         }
         i32x8 wr[2 * JP];                                // the next stage's w before it is widened
         T xn[MP];
-        if (last && kWide) {
+        const bool ahead = last && FRESH != 3;
+        if (ahead && kWide) {
 #pragma unroll
           for (int j = 0; j < JP; ++j) wr[j] = frag(nxt, BM + wn + 16 * j);
         }
@@ -625,7 +790,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
         for (int u = 0; u < NU; ++u) {
           f32x4 c[JP * MP];
           dot_block<JP>(&wf[u * JP], xa, c);
-          if (last && kWide && u + 1 < NU) {
+          if (ahead && kWide && u + 1 < NU) {
 #pragma unroll
             for (int j = 0; j < JP; ++j) wr[((u + 1) & 1) * JP + j] = frag(nxt, BM + wn + 16 * ((u + 1) * JP + j));
           }
@@ -637,22 +802,22 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
           if (at >= 0 && at < kSlots) {
 #pragma unroll
             for (int l = 0; l < kEarly; ++l)
-              if (l * kSlots / kEarly == at) load_early(l, block_of(k + ST), cur, far, tail);
+              if (l * kSlots / kEarly == at) load_early(l, far_block(), cur, far, tail);
           }
           if (last) {
 #pragma unroll
             for (int l = 0; l < kLate; ++l)
-              if (l * NU / kLate == u) load_late(l, block_of(k + ST), cur, tail);
+              if (l * NU / kLate == u) load_late(l, far_block(), cur, tail);
           }
           // the next step's x and the next stage's w are widened under the products, too
-          if (kAhead && u == NU - 1) {
+          if (kAhead && u == NU - 1 && (!last || ahead)) {
 #pragma unroll
             for (int i = 0; i < MP; ++i) {
               xn[i] = lift(xr[next_slot][i], kind);
               pin(xn[i]);
             }
           }
-          if (last) {
+          if (ahead) {
 #pragma unroll
             for (int j = 0; j < JP; ++j) {
               T& to = wf[u * JP + j];
@@ -681,7 +846,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
           }
           __builtin_amdgcn_sched_barrier(0);
         }
-        if (kAhead) {
+        if (kAhead && (!last || ahead)) {
 #pragma unroll
           for (int i = 0; i < MP; ++i) xa[i] = xn[i];
         }
@@ -690,12 +855,63 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
       cur = nxt;
       cs = ns;
     };
+    const std::integral_constant<int, 0> plain;
+    if constexpr (RUN) {
+      const std::integral_constant<int, 1> first;
+      const std::integral_constant<int, 2> second;
+      const std::integral_constant<int, 3> end;
+      for (int done = gridDim.x;; done += gridDim.x) {
+        const int to_m = bm, to_n = bn;
+        int to_r = r, to_g = g;
+        asm volatile("" : "+v"(off0), "+v"(at0), "+v"(to_r), "+v"(to_g));   // addresses formed anew, not kept while the output leaves
+        for (int k = 0; k < ST - 1; ++k) {
+          ask = k + ST;
+          stage(k, std::false_type{}, first);
+        }
+        ask = 2 * ST - 1;
+        stage(ST - 1, std::false_type{}, second);
+        for (int k = ST; k < nk - ST; ++k) {
+          ask = k + ST;
+          stage(k, std::false_type{}, plain);
+        }
+        // the operands of the workgroup's next tile, or nothing
+        const int left = min(per - done, static_cast<int>(gridDim.x));
+        const bool more = static_cast<int>(blockIdx.x) < left;
+        if (more) {
+          take(done + remap_block_id(blockIdx.x, left));
+        } else {
+          rows_m = 0;
+          ra.z = rb.z = 0;
+        }
+        float next = scales_of(lane);
+        for (int k = nk - ST; k < nk - 1; ++k) {
+          ask = k + ST - nk;
+          stage(k, std::false_type{}, plain);
+        }
+        ask = ST - 1;
+        stage(nk - 1, std::false_type{}, end);
+        add(Q - 1, NU - 1);
+        finish_tile<MI, NI, WN, BM>(p, acc, top_of, wm, to_m + wm, to_n + wn, to_r, to_g, w);
+        if (!more) return;
+        asm volatile("" : "+v"(next));
+        wscales = next;
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < MP; ++i) ds[i] = 0.f;
+#pragma unroll
+        for (int t = 0; t < JP * MP; ++t) d[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        begin();
+      }
+    }
     int k = 0;
     if constexpr (G == 1) {
-      for (; k < nk - ST; ++k) stage(k, std::false_type{});
-      for (; k < nk; ++k) stage(k, std::true_type{});
+      for (; k < nk - ST; ++k) stage(k, std::false_type{}, plain);
+      for (; k < nk; ++k) stage(k, std::true_type{}, plain);
     } else {
-      for (; k < nk; ++k) stage(k, std::false_type{});
+      for (; k < nk; ++k) stage(k, std::false_type{}, plain);
     }
     add(Q - 1, NU - 1);
   }
@@ -755,15 +971,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
         if (kg) break;
-        float top = 0.f;
-#pragma unroll
-        for (int j = 0; j < NI; ++j) {
-          acc[i][j][0] = silu(acc[i][j][0]) * acc[i][j][1];
-          acc[i][j][1] = silu(acc[i][j][2]) * acc[i][j][3];
-          top = fmaxf(top, fmaxf(magnitude(acc[i][j][0]), magnitude(acc[i][j][1])));
-        }
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float top = swiglu_tops<NI>(acc[i]);
         if (g == 0) top_of[w % WN][wm + 16 * i + r] = top;
       }
       __syncthreads();
@@ -1005,12 +1213,23 @@ void launch_few(const Fp8Params& p, hipStream_t stream) {
 void launch_join(const Fp8Params& p, hipStream_t stream) {
   hipLaunchKernelGGL(fp8_join, dim3((p.N + 1023) / 1024 * p.M), dim3(256), 0, stream, p);
 }
-template <typename T, int MI, int NI, int WM, int WN, int ST, int G = 1>
+template <typename T, int MI, int NI, int WM, int WN, int ST, int G = 1, bool RUN = false>
 void launch_tile(Fp8Params p, int splits, hipStream_t stream) {
   p.tiles_m = (p.M + 16 * MI * WM - 1) / (16 * MI * WM);
   p.tiles_n = (p.N + 16 * NI * WN - 1) / (16 * NI * WN);
   p.splits = splits;
-  hipLaunchKernelGGL((gemm_fp8_tile<T, MI, NI, WM, WN, ST, G>), dim3(static_cast<unsigned>(p.tiles_m) * p.tiles_n * splits), dim3(64 * WM * WN * G), 0, stream, p);
+  if constexpr (RUN) {
+    // A workgroup for each CU, one tile after another: 10,677 x 28,672 x 3,584 with SwiGLU 970 us (1,012 with a workgroup a tile),
+    // its 8-bit output 1,740 (1,773); 1,183 x 4,608 x 3,584, one tile a workgroup, 27.8 (28.8).  A residual that ends K's ring is
+    // quicker than one that its rows wait for until a few tiles have followed each other (39,168 x 1,280 x 3,424, three,
+    // 207 and 219; 10,677 x 3,584 x 3,584, two and a part, 172 and 162).
+    const long long tiles = static_cast<long long>(p.tiles_m) * p.tiles_n;
+    if (splits == 1 && !p.part && (p.cs || p.width == 8) && p.N < (1 << 20) && p.kb >= 2 * ST && (p.mode != kEpiResidual || tiles > 640)) {
+      hipLaunchKernelGGL((gemm_fp8_tile<T, MI, NI, WM, WN, ST, G, true>), dim3(tiles < 256 ? static_cast<unsigned>(tiles) : 256), dim3(64 * WM * WN * G), 0, stream, p);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((gemm_fp8_tile<T, MI, NI, WM, WN, ST, G, false>), dim3(static_cast<unsigned>(p.tiles_m) * p.tiles_n * splits), dim3(64 * WM * WN * G), 0, stream, p);
 }
 
 // What a product of M rows is made of: one launch or two (whole rounds of the largest tiles, and the rows that are left),
@@ -1036,17 +1255,17 @@ struct Fp8Tile {
   void (*launch)(Fp8Params, int, hipStream_t);
 };
 const Fp8Tile kTiles[] = {
-    {256, 256, 1, 1, 512, false, 2.73f, 1.426f, 0.000f, 10.52f, launch_tile<Codes, 8, 4, 2, 4, 2>},
-    {192, 256, 1, 1, 512, false, 3.28f, 1.324f, 0.000f, 7.43f, launch_tile<Codes, 6, 4, 2, 4, 2>},
-    {256, 128, 1, 1, 512, false, 3.29f, 0.890f, 0.000f, 7.03f, launch_tile<Codes, 4, 4, 4, 2, 3>},
-    {192, 128, 1, 1, 512, false, 3.02f, 0.734f, 0.000f, 5.73f, launch_tile<Codes, 3, 4, 4, 2, 3>},
+    {256, 256, 1, 1, 512, false, 2.73f, 1.426f, 0.000f, 10.52f, launch_tile<Codes, 8, 4, 2, 4, 2, 1, true>},
+    {192, 256, 1, 1, 512, false, 3.28f, 1.324f, 0.000f, 7.43f, launch_tile<Codes, 6, 4, 2, 4, 2, 1, true>},
+    {256, 128, 1, 1, 512, false, 3.29f, 0.890f, 0.000f, 7.03f, launch_tile<Codes, 4, 4, 4, 2, 3, 1, true>},
+    {192, 128, 1, 1, 512, false, 3.02f, 0.734f, 0.000f, 5.73f, launch_tile<Codes, 3, 4, 4, 2, 3, 1, true>},
     {160, 128, 1, 2, 256, false, 1.70f, 0.817f, 0.429f, 7.04f, launch_tile<Codes, 5, 4, 2, 2, 2>},
     {96, 128, 2, 1, 512, false, 2.02f, 1.111f, 0.000f, 4.81f, launch_tile<Codes, 3, 4, 2, 2, 2, 2>},
     {64, 128, 2, 1, 512, false, 1.61f, 0.697f, 0.000f, 4.58f, launch_tile<Codes, 4, 2, 1, 4, 3, 2>},
     {64, 64, 2, 1, 512, false, 1.55f, 0.487f, 0.000f, 3.40f, launch_tile<Codes, 4, 1, 1, 4, 3, 2>},
     {32, 64, 2, 2, 512, false, 1.18f, 0.361f, 0.311f, 3.04f, launch_tile<Codes, 2, 1, 1, 4, 3, 2>},
-    {192, 256, 1, 1, 512, true, 6.17f, 2.078f, 0.000f, 3.76f, launch_tile<Values, 6, 4, 2, 4, 2>},
-    {128, 256, 1, 1, 512, true, 4.93f, 1.574f, 0.000f, 3.91f, launch_tile<Values, 4, 4, 2, 4, 2>},
+    {192, 256, 1, 1, 512, true, 6.17f, 2.078f, 0.000f, 3.76f, launch_tile<Values, 6, 4, 2, 4, 2, 1, true>},
+    {128, 256, 1, 1, 512, true, 4.93f, 1.574f, 0.000f, 3.91f, launch_tile<Values, 4, 4, 2, 4, 2, 1, true>},
     {64, 256, 1, 1, 256, true, 3.65f, 1.138f, 0.000f, 4.61f, launch_tile<Values, 4, 4, 1, 4, 3>},
     {32, 256, 2, 1, 512, true, 2.03f, 1.472f, 0.000f, 3.66f, launch_tile<Values, 2, 4, 1, 4, 2, 2>},
     {128, 128, 1, 2, 256, true, 6.03f, 0.904f, 0.733f, 1.45f, launch_tile<Values, 4, 4, 2, 2, 2>},

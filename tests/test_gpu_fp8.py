@@ -339,3 +339,20 @@ def test_outputs_that_nothing_would_fill_are_refused():
     w, ws = pace.quantize_fp8(torch.ones((64, 256), dtype=torch.bfloat16, device="cuda"), rows=128)
     with pytest.raises(pace.PaceError, match="out_scale"):
         pace.gemm_fp8(q, s, w, ws, epilogue=2, out_scale=torch.empty((1, 4), device="cuda"))
+
+
+# whole columns of 8, several tiles to a workgroup: K of as few stages as that takes, of one less, and of more than 64 blocks
+RUNS = [(7780, 4160, 512), (7771, 5840, 512), (4300, 5200, 384), (4985, 3184, 960), (3826, 6672, 8464), (3110, 3888, 800), (2690, 5936, 976)]
+
+
+@pytest.mark.parametrize("sums", [FAST, WIDE])
+@pytest.mark.parametrize("epilogue,bits", [(0, 16), (1, 16), (2, 16), (2, 8)])
+@pytest.mark.parametrize("M,N,K", RUNS)
+def test_gemm_fp8_several_tiles_a_workgroup(M, N, K, epilogue, bits, sums):
+    if bits == 8:
+        N += -N % 32
+    rs = np.random.default_rng(N)
+    cols = N // 2 if epilogue == 2 else N
+    m = np.unique(np.concatenate([rs.permutation(M)[:60], [0, 127, 128, 255, 256, M - 1]]))
+    c = np.unique(np.concatenate([rs.permutation(cols)[:3 if bits == 8 else 60], [0, 63, 64, cols - 1]]))
+    run_product(M, N, K, epilogue, bits, sums, (m, c))
