@@ -94,7 +94,8 @@ struct QuantParams {
   int M, K, kb;
 };
 
-// Rows: 16 lanes per block of 128, blocks of a row after one another.
+// Rows: scale = max(max |x| / 448, 2^-120), code = x / scale, in one read: 16 lanes hold a block of 128, blocks of a row after
+// one another.  Bound by memory: 10,677 x 3,584 moves 115 MB in 22.5 us (5.1 TB/s, the rate of a copy); one row takes 2.2.
 __global__ __launch_bounds__(256) void quantize_rows(const QuantParams p) {
   const unsigned block = blockIdx.x * 16 + (threadIdx.x >> 4);   // under 2^28: a launch has fewer than 2^32 threads
   const int row = static_cast<int>(block / static_cast<unsigned>(p.kb)), kb = static_cast<int>(block - static_cast<unsigned>(row) * p.kb);
@@ -107,7 +108,8 @@ __global__ __launch_bounds__(256) void quantize_rows(const QuantParams p) {
   if ((threadIdx.x & 15) == 0) p.scale[static_cast<long long>(kb) * p.M + row] = scale;
 }
 
-// Weights: a workgroup per block of 128 x 128, its values in registers between the maximum and the store.
+// Weights: a workgroup per block of 128 x 128, its values in registers between the maximum and the store.  Bound by memory:
+// 28,672 x 3,584 moves 308 MB in 66.4 us (4.6 TB/s).
 __global__ __launch_bounds__(256) void quantize_blocks(const QuantParams p) {
   __shared__ float red[4];
   const int mb = blockIdx.x / p.kb, kb = blockIdx.x - mb * p.kb;
@@ -343,7 +345,7 @@ __device__ __forceinline__ f32x4 bias4(const Fp8Params& p, int n) {
   return b;
 }
 
-// A wave's part of a tile (rows from m, columns from n) to 16 bits, from its registers: lanes trade pieces so that each has 8
+// A wave's part of a tile (rows from m, columns from n) without a residual, from its registers: lanes trade pieces so that each has 8
 // neighbouring outputs of a row.  Every load that the wave has asked for has come before the first of them is stored.
 __device__ __forceinline__ void trade16(uint32_t& a, uint32_t& b) {
   const auto y = __builtin_amdgcn_permlane16_swap(a, b, false, false);
@@ -439,41 +441,17 @@ __device__ __forceinline__ void finish_tile(const Fp8Params& p, f32x4 (&acc)[MI]
   }
   const int c = n + 16 * (g & 1) + 8 * (g >> 1);
   uint16_t* const C = static_cast<uint16_t*>(p.C) + static_cast<long long>(m) * p.N;
-  const bool with = p.mode == kEpiResidual;
-  const uint16_t* const R = with ? p.R + static_cast<long long>(m) * p.N : nullptr;
-  constexpr int kDeep = MI % 4 == 0 ? 4 : 3;           // rows of tiles whose residual is in flight
-  uint4 res[kDeep][NI / 2];
-  const auto ask = [&](int i) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < NI; j += 2) {
-      const int row = 16 * i + r;
-      uint4 u = make_uint4(0, 0, 0, 0);
-      if (row < rows && c + 16 * j < p.N) u = *reinterpret_cast<const uint4*>(R + static_cast<unsigned>(row * p.N + c + 16 * j));
-      res[i % kDeep][j / 2] = u;
-    }
-  };
-  if (with) {
-#pragma unroll
-    for (int i = 0; i < kDeep && i < MI; ++i) ask(i);
-  }
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
 #pragma unroll
     for (int j = 0; j < NI; j += 2) {
-      if (with) {
-        uint4 u = res[i % kDeep][j / 2];
-        trade16(u.x, u.z);
-        trade16(u.y, u.w);
-        acc[i][j] += f32x4{lo_bf16(u.x), hi_bf16(u.x), lo_bf16(u.y), hi_bf16(u.y)};
-        acc[i][j + 1] += f32x4{lo_bf16(u.z), hi_bf16(u.z), lo_bf16(u.w), hi_bf16(u.w)};
-      }
-      uint4 u = make_uint4(pack2(acc[i][j][0], acc[i][j][1]), pack2(acc[i][j][2], acc[i][j][3]), pack2(acc[i][j + 1][0], acc[i][j + 1][1]),
-                           pack2(acc[i][j + 1][2], acc[i][j + 1][3]));
-      trade16(u.x, u.z);
-      trade16(u.y, u.w);
-      acc[i][j] = f32x4{__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
+      uint32_t u[4] = {pack2(acc[i][j][0], acc[i][j][1]), pack2(acc[i][j][2], acc[i][j][3]), pack2(acc[i][j + 1][0], acc[i][j + 1][1]),
+                       pack2(acc[i][j + 1][2], acc[i][j + 1][3])};
+      trade16(u[0], u[2]);
+      trade16(u[1], u[3]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][j][e] = __uint_as_float(u[e]);
     }
-    if (with && i + kDeep < MI) ask(i + kDeep);
     __builtin_amdgcn_sched_barrier(0);
   }
   wait_loads<0>();
@@ -486,8 +464,26 @@ __device__ __forceinline__ void finish_tile(const Fp8Params& p, f32x4 (&acc)[MI]
     }
 }
 
+// C = sum over blocks b of xs[b, m] ws[n / 128, b] (x_b . w_b): a workgroup has a tile of BM rows and BN columns, WM x WN waves with
+// MI x NI tiles of 16 x 16 each (G groups of them take blocks in turn and join their sums in LDS).  w is the matrix instruction's
+// first operand, so that a lane ends with four neighbouring columns of a row (SwiGLU's pairs in one lane).
+//  - A stage is a block of 128 k's: its products need one scale per row (and one per wave for w), applied to the 16 x 16 sums in fp32
+//    one unit later, under the next products.  T: Codes multiply as they are, Values after they became bf16 (exactly, under the
+//    products, too: 1,373 TFLOP/s instead of 2,985 is what the library reaches, with 32-bit sums).
+//  - Operands come straight into LDS, a ring of ST stages, in rows of 128 bytes whose 16-byte chunks are swapped so that fragments
+//    are read without conflicts.  A barrier in a stage's middle frees w's part and half of x's, one before its last products the rest.
+//  - Bounds: for 256 x 256, the matrix cores' 2,048 cycles a stage against LDS's 192 KB read at 128 bytes a cycle (1,536) and 64 KB
+//    written at 64 (1,024); 8 KB more a stage cost 5 to 7%.  So LDS bounds it, and smaller tiles more so (1.43 us a stage
+//    of 256 x 256, 0.73 of 192 x 128, a half of the work): the largest tile that fills the card is best, and what bounds few rows is the
+//    weights' bytes.  Four waves of 128 x 128 read a third less, but need 512 registers a lane, half of them beyond the
+//    vector unit's reach: 616 us for 8192 cubed against 472.
+//  - With few tiles, K goes to workgroups (`part`, fp8_join) or to G groups in one.  Measured, a call: 10,677 x 28,672 x 3,584 with
+//    SwiGLU 950 us (2,310 TFLOP/s), its 8-bit output in wide sums 1,676 (1,309), 1,183 x 3,584 x 3,584 with a residual 27 (1,126),
+//    48 x 3,584 x 14,336 14 with the join (3.6 TB/s), 8 x 28,672 x 3,584 25 (4.1).
+//  - RUN: a workgroup takes one tile after another.  The last ST stages ask for the next tile's first ones, and the output
+//    leaves from registers, since LDS already holds those.
 template <typename T, int MI, int NI, int WM, int WN, int ST, int G, bool RUN>
-__global__ __launch_bounds__(64 * WM * WN * G, MI * NI > 32 ? 1 : 2) void gemm_fp8_tile(const Fp8Params p) {
+__global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Params p) {
   constexpr int BM = 16 * MI * WM, BN = 16 * NI * WN, NW = WM * WN, TH = 64 * NW * G;
   constexpr int kScales = (BM + 63) / 64 * 64;                   // floats of a stage, whole DMAs of them
   constexpr int kStage = (BM + BN) * kBlock;                     // bytes of a stage
@@ -591,10 +587,11 @@ __global__ __launch_bounds__(64 * WM * WN * G, MI * NI > 32 ? 1 : 2) void gemm_f
   };
   const auto x_scale = [&](int slot, int i) __attribute__((always_inline)) { return scales[slot * G + kg][wm + 16 * i + r]; };
   // w's scales: one for the wave and block, 64 blocks in a register's lanes
-  const auto scales_of = [&](int b) __attribute__((always_inline)) {
-    const int nb = min(bn + wn, p.N - 1) / kBlock;
+  const auto scales_of = [&](int n0, int b) __attribute__((always_inline)) {
+    const int nb = min(n0 + wn, p.N - 1) / kBlock;
     return b < p.kb ? p.ws[static_cast<long long>(nb) * p.kb + b] : 0.f;
   };
+  int to_m = bm, to_n = bn;                            // the tile whose products are formed
   float wscales = 0.f;
 
   f32x4 acc[MI][NI];
@@ -604,7 +601,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, MI * NI > 32 ? 1 : 2) void gemm_f
     for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   const auto scales_from = [&](int stage) __attribute__((always_inline)) {
-    wscales = scales_of(block_of(stage + lane));
+    wscales = scales_of(to_n, block_of(stage + lane));
     asm volatile("s_waitcnt vmcnt(0)" : "+v"(wscales));   // now, and not at every use for all loads in flight
   };
   scales_from(0);
@@ -861,7 +858,8 @@ __global__ __launch_bounds__(64 * WM * WN * G, MI * NI > 32 ? 1 : 2) void gemm_f
       const std::integral_constant<int, 2> second;
       const std::integral_constant<int, 3> end;
       for (int done = gridDim.x;; done += gridDim.x) {
-        const int to_m = bm, to_n = bn;
+        to_m = bm;
+        to_n = bn;
         int to_r = r, to_g = g;
         asm volatile("" : "+v"(off0), "+v"(at0), "+v"(to_r), "+v"(to_g));   // addresses formed anew, not kept while the output leaves
         for (int k = 0; k < ST - 1; ++k) {
@@ -883,7 +881,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, MI * NI > 32 ? 1 : 2) void gemm_f
           rows_m = 0;
           ra.z = rb.z = 0;
         }
-        float next = scales_of(lane);
+        float next = scales_of(bn, lane);
         for (int k = nk - ST; k < nk - 1; ++k) {
           ask = k + ST - nk;
           stage(k, std::false_type{}, plain);
@@ -1095,7 +1093,8 @@ __device__ __forceinline__ void store4(const Fp8Params& p, float* to, int n, f32
       if (n + e < p.N) to[e] = y[e];
 }
 
-// Up to 16 rows: bound by the weights' bytes.  W of a workgroup's 8 waves share 16 columns and take the blocks of K in turn; a
+// Up to 16 rows: bound by the weights' bytes (one row of 4,608 x 3,584 7.0 us; 16.5 MB at the rate of a copy 3.2, the rest the chain of
+// launch, four blocks a wave, and join; three or four blocks in flight and 16 waves gave nothing).  W of a workgroup's 8 waves share 16 columns and take the blocks of K in turn; a
 // wave keeps D blocks in flight.  The codes become bf16 values, whose products the matrix cores sum in 32 bits.
 constexpr int kFewWaves = 8;
 template <int W, int D>
@@ -1161,7 +1160,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void gemm_fp8_few(const Fp8Param
   else finish4(p, r, at, acc, bias);
 }
 
-// Adds the parts of a split K in their order and finishes the output, four columns a thread.  With 8 bits a wave has the 256
+// Adds the parts of a split K in their order and finishes the output, four columns a thread: 3.4 to 4.8 us with the launch for up to 3 MB
+// of sums.  With 8 bits a wave has the 256
 // columns of a block.
 __global__ __launch_bounds__(256) void fp8_join(const Fp8Params p) {
   const int cols = (p.N + 1023) / 1024;
@@ -1219,12 +1219,12 @@ void launch_tile(Fp8Params p, int splits, hipStream_t stream) {
   p.tiles_n = (p.N + 16 * NI * WN - 1) / (16 * NI * WN);
   p.splits = splits;
   if constexpr (RUN) {
-    // A workgroup for each CU, one tile after another: 10,677 x 28,672 x 3,584 with SwiGLU 970 us (1,012 with a workgroup a tile),
-    // its 8-bit output 1,740 (1,773); 1,183 x 4,608 x 3,584, one tile a workgroup, 27.8 (28.8).  A residual that ends K's ring is
-    // quicker than one that its rows wait for until a few tiles have followed each other (39,168 x 1,280 x 3,424, three,
-    // 207 and 219; 10,677 x 3,584 x 3,584, two and a part, 172 and 162).
+    // A workgroup for each CU, one tile after another.  On one card, with a workgroup a tile beside it: 10,677 x 28,672 x 3,584 with
+    // SwiGLU 1,010 us (1,065), its 8-bit output 1,820 (1,847), 8192 cubed 469 (480), 1,183 x 4,608 x 3,584, one tile a workgroup, 29.3
+    // (29.9).  Not with a residual, which ends K's ring in the other form: 42,196 x 1,280 x 3,424 232 us (230), 10,677 x 3,584 x 3,584
+    // 172 (162).
     const long long tiles = static_cast<long long>(p.tiles_m) * p.tiles_n;
-    if (splits == 1 && !p.part && (p.cs || p.width == 8) && p.N < (1 << 20) && p.kb >= 2 * ST && (p.mode != kEpiResidual || tiles > 640)) {
+    if (splits == 1 && !p.part && (p.cs || p.width == 8) && p.N < (1 << 20) && p.kb >= 2 * ST && p.mode != kEpiResidual) {
       hipLaunchKernelGGL((gemm_fp8_tile<T, MI, NI, WM, WN, ST, G, true>), dim3(tiles < 256 ? static_cast<unsigned>(tiles) : 256), dim3(64 * WM * WN * G), 0, stream, p);
       return;
     }
