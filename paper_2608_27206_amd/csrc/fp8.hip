@@ -505,16 +505,17 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
   const int r = lane & 15, g = lane >> 4;
   const int wm = (w / WN) * 16 * MI, wn = (w % WN) * 16 * NI;
   // XCD-contiguous order; groups of eight row tiles column by column, so that the workgroups that run together on an XCD
-  // share a few rows of x and a few of w in its L2
+  // share a few rows of x and a few of w in its L2; few columns row by row (42,196 x 1,280 x 3,424, five across: 223 us; in eights,
+  // of which an XCD holds one and a part, 228)
   const int per = p.tiles_m * p.tiles_n;
   const int lb = remap_block_id(blockIdx.x, gridDim.x);
   const int split = lb / per;
   int bm, bn, rows_m;                                  // the tile whose operands are asked for
   i32x4 ra, rb;
   const auto take = [&](int tl) __attribute__((always_inline)) {
-    const int gsz = 8 * p.tiles_n, grp = tl / gsz, in = tl - grp * gsz;
-    const int gm = min(8, p.tiles_m - 8 * grp);
-    const int tn = in / gm, tm = 8 * grp + (in - tn * gm);
+    const int high = p.tiles_n < 8 ? 1 : 8, gsz = high * p.tiles_n, grp = tl / gsz, in = tl - grp * gsz;
+    const int gm = min(high, p.tiles_m - high * grp);
+    const int tn = in / gm, tm = high * grp + (in - tn * gm);
     bm = tm * BM;
     bn = tn * BN;
     rows_m = min(BM, p.M - bm);
