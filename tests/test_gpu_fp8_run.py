@@ -98,14 +98,14 @@ def test_layer_over_kept_rows_and_decode_steps():
 
 @pytest.fixture(scope="module")
 def calls():
-    """Calls of every kind of plan (few rows, tiles, parts of K and their join, two launches) on fixed inputs, each with a workspace
-    and outputs of its own."""
+    """Calls of every kind of plan (few rows, tiles, parts of K and their join, two launches, several tiles to a workgroup) on fixed
+    inputs, each with a workspace and outputs of its own."""
     import torch
     from paper_2608_27206_amd import pace
     rs = np.random.default_rng(3)
     made = []
     for M, N, K, epilogue, bits, sums in ((1, 640, 3584, 0, 16, 0), (9, 1024, 1040, 2, 8, 0), (48, 384, 4112, 1, 16, 0), (300, 1056, 1552, 2, 8, 1), (300, 520, 656, 1, 16, 0),
-                                          (700, 3616, 272, 2, 8, 0), (2700, 6700, 1040, 1, 16, 0)):
+                                          (700, 3616, 272, 2, 8, 0), (2700, 6700, 1040, 1, 16, 0), (5300, 5136, 528, 0, 16, 0), (3000, 6144, 528, 2, 8, 0)):
         x, xs = pace.quantize_fp8(dev_bf16(bits_of(rs.standard_normal((M, K)))))
         w, ws = pace.quantize_fp8(dev_bf16(bits_of(rs.standard_normal((N, K)))), rows=128)
         cols = N // 2 if epilogue == 2 else N
@@ -278,3 +278,18 @@ def test_output_and_residual_past_four_gib():
         rows = slice(a, a + 40)
         ref = o8.product(code_values(x[rows]), host(xs[:, rows].contiguous()).astype(np.float64), code_values(w), host(ws).astype(np.float64), None, f64(res[rows]), 1, False)
         check_product(y[rows], None, ref, 16)
+
+
+@pytest.mark.parametrize("M,N,epilogue,bits", [(70_000, 32_776, 0, 16), (140_000, 32_800, 2, 16), (140_000, 65_536, 2, 8)])
+def test_output_past_four_gib_of_several_tiles_a_workgroup(M, N, epilogue, bits):
+    import torch
+    from paper_2608_27206_amd import pace
+    K = 528
+    x, xs = pace.quantize_fp8(torch.randn(M, K, device="cuda").to(torch.bfloat16))
+    w, ws = pace.quantize_fp8(torch.randn(N, K, device="cuda").to(torch.bfloat16), rows=128)
+    y, ys = pace.gemm_fp8(x, xs, w, ws, epilogue=epilogue, bits=bits)
+    torch.cuda.synchronize()
+    for a in (0, M // 2 - 6, M - 12):
+        rows = slice(a, a + 12)
+        ref = o8.product(code_values(x[rows]), host(xs[:, rows].contiguous()).astype(np.float64), code_values(w), host(ws).astype(np.float64), epilogue=epilogue, wide=bits == 8)
+        check_product(y[rows], ys[:, rows].contiguous() if bits == 8 else None, ref, bits)
