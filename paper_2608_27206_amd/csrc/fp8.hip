@@ -475,7 +475,7 @@ __device__ __forceinline__ void finish_tile(const Fp8Params& p, f32x4 (&acc)[MI]
 //  - Operands come straight into LDS, a ring of ST stages, in rows of 128 bytes whose 16-byte chunks are swapped so that fragments
 //    are read without conflicts.  A barrier in a stage's middle frees w's part and half of x's, one before its last products the rest.
 //  - Bounds: for 256 x 256, the matrix cores' 2,048 cycles a stage against LDS's 192 KB read at 128 bytes a cycle (1,536) and 64 KB
-//    written at 64 (1,024); 8 KB more a stage cost 5 to 7%.  So LDS bounds it, and smaller tiles more so (1.43 us a stage
+//    written at 64 (1,024); 8 KB more a stage cost 5 to 7%.  So LDS is the busiest part by this count, in smaller tiles more so (1.43 us a stage
 //    of 256 x 256, 0.73 of 192 x 128, a half of the work): the largest tile that fills the card is best, and what bounds few rows is the
 //    weights' bytes.  Four waves of 128 x 128 read a third less, but need 512 registers a lane, half of them beyond the
 //    vector unit's reach: 616 us for 8192 cubed against 472.
