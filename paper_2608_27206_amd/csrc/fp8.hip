@@ -476,12 +476,12 @@ __device__ __forceinline__ void finish_tile(const Fp8Params& p, f32x4 (&acc)[MI]
 //    are read without conflicts.  A barrier in a stage's middle frees w's part and half of x's, one before its last products the rest.
 //  - Bounds: for 256 x 256, the matrix cores' 2,048 cycles a stage against LDS's 192 KB read at 128 bytes a cycle (1,536) and 64 KB
 //    written at 64 (1,024); 8 KB more a stage cost 5 to 7%.  So LDS is the busiest part by this count, in smaller tiles more so (1.43 us a stage
-//    of 256 x 256, 0.73 of 192 x 128, a half of the work): the largest tile that fills the card is best, and what bounds few rows is the
+//    of 256 x 256, 0.73 of 192 x 128, three eighths of its work): the largest tile that fills the card is best, and what bounds few rows is the
 //    weights' bytes.  Four waves of 128 x 128 read a third less, but need 512 registers a lane, half of them beyond the
 //    vector unit's reach: 616 us for 8192 cubed against 472.
 //  - With few tiles, K goes to workgroups (`part`, fp8_join) or to G groups in one.  Measured, a call: 10,677 x 28,672 x 3,584 with
 //    SwiGLU 950 us (2,310 TFLOP/s), its 8-bit output in wide sums 1,676 (1,309), 1,183 x 3,584 x 3,584 with a residual 27 (1,126),
-//    48 x 3,584 x 14,336 14 with the join (3.6 TB/s), 8 x 28,672 x 3,584 25 (4.1).
+//    48 x 3,584 x 14,336 14 with the join (3.6 TB/s), 8 x 28,672 x 3,584 24 (4.3).
 //  - RUN: a workgroup takes one tile after another.  The last ST stages ask for the next tile's first ones, and the output
 //    leaves from registers, since LDS already holds those.
 template <typename T, int MI, int NI, int WM, int WN, int ST, int G, bool RUN>
@@ -1248,34 +1248,34 @@ struct Fp8Plan {
 };
 
 // The tiles' times in us: a launch's start and end, a stage of 128 k's (for each group of waves) alone on a CU and what a further
-// workgroup there adds to it, a round's end.  Fitted to 13,800 timings over 210 shapes (1 to 10,677 rows, 64 to 28,672 columns, K 128
-// to 14,336, K in 1 to 12 parts, weights from memory): what the plan picks takes 1.02 times the best that was measured in the
-// mean, at most 1.4 times (8-bit outputs 1.2).  Of 29 tiles tried these are the ones that bring it there.
+// workgroup there adds to it, a round's end, TB/s of operands that come from memory once.  Fitted to 13,800 timings over 210 shapes
+// (1 to 10,677 rows, 64 to 28,672 columns, K 128 to 14,336, K in 1 to 12 parts, weights from memory): what the plan picks takes 1.01
+// to 1.02 times the best that was measured in the mean, at most 1.4 times (8-bit outputs 1.2).  Of 29 tiles tried these are the ones
+// that bring it there.
 struct Fp8Tile {
   int bm, bn, groups, per_cu, threads;
   bool wide;
-  float fixed, stage, shared, round;
+  float fixed, stage, shared, round, memory;
   void (*launch)(Fp8Params, int, hipStream_t);
 };
 const Fp8Tile kTiles[] = {
-    {256, 256, 1, 1, 512, false, 2.73f, 1.426f, 0.000f, 10.52f, launch_tile<Codes, 8, 4, 2, 4, 2, 1, true>},
-    {192, 256, 1, 1, 512, false, 3.28f, 1.324f, 0.000f, 7.43f, launch_tile<Codes, 6, 4, 2, 4, 2, 1, true>},
-    {256, 128, 1, 1, 512, false, 3.29f, 0.890f, 0.000f, 7.03f, launch_tile<Codes, 4, 4, 4, 2, 3, 1, true>},
-    {192, 128, 1, 1, 512, false, 3.02f, 0.734f, 0.000f, 5.73f, launch_tile<Codes, 3, 4, 4, 2, 3, 1, true>},
-    {160, 128, 1, 2, 256, false, 1.70f, 0.817f, 0.429f, 7.04f, launch_tile<Codes, 5, 4, 2, 2, 2>},
-    {96, 128, 2, 1, 512, false, 2.02f, 1.111f, 0.000f, 4.81f, launch_tile<Codes, 3, 4, 2, 2, 2, 2>},
-    {64, 128, 2, 1, 512, false, 1.61f, 0.697f, 0.000f, 4.58f, launch_tile<Codes, 4, 2, 1, 4, 3, 2>},
-    {64, 64, 2, 1, 512, false, 1.55f, 0.487f, 0.000f, 3.40f, launch_tile<Codes, 4, 1, 1, 4, 3, 2>},
-    {32, 64, 2, 2, 512, false, 1.18f, 0.361f, 0.311f, 3.04f, launch_tile<Codes, 2, 1, 1, 4, 3, 2>},
-    {192, 256, 1, 1, 512, true, 6.17f, 2.078f, 0.000f, 3.76f, launch_tile<Values, 6, 4, 2, 4, 2, 1, true>},
-    {128, 256, 1, 1, 512, true, 4.93f, 1.574f, 0.000f, 3.91f, launch_tile<Values, 4, 4, 2, 4, 2, 1, true>},
-    {64, 256, 1, 1, 256, true, 3.65f, 1.138f, 0.000f, 4.61f, launch_tile<Values, 4, 4, 1, 4, 3>},
-    {32, 256, 2, 1, 512, true, 2.03f, 1.472f, 0.000f, 3.66f, launch_tile<Values, 2, 4, 1, 4, 2, 2>},
-    {128, 128, 1, 2, 256, true, 6.03f, 0.904f, 0.733f, 1.45f, launch_tile<Values, 4, 4, 2, 2, 2>},
-    {32, 64, 2, 2, 512, true, 2.22f, 0.536f, 0.398f, 2.71f, launch_tile<Values, 2, 1, 1, 4, 3, 2>},
+    {256, 256, 1, 1, 512, false, 2.73f, 1.426f, 0.000f, 10.52f, 5.00f, launch_tile<Codes, 8, 4, 2, 4, 2, 1, true>},
+    {192, 256, 1, 1, 512, false, 3.28f, 1.324f, 0.000f, 7.43f, 5.00f, launch_tile<Codes, 6, 4, 2, 4, 2, 1, true>},
+    {256, 128, 1, 1, 512, false, 3.29f, 0.890f, 0.000f, 7.03f, 5.00f, launch_tile<Codes, 4, 4, 4, 2, 3, 1, true>},
+    {192, 128, 1, 1, 512, false, 3.02f, 0.734f, 0.000f, 5.73f, 5.00f, launch_tile<Codes, 3, 4, 4, 2, 3, 1, true>},
+    {160, 128, 1, 2, 256, false, 1.70f, 0.817f, 0.429f, 7.04f, 5.00f, launch_tile<Codes, 5, 4, 2, 2, 2>},
+    {96, 128, 2, 1, 512, false, 2.02f, 1.111f, 0.000f, 4.81f, 5.00f, launch_tile<Codes, 3, 4, 2, 2, 2, 2>},
+    {64, 128, 2, 1, 512, false, 1.61f, 0.697f, 0.000f, 4.58f, 5.00f, launch_tile<Codes, 4, 2, 1, 4, 3, 2>},
+    {64, 64, 2, 1, 512, false, 1.55f, 0.487f, 0.000f, 3.40f, 5.00f, launch_tile<Codes, 4, 1, 1, 4, 3, 2>},
+    {32, 64, 2, 2, 512, false, 1.18f, 0.361f, 0.311f, 3.04f, 5.00f, launch_tile<Codes, 2, 1, 1, 4, 3, 2>},
+    {192, 256, 1, 1, 512, true, 6.17f, 2.078f, 0.000f, 3.76f, 5.00f, launch_tile<Values, 6, 4, 2, 4, 2, 1, true>},
+    {128, 256, 1, 1, 512, true, 4.93f, 1.574f, 0.000f, 3.91f, 5.00f, launch_tile<Values, 4, 4, 2, 4, 2, 1, true>},
+    {64, 256, 1, 1, 256, true, 2.84f, 1.143f, 0.000f, 5.06f, 6.10f, launch_tile<Values, 4, 4, 1, 4, 3>},
+    {32, 256, 2, 1, 512, true, 1.50f, 1.447f, 0.000f, 3.62f, 4.05f, launch_tile<Values, 2, 4, 1, 4, 2, 2>},
+    {128, 128, 1, 2, 256, true, 6.03f, 0.904f, 0.733f, 1.45f, 5.00f, launch_tile<Values, 4, 4, 2, 2, 2>},
+    {32, 64, 2, 2, 512, true, 1.41f, 0.542f, 0.426f, 2.78f, 5.62f, launch_tile<Values, 2, 1, 1, 4, 3, 2>},
 };
 constexpr int kNumTiles = sizeof(kTiles) / sizeof(kTiles[0]);
-constexpr float kMemory = 5.0e6f;      // bytes per us of operands that come from memory once
 constexpr int kMostSplits = 12, kMostRows = 1 << 26;
 constexpr double kMostSums = 5e7;      // of the parts of K together
 
@@ -1288,17 +1288,18 @@ float tile_time(const Fp8Tile& t, int rows, int N, int K, int splits) {
   const int left = static_cast<int>((n - full * round + 255) / 256);      // workgroups of a CU in the last round
   const auto turn = [&](int there) { return stages * (t.stage + t.shared * (there - 1)) + t.round; };
   const float work = t.fixed + full * turn(t.per_cu) + (left ? turn(left) : 0.f);
-  const float bytes = 1.8f + (static_cast<float>(rows) * K + static_cast<float>(N) * K + 2.f * rows * N) / kMemory;
+  const float bytes = 1.8f + (static_cast<float>(rows) * K + static_cast<float>(N) * K + 2.f * rows * N) / (t.memory * 1e6f);
   return sqrtf(work * work + bytes * bytes);
 }
-// gemm_fp8_few: a column's 8 waves take kb / 8 blocks one after the other; over many columns they read memory less well than the
-// tiles (one row of 28,672 columns of 3,584: 26 us against 22.6; of 3,584 columns 6.2 against 9.4 with parts and their join).
+// gemm_fp8_few: a column's 8 waves take kb / 8 blocks one after the other, and read x again for each 16 columns.  Over many columns
+// the tiles read memory better (one row of 28,672 columns of 3,584: 23.6 us against 22.6, 16 rows 33.5 against 24; of 3,584 columns
+// 5.8 and 6.7 against 9.4 with parts and their join).  Fitted to 86 timings, within 8%.
 bool join_fits(int rows, int N) { return fits((N + 1023ll) / 1024 * rows, 256); }
 float few_time(int rows, int N, int K) {
   const int kb = (K + kBlock - 1) / kBlock, blocks = (kb + kFewWaves - 1) / kFewWaves;
-  const float n = (N + 15) / 16 / 256.f, work = 2.f + (n > 1.f ? n : 1.f) * blocks * (0.77f + 0.024f * rows);
-  const float bytes = 2.5f + static_cast<float>(N) * K / 3.2e6f;
-  return work > bytes ? work : bytes;
+  const float n = (N + 15) / 16 / 256.f, work = 2.07f + (n > 1.f ? powf(n, 0.81f) : 1.f) * blocks * (0.575f + 0.0088f * rows);
+  const float bytes = 2.6f + static_cast<float>(N) * K * (1.f + 0.03f * rows) / 4.6e6f;
+  return sqrtf(sqrtf(work * work * work * work + bytes * bytes * bytes * bytes));
 }
 
 // A tile whose columns hold whole blocks of 128 SwiGLU outputs quantises them itself.
