@@ -534,8 +534,8 @@ pace_status_t pace_gemm_w4(const uint16_t* x, const uint8_t* w, const uint16_t* 
  */
 
 /*
- * Quantises rows or weights: scale = max(largest finite |x| of the block / 448, 2^-120), code = x / scale, rounded to
- * nearest even; values that are not finite become NaN.
+ * Quantises rows or weights: scale = max(largest finite |x| of the block / 448, 2^-120), code = x / scale (the fp32 quotient), rounded
+ * to nearest even; values that are not finite become NaN.
  *   x       bf16 [M, K], row i at x + i * x_stride (in elements, a multiple of 8, at least K); 16-byte aligned, K a
  *           multiple of 16, at most 2^20.
  *   rows    1: activations, scale fp32 [ceil(K / 128), M]; 128: weights, scale fp32 [ceil(M / 128), ceil(K / 128)].

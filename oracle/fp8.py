@@ -44,7 +44,7 @@ def scales(x: np.ndarray, rows: int) -> np.ndarray:
 
 def codes_ok(got: np.ndarray, y: np.ndarray, scale: np.ndarray, rows: int, tol) -> np.ndarray:
     """Which codes (as values) lie within half a step of y / scale, for the scales that came with them; y known to `tol`,
-    and quantised through the scale's reciprocal in 32 bits (three roundings: 2^-22)."""
+    and divided in 32 bits (2^-22 is ample for the quotient's rounding)."""
     s = per_value(scale, y.shape, rows)
     with np.errstate(invalid="ignore"):
         v, t = y / s, tol / s

@@ -49,22 +49,30 @@ __device__ __forceinline__ float silu(float x) {
 // What a value adds to its block's maximum: its magnitude, 0 where it is not finite.
 __device__ __forceinline__ float magnitude(float x) { return fabsf(x) <= FLT_MAX ? fabsf(x) : 0.f; }
 __device__ __forceinline__ float scale_of(float top) { return fmaxf(top / kE4m3Max, kMinScale); }
-// x / scale by the reciprocal: within 2^-22 of the quotient, so a code differs from the quotient's only where that lies as
-// near to the middle between two codes.  The largest scale is 2^128 / 448 and the least 2^-120: both reciprocals are normal.
-// What is not finite becomes NaN (what the conversion makes of infinities depends on a mode bit); the others are at most
-// 448 (1 + 2^-22), which rounds to 448.
-__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d, float inv) {
-  const float nan = __uint_as_float(0x7fc00000u);
-  a = fabsf(a) <= FLT_MAX ? a * inv : nan;
-  b = fabsf(b) <= FLT_MAX ? b * inv : nan;
-  c = fabsf(c) <= FLT_MAX ? c * inv : nan;
-  d = fabsf(d) <= FLT_MAX ? d * inv : nan;
-  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-  r = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+// What a block's codes are divided by.  Under 2^-92 both sides of the division grow by 2^64, so that its remainder stays normal.
+struct Divisor {
+  float scale, inv, up;
+};
+__device__ __forceinline__ Divisor divisor_of(float scale) {
+  const float up = scale < 0x1p-92f ? 0x1p64f : 1.f;
+  return {scale * up, 1.f / (scale * up), up};
+}
+// x / scale in fp32 (-0 stays -0): the product with the reciprocal, put right by its remainder, which one fused multiply-add gives.  For
+// every mantissa of the scale this is the rounded quotient of every bf16 value, and of the fp32 values about each middle between two codes
+// (2.3e9 quotients compared).  The product alone is another fp32 value for a quarter of the quotients, and another code where one of them is a
+// middle.  What is not finite becomes NaN: an infinity's remainder is one (what the conversion makes of infinities depends on a mode bit).
+__device__ __forceinline__ float quotient(float x, const Divisor& d) {
+  const float a = x * d.up, q = a * d.inv;
+  return fmaf(-fmaf(q, d.scale, -a), d.inv, q);
+}
+// The codes of x / scale: quotients are at most 448 (1 + 2^-23), which rounds to 448.
+__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float e, const Divisor& d) {
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(a, d), quotient(b, d), 0, false);
+  r = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(c, d), quotient(e, d), r, true);
   return static_cast<uint32_t>(r);
 }
-__device__ __forceinline__ uint2 to_e4m3(const float (&x)[8], float inv) {
-  return make_uint2(to_e4m3(x[0], x[1], x[2], x[3], inv), to_e4m3(x[4], x[5], x[6], x[7], inv));
+__device__ __forceinline__ uint2 to_e4m3(const float (&x)[8], const Divisor& d) {
+  return make_uint2(to_e4m3(x[0], x[1], x[2], x[3], d), to_e4m3(x[4], x[5], x[6], x[7], d));
 }
 __device__ __forceinline__ float magnitude8(const float (&x)[8]) {
   float m = 0.f;
@@ -104,7 +112,7 @@ __global__ __launch_bounds__(256) void quantize_rows(const QuantParams p) {
   float x[8] = {};
   if (k < p.K) unpack8(*reinterpret_cast<const uint4*>(p.x + row * p.stride + k), x);
   const float scale = scale_of(max16(magnitude8(x)));
-  if (k < p.K) *reinterpret_cast<uint2*>(p.q + static_cast<long long>(row) * p.K + k) = to_e4m3(x, 1.f / scale);
+  if (k < p.K) *reinterpret_cast<uint2*>(p.q + static_cast<long long>(row) * p.K + k) = to_e4m3(x, divisor_of(scale));
   if ((threadIdx.x & 15) == 0) p.scale[static_cast<long long>(kb) * p.M + row] = scale;
 }
 
@@ -121,11 +129,12 @@ __global__ __launch_bounds__(256) void quantize_blocks(const QuantParams p) {
     if (k < p.K && r0 + 16 * i < p.M) unpack8(*reinterpret_cast<const uint4*>(p.x + (r0 + 16 * i) * p.stride + k), x[i]);
 #pragma unroll
   for (int i = 0; i < 8; ++i) top = fmaxf(top, magnitude8(x[i]));
-  const float scale = scale_of(block_reduce<1>(top, red)), inv = 1.f / scale;
+  const float scale = scale_of(block_reduce<1>(top, red));
+  const Divisor d = divisor_of(scale);
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     if (k < p.K && r0 + 16 * i < p.M)
-      *reinterpret_cast<uint2*>(p.q + static_cast<long long>(r0 + 16 * i) * p.K + k) = to_e4m3(x[i], inv);
+      *reinterpret_cast<uint2*>(p.q + static_cast<long long>(r0 + 16 * i) * p.K + k) = to_e4m3(x[i], d);
   if (threadIdx.x == 0) p.scale[blockIdx.x] = scale;
 }
 
@@ -213,7 +222,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_rows(const NormPara
     }
     const float scale = scale_of(max16(magnitude8(y)));
     if (in) {
-      reinterpret_cast<uint2*>(p.q + static_cast<long long>(row) * p.K)[c] = to_e4m3(y, 1.f / scale);
+      reinterpret_cast<uint2*>(p.q + static_cast<long long>(row) * p.K)[c] = to_e4m3(y, divisor_of(scale));
       if ((t & 15) == 0) p.scale[static_cast<long long>(c / 16) * p.M + row] = scale;
     }
   }
@@ -405,9 +414,10 @@ __device__ __forceinline__ void finish_tile(const Fp8Params& p, f32x4 (&acc)[MI]
           float top = top_of[0][wm + row];
 #pragma unroll
           for (int o = 1; o < WN; ++o) top = fmaxf(top, top_of[o][wm + row]);
-          const float scale = scale_of(top), inv = 1.f / scale;
-          uint32_t a = to_e4m3(acc[i][0][0], acc[i][0][1], acc[i][1][0], acc[i][1][1], inv);
-          uint32_t b = to_e4m3(acc[i][2][0], acc[i][2][1], acc[i][3][0], acc[i][3][1], inv);
+          const float scale = scale_of(top);
+          const Divisor d = divisor_of(scale);
+          uint32_t a = to_e4m3(acc[i][0][0], acc[i][0][1], acc[i][1][0], acc[i][1][1], d);
+          uint32_t b = to_e4m3(acc[i][2][0], acc[i][2][1], acc[i][3][0], acc[i][3][1], d);
           trade32(a, b);
           uint32_t even = (a & 0xffffu) | b << 16, odd = a >> 16 | (b & 0xffff0000u);
           trade16(even, odd);
@@ -986,12 +996,12 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
       for (int i = 0; i < MI; ++i) {
         if (kg) break;
         const int row = wm + 16 * i + r;
-        const float inv = 1.f / row_scale(row);
+        const Divisor d = divisor_of(row_scale(row));
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
           const int c = (wn + 16 * j + 4 * g) / 2;
           *reinterpret_cast<uint16_t*>(lds + row * 128 + (((c >> 4) ^ (row & 7)) << 4) + (c & 15)) =
-              static_cast<uint16_t>(to_e4m3(acc[i][j][0], acc[i][j][1], 0.f, 0.f, inv));
+              static_cast<uint16_t>(to_e4m3(acc[i][j][0], acc[i][j][1], 0.f, 0.f, d));
         }
       }
       __syncthreads();
@@ -1198,7 +1208,7 @@ __global__ __launch_bounds__(256) void fp8_join(const Fp8Params p) {
   const float a = silu(y[0]) * y[1], b = silu(y[2]) * y[3];
   const float scale = scale_of(wave_reduce_dpp(fmaxf(magnitude(a), magnitude(b)), [](float u, float v) { return fmaxf(u, v); }));
   if (n >= p.N) return;
-  static_cast<uint16_t*>(p.C)[(static_cast<long long>(m) * (p.N / 2) + n / 2) / 2] = static_cast<uint16_t>(to_e4m3(a, b, 0.f, 0.f, 1.f / scale));
+  static_cast<uint16_t*>(p.C)[(static_cast<long long>(m) * (p.N / 2) + n / 2) / 2] = static_cast<uint16_t>(to_e4m3(a, b, 0.f, 0.f, divisor_of(scale)));
   if ((threadIdx.x & 63) == 0) p.cs[n / 256 * p.cs_stride + m] = scale;
 }
 
