@@ -182,7 +182,6 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_rows(const NormPara
     }
   }
   float h[NC][8];
-  float ss = 0.f;
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
     float add[8];
@@ -191,13 +190,22 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_rows(const NormPara
 #pragma unroll
     for (int e = 0; e < 8; ++e) h[i][e] += add[e];
   }
+  const auto squares = [&](float by) __attribute__((always_inline)) {     // the sum of the row's (h * by)^2
+    float ss = 0.f;
 #pragma unroll
-  for (int i = 0; i < NC; ++i)
+    for (int i = 0; i < NC; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ss = fmaf(h[i][e], h[i][e], ss);
-  if constexpr (T == 64) ss = wave_reduce_dpp(ss, [](float a, float b) { return a + b; });
-  else ss = block_reduce<0>(ss, red);
-  const float inv = 1.f / sqrtf(ss / static_cast<float>(p.K) + p.eps);
+      for (int e = 0; e < 8; ++e) ss = fmaf(h[i][e] * by, h[i][e] * by, ss);
+    if constexpr (T == 64) return wave_reduce_dpp(ss, [](float a, float b) { return a + b; });
+    else return block_reduce<0>(ss, red);
+  };
+  // A sum past fp32 is taken again of values 2^-80 times as large: h is under 2^128, so K of their squares stay under 2^112.
+  float by = 1.f, ss = squares(1.f);
+  if (ss > FLT_MAX) {                                  // the same for all of a row's threads
+    by = 0x1p-80f;
+    ss = squares(by);
+  }
+  const float inv = by / sqrtf(ss / static_cast<float>(p.K) + p.eps * by * by);
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
     const int c = i * T + t;
