@@ -554,7 +554,7 @@ pace_status_t pace_quantize_fp8(const uint16_t* x, long long x_stride, int M, in
  *   sum     bf16 [M, K] = h, or NULL.  It may be the memory of x or residual (with rows K apart).
  *   y       bf16 [M, K], or NULL and instead of it
  *   q, scale  codes [M, K] and scales [ceil(K / 128), M] of y, as pace_quantize_fp8 (rows = 1) makes them of y's fp32 values.
- * Tensors are 16-byte aligned (scale: 4).  Squares are summed in fp32, of shrunken values where their sum would leave it.  A row that holds
+ * Tensors are 16-byte aligned (scale: 4).  Squares are summed in fp32, of shrunken or grown values where they would leave it.  A row that holds
  * a NaN becomes NaN, one that holds an infinity NaN there and 0 elsewhere.  M = 0 is a no-op.  y may be the memory of x or residual (with rows K apart), but not sum's.
  * Asynchronous on `stream`; no workspace.
  */

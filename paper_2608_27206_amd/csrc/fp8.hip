@@ -199,10 +199,11 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_rows(const NormPara
     if constexpr (T == 64) return wave_reduce_dpp(ss, [](float a, float b) { return a + b; });
     else return block_reduce<0>(ss, red);
   };
-  // A sum past fp32 is taken again of values 2^-80 times as large: h is under 2^128, so K of their squares stay under 2^112.
+  // A sum past fp32 is taken again of values 2^-80 times as large: h is under 2^128, so K of their squares stay under 2^112.  One so small
+  // that its squares lose bits, where eps is no larger, is taken again of values 2^64 times as large.
   float by = 1.f, ss = squares(1.f);
-  if (ss > FLT_MAX) {                                  // the same for all of a row's threads
-    by = 0x1p-80f;
+  if (ss > FLT_MAX || (ss < 0x1p-90f && p.eps < 0x1p-90f)) {             // the same for all of a row's threads
+    by = ss > FLT_MAX ? 0x1p-80f : 0x1p64f;
     ss = squares(by);
   }
   const float inv = by / sqrtf(ss / static_cast<float>(p.K) + p.eps * by * by);
