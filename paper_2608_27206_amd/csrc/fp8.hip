@@ -36,14 +36,18 @@ __device__ __forceinline__ void unpack8(uint4 u, float (&x)[8]) {
     x[2 * i + 1] = hi_bf16(v[i]);
   }
 }
-// x / (1 + e^-x).  The exponent x log2(e) is taken to twice 24 bits (its rounding alone would cost 2^-18 at x = -20), the
-// exponential and reciprocal units round once each: within 2^-21 of the value (one under 2^-126 may come as 0), and half the time
-// of expf and a division.
+// x / (1 + e^-x) = x 2^-8 / (2^-8 + 2^(t - 8) e^rest), t = -x log2(e) to a multiple of 2^-13 (from which 8 is taken exactly; t's rounding to
+// fp32 alone would cost 2^-18 at x = -20) and rest = -x - t ln 2, under 2^-14.  The factor keeps the denominator in the range, to 2^126,
+// whose reciprocals the unit gives.  The exponential and reciprocal units round once each, fp32's ln 2 adds 2^-29 of t: within 2^-20.5 of
+// the value (2^-21 for x > -20) down to 2^-120 (x = -88, where the sigmoid becomes subnormal), 2^-16 down to 2^-127 (x = -92.9), where it
+// comes as 0.  x / (1 + expf(-x)) would lose everything below x = -88.7.
 __device__ __forceinline__ float silu(float x) {
-  constexpr float kL = 1.44269504f, kLo = 1.92596303e-8f, kLn2 = 0.693147181f;   // log2(e) = kL + kLo
+  constexpr float kL = 1.44269504f, kLn2 = 0.693147181f;
+  constexpr float kRound = 0x1.8p10f;                                            // fp32 ends at 2^-13 there
   const float c = __builtin_amdgcn_fmed3f(x, -200.f, 200.f);                     // past them e^-x is infinite, or 0 beside 1
-  const float t = c * -kL, lo = fmaf(c, -kL, -t) - c * kLo;
-  return x * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(t), fmaf(lo, kLn2, 1.f), 1.f));
+  const float r = fmaf(c, -kL, kRound), t = r - kRound, rest = fmaf(t, -kLn2, -c);
+  const float d = fmaf(__builtin_amdgcn_exp2f(r - (kRound + 8.f)), 1.f + rest, 0x1p-8f);
+  return x * (__builtin_amdgcn_rcpf(d) * 0x1p-8f);
 }
 
 // What a value adds to its block's maximum: its magnitude, 0 where it is not finite.

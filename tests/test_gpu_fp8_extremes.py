@@ -5,7 +5,8 @@ import pytest
 from oracle import fp8 as o8
 from paper_2608_27206_amd import workloads as wl
 from tests.gpu_util import dev_bf16, dev_f32, say
-from tests.test_gpu_fp8 import bits_of, check_norm
+from tests.test_gpu_cache import f64
+from tests.test_gpu_fp8 import bits_of, check_norm, check_product
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +53,41 @@ def test_norm_of_rows_whose_squares_are_subnormal(M, K, bits):
         H, Y, tol = o8.norm(wl.bf16_bits_to_f64(x), None, gamma.astype(np.float64), float(np.float32(eps)))
         # an output under 2^-126 may be subnormal in bf16
         check_norm(y, s, h, H, Y, tol + 2.0 ** -134, False, bits)
+
+
+# gates around every place where e^-x, the sigmoid or their reciprocals leave fp32, and between
+GATES = np.concatenate([np.linspace(-96, -80, 129), np.linspace(-80, 96, 177), [-3e38, -6e4, -300.0, -201, -200, -199, -1e-3, -1e-30, -2.0 ** -140, 0, 2.0 ** -149,
+                                                                                2.0 ** -140, 1e-30, 1e-3, 199, 200, 201, 300, 6e4, 1e30]]).astype(np.float32)
+
+
+@pytest.mark.parametrize("bits,sums", [(16, 0), (16, 2), (8, 0), (8, 1)])
+@pytest.mark.parametrize("M,N,K", [(2, 704, 128), (40, 704, 128), (300, 704, 128), (100, 704, 3600), (700, 3616, 272), (2690, 5952, 976), (4300, 6016, 528)])
+def test_swiglu_of_far_gates_within_its_roundings(M, N, K, bits, sums):
+    """silu(g) u of biases beside products of zeros: g and u are exact.  What silu may be off: 2^-20.5 of its value and 2^-142 (the sigmoid's
+    last subnormal bit, 2^-150, times 93, and the product's), all of it below g = -92.8; the product with u 2^-24, bf16 2^-8 and half its least step."""
+    import torch
+    from paper_2608_27206_amd import pace
+    rs = np.random.default_rng(M + N)
+    x = torch.zeros((M, K), dtype=torch.float8_e4m3fn, device="cuda")
+    w = torch.zeros((N, K), dtype=torch.float8_e4m3fn, device="cuda")
+    xs, ws = torch.ones((o8.blocks(K), M), device="cuda"), torch.ones((o8.blocks(N), o8.blocks(K)), device="cuda")
+    for e in (0, 20, 100, 127):
+        g = np.resize(GATES, N // 2)
+        u = (rs.uniform(0.5, 1, N // 2) * 2.0 ** np.where(g < -80, e, min(e, 20)) * rs.choice([-1, 1], N // 2)).astype(np.float32)
+        bias = np.stack([g, u], 1).ravel()
+        say(f"far gates M={M} N={N} K={K} bits={bits} sums={sums} u to 2^{e}")
+        y, s = pace.gemm_fp8(x, xs, w, ws, dev_f32(bias), None, 2, bits, sums)
+        torch.cuda.synchronize()
+        g, u = g.astype(np.float64), u.astype(np.float64)
+        with np.errstate(over="ignore"):
+            silu = g / (1 + np.exp(-g))
+        off = np.where(g < -92.8, np.abs(silu), 2.0 ** -20.5 * np.abs(silu) + 2.0 ** -142)
+        ref, tol = silu * u, off * np.abs(u) + 2.0 ** -24 * np.abs(silu * u) + 2.0 ** -149
+        rows = np.unique(np.append(np.arange(0, M, 61), M - 1))
+        at = torch.from_numpy(rows).cuda()
+        ref, tol = np.repeat(ref[None], len(rows), 0), np.repeat(tol[None], len(rows), 0)
+        if bits == 16:
+            err = np.abs(f64(y[at]) - ref)
+            assert np.all(err <= 2.0 ** -8 * (np.abs(ref) + tol) + tol + 2.0 ** -134)
+        else:
+            check_product(y.view(torch.uint8)[at].view(torch.float8_e4m3fn), s[:, at], (ref, tol, None), 8)
