@@ -10,7 +10,10 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
 from concurrent.futures import ThreadPoolExecutor
+
+from paper_2608_27206_amd import wait_states
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -32,17 +35,36 @@ def hipcc() -> str:
 
 def _compile(src: str) -> str:
     obj = os.path.join(BUILD, os.path.splitext(src)[0] + ".o")
-    cmd = [hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall",
-           "-Wno-unused-function", "-I", os.path.join(ROOT, "include"), "-c",
-           os.path.join(CSRC, src), "-o", obj] + DEVICE_FLAGS
     if src.endswith(".cpp"):
         cmd = [hipcc(), "-O3", "-std=c++17", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__",
                "-I", os.path.join(ROOT, "include"), "-c", os.path.join(CSRC, src), "-o", obj]
+        _run(cmd, src)
+        return obj
+    # a folder of its own for what the compiler leaves on the way, of which the device's assembly is looked at
+    with tempfile.TemporaryDirectory(dir=BUILD) as tmp:
+        new = os.path.join(tmp, os.path.basename(obj))
+        _run([hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall",
+              "-Wno-unused-function", "-I", os.path.join(ROOT, "include"), "-save-temps=obj", "-c",
+              os.path.join(CSRC, src), "-o", new] + DEVICE_FLAGS, src)
+        _check_assembly(src, [f for f in os.listdir(tmp) if f.endswith(f"{ARCH}.s")], tmp)
+        os.replace(new, obj)
+    return obj
+
+
+def _run(cmd: list, src: str) -> None:
     r = subprocess.run(cmd, capture_output=True, text=True)
     errs = "\n".join(l for l in (r.stderr or "").splitlines() if "packed-fp32-ops" not in l)
     if r.returncode != 0:
         raise RuntimeError(f"compile failed: {src}\n{errs}")
-    return obj
+
+
+def _check_assembly(src: str, files: list, folder: str) -> None:
+    if len(files) != 1:
+        raise RuntimeError(f"{src}: the device's assembly is not among what the compiler left: {files}")
+    with open(os.path.join(folder, files[0])) as f:
+        found = wait_states.problems(f.read())
+    if found:
+        raise RuntimeError(f"{src}: {len(found)} loads in inline asm come too early\n" + "\n".join(found[:5]))
 
 
 # Host-side AddressSanitizer + UndefinedBehaviorSanitizer build of the whole library (device code is

@@ -331,8 +331,8 @@ __device__ __forceinline__ i32x4 rsrc_of(const void* base, unsigned bytes) {
   return r;
 }
 // 64 lanes x 16 (4) bytes from the buffer to lds .. lds + 1023 (255); untracked by the compiler, awaited with wait_loads.  Nor does the
-// compiler see here that a scalar which the vector unit wrote (a spilled descriptor's v_readlane) is read: that needs five wait states,
-// which tests/test_fp8_wait_states.py finds in what is built (s_nop 4 instead would cost up to 2%: 982 us for 967).
+// compiler see here that a scalar which the vector unit wrote (a spilled descriptor's v_readlane) is read: that needs five wait states.
+// build.py looks for them in what it has compiled and ends without them (wait_states.py; s_nop 4 here would cost up to 2%: 982 us for 967).
 __device__ __forceinline__ void dma16(i32x4 r, unsigned lds, unsigned voff) {
   const unsigned m0 = __builtin_amdgcn_readfirstlane(lds);
   asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(r), "{m0}"(m0) : "memory");
