@@ -5,6 +5,7 @@
 
 #include <type_traits>
 
+#include "fp8_plan.h"
 #include "pace_internal.h"
 
 namespace pace {
@@ -17,7 +18,6 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kBlock = 128;                    // values that share a scale
 constexpr float kE4m3Max = 448.f;
 constexpr float kMinScale = 0x1p-120f;
 
@@ -94,8 +94,6 @@ __device__ __forceinline__ float max16(float x) {
 
 template <typename T>
 bool whole(const T* p) { return reinterpret_cast<uintptr_t>(p) % sizeof(T) == 0; }   // lies at a multiple of its own size
-// A launch has fewer than 2^32 threads.
-bool fits(long long groups, int threads) { return groups * threads < (1ll << 32); }
 
 // ---------------------------------------------------------------- quantisation
 struct QuantParams {
@@ -1122,7 +1120,6 @@ __device__ __forceinline__ void store4(const Fp8Params& p, float* to, int n, f32
 // Up to 16 rows: bound by the weights' bytes (one row of 4,608 x 3,584 7.0 us; 16.5 MB at the rate of a copy 3.2, the rest the chain of
 // launch, four blocks a wave, and join; three or four blocks in flight and 16 waves gave nothing).  W of a workgroup's 8 waves share 16 columns and take the blocks of K in turn; a
 // wave keeps D blocks in flight.  The codes become bf16 values, whose products the matrix cores sum in 32 bits.
-constexpr int kFewWaves = 8;
 template <int W, int D>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void gemm_fp8_few(const Fp8Params p) {
   constexpr int SETS = kFewWaves / W;
@@ -1250,7 +1247,7 @@ void launch_tile(Fp8Params p, int splits, hipStream_t stream) {
     // (29.9).  Not with a residual, which ends K's ring in the other form: 42,196 x 1,280 x 3,424 232 us (230), 10,677 x 3,584 x 3,584
     // 172 (162).
     const long long tiles = static_cast<long long>(p.tiles_m) * p.tiles_n;
-    if (splits == 1 && !p.part && (p.cs || p.width == 8) && p.N < (1 << 20) && p.kb >= 2 * ST && p.mode != kEpiResidual) {
+    if (in_turn(ST, splits, p.part, p.N, p.K, p.cs || p.width == 8, p.mode == kEpiResidual)) {
       hipLaunchKernelGGL((gemm_fp8_tile<T, MI, NI, WM, WN, ST, G, true>), dim3(tiles < 256 ? static_cast<unsigned>(tiles) : 256), dim3(64 * WM * WN * G), 0, stream, p);
       return;
     }
@@ -1258,130 +1255,11 @@ void launch_tile(Fp8Params p, int splits, hipStream_t stream) {
   hipLaunchKernelGGL((gemm_fp8_tile<T, MI, NI, WM, WN, ST, G, false>), dim3(static_cast<unsigned>(p.tiles_m) * p.tiles_n * splits), dim3(64 * WM * WN * G), 0, stream, p);
 }
 
-// What a product of M rows is made of: one launch or two (whole rounds of the largest tiles, and the rows that are left),
-// each of one kernel with K in `splits` parts.
-struct Fp8Launch {
-  int tile, m0, rows, splits;          // tile: of kTiles, -1: gemm_fp8_few
-  bool part;                           // sums go through the workspace and fp8_join
+void (*const kLaunch[])(Fp8Params, int, hipStream_t) = {      // by the plan's tiles
+#define PACE_FP8_LAUNCH(T, MI, NI, WM, WN, ST, G, RUN, ...) launch_tile<T, MI, NI, WM, WN, ST, G, RUN>,
+    PACE_FP8_TILES(PACE_FP8_LAUNCH)
+#undef PACE_FP8_LAUNCH
 };
-struct Fp8Plan {
-  Fp8Launch run[2];
-  int runs;
-  size_t bytes;
-};
-
-// The tiles' times in us: a launch's start and end, a stage of 128 k's (for each group of waves) alone on a CU and what a further
-// workgroup there adds to it, a round's end, TB/s of operands that come from memory once.  Fitted to 13,800 timings over 210 shapes
-// (1 to 10,677 rows, 64 to 28,672 columns, K 128 to 14,336, K in 1 to 12 parts, weights from memory): what the plan picks takes 1.01
-// to 1.02 times the best that was measured in the mean, at most 1.4 times (8-bit outputs 1.2).  Of 29 tiles tried these are the ones
-// that bring it there.
-struct Fp8Tile {
-  int bm, bn, groups, per_cu, threads;
-  bool wide;
-  float fixed, stage, shared, round, memory;
-  void (*launch)(Fp8Params, int, hipStream_t);
-};
-const Fp8Tile kTiles[] = {
-    {256, 256, 1, 1, 512, false, 2.73f, 1.426f, 0.000f, 10.52f, 5.00f, launch_tile<Codes, 8, 4, 2, 4, 2, 1, true>},
-    {192, 256, 1, 1, 512, false, 3.28f, 1.324f, 0.000f, 7.43f, 5.00f, launch_tile<Codes, 6, 4, 2, 4, 2, 1, true>},
-    {256, 128, 1, 1, 512, false, 3.29f, 0.890f, 0.000f, 7.03f, 5.00f, launch_tile<Codes, 4, 4, 4, 2, 3, 1, true>},
-    {192, 128, 1, 1, 512, false, 3.02f, 0.734f, 0.000f, 5.73f, 5.00f, launch_tile<Codes, 3, 4, 4, 2, 3, 1, true>},
-    {160, 128, 1, 2, 256, false, 1.70f, 0.817f, 0.429f, 7.04f, 5.00f, launch_tile<Codes, 5, 4, 2, 2, 2>},
-    {96, 128, 2, 1, 512, false, 2.02f, 1.111f, 0.000f, 4.81f, 5.00f, launch_tile<Codes, 3, 4, 2, 2, 2, 2>},
-    {64, 128, 2, 1, 512, false, 1.61f, 0.697f, 0.000f, 4.58f, 5.00f, launch_tile<Codes, 4, 2, 1, 4, 3, 2>},
-    {64, 64, 2, 1, 512, false, 1.55f, 0.487f, 0.000f, 3.40f, 5.00f, launch_tile<Codes, 4, 1, 1, 4, 3, 2>},
-    {32, 64, 2, 2, 512, false, 1.18f, 0.361f, 0.311f, 3.04f, 5.00f, launch_tile<Codes, 2, 1, 1, 4, 3, 2>},
-    {192, 256, 1, 1, 512, true, 6.17f, 2.078f, 0.000f, 3.76f, 5.00f, launch_tile<Values, 6, 4, 2, 4, 2, 1, true>},
-    {128, 256, 1, 1, 512, true, 4.93f, 1.574f, 0.000f, 3.91f, 5.00f, launch_tile<Values, 4, 4, 2, 4, 2, 1, true>},
-    {64, 256, 1, 1, 256, true, 2.84f, 1.143f, 0.000f, 5.06f, 6.10f, launch_tile<Values, 4, 4, 1, 4, 3>},
-    {32, 256, 2, 1, 512, true, 1.50f, 1.447f, 0.000f, 3.62f, 4.05f, launch_tile<Values, 2, 4, 1, 4, 2, 2>},
-    {128, 128, 1, 2, 256, true, 6.03f, 0.904f, 0.733f, 1.45f, 5.00f, launch_tile<Values, 4, 4, 2, 2, 2>},
-    {32, 64, 2, 2, 512, true, 1.41f, 0.542f, 0.426f, 2.78f, 5.62f, launch_tile<Values, 2, 1, 1, 4, 3, 2>},
-};
-constexpr int kNumTiles = sizeof(kTiles) / sizeof(kTiles[0]);
-constexpr int kMostSplits = 12, kMostRows = 1 << 26;
-constexpr double kMostSums = 5e7;      // of the parts of K together
-
-long long tiles_of(const Fp8Tile& t, int rows, int N) { return (rows + t.bm - 1ll) / t.bm * ((N + t.bn - 1ll) / t.bn); }
-float join_time(int rows, int N, int splits) { return 2.9f + 1.1e-6f * splits * rows * static_cast<float>(N); }
-float tile_time(const Fp8Tile& t, int rows, int N, int K, int splits) {
-  const int kb = (K + kBlock - 1) / kBlock, stages = ((kb + splits - 1) / splits + t.groups - 1) / t.groups;
-  const long long n = tiles_of(t, rows, N) * splits, round = 256ll * t.per_cu;
-  const long long full = n / round;
-  const int left = static_cast<int>((n - full * round + 255) / 256);      // workgroups of a CU in the last round
-  const auto turn = [&](int there) { return stages * (t.stage + t.shared * (there - 1)) + t.round; };
-  const float work = t.fixed + full * turn(t.per_cu) + (left ? turn(left) : 0.f);
-  const float bytes = 1.8f + (static_cast<float>(rows) * K + static_cast<float>(N) * K + 2.f * rows * N) / (t.memory * 1e6f);
-  return sqrtf(work * work + bytes * bytes);
-}
-// gemm_fp8_few: a column's 8 waves take kb / 8 blocks one after the other, and read x again for each 16 columns.  Over many columns
-// the tiles read memory better (one row of 28,672 columns of 3,584: 23.6 us against 22.6, 16 rows 33.5 against 24; of 3,584 columns
-// 5.8 and 6.7 against 9.4 with parts and their join).  Fitted to 86 timings, within 8%.
-bool join_fits(int rows, int N) { return fits((N + 1023ll) / 1024 * rows, 256); }
-float few_time(int rows, int N, int K) {
-  const int kb = (K + kBlock - 1) / kBlock, blocks = (kb + kFewWaves - 1) / kFewWaves;
-  const float n = (N + 15) / 16 / 256.f, work = 2.07f + (n > 1.f ? powf(n, 0.81f) : 1.f) * blocks * (0.575f + 0.0088f * rows);
-  const float bytes = 2.6f + static_cast<float>(N) * K * (1.f + 0.03f * rows) / 4.6e6f;
-  return sqrtf(sqrtf(work * work * work * work + bytes * bytes * bytes * bytes));
-}
-
-// A tile whose columns hold whole blocks of 128 SwiGLU outputs quantises them itself.
-bool finishes_eight(const Fp8Tile& t) { return t.bn == 256; }
-
-// The quickest single launch for these rows; 1e30: every one would take 2^32 threads.
-float plan_rows(int rows, int N, int K, bool eight, bool wide, Fp8Launch* out) {
-  const int kb = (K + kBlock - 1) / kBlock;
-  float best = 1e30f;
-  if (rows <= 16 && fits((N + 15ll) / 16, 64 * kFewWaves) && (!eight || join_fits(rows, N))) {
-    best = few_time(rows, N, K) + (eight ? join_time(rows, N, 1) : 0.f);
-    *out = {-1, 0, rows, 1, eight};
-  }
-  for (int i = 0; i < kNumTiles; ++i) {
-    const Fp8Tile& t = kTiles[i];
-    if (t.wide != wide || (t.bm > 32 && t.bm >= 2 * rows)) continue;
-    for (int s = 1; s <= kMostSplits; ++s) {
-      if (s > 1 && (2 * s > kb || static_cast<double>(s) * rows * N > kMostSums)) break;
-      const bool part = s > 1 || (eight && !finishes_eight(t));
-      if (!fits(tiles_of(t, rows, N) * s, t.threads) || (part && !join_fits(rows, N))) break;
-      const float time = tile_time(t, rows, N, K, s) + (part ? join_time(rows, N, s) : 0.f);
-      if (time < best) {
-        best = time;
-        *out = {i, 0, rows, s, part};
-      }
-    }
-  }
-  return best;
-}
-
-Fp8Plan make_plan(int M, int N, int K, bool eight, bool wide) {
-  Fp8Plan a{};
-  float best = plan_rows(M, N, K, eight, wide, &a.run[0]);
-  a.runs = best < 1e30f ? 1 : 0;
-  best *= 0.98f;                                       // a second launch has to be worth it
-  // The largest tiles come in rounds of 256; rows that would fill a small part of a last round may be quicker in a launch of
-  // their own.
-  for (int i = 0; i < kNumTiles; ++i) {
-    const Fp8Tile& t = kTiles[i];
-    if (t.wide != wide || t.per_cu != 1 || t.groups != 1 || (eight && !finishes_eight(t))) continue;
-    const long long across = (N + t.bn - 1ll) / t.bn, rounds = tiles_of(t, M, N) / 256, down = rounds * 256 / across;
-    const int rows = static_cast<int>(down * t.bm < M ? down * t.bm : M);
-    if (rounds < 1 || rows < 1 || rows >= M || a.runs == 0 || !fits(rounds * 256, t.threads)) continue;
-    Fp8Launch rest;
-    const float two = tile_time(t, rows, N, K, 1) + plan_rows(M - rows, N, K, eight, wide, &rest);
-    if (two < best) {
-      best = two;
-      rest.m0 = rows;
-      a.run[0] = {i, 0, rows, 1, false};
-      a.run[1] = rest;
-      a.runs = 2;
-    }
-  }
-  for (int i = 0; i < a.runs; ++i) {
-    const size_t need = a.run[i].part ? static_cast<size_t>(a.run[i].splits) * a.run[i].rows * N * sizeof(float) : 0;
-    if (need > a.bytes) a.bytes = need;
-  }
-  return a;
-}
 
 // A call asks for the workspace's size and then runs: the plan, which takes 0.3 to 6 us, is made once for both.
 const Fp8Plan& plan_fp8(int M, int N, int K, bool eight, bool wide) {
@@ -1500,7 +1378,7 @@ pace_status_t pace_gemm_fp8(const uint8_t* x, const float* x_scale, long long x_
     p.splits = l.splits;
     p.width = width_of(p);
     if (l.tile < 0) launch_few<8, 2>(p, stream);
-    else kTiles[l.tile].launch(p, l.splits, stream);
+    else kLaunch[l.tile](p, l.splits, stream);
     if (l.part) launch_join(p, stream);
   }
   return check_launch("pace_gemm_fp8");
