@@ -588,7 +588,8 @@ size_t pace_gemm_fp8_workspace_size(int M, int N, int K, int bits, int sums);
  *           (16-byte aligned) with c_scale fp32 [ceil(N / 256), M], quantised from fp32 as by pace_quantize_fp8 (rows = 1).
  *   sums    PACE_SUMS_AUTO, _FAST or _WIDE (above).
  * Results are in an order fixed by the shape, bits and sums: equal calls give equal bits.  A NaN in x makes its row of C NaN, one
- * in w its column.  Scales and their products must be finite.  C may be the residual's memory.  M = 0 is a no-op; the plan of large products is made for 256 CUs.
+ * in w its column.  Scales and their products must be finite; a product of two scales under 2^-126 is rounded to a multiple of 2^-149, so
+ * that outputs under about 2^-100 lose bits with such scales.  C may be the residual's memory.  M = 0 is a no-op; the plan of large products is made for 256 CUs.
  * The workspace must be 16-byte aligned; calls that may run at the same time need one each.
  */
 pace_status_t pace_gemm_fp8(const uint8_t* x, const float* x_scale, long long x_scale_stride, const uint8_t* w, const float* w_scale,

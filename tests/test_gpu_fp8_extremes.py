@@ -6,7 +6,7 @@ from oracle import fp8 as o8
 from paper_2608_27206_amd import workloads as wl
 from tests.gpu_util import dev_bf16, dev_f32, say
 from tests.test_gpu_cache import f64
-from tests.test_gpu_fp8 import bits_of, check_norm, check_product
+from tests.test_gpu_fp8 import bits_of, check_norm, check_product, make_codes
 
 pytestmark = pytest.mark.gpu
 
@@ -91,3 +91,26 @@ def test_swiglu_of_far_gates_within_its_roundings(M, N, K, bits, sums):
             assert np.all(err <= 2.0 ** -8 * (np.abs(ref) + tol) + tol + 2.0 ** -134)
         else:
             check_product(y.view(torch.uint8)[at].view(torch.float8_e4m3fn), s[:, at], (ref, tol, None), 8)
+
+
+@pytest.mark.parametrize("sums", [1, 2])
+@pytest.mark.parametrize("M,N,K", [(3, 264, 400), (40, 264, 1040), (300, 520, 2064), (2690, 5936, 976)])
+def test_products_of_scales_that_are_subnormal(M, N, K, sums):
+    """Scales down to 2^-110 each: a block's product of scales is off by at most half a multiple of 2^-149, as are the sums that it enters."""
+    import torch
+    from paper_2608_27206_amd import pace
+    rs = np.random.default_rng(M + sums)
+    x, _, X, _ = make_codes(rs, M, K, 1)
+    w, _, W, _ = make_codes(rs, N, K, 128)
+    XS = (rs.uniform(1, 2, (o8.blocks(K), M)) * 2.0 ** -rs.integers(58, 80, (1, M))).astype(np.float32)
+    WS = (rs.uniform(1, 2, (o8.blocks(N), o8.blocks(K))) * 2.0 ** -rs.integers(58, 80, (o8.blocks(N), 1))).astype(np.float32)
+    say(f"subnormal products of scales M={M} N={N} K={K} sums={sums}")
+    y, _ = pace.gemm_fp8(x, dev_f32(XS), w, dev_f32(WS), sums=sums)
+    torch.cuda.synchronize()
+    m, n = np.unique(np.append(rs.permutation(M)[:40], M - 1)), np.unique(np.append(rs.permutation(N)[:40], N - 1))
+    Wn = W[n] * o8.per_value(WS.astype(np.float64), (N, K), 128)[n]
+    ref, tol, _ = o8.product(X[m], XS[:, m].astype(np.float64), Wn, np.ones((o8.blocks(len(n)), o8.blocks(K))), wide=sums == 2)
+    blocks = sum(np.abs(X[m, k:k + 128]) @ np.abs(W[n, k:k + 128]).T for k in range(0, K, 128))
+    tol = tol + 2.0 ** -150 * blocks + (o8.blocks(K) + 64) * 2.0 ** -150
+    got = f64(y[torch.from_numpy(m).cuda()][:, torch.from_numpy(n).cuda()])
+    assert np.all(np.abs(got - ref) <= 2.0 ** -8 * (np.abs(ref) + tol) + tol + 2.0 ** -134)
