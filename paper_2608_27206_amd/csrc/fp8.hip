@@ -671,7 +671,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
         asm volatile("" : "+v"(to));                   // here, not behind the stage's branches
       }
     };
-    const auto stage = [&](int k, auto from, auto tail) __attribute__((always_inline)) {
+    const auto stage = [&](int k, auto from) __attribute__((always_inline)) {
       constexpr int P = decltype(from)::value;
       const int nxt = cur == ST - 1 ? 0 : cur + 1, ns = cs == kScaleSlots - 1 ? 0 : cs + 1, far = cs == 0 ? kScaleSlots - 1 : cs - 1;
       const float sw = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wscales), k & 63));
@@ -694,7 +694,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
           if (l * kReadIn / kReads == u) read(l, std::integral_constant<int, 1 - P>{}, nxt, ns);
 #pragma unroll
         for (int l = 0; l < kEarly; ++l)
-          if (l * U / kEarly == u) load_early(l, block_of(k + ST), cur, far, tail);
+          if (l * U / kEarly == u) load_early(l, block_of(k + ST), cur, far, std::false_type{});
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           d[t] = c[t];
@@ -711,19 +711,11 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
     const std::integral_constant<int, 0> even;
     const std::integral_constant<int, 1> odd;
     int k = 0;
-    const int plain = G == 1 ? nk - ST : nk;             // the stages after them ask for no block of K
-    for (; k + 1 < plain; k += 2) {
-      stage(k, even, std::false_type{});
-      stage(k + 1, odd, std::false_type{});
+    for (; k + 1 < nk; k += 2) {
+      stage(k, even);
+      stage(k + 1, odd);
     }
-    if constexpr (G == 1) {
-      for (; k < nk; ++k) {
-        if (k & 1) stage(k, odd, std::true_type{});
-        else stage(k, even, std::true_type{});
-      }
-    } else if (k < nk) {
-      stage(k, even, std::false_type{});
-    }
+    if (k < nk) stage(k, even);
     add(U - 1);
   } else {
     T* const kind = nullptr;
@@ -828,7 +820,7 @@ __global__ __launch_bounds__(64 * WM * WN * G, 2) void gemm_fp8_tile(const Fp8Pa
           if (last) {
 #pragma unroll
             for (int l = 0; l < kLate; ++l)
-              if (l * NU / kLate == u) load_late(l, far_block(), cur, tail);
+              if (l * NU / (kLate ? kLate : 1) == u) load_late(l, far_block(), cur, tail);
           }
           // the next step's x and the next stage's w are widened under the products, too
           if (kAhead && u == NU - 1 && (!last || ahead)) {
@@ -1118,15 +1110,13 @@ __device__ __forceinline__ void store4(const Fp8Params& p, float* to, int n, f32
 }
 
 // Up to 16 rows: bound by the weights' bytes (one row of 4,608 x 3,584 7.0 us; 16.5 MB at the rate of a copy 3.2, the rest the chain of
-// launch, four blocks a wave, and join; three or four blocks in flight and 16 waves gave nothing).  W of a workgroup's 8 waves share 16 columns and take the blocks of K in turn; a
-// wave keeps D blocks in flight.  The codes become bf16 values, whose products the matrix cores sum in 32 bits.
-template <int W, int D>
+// launch, four blocks a wave, and join; three or four blocks in flight and 16 waves gave nothing).  A workgroup's 8 waves share 16 columns and take the blocks of K in turn; a
+// wave keeps two blocks in flight.  The codes become bf16 values, whose products the matrix cores sum in 32 bits.
 __global__ __launch_bounds__(64 * kFewWaves, 2) void gemm_fp8_few(const Fp8Params p) {
-  constexpr int SETS = kFewWaves / W;
-  __shared__ f32x4 join[SETS][W > 1 ? W - 1 : 1][64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-  const int w = wave % W, set = wave / W;
-  const int n0 = (remap_block_id(blockIdx.x, gridDim.x) * SETS + set) * 16;
+  constexpr int W = kFewWaves, D = 2;
+  __shared__ f32x4 join[W - 1][64];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  const int n0 = remap_block_id(blockIdx.x, gridDim.x) * 16;
   const int n = n0 + r < p.N ? n0 + r : p.N - 1;
   const uint8_t* wrow = p.w + static_cast<long long>(n) * p.K + 16 * g;
   const uint8_t* xrow = p.x + static_cast<long long>(r < p.M ? r : 0) * p.K + 16 * g;
@@ -1170,13 +1160,11 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void gemm_fp8_few(const Fp8Param
       if (b + D * W < p.kb) load(i, b + D * W);
     }
   }
-  if constexpr (W > 1) {
-    if (w) join[set][w - 1][lane] = acc;
-    __syncthreads();
-    if (w) return;
+  if (w) join[w - 1][lane] = acc;
+  __syncthreads();
+  if (w) return;
 #pragma unroll
-    for (int i = 0; i < W - 1; ++i) acc += join[set][i][lane];
-  }
+  for (int i = 0; i < W - 1; ++i) acc += join[i][lane];
   const int at = n0 + 4 * g;
   if (r >= p.M || at >= p.N) return;
   if (p.part) store4(p, p.part + static_cast<long long>(r) * p.N + at, at, acc);
@@ -1228,10 +1216,8 @@ int width_of(const Fp8Params& p) {
                          (p.mode == kEpiResidual ? reinterpret_cast<uintptr_t>(p.R) : 0);
   return bits % 16 == 0 ? 8 : bits % 8 == 0 ? 4 : bits % 4 == 0 ? 2 : 1;
 }
-template <int W, int D>
 void launch_few(const Fp8Params& p, hipStream_t stream) {
-  const int sets = kFewWaves / W, tiles = (p.N + 15) / 16;
-  hipLaunchKernelGGL((gemm_fp8_few<W, D>), dim3((tiles + sets - 1) / sets), dim3(64 * kFewWaves), 0, stream, p);
+  hipLaunchKernelGGL(gemm_fp8_few, dim3((p.N + 15) / 16), dim3(64 * kFewWaves), 0, stream, p);
 }
 void launch_join(const Fp8Params& p, hipStream_t stream) {
   hipLaunchKernelGGL(fp8_join, dim3((p.N + 1023) / 1024 * p.M), dim3(256), 0, stream, p);
@@ -1377,7 +1363,7 @@ pace_status_t pace_gemm_fp8(const uint8_t* x, const float* x_scale, long long x_
     p.mode = epilogue;
     p.splits = l.splits;
     p.width = width_of(p);
-    if (l.tile < 0) launch_few<8, 2>(p, stream);
+    if (l.tile < 0) launch_few(p, stream);
     else kLaunch[l.tile](p, l.splits, stream);
     if (l.part) launch_join(p, stream);
   }
