@@ -238,10 +238,18 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_rows(const NormPara
     }
   }
 }
-// A wave a row where it holds few values and there are rows enough to fill the card (42,196 x 1,280: 76.9 us, 78.6 with 256
-// threads a row; 20,000 x 1,024: 28.5 and 34.5; 1,183 x 1,280: 6.9 and 6.3).  5,000 x 8,192: 52.8 us with 512 threads, 58.7 with
-// 256, 60.5 with 1,024.
-constexpr int kManyRows = 1024;
+// A wave a row, without a barrier, where it holds few values and there are rows enough to fill the card; a residual doubles the loads that it
+// has to hold in flight.  A wave a row and 256 threads a row, captured, one card:
+//   1,024 values: with the residual to 8 bits 1,183 rows 5.3 and 5.0 us, 4,096 9.6 and 10.3, 42,196 57.3 and 68.9 (to 16 bits 4.8 and 4.5,
+//   8.6 and 8.6, 65.0 and 63.6); without 1,183 3.6 and 3.9, 42,196 33.3 and 56.6;
+//   1,280 with the residual to 8 bits: 1,183 rows 6.6 and 5.4, 12,000 28.7 and 26.9, 20,000 40.8 and 42.0, 42,196 74.4 and 83.2; to 16
+//   bits 83.1 and 76.8; 1,536 to 8 bits 20,000 rows 47.1 and 44.1;
+//   1,280 without: 2,048 rows 5.4 and 5.2, 4,096 7.7 and 8.1, 42,196 43.6 and 63.4; 2,048 4,096 rows 10.5 and 10.2.
+// 5,000 x 8,192: 52.8 us with 512 threads, 58.7 with 256, 60.5 with 1,024.
+bool wave_a_row(int M, int K, bool residual, bool eight) {
+  if (K <= 1024) return M >= 1024;
+  return residual ? K <= 1280 && M >= 20000 && eight : K <= 1536 && M >= 4096;
+}
 template <int T, int NC, bool GAMMA>
 void launch_norm(const NormParams& p, hipStream_t stream) {
   constexpr int rows = T < 256 ? 256 / T : 1;
@@ -1300,10 +1308,11 @@ pace_status_t pace_rmsnorm(const uint16_t* x, long long x_stride, const uint16_t
   PACE_REQUIRE(x_stride >= K && x_stride % 8 == 0 && x_stride < (1ll << 31), "pace_rmsnorm: row stride %lld (a multiple of 8, at least K=%d)", x_stride, K);
   PACE_REQUIRE(!residual || (residual_stride >= K && residual_stride % 8 == 0 && residual_stride < (1ll << 31)),
                "pace_rmsnorm: residual's row stride %lld (a multiple of 8, at least K=%d)", residual_stride, K);
-  PACE_REQUIRE(fits(M, M >= kManyRows && K <= 2048 ? 64 : K <= 4096 ? 256 : K <= 16384 ? 512 : 1024), "pace_rmsnorm: too many rows (M=%d)", M);
+  const bool wave = wave_a_row(M, K, residual, q);
+  PACE_REQUIRE(fits(M, wave ? 64 : K <= 4096 ? 256 : K <= 16384 ? 512 : 1024), "pace_rmsnorm: too many rows (M=%d)", M);
   const NormParams p{x, residual, gamma, sum, y, q, scale, x_stride, residual_stride, eps, M, K};
-  if (M >= kManyRows && K <= 1024) launch_norm<64, 2, false>(p, stream);
-  else if (M >= kManyRows && K <= 2048) launch_norm<64, 4, false>(p, stream);
+  if (wave && K <= 1024) launch_norm<64, 2, false>(p, stream);
+  else if (wave) launch_norm<64, 3, false>(p, stream);
   else if (K <= 2048) launch_norm<256, 1, true>(p, stream);
   else if (K <= 4096) launch_norm<256, 2, true>(p, stream);
   else if (K <= 8192) launch_norm<512, 2, false>(p, stream);

@@ -4,9 +4,10 @@ import numpy as np
 import pytest
 
 from oracle import fp8 as o8
-from tests.gpu_util import host
+from paper_2608_27206_amd import workloads as wl
+from tests.gpu_util import dev_bf16, dev_f32, host
 from tests.test_gpu_cache import f64
-from tests.test_gpu_fp8 import check_norm
+from tests.test_gpu_fp8 import check_norm, rows_of
 from tests.test_gpu_fp8_run import calls, outputs, run, same   # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -79,3 +80,21 @@ def test_streams_write_codes_and_scales(calls):   # noqa: F811
         for s in streams:
             torch.cuda.current_stream().wait_stream(s)
         assert all(same(outputs(c), w) for c, w in zip(calls, want))
+
+
+@pytest.mark.parametrize("M,K,residual,bits", [(1023, 1024, True, 8), (1024, 1024, True, 8), (1024, 1008, False, 16), (1024, 1040, True, 16), (4095, 1536, False, 8), (4096, 1536, False, 8),
+                                               (4097, 1040, False, 16), (4096, 1552, False, 16), (19_999, 1280, True, 8), (20_001, 1280, True, 8), (20_000, 1072, True, 8),
+                                               (20_000, 1280, True, 16), (20_000, 1296, True, 8)])
+def test_norm_on_both_sides_of_its_rule(M, K, residual, bits):
+    """Rows that a wave holds, and those that 256 threads hold."""
+    import torch
+    from paper_2608_27206_amd import pace
+    rs = np.random.default_rng(M + K)
+    x, r, gamma = rows_of(rs, M, K), rows_of(rs, M, K), (1 + 0.1 * rs.standard_normal(K)).astype(np.float32)
+    y, s, h = pace.rmsnorm(dev_bf16(x), dev_f32(gamma), dev_bf16(r) if residual else None, bits=bits)
+    torch.cuda.synchronize()
+    m = np.unique(np.concatenate([np.arange(0, M, 61), np.arange(M - 8, M)]))
+    at = torch.from_numpy(m).cuda()
+    H, Y, tol = o8.norm(wl.bf16_bits_to_f64(x[m]), wl.bf16_bits_to_f64(r[m]) if residual else None, gamma.astype(np.float64), float(np.float32(1e-6)))
+    y = y[at] if bits == 16 else y.view(torch.uint8)[at].view(torch.float8_e4m3fn)
+    check_norm(y, None if s is None else s[:, at], None if h is None else h[at], H, Y, tol, residual, bits)
