@@ -105,7 +105,7 @@ struct QuantParams {
 };
 
 // Rows: scale = max(max |x| / 448, 2^-120), code = x / scale, in one read: 16 lanes hold a block of 128, blocks of a row after
-// one another.  Bound by memory: 10,677 x 3,584 moves 115 MB in 22.5 us (5.1 TB/s, the rate of a copy); one row takes 2.2.
+// one another.  Bound by memory: 10,677 x 3,584 moves 115 MB in 23.2 us (4.9 TB/s; a copy reaches 5.1); one row takes 2.1.
 __global__ __launch_bounds__(256) void quantize_rows(const QuantParams p) {
   const unsigned block = blockIdx.x * 16 + (threadIdx.x >> 4);   // under 2^28: a launch has fewer than 2^32 threads
   const int row = static_cast<int>(block / static_cast<unsigned>(p.kb)), kb = static_cast<int>(block - static_cast<unsigned>(row) * p.kb);
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(256) void quantize_rows(const QuantParams p) {
 }
 
 // Weights: a workgroup per block of 128 x 128, its values in registers between the maximum and the store.  Bound by memory:
-// 28,672 x 3,584 moves 308 MB in 66.4 us (4.6 TB/s).
+// 28,672 x 3,584 moves 308 MB in 66.3 us (4.6 TB/s).
 __global__ __launch_bounds__(256) void quantize_blocks(const QuantParams p) {
   __shared__ float red[4];
   const int mb = blockIdx.x / p.kb, kb = blockIdx.x - mb * p.kb;
@@ -509,7 +509,7 @@ __device__ __forceinline__ void finish_tile(const Fp8Params& p, f32x4 (&acc)[MI]
 //    weights' bytes.  Four waves of 128 x 128 read a third less, but need 512 registers a lane, half of them beyond the
 //    vector unit's reach: 616 us for 8192 cubed against 472.
 //  - With few tiles, K goes to workgroups (`part`, fp8_join) or to G groups in one.  Measured, a call: 10,677 x 28,672 x 3,584 with
-//    SwiGLU 950 us (2,310 TFLOP/s), its 8-bit output in wide sums 1,676 (1,309), 1,183 x 3,584 x 3,584 with a residual 27 (1,126),
+//    SwiGLU 967 us (2,270 TFLOP/s), its 8-bit output in wide sums 1,717 (1,278), 1,183 x 3,584 x 3,584 with a residual 27 (1,126),
 //    48 x 3,584 x 14,336 14 with the join (3.6 TB/s), 8 x 28,672 x 3,584 24 (4.3).
 //  - RUN: a workgroup takes one tile after another.  The last ST stages ask for the next tile's first ones, and the output
 //    leaves from registers, since LDS already holds those.
@@ -1255,7 +1255,7 @@ void (*const kLaunch[])(Fp8Params, int, hipStream_t) = {      // by the plan's t
 #undef PACE_FP8_LAUNCH
 };
 
-// A call asks for the workspace's size and then runs: the plan, which takes 0.3 to 6 us, is made once for both.
+// A call asks for the workspace's size and then runs: the plan, which takes 0.4 us (one row) to 12 (42,196), is made once for both.
 const Fp8Plan& plan_fp8(int M, int N, int K, bool eight, bool wide) {
   static thread_local struct {
     int M, N, K;

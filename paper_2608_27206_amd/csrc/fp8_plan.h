@@ -30,7 +30,7 @@ struct Fp8Plan {
 // fitted figure: part of them comes from caches; 5 where nothing else fitted better).  Fitted to 13,800 timings over 210 shapes
 // (1 to 10,677 rows, 64 to 28,672 columns, K 128 to 14,336, K in 1 to 12 parts, weights from memory): what the plan picks takes 1.01
 // to 1.02 times the best that was measured in the mean, at most 1.4 times (8-bit outputs 1.2).  Of 29 tiles tried these are the ones
-// that bring it there.
+// that bring it there.  The epilogue is not known here: a round's end with a residual takes up to 27 us (42,196 x 1,280 x 3,424).
 #define PACE_FP8_TILES(X) \
   X(Codes, 8, 4, 2, 4, 2, 1, true, 1, 2.73f, 1.426f, 0.000f, 10.52f, 5.00f) \
   X(Codes, 6, 4, 2, 4, 2, 1, true, 1, 3.28f, 1.324f, 0.000f, 7.43f, 5.00f) \
